@@ -60,6 +60,7 @@ typedef void* echo_stream_t; /* hipStream_t */
 #define ECHO_DATA_OVER_CAPACITY (1 << 5)   /* more selected nodes than budget               */
 #define ECHO_DATA_BAD_SLOT_PARENT (1 << 6) /* slot_parent not in [0, slot)                  */
 #define ECHO_DATA_BAD_OFFSETS (1 << 7)     /* decreasing / out-of-capacity offsets          */
+#define ECHO_DATA_NO_PAGES (1 << 8)        /* a request or row without the pages it wants   */
 
 /* ---- limits ------------------------------------------------------------ */
 #define ECHO_MAX_DEPTH 16       /* deepest draft node that can be selected           */
@@ -67,6 +68,11 @@ typedef void* echo_stream_t; /* hipStream_t */
 #define ECHO_MAX_BUDGET 16384   /* largest budget B                                  */
 #define ECHO_MAX_REQUESTS 4095  /* largest batch R                                   */
 #define ECHO_MAX_CHECKPOINTS 16 /* entries of a sparse-gating checkpoint table       */
+
+/* ---- 8-bit KV cache ---------------------------------------------------- */
+#define ECHO_KV_E4M3 0   /* 8-bit float, 4 exponent bits, largest value 448 (OCP)   */
+#define ECHO_KV_E5M2 1   /* 8-bit float, 5 exponent bits, largest value 57344 (OCP) */
+#define ECHO_KV_BLOCK 32 /* tokens that share a scale (per head)                    */
 
 /*
  * echo_gate -- path scores and the global top-B selection.
@@ -389,6 +395,145 @@ int32_t echo_commit_kv(const int32_t* q_offsets, const int32_t* accept_len,
                        uint16_t* k_pages, uint16_t* v_pages, int64_t num_pages, int32_t page_size,
                        const int32_t* block_table, int32_t max_pages_per_request,
                        int32_t* prefix_len, int32_t* status, echo_stream_t stream);
+
+/*
+ * The 8-bit paged KV cache -- the paged cache at half the bytes, for the
+ * attention that is bound by reading it.  Two tensors of bytes and two of
+ * scales:
+ *   k_pages, v_pages [num_pages][Hkv][page_size][128]       uint8
+ *   k_scale, v_scale [num_pages][Hkv][page_size / 32]       float
+ * A byte is an 8-bit float of kv_format (ECHO_KV_E4M3 or ECHO_KV_E5M2); the
+ * value it stands for is that float times the scale of its block, which is the
+ * 32 tokens [32 i, 32 i + 32) of one page and head.  Page size, block tables
+ * and lengths are those of echo_tree_verify_attn_paged; the pages are
+ * head-major, so that a block is 4 KB in one piece.
+ *
+ * The writers (echo_store_kv_q8, echo_commit_kv_q8) fill a block's tokens in
+ * order.  Appending rows to a block whose first o tokens are written:
+ *   need  the smallest power of two from 2^-60 to 2^60 with
+ *         max |x| <= largest * need over the finite new values x of the block
+ *   scale max(scale, need) if o > 0, else need (whatever the scale held)
+ *   byte  x / scale rounded to nearest even; values beyond the largest (an
+ *         infinity, or a magnitude above largest * 2^60) become the largest,
+ *         NaN stays NaN.  Where the scale grows, the o tokens' bytes are
+ *         multiplied by old / new and rounded again: powers of two, so their
+ *         values stay the same unless they become subnormal.
+ * The tokens behind the appended ones are left as they are.  Readers take any
+ * positive finite scale from 2^-60 to 2^60, not only powers of two.
+ */
+
+/*
+ * echo_tree_verify_attn_paged_q8 -- echo_tree_verify_attn_paged over an 8-bit
+ * cache; the new keys and values of the tree's slots are bfloat16 as there.
+ * With one slot per request it is plain decoding.  Scores, softmax and sums
+ * are fp32; the cached bytes enter the products exactly, their scales in fp32;
+ * each probability is rounded to bf16 for the product with V (2^-8) and the
+ * output divided by the sum of the weights used; the merge of rows that are
+ * split between waves rounds partial sums to fp16 (2^-11 of the row's largest).
+ * Cached values that are NaN or infinite, and such inputs, give unspecified
+ * outputs for the rows of their request; bytes past a request's prefix are not
+ * used, whatever they hold.
+ *   q        [max_rows][Hq][128]  bf16
+ *   out      [max_rows][Hq][128]  bf16 (the next projection's input), rounded from
+ *                                 fp32 (2^-8)
+ *   lse      [max_rows][Hq]       float (nullable), natural log; -inf with out = 0
+ *                                 for a row that sees no key
+ * All other arguments, the skipped requests (ECHO_DATA_BAD_OFFSETS) and the
+ * limits are those of echo_tree_verify_attn_paged.  k_scale and v_scale are
+ * 4-byte aligned, all other tensors 16-byte aligned.  Deterministic.
+ * The workspace: echo_tree_verify_attn_paged_q8_workspace_size.
+ */
+int32_t echo_tree_verify_attn_paged_q8(
+    const uint16_t* q, const uint16_t* k_new, const uint16_t* v_new, int32_t kv_format,
+    const uint8_t* k_pages, const uint8_t* v_pages, const float* k_scale, const float* v_scale,
+    int64_t num_pages, int32_t page_size, const int32_t* block_table,
+    int32_t max_pages_per_request, const int32_t* prefix_len, const int32_t* q_offsets,
+    const uint32_t* tree_mask, int32_t mask_words, int32_t R, int32_t max_rows,
+    int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim, float sm_scale, uint16_t* out,
+    float* lse, void* workspace, size_t workspace_bytes, int32_t* status, echo_stream_t stream);
+size_t echo_tree_verify_attn_paged_q8_workspace_size(int32_t R, int32_t max_rows,
+                                                     int32_t num_q_heads, int32_t num_kv_heads,
+                                                     int32_t head_dim,
+                                                     int32_t max_pages_per_request);
+
+/*
+ * echo_store_kv_q8 -- quantise rows into an 8-bit cache at the slots of a slot
+ * map: prompts, or the token that each request decoded.
+ *
+ * Row i goes to slot slot_map[i] = page * page_size + token, as
+ * echo_build_block_tables writes them.  A negative slot leaves its row out (a
+ * captured call's padding); a slot of num_pages * page_size or more does too,
+ * with ECHO_DATA_BAD_OFFSETS.  Rows of one block are a run: neighbours in the map, at
+ * consecutive slots.  A run that starts at token o of its block appends to the
+ * o tokens before it.  A block that two runs name (the same slot twice, or
+ * slots out of order) gets unspecified contents; nothing else does.
+ *   k, v     [num_rows] rows of [Hkv][128] bf16, k_stride and v_stride elements
+ *            apart (multiples of 8, at least Hkv * 128: K and V may be parts of
+ *            one projection's output); 16-byte aligned
+ *   slot_map [num_rows] int64
+ */
+int32_t echo_store_kv_q8(const uint16_t* k, const uint16_t* v, int64_t k_stride, int64_t v_stride,
+                         const int64_t* slot_map, int32_t num_rows, int32_t num_kv_heads,
+                         int32_t head_dim, int32_t kv_format, uint8_t* k_pages, uint8_t* v_pages,
+                         float* k_scale, float* v_scale, int64_t num_pages, int32_t page_size,
+                         int32_t* status, echo_stream_t stream);
+
+/*
+ * echo_commit_kv_q8 -- echo_commit_kv into an 8-bit cache: each request's root
+ * and accepted rows are appended at positions prefix_len[r], prefix_len[r] + 1,
+ * ... and new_len[r] = prefix_len[r] + 1 + accept_len[r].  A request with a
+ * missing page or a bad slot is left as it is (ECHO_DATA_BAD_OFFSETS) and one
+ * without slots too: new_len[r] = prefix_len[r].
+ *   new_len  [R] int32, may be prefix_len itself
+ *   page_size a power of two, >= 32; the other arguments as for echo_commit_kv
+ */
+int32_t echo_commit_kv_q8(const int32_t* q_offsets, const int32_t* accept_len,
+                          const int32_t* accept_slots, int32_t max_depth, const uint16_t* k_new,
+                          const uint16_t* v_new, int32_t R, int32_t max_rows,
+                          int32_t num_kv_heads, int32_t head_dim, int32_t kv_format,
+                          uint8_t* k_pages, uint8_t* v_pages, float* k_scale, float* v_scale,
+                          int64_t num_pages, int32_t page_size, const int32_t* block_table,
+                          int32_t max_pages_per_request, const int32_t* prefix_len,
+                          int32_t* new_len, int32_t* status, echo_stream_t stream);
+
+/*
+ * echo_build_block_tables -- the pages of a batch from its lengths (block
+ * tables), and the slots of its new rows (slot map), for any of the paged
+ * caches above.
+ *
+ * Request r holds pages block_table[r][0 .. num_held[r]) and wants
+ * need = ceil(want_len[r] / page_size) of them: its cached tokens and those of
+ * the step to come; 0 ends it.  Free pages are a stack, free_pages[0 ..
+ * num_free[0]).  First the requests that hold more than they need give theirs
+ * from block_table[r][need] on back, in request order, onto the stack's top.
+ * Then the others take theirs from its top, in request order.  A request gets
+ * all it wants or nothing: from the first that the rest of the stack cannot
+ * serve on, none takes any (ECHO_DATA_NO_PAGES).  Table entries past those that
+ * a request holds are left as they are and have no meaning.
+ *   want_len     [R] int32; a request with a negative length, more pages than
+ *                max_pages_per_request, or such a num_held, keeps what it has
+ *                (ECHO_DATA_BAD_OFFSETS)
+ *   num_held_out [R] int32 and num_free_out [1] int32: the new counts; they may be
+ *                num_held and num_free themselves
+ *   free_pages   [max_free] int32; a stack that is not within [0, max_free], before
+ *                or after what is given back, changes nothing
+ *                (ECHO_DATA_BAD_OFFSETS)
+ *   page_size    a power of two
+ * slot_map (nullable; then the next three are not read): row i of [row_offsets[r],
+ * row_offsets[r+1]) is token row_start[r] + i - row_offsets[r] of request r,
+ * and slot_map[i] = page * page_size + token % page_size.  It is -1 where the
+ * request does not hold that page (ECHO_DATA_NO_PAGES), and for the rows that no request
+ * has, up to max_rows.
+ *   row_offsets  [R+1] int32; row_start [R] int32; slot_map [max_rows] int64
+ * The library does not look at the pages' ids.  R * max_pages_per_request < 2^31.
+ */
+int32_t echo_build_block_tables(const int32_t* want_len, int32_t R, int32_t page_size,
+                                int32_t* block_table, int32_t max_pages_per_request,
+                                const int32_t* num_held, int32_t* num_held_out,
+                                int32_t* free_pages, int32_t max_free, const int32_t* num_free,
+                                int32_t* num_free_out, const int32_t* row_offsets,
+                                const int32_t* row_start, int32_t max_rows, int64_t* slot_map,
+                                int32_t* status, echo_stream_t stream);
 
 /*
  * echo_tree_verify_attn_timed, echo_tree_verify_attn_paged_timed -- the two

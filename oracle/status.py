@@ -8,5 +8,6 @@ OVER_CAPACITY = 1 << 5    # more selected nodes than the budget: only the first 
 BAD_SLOT_PARENT = 1 << 6  # slot_parent not in [0, slot): slot can never be accepted
 BAD_OFFSETS = 1 << 7      # malformed offsets: candidate CSR -> nothing scored or packed;
                           # slot or KV ranges -> that request's attention is skipped
+NO_PAGES = 1 << 8         # block tables: a request or row without the pages it wants
 
 MAX_DEPTH = 16

@@ -26,10 +26,15 @@ DATA_NOT_CLOSED = 1 << 4
 DATA_OVER_CAPACITY = 1 << 5
 DATA_BAD_SLOT_PARENT = 1 << 6
 DATA_BAD_OFFSETS = 1 << 7
+DATA_NO_PAGES = 1 << 8
 
 MAX_DEPTH = 16
 MAX_CHECKPOINTS = 16
 HEAD_DIM = 128
+
+KV_E4M3 = 0
+KV_E5M2 = 1
+KV_BLOCK = 32
 
 EXPORTS = [
     "echo_gate", "echo_gate_workspace_size", "echo_gate_sparse", "echo_gate_sparse_workspace_size",
@@ -39,7 +44,9 @@ EXPORTS = [
     "echo_tree_verify_attn_paged", "echo_accept_logits", "echo_commit_kv",
     "echo_accept", "echo_tree_verify_attn_timed", "echo_tree_verify_attn_paged_timed",
     "echo_probe_stream_read", "echo_gate_noalloc", "echo_verify_step", "echo_status_string",
-    "echo_version",
+    "echo_version", "echo_tree_verify_attn_paged_q8",
+    "echo_tree_verify_attn_paged_q8_workspace_size", "echo_store_kv_q8", "echo_commit_kv_q8",
+    "echo_build_block_tables",
 ]
 GATE_SCRATCH_BYTES = 8 << 20
 
@@ -87,6 +94,16 @@ _SIGS = {
                                 _P, _P, _P, _P, _P, _P, _I64, _I32, _I32, _I32, _I32, _F32, _P,
                                 _P, _P, _SZ,
                                 _P, _I32, _P, _P, _P, _P, _P]),
+    "echo_tree_verify_attn_paged_q8": (_I32, [_P, _P, _P, _I32, _P, _P, _P, _P, _I64, _I32, _P,
+                                              _I32, _P, _P, _P, _I32, _I32, _I32, _I32, _I32,
+                                              _I32, _F32, _P, _P, _P, _SZ, _P, _P]),
+    "echo_tree_verify_attn_paged_q8_workspace_size": (_SZ, [_I32, _I32, _I32, _I32, _I32, _I32]),
+    "echo_store_kv_q8": (_I32, [_P, _P, _I64, _I64, _P, _I32, _I32, _I32, _I32, _P, _P, _P, _P,
+                                _I64, _I32, _P, _P]),
+    "echo_commit_kv_q8": (_I32, [_P, _P, _P, _I32, _P, _P, _I32, _I32, _I32, _I32, _I32, _P, _P,
+                                 _P, _P, _I64, _I32, _P, _I32, _P, _P, _P, _P]),
+    "echo_build_block_tables": (_I32, [_P, _I32, _I32, _P, _I32, _P, _P, _P, _I32, _P, _P, _P,
+                                       _P, _I32, _P, _P, _P]),
     "echo_status_string": (ctypes.c_char_p, [_I32]),
     "echo_version": (ctypes.c_char_p, []),
 }
@@ -378,4 +395,79 @@ def echo_commit_kv(q_offsets, accept_len, accept_slots, max_depth, k_new, v_new,
                                  _ptr(status), _stream(stream))
     if check:
         _check(code, "echo_commit_kv")
+    return code
+
+
+def tree_verify_attn_paged_q8_workspace_size(R, max_rows, hq, hkv, max_pages,
+                                             head_dim=HEAD_DIM) -> int:
+    return int(load().echo_tree_verify_attn_paged_q8_workspace_size(R, max_rows, hq, hkv,
+                                                                    head_dim, max_pages))
+
+
+def echo_tree_verify_attn_paged_q8(q, k_new, v_new, kv_format, k_pages, v_pages, k_scale, v_scale,
+                                   page_size, block_table, prefix_len, q_offsets, tree_mask,
+                                   mask_words, R, max_rows, hq, hkv, head_dim, sm_scale, out, lse,
+                                   workspace, status=None, stream=None, check=True):
+    """Verification attention over an 8-bit paged KV cache.  Device tensors; k_pages is
+    [num_pages, Hkv, page_size, 128] bytes, k_scale [num_pages, Hkv, page_size / 32] float32,
+    out [max_rows, Hq, 128] bf16 bits."""
+    code = load().echo_tree_verify_attn_paged_q8(
+        _ptr(q), _ptr(k_new), _ptr(v_new), kv_format, _ptr(k_pages), _ptr(v_pages), _ptr(k_scale),
+        _ptr(v_scale), k_pages.shape[0], page_size, _ptr(block_table), block_table.shape[1],
+        _ptr(prefix_len), _ptr(q_offsets), _ptr(tree_mask), mask_words, R, max_rows, hq, hkv,
+        head_dim, float(sm_scale), _ptr(out), _ptr(lse), _ptr(workspace),
+        workspace.numel() * workspace.element_size(), _ptr(status), _stream(stream))
+    if check:
+        _check(code, "echo_tree_verify_attn_paged_q8")
+    return code
+
+
+def echo_store_kv_q8(k, v, slot_map, num_rows, hkv, head_dim, kv_format, k_pages, v_pages, k_scale,
+                     v_scale, page_size, status=None, stream=None, check=True):
+    """Quantise rows into an 8-bit paged KV cache at the slots of a slot map.  Device tensors;
+    k and v are [num_rows, Hkv, 128] bf16 bits whose rows may be strided (parts of one
+    projection's output), slot_map int64."""
+    for t in (k, v):
+        if t.stride(-1) != 1 or (hkv > 1 and t.stride(-2) != head_dim):
+            raise ValueError("the heads of a row of k and v must be contiguous")
+    # (the stride of a dimension of size 1 says nothing)
+    strides = [t.stride(0) if t.shape[0] > 1 else hkv * head_dim for t in (k, v)]
+    code = load().echo_store_kv_q8(
+        _ptr(k), _ptr(v), *strides, _ptr(slot_map), num_rows, hkv, head_dim,
+        kv_format, _ptr(k_pages), _ptr(v_pages), _ptr(k_scale), _ptr(v_scale), k_pages.shape[0],
+        page_size, _ptr(status), _stream(stream))
+    if check:
+        _check(code, "echo_store_kv_q8")
+    return code
+
+
+def echo_commit_kv_q8(q_offsets, accept_len, accept_slots, max_depth, k_new, v_new, R, max_rows,
+                      hkv, head_dim, kv_format, k_pages, v_pages, k_scale, v_scale, page_size,
+                      block_table, prefix_len, new_len, status=None, stream=None, check=True):
+    """Append each request's root and accepted slots to its 8-bit paged KV cache; new_len may
+    be prefix_len."""
+    code = load().echo_commit_kv_q8(
+        _ptr(q_offsets), _ptr(accept_len), _ptr(accept_slots), max_depth, _ptr(k_new), _ptr(v_new),
+        R, max_rows, hkv, head_dim, kv_format, _ptr(k_pages), _ptr(v_pages), _ptr(k_scale),
+        _ptr(v_scale), k_pages.shape[0], page_size, _ptr(block_table), block_table.shape[1],
+        _ptr(prefix_len), _ptr(new_len), _ptr(status), _stream(stream))
+    if check:
+        _check(code, "echo_commit_kv_q8")
+    return code
+
+
+def echo_build_block_tables(want_len, R, page_size, block_table, num_held, num_held_out,
+                            free_pages, num_free, num_free_out, row_offsets=None, row_start=None,
+                            slot_map=None, status=None, stream=None, check=True):
+    """Block tables (and the slot map of new rows, if given) from the requests' lengths.
+    Device tensors; block_table is [R, max_pages] int32, free_pages the stack of free pages,
+    slot_map int64."""
+    code = load().echo_build_block_tables(
+        _ptr(want_len), R, page_size, _ptr(block_table), block_table.shape[1], _ptr(num_held),
+        _ptr(num_held_out), _ptr(free_pages), free_pages.numel(), _ptr(num_free),
+        _ptr(num_free_out), _ptr(row_offsets), _ptr(row_start),
+        0 if slot_map is None else slot_map.numel(), _ptr(slot_map), _ptr(status),
+        _stream(stream))
+    if check:
+        _check(code, "echo_build_block_tables")
     return code

@@ -21,7 +21,7 @@ FLAGS = [
 ]
 
 
-# Per-file flags for the attention kernel:
+# Per-file flags for the attention kernels:
 # * its MFMA accumulators stay in VGPRs: left to its heuristics the compiler
 #   holds them in AGPRs and copies all of them to VGPRs and back on every tile
 #   (a v_accvgpr read and write per register), which costs as many VALU cycles
@@ -33,6 +33,7 @@ FLAGS = [
 # The fused step's tail kernel holds the attention's combine and is built the
 # same way, so that its merges are the combine launch's to the bit.
 FILE_FLAGS = {
+    "attn_q8.hip": ["-mllvm", "--amdgpu-mfma-vgpr-form=1", "-fno-honor-nans"],
     "attn.hip": ["-mllvm", "--amdgpu-mfma-vgpr-form=1", "-fno-honor-nans"],
     "tail.hip": ["-mllvm", "--amdgpu-mfma-vgpr-form=1", "-fno-honor-nans"],
 }

@@ -497,3 +497,162 @@ int32_t echo_commit_kv(const int32_t* q_offsets, const int32_t* accept_len,
 }
 
 }  // extern "C"
+
+namespace {
+// The 8-bit cache's arguments: ECHO_OK with *c filled, or the error code.
+int32_t cache_q8_args(int32_t kv_format, uint8_t* k_pages, uint8_t* v_pages, float* k_scale,
+                      float* v_scale, int64_t num_pages, int32_t page_size, int32_t num_kv_heads,
+                      int32_t head_dim, echo::CacheQ8Args* c) {
+  if (num_pages < 1 || num_kv_heads < 1 || page_size < 1) return ECHO_ERR_INVALID_ARG;
+  if (kv_format != ECHO_KV_E4M3 && kv_format != ECHO_KV_E5M2) return ECHO_ERR_INVALID_ARG;
+  if (page_size < ECHO_KV_BLOCK || (page_size & (page_size - 1)) != 0) return ECHO_ERR_UNSUPPORTED;
+  if (head_dim != ECHO_HEAD_DIM || num_kv_heads > (1 << 20)) return ECHO_ERR_UNSUPPORTED;
+  // (compared by division: num_pages is any 64-bit number)
+  if (num_pages >= (int64_t(1) << 31) / page_size) return ECHO_ERR_UNSUPPORTED;
+  if (!k_pages || !v_pages || !k_scale || !v_scale) return ECHO_ERR_INVALID_ARG;
+  if ((reinterpret_cast<uintptr_t>(k_pages) | reinterpret_cast<uintptr_t>(v_pages)) & 15u)
+    return ECHO_ERR_INVALID_ARG;
+  if ((reinterpret_cast<uintptr_t>(k_scale) | reinterpret_cast<uintptr_t>(v_scale)) & 3u)
+    return ECHO_ERR_INVALID_ARG;
+  *c = echo::CacheQ8Args{kv_format, k_pages, v_pages, k_scale, v_scale, num_pages, page_size,
+                         num_kv_heads};
+  return ECHO_OK;
+}
+}  // namespace
+
+extern "C" {
+
+size_t echo_tree_verify_attn_paged_q8_workspace_size(int32_t R, int32_t max_rows,
+                                                     int32_t num_q_heads, int32_t num_kv_heads,
+                                                     int32_t head_dim,
+                                                     int32_t max_pages_per_request) {
+  if (R < 1 || max_rows < 0 || num_q_heads < 1 || num_kv_heads < 1 ||
+      head_dim != ECHO_HEAD_DIM || max_pages_per_request < 1)
+    return 0;
+  return echo::attn_q8_workspace_bytes(R, max_rows, num_q_heads, num_kv_heads,
+                                       max_pages_per_request);
+}
+
+int32_t echo_tree_verify_attn_paged_q8(
+    const uint16_t* q, const uint16_t* k_new, const uint16_t* v_new, int32_t kv_format,
+    const uint8_t* k_pages, const uint8_t* v_pages, const float* k_scale, const float* v_scale,
+    int64_t num_pages, int32_t page_size, const int32_t* block_table,
+    int32_t max_pages_per_request, const int32_t* prefix_len, const int32_t* q_offsets,
+    const uint32_t* tree_mask, int32_t mask_words, int32_t R, int32_t max_rows,
+    int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim, float sm_scale, uint16_t* out,
+    float* lse, void* workspace, size_t workspace_bytes, int32_t* status, echo_stream_t stream) {
+  if (R < 1 || max_rows < 0 || num_q_heads < 1 || num_kv_heads < 1 || mask_words < 1 ||
+      max_pages_per_request < 1)
+    return ECHO_ERR_INVALID_ARG;
+  if (num_q_heads % num_kv_heads != 0 || !scale_ok(sm_scale)) return ECHO_ERR_INVALID_ARG;
+  echo::AttnQ8Args a{};
+  const int32_t rc = cache_q8_args(kv_format, const_cast<uint8_t*>(k_pages),
+                                   const_cast<uint8_t*>(v_pages), const_cast<float*>(k_scale),
+                                   const_cast<float*>(v_scale), num_pages, page_size, num_kv_heads,
+                                   head_dim, &a.cache);
+  if (rc != ECHO_OK) return rc;
+  if (R > ECHO_MAX_REQUESTS) return ECHO_ERR_UNSUPPORTED;
+  if (int64_t(max_pages_per_request) * page_size >= (int64_t(1) << 31)) return ECHO_ERR_UNSUPPORTED;
+  if (int64_t(max_rows) * num_q_heads >= (int64_t(1) << 26)) return ECHO_ERR_UNSUPPORTED;
+  if (!q || !k_new || !v_new || !block_table || !prefix_len || !q_offsets || !tree_mask || !out ||
+      !workspace)
+    return ECHO_ERR_INVALID_ARG;
+  if (!aligned256(workspace) ||
+      workspace_bytes < echo::attn_q8_workspace_bytes(R, max_rows, num_q_heads, num_kv_heads,
+                                                      max_pages_per_request))
+    return ECHO_ERR_WORKSPACE;
+  const uintptr_t mis = reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(k_new) |
+                        reinterpret_cast<uintptr_t>(v_new) | reinterpret_cast<uintptr_t>(out);
+  if (mis & 15u) return ECHO_ERR_INVALID_ARG;
+  if (max_rows == 0) return ECHO_OK;
+  a.q = q;
+  a.k_new = k_new;
+  a.v_new = v_new;
+  a.block_table = block_table;
+  a.max_pages = max_pages_per_request;
+  a.prefix_len = prefix_len;
+  a.q_offsets = q_offsets;
+  a.tree_mask = tree_mask;
+  a.mask_words = mask_words;
+  a.R = R;
+  a.max_rows = max_rows;
+  a.hq = num_q_heads;
+  a.sm_scale = sm_scale;
+  a.out = out;
+  a.lse = lse;
+  a.workspace = workspace;
+  a.status = status;
+  return echo::launch_tree_verify_attn_q8(a, as_stream(stream));
+}
+
+int32_t echo_store_kv_q8(const uint16_t* k, const uint16_t* v, int64_t k_stride, int64_t v_stride,
+                         const int64_t* slot_map, int32_t num_rows, int32_t num_kv_heads,
+                         int32_t head_dim, int32_t kv_format, uint8_t* k_pages, uint8_t* v_pages,
+                         float* k_scale, float* v_scale, int64_t num_pages, int32_t page_size,
+                         int32_t* status, echo_stream_t stream) {
+  if (num_rows < 0) return ECHO_ERR_INVALID_ARG;
+  echo::CacheQ8Args c;
+  const int32_t rc = cache_q8_args(kv_format, k_pages, v_pages, k_scale, v_scale, num_pages,
+                                   page_size, num_kv_heads, head_dim, &c);
+  if (rc != ECHO_OK) return rc;
+  if (num_rows == 0) return ECHO_OK;
+  if (!k || !v || !slot_map) return ECHO_ERR_INVALID_ARG;
+  const int64_t row = int64_t(num_kv_heads) * ECHO_HEAD_DIM;
+  if (k_stride < row || v_stride < row || ((k_stride | v_stride) & 7) != 0)
+    return ECHO_ERR_INVALID_ARG;
+  if (k_stride >= (int64_t(1) << 31) || v_stride >= (int64_t(1) << 31)) return ECHO_ERR_UNSUPPORTED;
+  if ((reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v)) & 15u)
+    return ECHO_ERR_INVALID_ARG;
+  return echo::launch_store_kv_q8(k, v, k_stride, v_stride, slot_map, num_rows, c, status,
+                                  as_stream(stream));
+}
+
+int32_t echo_commit_kv_q8(const int32_t* q_offsets, const int32_t* accept_len,
+                          const int32_t* accept_slots, int32_t max_depth, const uint16_t* k_new,
+                          const uint16_t* v_new, int32_t R, int32_t max_rows,
+                          int32_t num_kv_heads, int32_t head_dim, int32_t kv_format,
+                          uint8_t* k_pages, uint8_t* v_pages, float* k_scale, float* v_scale,
+                          int64_t num_pages, int32_t page_size, const int32_t* block_table,
+                          int32_t max_pages_per_request, const int32_t* prefix_len,
+                          int32_t* new_len, int32_t* status, echo_stream_t stream) {
+  if (R < 1 || max_rows < 0 || max_pages_per_request < 1) return ECHO_ERR_INVALID_ARG;
+  if (max_depth < 1 || max_depth > ECHO_MAX_DEPTH || R > ECHO_MAX_REQUESTS)
+    return ECHO_ERR_UNSUPPORTED;
+  echo::CacheQ8Args c;
+  const int32_t rc = cache_q8_args(kv_format, k_pages, v_pages, k_scale, v_scale, num_pages,
+                                   page_size, num_kv_heads, head_dim, &c);
+  if (rc != ECHO_OK) return rc;
+  if (!q_offsets || !accept_len || !accept_slots || !k_new || !v_new || !block_table ||
+      !prefix_len || !new_len)
+    return ECHO_ERR_INVALID_ARG;
+  if ((reinterpret_cast<uintptr_t>(k_new) | reinterpret_cast<uintptr_t>(v_new)) & 15u)
+    return ECHO_ERR_INVALID_ARG;
+  return echo::launch_commit_kv_q8(q_offsets, accept_len, accept_slots, max_depth, k_new, v_new, R,
+                                   max_rows, c, block_table, max_pages_per_request, prefix_len,
+                                   new_len, status, as_stream(stream));
+}
+
+int32_t echo_build_block_tables(const int32_t* want_len, int32_t R, int32_t page_size,
+                                int32_t* block_table, int32_t max_pages_per_request,
+                                const int32_t* num_held, int32_t* num_held_out,
+                                int32_t* free_pages, int32_t max_free, const int32_t* num_free,
+                                int32_t* num_free_out, const int32_t* row_offsets,
+                                const int32_t* row_start, int32_t max_rows, int64_t* slot_map,
+                                int32_t* status, echo_stream_t stream) {
+  if (R < 1 || page_size < 1 || max_pages_per_request < 1 || max_free < 1)
+    return ECHO_ERR_INVALID_ARG;
+  if ((page_size & (page_size - 1)) != 0 || R > ECHO_MAX_REQUESTS ||
+      int64_t(R) * max_pages_per_request >= (int64_t(1) << 31))
+    return ECHO_ERR_UNSUPPORTED;
+  if (!want_len || !block_table || !num_held || !num_held_out || !free_pages || !num_free ||
+      !num_free_out)
+    return ECHO_ERR_INVALID_ARG;
+  if (slot_map != nullptr && (max_rows < 0 || !row_offsets || !row_start))
+    return ECHO_ERR_INVALID_ARG;
+  const echo::TablesArgs a{want_len, R, page_size, block_table, max_pages_per_request, num_held,
+                           num_held_out, free_pages, max_free, num_free, num_free_out,
+                           row_offsets, row_start, max_rows, slot_map, status};
+  return echo::launch_build_block_tables(a, as_stream(stream));
+}
+
+}  // extern "C"

@@ -114,6 +114,69 @@ int32_t launch_commit_kv(const int32_t* q_offsets, const int32_t* accept_len,
 
 int device_cu_count();
 
+// The 8-bit paged cache (kvq8.hip, attn_q8.hip): ECHO_KV_* format, pages
+// [num_pages][Hkv][page_size][128] bytes, scales [num_pages][Hkv][page_size / 32].
+struct CacheQ8Args {
+  int32_t format;
+  uint8_t* k_pages;
+  uint8_t* v_pages;
+  float* k_scale;
+  float* v_scale;
+  int64_t num_pages;
+  int32_t page_size;
+  int32_t hkv;
+};
+int32_t launch_store_kv_q8(const uint16_t* k, const uint16_t* v, int64_t k_stride, int64_t v_stride,
+                           const int64_t* slot_map, int32_t num_rows, const CacheQ8Args& a,
+                           int32_t* status, hipStream_t stream);
+int32_t launch_commit_kv_q8(const int32_t* q_offsets, const int32_t* accept_len,
+                            const int32_t* accept_slots, int32_t max_depth, const uint16_t* k_new,
+                            const uint16_t* v_new, int32_t R, int32_t max_rows,
+                            const CacheQ8Args& a, const int32_t* block_table, int32_t max_pages,
+                            const int32_t* prefix_len, int32_t* new_len, int32_t* status,
+                            hipStream_t stream);
+struct AttnQ8Args {
+  const uint16_t* q;
+  const uint16_t* k_new;
+  const uint16_t* v_new;
+  CacheQ8Args cache;
+  const int32_t* block_table;
+  int32_t max_pages;
+  const int32_t* prefix_len;
+  const int32_t* q_offsets;
+  const uint32_t* tree_mask;
+  int32_t mask_words;
+  int32_t R, max_rows, hq;
+  float sm_scale;
+  uint16_t* out;
+  float* lse;
+  void* workspace;
+  int32_t* status;
+};
+int32_t launch_tree_verify_attn_q8(const AttnQ8Args& a, hipStream_t stream);
+size_t attn_q8_workspace_bytes(int32_t R, int32_t max_rows, int32_t hq, int32_t hkv,
+                               int32_t max_pages);
+
+// Block tables from lengths (tables.hip); slot_map null: no slot map.
+struct TablesArgs {
+  const int32_t* want_len;
+  int32_t R, page_size;
+  int32_t* block_table;
+  int32_t max_pages;
+  const int32_t* num_held;
+  int32_t* num_held_out;
+  int32_t* free_pages;
+  int32_t max_free;
+  const int32_t* num_free;
+  int32_t* num_free_out;
+  const int32_t* row_offsets;
+  const int32_t* row_start;
+  int32_t max_rows;
+  int64_t* slot_map;
+  int32_t* status;
+};
+int32_t launch_build_block_tables(const TablesArgs& a, hipStream_t stream);
+
 // Fused step (front.hip): the end of the gate, flatten & pack and the attention plan
 // (contiguous cache) in one launch, after launch_gate_select_only (unless
 // front_gate_list is negative) and before launch_tree_verify_attn_main.
