@@ -554,6 +554,10 @@ int32_t echo_tree_verify_attn_paged_q8(
   if (R > ECHO_MAX_REQUESTS) return ECHO_ERR_UNSUPPORTED;
   if (int64_t(max_pages_per_request) * page_size >= (int64_t(1) << 31)) return ECHO_ERR_UNSUPPORTED;
   if (int64_t(max_rows) * num_q_heads >= (int64_t(1) << 26)) return ECHO_ERR_UNSUPPORTED;
+  // (32-bit numbers of the cache's blocks and of the tables' entries)
+  if (num_pages * (page_size / ECHO_KV_BLOCK) >= (int64_t(1) << 32) / num_kv_heads ||
+      int64_t(R) * max_pages_per_request >= (int64_t(1) << 31))
+    return ECHO_ERR_UNSUPPORTED;
   if (!q || !k_new || !v_new || !block_table || !prefix_len || !q_offsets || !tree_mask || !out ||
       !workspace)
     return ECHO_ERR_INVALID_ARG;

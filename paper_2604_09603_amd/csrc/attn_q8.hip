@@ -3,7 +3,7 @@
 // for large block tables:
 //
 //   q8_pages    checks the page ids (small tables: the plan does).
-//   q8_plan     one workgroup.  A unit is one KV head of one request with up to 64 of
+//   q8_plan     one workgroup.  A unit is one KV head of one request with up to 48 of
 //               its rows (verify slots x query heads of the GQA group); its tiles
 //               are first the tree's (32 new keys each), then the prefix's, one
 //               32-token block each.  The tiles of all units are cut into equal
@@ -11,7 +11,7 @@
 //               lie in one piece, so nothing is gained by waves that read the heads
 //               of the same tokens side by side, and one head's keys are spread over
 //               as many waves as they can feed.
-//   q8_main     persistent, one workgroup of four independent waves per CU.  A wave
+//   q8_main     persistent, one workgroup of eight independent waves per CU.  A wave
 //               copies its tiles HBM -> LDS into a ring of its own with direct-to-LDS
 //               loads, converts a tile to bfloat16 (exact) and multiplies it with
 //               all rows of the unit: S^T = K Q^T and O^T = V^T P^T on
@@ -33,45 +33,76 @@
 namespace echo {
 namespace {
 
-constexpr int kQ8Rows = 64;        // rows per unit
-constexpr int kQ8Waves = 4;        // waves per workgroup and CU
-constexpr int kQ8Stages = 4;       // tiles in a wave's ring
-constexpr int kQ8ScaleOff = 2 * kBlockBytes;      // a stage: K, V, then the two scales
-constexpr int kQ8StageBytes = 2 * kBlockBytes + 256;
+constexpr int kQ8Rows = 32;        // rows per unit
+constexpr int kQ8Waves = 4;        // waves per workgroup
+constexpr int kQ8Wgs = 2;          // workgroups per CU: two waves per SIMD
+constexpr int kQ8StepKeys = 64;    // keys per step of the main loop: two tiles
+constexpr int kQ8Slot = 2 * kBlockBytes;          // one tensor's tiles of a step
 constexpr int kQ8Scratch = 16 * kD * 2;           // 16 rows of bfloat16 V (tree tiles)
-constexpr int kQ8WaveLds = kQ8Stages * kQ8StageBytes + kQ8Scratch;
-static_assert(kQ8Waves * kQ8WaveLds <= 160 * 1024, "gfx950 LDS per workgroup");
-constexpr int kQ8Copies = 9;       // copy instructions per tile: 4 of K, 4 of V, the scales
+constexpr int kQ8WaveLds = 2 * kQ8Slot + kQ8Scratch;  // K, V, scratch
+static_assert(kQ8Wgs * kQ8Waves * kQ8WaveLds <= 160 * 1024, "gfx950 LDS per CU");
+constexpr int kQ8Copies = 8;       // copy instructions per step and tensor
+constexpr int kSplitBytes = 2 * kD;               // a row as two 8-bit numbers per dim
+// What a step costs a workgroup that has 4, 2 or 1 gangs at work, relative to each other.
+constexpr double kQ8Cost1 = 1.4, kQ8Cost2 = 2.2, kQ8Cost4 = 4.0;
 constexpr int kPlanThreads = 1024;
+constexpr int kPlanRows = kPlanThreads / 16;      // rows that a workgroup beside the plan's splits
 constexpr int kPlanPages = 8 * kPlanThreads;      // block-table entries the plan checks itself
 
 typedef int intx2 __attribute__((ext_vector_type(2)));
+typedef int intx8 __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) intx2 lds_intx2_t;
+typedef uint32_t uint4v __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) const uint4v lds_uint4_t;
+typedef __attribute__((address_space(3))) char lds_char_t;
+typedef float floatx16 __attribute__((ext_vector_type(16)));
 
-// One request as the plan shapes it: `units` = Hkv * passes units of tpu tiles from tile0
-// on (unit = head * passes + pass), ntail of each unit's tiles are the tree's.
+// The LDS byte address x as a pointer (constant offsets go into the instructions).
+__device__ __forceinline__ lds_char_t* lds_at(uint32_t x) { return (lds_char_t*)(uintptr_t(x)); }
+
+// A gang is the k waves (1, 2 or 4, of one workgroup) that take the same steps of a unit,
+// each with up to 32 of its rows: one copies the tiles from HBM, the others at about the
+// same time from the caches.  A request's k follows its rows per head; requests of
+// the same k form a class, whose steps are cut into equal ranges, one per gang.
+constexpr int kQ8Classes = 3;  // k = 1 << class
+
+// One request as the plan shapes it, in the list of its class: Hkv * passes units (unit =
+// head * passes + pass) of tpu steps each, from step tile0 of the class on; gang member
+// m has rows rpp (k pass + m) .. of a head.
 struct Q8Req {
   int32_t tile0, tpu;
   int32_t q0, nslots;
-  int32_t P, passes, rpp, ntail;
+  int32_t P, r, passes, rpp;
 };
 
-// A wave's range of tiles and where it starts.  cut_last: if the range's first tile lies
-// inside a unit, and is the first range start that does, the last wave of that unit
-// (else 0): the unit's sums are merged from waves b - 1 .. cut_last.
+// A wave's range of steps and where it starts (req: place in the class's list).
+// Gang g of the class is members m = 0 .. k - 1 at wave wave_of(g) + m.  cut_last: if the
+// range's first step lies inside a unit, and is the first range start that does, the
+// last gang of that unit (else 0): the unit's sums are merged from gangs gang - 1 ..
+// cut_last.
 struct Q8Start {
-  int32_t lo, hi, r, unit;
-  int32_t cut_last, pad[3];
+  int32_t lo, hi, req, unit;
+  int32_t gang, cut_last, k, member;
+  int32_t wg0, nwg, pad[2];  // the class's workgroups
   Q8Req q;
 };
-static_assert(sizeof(Q8Start) == 64, "one 64-byte record");
+static_assert(sizeof(Q8Start) == 80, "20 words");
+
+// Gangs go round the class's workgroups, so that few of them spread over the CUs.
+__device__ __forceinline__ int q8_wave_of(int g, int k, int wg0, int nwg) {
+  return (wg0 + g % nwg) * kQ8Waves + g / nwg * k;
+}
 
 struct Q8Ws {
   Q8Start* starts;   // [waves]
-  Q8Req* reqs;       // [R]
+  Q8Req* reqs;       // [R], class by class
   int32_t* bad;      // [R][chunks] flags of q8_pages
-  float* part_ml;    // [waves][2][64][4]: max, sum, sum of the weights used, scale exponent
-  _Float16* part_o;  // [waves][2][64][128]
+  uint8_t* qs;       // [max_rows][Hq] rows split in two 8-bit numbers: see q8_split
+  int32_t* qe;       // [max_rows][Hq] their scale exponents
+  uint8_t* ks;       // [max_rows][Hkv] the new keys, the same
+  int32_t* ke;
+  float* part_ml;    // [waves][2][32][4]: max, sum, sum of the weights used, scale exponent
+  _Float16* part_o;  // [waves][2][32][128]
 };
 
 struct Q8Args {
@@ -102,7 +133,8 @@ __host__ inline bool q8_plan_checks(int R, int max_pages) {
   return (long long)R * max_pages <= kPlanPages;
 }
 
-__host__ inline Q8Ws q8_layout(void* base, int R, int max_pages, int nw, size_t* bytes) {
+__host__ inline Q8Ws q8_layout(void* base, int R, int max_rows, int hq, int hkv, int max_pages,
+                               int nw, size_t* bytes) {
   char* p = static_cast<char*>(base);
   Q8Ws w;
   w.starts = reinterpret_cast<Q8Start*>(p);
@@ -111,6 +143,15 @@ __host__ inline Q8Ws q8_layout(void* base, int R, int max_pages, int nw, size_t*
   p += al(size_t(R) * sizeof(Q8Req));
   w.bad = reinterpret_cast<int32_t*>(p);
   if (!q8_plan_checks(R, max_pages)) p += al(size_t(R) * size_t(q8_page_chunks(max_pages)) * 4);
+  const size_t nq = size_t(max_rows) * size_t(hq), nk = size_t(max_rows) * size_t(hkv);
+  w.qs = reinterpret_cast<uint8_t*>(p);
+  p += al(nq * kSplitBytes);
+  w.qe = reinterpret_cast<int32_t*>(p);
+  p += al(nq * 4);
+  w.ks = reinterpret_cast<uint8_t*>(p);
+  p += al(nk * kSplitBytes);
+  w.ke = reinterpret_cast<int32_t*>(p);
+  p += al(nk * 4);
   w.part_ml = reinterpret_cast<float*>(p);
   p += al(size_t(nw) * 2 * kQ8Rows * 4 * sizeof(float));
   w.part_o = reinterpret_cast<_Float16*>(p);
@@ -119,7 +160,7 @@ __host__ inline Q8Ws q8_layout(void* base, int R, int max_pages, int nw, size_t*
   return w;
 }
 
-int q8_waves() { return device_cu_count() * kQ8Waves; }
+int q8_waves() { return device_cu_count() * kQ8Wgs * kQ8Waves; }
 
 // Pages of a request's prefix, or -1 if its length does not fit its table row.
 __device__ __forceinline__ int prefix_pages(long long P, const Q8Args& a) {
@@ -141,28 +182,79 @@ __global__ __launch_bounds__(kPageChunk) void q8_pages_kernel(Q8Args a, int32_t*
 }
 
 // ---------------------------------------------------------------- plan ----
-__device__ __forceinline__ Q8Req shape_of(const Q8Args& a, int r, bool ok) {
+// The request's shape and class (-1: nothing to do).
+__device__ __forceinline__ Q8Req shape_of(const Q8Args& a, int r, bool ok, int& cls) {
   Q8Req s = {};
+  cls = -1;
   if (!ok) return s;
   s.q0 = a.q_offsets[r];
   s.nslots = a.q_offsets[r + 1] - s.q0;
   s.P = a.prefix_len[r];
+  s.r = r;
   const int rows = s.nslots * a.G;
-  s.passes = (rows + kQ8Rows - 1) / kQ8Rows;
-  if (s.passes == 0) return s;
-  s.rpp = (rows + s.passes - 1) / s.passes;
-  s.ntail = (s.nslots + kTileKeys - 1) / kTileKeys;
-  s.tpu = s.ntail + int(((long long)s.P + kTileKeys - 1) / kTileKeys);
+  if (rows == 0) return s;
+  cls = rows <= kQ8Rows ? 0 : rows <= 2 * kQ8Rows ? 1 : 2;
+  const int k = 1 << cls;
+  s.passes = (rows + k * kQ8Rows - 1) / (k * kQ8Rows);
+  s.rpp = (rows + k * s.passes - 1) / (k * s.passes);
+  s.tpu = (s.nslots + kTileKeys - 1) / kTileKeys +
+          int(((long long)s.P + kQ8StepKeys - 1) / kQ8StepKeys);
   return s;
 }
 
+// A row in bfloat16 as two e4m3 numbers per dim: x = 2^(e - 127) (hi + lo / 16), 2^(127 - e)
+// bringing the row's largest magnitude to [128, 256).  That holds a bfloat16's eight
+// bits exactly, and values below 2^-14 of the row's largest to 2^-22 of it.  A row is
+// stored as its 128 hi, then its 128 lo.  16 lanes per row, eight dims each.
+__device__ __forceinline__ void q8_split(const uint16_t* rows, uint8_t* split, int32_t* exps,
+                                         long long r, int lane16) {
+  const uint4 x = reinterpret_cast<const uint4*>(rows + r * kD)[lane16];
+  uint32_t m = max(max(finite_mag2(x.x), finite_mag2(x.y)), max(finite_mag2(x.z), finite_mag2(x.w)));
+#pragma unroll
+  for (int d = 8; d > 0; d >>= 1) m = max(m, uint32_t(__shfl_xor(int(m), d)));
+  // (m >> 7: the exponent's bits; a zero row takes any scale.  Both exponents, e and
+  // e - 4, and 2^(127 - e) are representable)
+  const int e = min(max(int(m >> 7) - 7, 7), 247);
+  const float s = __uint_as_float(uint32_t(254 - e) << 23);
+  const auto two = [&](uint32_t w, float (&y)[2]) {
+    y[0] = __uint_as_float(w << 16) * s;
+    y[1] = __uint_as_float(w & 0xFFFF0000u) * s;
+  };
+  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+  uint32_t hi[2], lo[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    float a[2], b[2];
+    two(w[2 * h], a);
+    two(w[2 * h + 1], b);
+    hi[h] = encode4<ECHO_KV_E4M3>(a[0], a[1], b[0], b[1]);
+    const floatx2v c = __builtin_amdgcn_cvt_pk_f32_fp8(int(hi[h]), false);
+    const floatx2v d = __builtin_amdgcn_cvt_pk_f32_fp8(int(hi[h]), true);
+    lo[h] = encode4<ECHO_KV_E4M3>((a[0] - c[0]) * 16.0f, (a[1] - c[1]) * 16.0f, (b[0] - d[0]) * 16.0f,
+                                  (b[1] - d[1]) * 16.0f);
+  }
+  uint8_t* p = split + r * kSplitBytes;
+  reinterpret_cast<uint2*>(p)[lane16] = make_uint2(hi[0], hi[1]);
+  reinterpret_cast<uint2*>(p + kD)[lane16] = make_uint2(lo[0], lo[1]);
+  if (lane16 == 0) exps[r] = e;
+}
+
+// Workgroup 0 plans; the others split the query rows and the new keys.
 __global__ __launch_bounds__(kPlanThreads) void q8_plan_kernel(Q8Args a, Q8Ws ws, int nw_max,
                                                                int chunks) {
-  extern __shared__ int32_t s_tile0[];  // R + 1: first tile of each request
+  extern __shared__ int32_t s_tile0[];  // [R] first step of each listed request, [R] the request
   __shared__ uint8_t s_bad[ECHO_MAX_REQUESTS + 1];
-  __shared__ long long s_total[kPlanThreads / kWave + 1];
-  __shared__ int s_scan[kPlanThreads / kWave + 1];
+  __shared__ long long s_total[kQ8Classes][kPlanThreads / kWave];
+  __shared__ int2 s_scan[kPlanThreads / kWave + 1];
+  int32_t* s_req = s_tile0 + a.R;
   const int tid = threadIdx.x;
+  if (blockIdx.x > 0) {
+    const long long r = (long long)(blockIdx.x - 1) * kPlanRows + tid / 16;
+    const long long nq = (long long)a.max_rows * a.hq, nk = (long long)a.max_rows * a.hkv;
+    if (r < nq) q8_split(a.q, ws.qs, ws.qe, r, tid & 15);
+    else if (r - nq < nk) q8_split(a.k_new, ws.ks, ws.ke, r - nq, tid & 15);
+    return;
+  }
   const int R = a.R;
   int bits = 0;
   // requests whose offsets, length or pages cannot be used
@@ -193,71 +285,132 @@ __global__ __launch_bounds__(kPlanThreads) void q8_plan_kernel(Q8Args a, Q8Ws ws
     }
     __syncthreads();
   }
-  // tiles of every request; 64-bit first, as offsets that overlap may ask for any number
-  long long mine = 0;
+  // requests and steps of every class; 64-bit and capped, as offsets that overlap may ask
+  // for any number
+  long long mine[kQ8Classes] = {};  // steps, and requests above bit 48
   for (int r = tid; r < R; r += kPlanThreads) {
     if (s_bad[r]) bits |= ECHO_DATA_BAD_OFFSETS;
-    const Q8Req s = shape_of(a, r, !s_bad[r]);
-    mine += (long long)a.hkv * s.passes * s.tpu;
+    int cls;
+    const Q8Req s = shape_of(a, r, !s_bad[r], cls);
+    for (int c = 0; c < kQ8Classes; ++c)
+      if (c == cls) mine[c] += min((long long)a.hkv * s.passes * s.tpu, 1ll << 32) + (1ll << 48);
   }
-  for (int d = kWave / 2; d > 0; d >>= 1) mine += __shfl_xor(mine, d);
-  if ((tid & (kWave - 1)) == 0) s_total[tid / kWave] = mine;
+#pragma unroll
+  for (int c = 0; c < kQ8Classes; ++c) {
+    for (int d = kWave / 2; d > 0; d >>= 1) mine[c] += __shfl_xor(mine[c], d);
+    if ((tid & (kWave - 1)) == 0) s_total[c][tid / kWave] = mine[c];
+  }
   __syncthreads();
-  long long T = 0;
-  for (int k = 0; k < kPlanThreads / kWave; ++k) T += s_total[k];
-  if (T > 0x7FFFFFFFll) {
+  long long T[kQ8Classes], all = 0;
+  int count[kQ8Classes];
+#pragma unroll
+  for (int c = 0; c < kQ8Classes; ++c) {
+    long long x = 0;
+    for (int k = 0; k < kPlanThreads / kWave; ++k) x += s_total[c][k];
+    count[c] = int(x >> 48);
+    T[c] = x & ((1ll << 48) - 1);
+    all += T[c];
+  }
+  if (all > 0x7FFFFFFFll) {
     bits |= ECHO_DATA_BAD_OFFSETS;
-    T = 0;
+    all = 0;
   }
   wave_status_or(a.status, bits);
-  const int nw = T < nw_max ? int(T) : nw_max;
-  for (int b = nw + tid; b < nw_max; b += kPlanThreads) ws.starts[b] = Q8Start{};
-  if (T == 0) return;
-  int run = 0;
+  for (int b = tid; b < nw_max; b += kPlanThreads) ws.starts[b].lo = ws.starts[b].hi = ws.starts[b].cut_last = 0;
+  if (all == 0) return;
+  // the workgroups of each class: by cost, at least one where there is work
+  const int wgs = nw_max / kQ8Waves;
+  int wg0[kQ8Classes], nwg[kQ8Classes];
+  {
+    const double cost[kQ8Classes] = {kQ8Cost1 * double(T[0]), kQ8Cost2 * double(T[1]),
+                                     kQ8Cost4 * double(T[2])};
+    const double total = cost[0] + cost[1] + cost[2];
+    int left = wgs, need = (T[0] > 0) + (T[1] > 0) + (T[2] > 0);
+    int at = 0;
+#pragma unroll
+    for (int c = 0; c < kQ8Classes; ++c) {
+      int n = 0;
+      if (T[c] > 0) {
+        need -= 1;
+        n = need == 0 ? left : min(max(int(wgs * cost[c] / total + 0.5), 1), left - need);
+      }
+      wg0[c] = at;
+      nwg[c] = n;
+      at += n;
+      left -= n;
+    }
+  }
+  // the classes' lists of requests
+  int run_n[kQ8Classes] = {0, count[0], count[0] + count[1]}, run_t[kQ8Classes] = {};
   for (int base = 0; base < R; base += kPlanThreads) {
     const int r = base + tid;
     Q8Req s = {};
-    if (r < R) s = shape_of(a, r, !s_bad[r]);
-    int tot;
-    const int ex = block_exclusive_sum<kPlanThreads>(a.hkv * s.passes * s.tpu, s_scan, &tot);
-    s.tile0 = run + ex;
-    if (r < R) {
-      s_tile0[r] = s.tile0;
-      ws.reqs[r] = s;
+    int cls = -1;
+    if (r < R) s = shape_of(a, r, !s_bad[r], cls);
+    const int steps = a.hkv * s.passes * s.tpu;
+#pragma unroll
+    for (int c = 0; c < kQ8Classes; ++c) {
+      int n_tot, t_tot;
+      const int2 ex = block_exclusive_sum2<kPlanThreads>(
+          make_int2(c == cls ? 1 : 0, c == cls ? steps : 0), s_scan, &n_tot, &t_tot);
+      if (c == cls) {
+        s.tile0 = run_t[c] + ex.y;
+        s_tile0[run_n[c] + ex.x] = s.tile0;
+        s_req[run_n[c] + ex.x] = r;
+        ws.reqs[run_n[c] + ex.x] = s;
+      }
+      run_n[c] += n_tot;
+      run_t[c] += t_tot;
     }
-    run += tot;
   }
-  if (tid == 0) s_tile0[R] = run;
   __syncthreads();
-  const DivBy by_t(T), by_nw(nw);
-  for (int b = tid; b < nw; b += kPlanThreads) {
-    Q8Start st = {};
-    st.lo = int(range_lo(T, b, by_nw));
-    st.hi = int(range_lo(T, b + 1, by_nw));
-    st.r = upper_bound_idx(s_tile0, R + 1, st.lo);
-    st.q = shape_of(a, st.r, true);
-    st.q.tile0 = s_tile0[st.r];
-    st.unit = (st.lo - st.q.tile0) / st.q.tpu;
-    const int u0 = st.q.tile0 + st.unit * st.q.tpu;
-    if (u0 < st.lo && int(range_lo(T, b - 1, by_nw)) <= u0)
-      st.cut_last = range_of((long long)u0 + st.q.tpu - 1, T, nw, by_t);
-    ws.starts[b] = st;
+  int first = 0;
+#pragma unroll
+  for (int c = 0; c < kQ8Classes; ++c) {
+    if (T[c] > 0) {
+      const int k = 1 << c;
+      const long long gangs = (long long)nwg[c] * (kQ8Waves / k);
+      const int ng = int(T[c] < gangs ? T[c] : gangs);
+      const DivBy by_t(T[c]), by_n(ng);
+      for (int x = tid; x < ng * k; x += kPlanThreads) {
+        Q8Start st = {};
+        st.gang = x >> c;
+        st.member = x & (k - 1);
+        st.k = k;
+        st.wg0 = wg0[c];
+        st.nwg = nwg[c];
+        st.lo = int(range_lo(T[c], st.gang, by_n));
+        st.hi = int(range_lo(T[c], st.gang + 1, by_n));
+        st.req = first + upper_bound_idx(s_tile0 + first, count[c], st.lo);
+        int cls;
+        st.q = shape_of(a, s_req[st.req], true, cls);
+        st.q.tile0 = s_tile0[st.req];
+        st.unit = (st.lo - st.q.tile0) / st.q.tpu;
+        const int u0 = st.q.tile0 + st.unit * st.q.tpu;
+        if (u0 < st.lo && int(range_lo(T[c], st.gang - 1, by_n)) <= u0)
+          st.cut_last = range_of((long long)u0 + st.q.tpu - 1, T[c], ng, by_t);
+        ws.starts[q8_wave_of(st.gang, k, wg0[c], nwg[c]) + st.member] = st;
+      }
+    }
+    first += count[c];
   }
 }
 
 // ---------------------------------------------------------------- main ----
 // A tile in LDS: 32 rows x 128 bytes per tensor.  The 16-byte chunk c of row r is at chunk
-// position c ^ f(r), f(r) = ((r >> 1) ^ 4 (r >> 4)) & 7: the 16 rows of a K read (one
-// chunk each), and the 16 rows that half a wave's transposed V read takes one chunk
-// of (rows 8 g .. 8 g + 7 and 16 more), fall into 16 different sixteenths of the banks.
-__device__ __forceinline__ int q8_swz(int row) { return ((row >> 1) ^ ((row >> 4) << 2)) & 7; }
+// position c ^ f(r), with bits 2, 1, 3 of r as bits 0, 1, 2 of f: the 16 rows of which
+// a phase of a K read takes one chunk each, and the eight rows (four of each parity)
+// of which half a wave's transposed V read takes two chunks, fall into 16 different
+// sixteenths of the banks.
+__device__ __forceinline__ int q8_swz(int row) {
+  return ((row >> 2) & 1) | (row & 2) | ((row >> 1) & 4);
+}
 
-template <int N>
-__device__ __forceinline__ void q8_wait(int later) {  // later < N tiles may still be in flight
-  if (N > 1 && later >= N - 1) wait_vm<(N - 1) * kQ8Copies>();
-  else if constexpr (N > 1) q8_wait<N - 1>(later);
+// All copies but those of the youngest tensor of a step (one: it was sent) have landed.
+__device__ __forceinline__ void q8_wait(bool one) {  // uniform
+  if (one) wait_vm<kQ8Copies>();
   else wait_vm<0>();
-  asm volatile("" ::: "memory");  // the tile's reads stay behind the wait
+  asm volatile("" ::: "memory");  // the tiles' reads stay behind the wait
 }
 
 // Every LDS read so far has its data (and stays ahead of what follows).
@@ -265,53 +418,51 @@ __device__ __forceinline__ void q8_wait_lds() {
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 }
 
-// Copies one tile into the stage at LDS address lds: K, V and the scales.  Lane offsets
-// offa (rows 0-7 and 24-31 of a tile) and offb (rows 8-23) of a full tile; the
-// instructions' offset moves both addresses.  In inline assembly because the compiler
-// would wait for every copy in flight before each LDS read; M0 (the LDS address) is the
-// compiler's and is restored, and needs a wait state before a load reads it.
-__device__ __forceinline__ void q8_copy(uint32_t lds, uint64_t kb, uint64_t vb, uint32_t offa,
-                                        uint32_t offb, uint64_t scale) {
+// Copies a step's two tiles of one tensor to LDS address lds.  Lane offsets offa (rows 0-7
+// and 16-23 of a tile) and offb (the other rows); the instructions' offset moves both
+// addresses.  In inline assembly because the compiler would wait for every copy in
+// flight before each LDS read; M0 (the LDS address) is the compiler's and is restored,
+// and needs a wait state before a load reads it.  Non-temporal where no other wave of a
+// gang reads the tiles (alone).
+#define ECHO_Q8_COPY(POL)                                                              \
+  "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\t"                                 \
+  "global_load_lds_dwordx4 %2, %4" POL "\n\t"                                          \
+  "global_load_lds_dwordx4 %3, %4 offset:1024" POL "\n\t"                              \
+  "global_load_lds_dwordx4 %2, %4 offset:2048" POL "\n\t"                              \
+  "global_load_lds_dwordx4 %3, %4 offset:3072" POL "\n\t"                              \
+  "s_add_u32 m0, m0, 0x1000\n\ts_nop 0\n\t"                                            \
+  "global_load_lds_dwordx4 %2, %5" POL "\n\t"                                          \
+  "global_load_lds_dwordx4 %3, %5 offset:1024" POL "\n\t"                              \
+  "global_load_lds_dwordx4 %2, %5 offset:2048" POL "\n\t"                              \
+  "global_load_lds_dwordx4 %3, %5 offset:3072" POL "\n\t"                              \
+  "s_mov_b32 m0, %0"
+__device__ __forceinline__ void q8_copy(uint32_t lds, uint64_t tile0, uint64_t tile1, uint32_t offa,
+                                        uint32_t offb, bool alone) {
   uint32_t saved;
-  asm volatile(
-      "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\t"
-      "global_load_lds_dwordx4 %2, %4 nt\n\t"
-      "global_load_lds_dwordx4 %3, %4 offset:1024 nt\n\t"
-      "global_load_lds_dwordx4 %3, %4 offset:2048 nt\n\t"
-      "global_load_lds_dwordx4 %2, %4 offset:3072 nt\n\t"
-      "s_add_u32 m0, m0, 0x1000\n\ts_nop 0\n\t"
-      "global_load_lds_dwordx4 %2, %5 nt\n\t"
-      "global_load_lds_dwordx4 %3, %5 offset:1024 nt\n\t"
-      "global_load_lds_dwordx4 %3, %5 offset:2048 nt\n\t"
-      "global_load_lds_dwordx4 %2, %5 offset:3072 nt\n\t"
-      "s_add_u32 m0, m0, 0x1000\n\ts_nop 0\n\t"
-      "global_load_lds_dword %6, off\n\t"
-      "s_mov_b32 m0, %0"
-      : "=&s"(saved)
-      : "s"(lds), "v"(offa), "v"(offb), "s"(kb), "s"(vb), "v"(scale)
-      : "memory", "scc");
+  if (alone)  // uniform
+    asm volatile(ECHO_Q8_COPY(" nt")
+                 : "=&s"(saved)
+                 : "s"(lds), "v"(offa), "v"(offb), "s"(tile0), "s"(tile1)
+                 : "memory", "scc");
+  else
+    asm volatile(ECHO_Q8_COPY("")
+                 : "=&s"(saved)
+                 : "s"(lds), "v"(offa), "v"(offb), "s"(tile0), "s"(tile1)
+                 : "memory", "scc");
 }
+#undef ECHO_Q8_COPY
 
-// The same with an offset for each group of eight rows (a tile whose last rows hold no
-// tokens: they read its last token's row again, so that nothing unwritten is
-// multiplied, and are masked).
-__device__ __forceinline__ void q8_copy_part(uint32_t lds, uint64_t kb, uint64_t vb, uint32_t o0,
-                                             uint32_t o1, uint32_t o2, uint32_t o3,
-                                             uint64_t scale) {
+// 4 KB to LDS address lds: 1 KB from base + each of the lane's four offsets.
+__device__ __forceinline__ void q8_copy4(uint32_t lds, uint64_t base, const uint32_t (&o)[4]) {
   uint32_t saved;
   asm volatile(
       "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %6\n\t"
       "s_add_u32 m0, m0, 0x400\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %3, %6\n\t"
       "s_add_u32 m0, m0, 0x400\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %4, %6\n\t"
       "s_add_u32 m0, m0, 0x400\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %5, %6\n\t"
-      "s_add_u32 m0, m0, 0x400\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %7\n\t"
-      "s_add_u32 m0, m0, 0x400\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %3, %7\n\t"
-      "s_add_u32 m0, m0, 0x400\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %4, %7\n\t"
-      "s_add_u32 m0, m0, 0x400\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %5, %7\n\t"
-      "s_add_u32 m0, m0, 0x400\n\ts_nop 0\n\tglobal_load_lds_dword %8, off\n\t"
       "s_mov_b32 m0, %0"
       : "=&s"(saved)
-      : "s"(lds), "v"(o0), "v"(o1), "v"(o2), "v"(o3), "s"(kb), "s"(vb), "v"(scale)
+      : "s"(lds), "v"(o[0]), "v"(o[1]), "v"(o[2]), "v"(o[3]), "s"(base)
       : "memory", "scc");
 }
 
@@ -325,450 +476,542 @@ __device__ __forceinline__ Q8Req load_req(const Q8Req* reqs, int r) {
 
 __device__ __forceinline__ Q8Start load_start(const Q8Start* starts, int b) {
   const_i32_t* p = (const_i32_t*)(starts + b);
-  int32_t w[16];
+  int32_t w[20];
 #pragma unroll
-  for (int k = 0; k < 16; ++k) w[k] = p[k];
+  for (int k = 0; k < 20; ++k) w[k] = p[k];
   return __builtin_bit_cast(Q8Start, w);
 }
 
-// A place in the tile stream (wave-uniform): the unit and its first tile.
+// A place in the class's steps (wave-uniform): the unit and its first step.
 struct Q8Walk {
   Q8Req q;
-  int r, unit, u0;
+  int req, unit, u0;
+  __device__ __forceinline__ int ntail() const { return (q.nslots + kTileKeys - 1) / kTileKeys; }
 };
 
+// (Only called where steps are left: there is a next unit.)
 __device__ __forceinline__ void q8_next_unit(Q8Walk& w, const Q8Args& a, const Q8Ws& ws) {
   if (w.unit + 1 < a.hkv * w.q.passes) {
     w.unit += 1;
     w.u0 += w.q.tpu;
     return;
   }
-  while (w.r + 1 < a.R) {
-    w.r = __builtin_amdgcn_readfirstlane(w.r + 1);
-    w.q = load_req(ws.reqs, w.r);
-    if (w.q.passes > 0) break;
-  }
+  w.req = __builtin_amdgcn_readfirstlane(w.req + 1);
+  w.q = load_req(ws.reqs, w.req);
   w.unit = 0;
   w.u0 = w.q.tile0;
 }
 
-// The copy side: `t` is the next tile to look at, `sent` the prefix tiles copied so far.
-struct Q8Issue {
-  Q8Walk w;
-  int t, sent;
+// What a wave knows of the next 32 steps of its range, tile i (two per step) in lane
+// i & 63: the block, the tokens it holds (32 or more: all), and what the softmax takes
+// of its scales.  A request's last step may have one tile: its second entry is that
+// block again, without tokens.  One vector of loads instead of scalar ones for every
+// tile; the ring runs empty once in 32 steps for it.  Steps [.., known) are in the
+// table; K of those below k_sent and V of those below v_sent have been copied, and
+// those below `done` multiplied.
+struct Q8Table {
+  uint32_t blk;
+  int tokens;
+  float c, lvs, ivs;  // softmax factor x K scale; log2 of the V scale, and its reciprocal
+  int known, k_sent, v_sent, done;
+  bool alone;
 };
 
-__device__ __forceinline__ void q8_send(Q8Issue& is, const Q8Args& a, const Q8Ws& ws, int hi,
-                                        uint32_t ring, uint32_t offa, uint32_t offb,
-                                        uint64_t scale_base) {
-  while (is.t < hi) {
-    if (is.t >= is.w.u0 + is.w.q.tpu) q8_next_unit(is.w, a, ws);
-    else if (is.t - is.w.u0 < is.w.q.ntail) is.t = min(hi, is.w.u0 + is.w.q.ntail);
-    else break;
+// Fills the table from step t of the unit at w on.
+__device__ __forceinline__ void q8_fill(Q8Table& tb, const Q8Args& a, const Q8Ws& ws, Q8Walk w, int t,
+                                        int hi) {
+  const int lane = threadIdx.x & (kWave - 1);
+  int n = 0;  // lanes filled
+  uint32_t entry = 0, head = 0;
+  int key = 0, tokens = 0;
+  while (n < kWave && t < hi) {  // uniform
+    const int end = min(hi, w.u0 + w.q.tpu);
+    const int p0 = w.u0 + w.ntail();
+    t = max(t, min(end, p0));
+    const int m = min((kWave - n) / 2, end - t);
+    if (lane >= n && lane < n + 2 * m) {
+      key = (t - p0) * kQ8StepKeys + (lane - n) * kTileKeys;
+      tokens = max(w.q.P - key, 0);
+      if (tokens == 0) key -= kTileKeys;
+      entry = uint32_t(w.q.r) * uint32_t(a.max_pages) + uint32_t(key >> a.page_shift);
+      head = uint32_t(w.unit / w.q.passes);
+    }
+    n += 2 * m;
+    t += m;
+    if (t >= end && t < hi) q8_next_unit(w, a, ws);
   }
-  if (is.t >= hi) return;
-  const int key = (is.t - is.w.u0 - is.w.q.ntail) * kTileKeys;
-  const int head = is.w.unit / is.w.q.passes;
-  const int page = ((const const_i32_t*)(a.block_table + size_t(is.w.r) * size_t(a.max_pages)))
-      [key >> a.page_shift];
-  const uint64_t blk =
-      ((uint64_t(page) * uint32_t(a.hkv) + uint32_t(head)) << (a.page_shift - 5)) +
-      uint32_t((key & ((1 << a.page_shift) - 1)) >> 5);
-  const uint64_t kb = uniform64(reinterpret_cast<uint64_t>(a.k_pages) + blk * kBlockBytes);
-  const uint64_t vb = uniform64(reinterpret_cast<uint64_t>(a.v_pages) + blk * kBlockBytes);
-  const uint32_t lds = __builtin_amdgcn_readfirstlane(
-      ring + uint32_t((is.sent & (kQ8Stages - 1)) * kQ8StageBytes));
-  const uint64_t scale = scale_base + blk * 4;
-  const int tn = is.w.q.P - key;
-  if (tn >= kTileKeys) {
-    q8_copy(lds, kb, vb, offa, offb, scale);
+  tb.known += n / 2;
+  if (lane < n) {
+    const uint32_t page = uint32_t(a.block_table[entry]);
+    tb.blk = ((page * uint32_t(a.hkv) + head) << (a.page_shift - 5)) +
+             (uint32_t(key & ((1 << a.page_shift) - 1)) >> 5);
+    tb.tokens = tokens;
+    const float ks = a.k_scale[tb.blk], vs = a.v_scale[tb.blk];
+    tb.c = a.scale2 * ks;
+    tb.lvs = __builtin_amdgcn_logf(vs);
+    tb.ivs = __builtin_amdgcn_rcpf(vs);
+  }
+}
+
+__device__ __forceinline__ int lane_of(int v, int i) { return __builtin_amdgcn_readlane(v, i); }
+__device__ __forceinline__ float lane_of(float v, int i) {
+  return __uint_as_float(uint32_t(__builtin_amdgcn_readlane(int(__float_as_uint(v)), i)));
+}
+
+// The lane's LDS and copy offsets in one register (three would be reloaded from memory in
+// the main loop, behind every copy in flight).
+//   K reads   row lane % 32, chunks 4 j + 2 (lane / 32) + e: an exclusive-or of bits 6 and 4
+//   V reads   (transposed) of a 16-key group, keys 4 h + 0..3 and the same + 8 (h: lane / 32;
+//             the order in which S^T leaves them in the lanes), dims 32 dt + lane % 32: the
+//             lane supplies half of one key's 16-byte chunk 2 dt + (lane / 16) % 2, an
+//             exclusive-or of bits 5 and 6
+//   copies    rows 0-7 of a tile (and 16-23); the other rows have bit 6 flipped
+__device__ __forceinline__ uint32_t q8_lane_offsets() {
+  const int lane = threadIdx.x & (kWave - 1);
+  const int row = lane & 31, h = lane >> 5, i = lane & 15;
+  const int vkey = 4 * h + ((i >> 1) & 3) + ((i >> 3) << 3);
+  const uint32_t k = uint32_t(row * kD + (((2 * h) ^ q8_swz(row)) << 4));
+  const uint32_t v = uint32_t(vkey * kD + ((((lane >> 4) & 1) ^ q8_swz(vkey)) << 4) + ((i & 1) << 3));
+  const uint32_t c = uint32_t((lane >> 3) * kD + (((lane & 7) ^ q8_swz(lane >> 3)) << 4));
+  return (k >> 4) | (v << 8) | (c << 16);  // k a multiple of 16 and v of 8 below 2^12 (2^11)
+}
+__device__ __forceinline__ uint32_t q8_opaque(uint32_t x) {  // (not kept unpacked)
+  asm volatile("" : "+v"(x));
+  return x;
+}
+__device__ __forceinline__ uint32_t k_offset(uint32_t p) { return (q8_opaque(p) & 0xFFu) << 4; }
+__device__ __forceinline__ uint32_t v_offset(uint32_t p) { return (q8_opaque(p) >> 8) & 0x7FFu; }
+__device__ __forceinline__ uint32_t copy_offset(uint32_t p) { return (q8_opaque(p) >> 20) << 4; }
+
+// Copies a tensor's tiles of the next step, if the table has one.  Where a tile's last rows
+// hold no tokens they read its last token's row again, so that nothing unwritten is
+// multiplied (they are masked).
+__device__ __forceinline__ void q8_send(const Q8Table& tb, int& sent, const uint8_t* pages,
+                                        uint32_t lds, uint32_t offs) {
+  if (sent >= tb.known) return;  // uniform
+  const int i = (2 * sent) & (kWave - 1);
+  const uint64_t base = reinterpret_cast<uint64_t>(pages);
+  const uint64_t t0 = base + uint64_t(uint32_t(lane_of(int(tb.blk), i))) * kBlockBytes;
+  const uint64_t t1 = base + uint64_t(uint32_t(lane_of(int(tb.blk), i + 1))) * kBlockBytes;
+  const int tn1 = lane_of(tb.tokens, i + 1);
+  if (tn1 >= kTileKeys) {
+    const uint32_t offa = copy_offset(offs);
+    q8_copy(lds, t0, t1, offa, offa ^ 64u, tb.alone);
   } else {
     const int lane = threadIdx.x & (kWave - 1);
+    const int tn0 = lane_of(tb.tokens, i);
+#pragma unroll 1
+    for (int k = 0; k < 2; ++k) {
+      const int last = min(max(k == 0 ? tn0 : tn1, 1), kTileKeys) - 1;
+      uint32_t o[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int row = 8 * j + (lane >> 3);
+        o[j] = uint32_t(min(row, last) * kD + (((lane & 7) ^ q8_swz(row)) << 4));
+      }
+      q8_copy4(lds + uint32_t(k * kBlockBytes), k == 0 ? t0 : t1, o);
+    }
+  }
+  sent += 1;
+}
+
+// Two bytes (the upper two of w if hi) as bfloat16 (exact).
+template <int kFmt>
+__device__ __forceinline__ uint32_t widen2(uint32_t w, bool hi) {  // hi: a constant
+  if (kFmt == ECHO_KV_E4M3)
+    return __builtin_bit_cast(uint32_t, hi ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true)
+                                           : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false));
+  return __builtin_bit_cast(uint32_t, hi ? __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(w, 1.0f, true)
+                                         : __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(w, 1.0f, false));
+}
+
+// Maximum and sum over the two lanes of a row.
+__device__ __forceinline__ float pair_max(float v) {
+  const uint32_t u = __float_as_uint(v);
+  const auto a = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+}
+__device__ __forceinline__ float pair_sum(float v) {
+  const uint32_t u = __float_as_uint(v);
+  const auto a = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return __uint_as_float(a[0]) + __uint_as_float(a[1]);
+}
+
+// A wave's 32 rows: the lane's row is lane % 32, which it shares with lane ^ 32.
+struct Q8Rows {
+  floatx16 o[4];  // O^T: dims 32 dt + 8 (r >> 2) + 4 (lane / 32) + (r & 3)
+  float m;        // reference maximum (log2 units)
+  float l, lq;    // the lane's share of the weights' sum, and of those multiplied with V
+  float mgrow;    // a logit above it raises the reference
+};
+
+// The reference is raised only when a logit (lmt: the largest of the lane's) exceeds it by
+// more than 2^8, so that weights stay <= 256.
+__device__ __forceinline__ void q8_raise(Q8Rows& rt, float lmt) {
+  if (__ballot(lmt > rt.mgrow) == 0ull) return;
+  const float mt = pair_max(lmt);
+  const bool grow = mt > rt.mgrow;
+  const float alpha = grow ? __builtin_amdgcn_exp2f(rt.m - mt) : 1.0f;  // 0 from -inf
+  rt.l *= alpha;
+  rt.lq *= alpha;
+#pragma unroll
+  for (int dt = 0; dt < 4; ++dt) rt.o[dt] *= alpha;
+  rt.m = grow ? mt : rt.m;
+  rt.mgrow = rt.m + kRescaleSlack;
+}
+
+// Scores that a row does not see (bit k of word: key k of the tile) become -inf.
+__device__ __forceinline__ void q8_mask(floatx16& s, uint32_t word) {
+  const uint32_t w = word >> (4 * ((threadIdx.x & (kWave - 1)) >> 5));
+#pragma unroll
+  for (int r = 0; r < 16; ++r)
+    s[r] = ((w >> (8 * (r >> 2) + (r & 3))) & 1u) ? s[r] : -__builtin_inff();
+}
+
+__device__ __forceinline__ float max16(const floatx16& s) {
+  const float a = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(s[4], s[5]));
+  const float b = fmaxf(fmaxf(fmaxf(s[6], s[7]), fmaxf(s[8], s[9])), fmaxf(s[10], s[11]));
+  return fmaxf(fmaxf(a, b), fmaxf(fmaxf(s[12], s[13]), fmaxf(s[14], s[15])));
+}
+
+#define ECHO_FENCE() __builtin_amdgcn_sched_barrier(0)
+// The softmax of NT tiles' scores and O^T += V^T P^T.  frag(g, dt): V^T of 16-key group g
+// (2 per tile), dims 32 dt .., as four words of bfloat16.  c: softmax factor x K scale of
+// a tile; lvs: log2 of its V scale, which the weights take along (the sums are taken
+// without it).  The weights of a group are computed between the products of the group
+// before (a 32x32x16 product leaves room for five vector instructions).
+template <int NT, typename Frag>
+__device__ __forceinline__ void q8_values(const Frag& frag, floatx16 (&s)[NT], Q8Rows& rt,
+                                          const float (&c)[NT], const float (&lvs)[NT]) {
+  float lmt = max16(s[0]) * c[0];
+  if (NT == 2) lmt = fmaxf(lmt, max16(s[NT - 1]) * c[NT - 1]);
+  q8_raise(rt, lmt);
+  const float neg_m = rt.m == -__builtin_inff() ? 0.0f : -rt.m;
+  float off[NT], sum[NT][2], used[NT][2];
+#pragma unroll
+  for (int j = 0; j < NT; ++j) {
+    off[j] = lvs[j] + neg_m;
+    sum[j][0] = sum[j][1] = used[j][0] = used[j][1] = 0.0f;
+  }
+  uint32_t pk[2][4];
+  const auto two = [&](int g, int i) {  // weights 2 i and 2 i + 1 of the lane's 8 of group g
+    const int j = g >> 1, e = 8 * (g & 1) + 2 * i;
+    const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[j][e], c[j], off[j]));
+    const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[j][e + 1], c[j], off[j]));
+    sum[j][0] += p0;
+    sum[j][1] += p1;
+    pk[g & 1][i] = pack_bf16x2(p0, p1);
+    used[j][i & 1] = add_bf16x2(pk[g & 1][i], used[j][i & 1]);
+  };
+#pragma unroll
+  for (int i = 0; i < 4; ++i) two(0, i);
+#pragma unroll
+  for (int g = 0; g < 2 * NT; ++g) {
+    const bf16x8 pf = as_bf16x8(make_uint4(pk[g & 1][0], pk[g & 1][1], pk[g & 1][2], pk[g & 1][3]));
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt) {
+      const bf16x8 f = as_bf16x8(frag(g, dt));
+      ECHO_FENCE();
+      rt.o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, pf, rt.o[dt], 0, 0, 0);
+      ECHO_FENCE();
+      if (g + 1 < 2 * NT) two(g + 1, dt);
+    }
+  }
+  ECHO_FENCE();
+#pragma unroll
+  for (int j = 0; j < NT; ++j) {
+    const float ivs = __builtin_amdgcn_exp2f(-lvs[j]);
+    rt.l = __builtin_fmaf(sum[j][0] + sum[j][1], ivs, rt.l);
+    rt.lq = __builtin_fmaf(used[j][0] + used[j][1], ivs, rt.lq);
+  }
+}
+#undef ECHO_FENCE
+
+// 32 bytes of a split row (p: dims 64 j + 32 (lane / 32) on).
+__device__ __forceinline__ intx8 q8_half(const uint8_t* p) {
+  const uint4v a = *reinterpret_cast<const uint4v*>(p);
+  const uint4v b = *reinterpret_cast<const uint4v*>(p + 16);
+  return __builtin_bit_cast(intx8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+// A tile of the tree's new keys (tn <= 32 of them from slot s0 on): K split in two 8-bit
+// numbers like Q, so that S^T is the sum of four products; V in bfloat16 through 4 KB
+// of LDS at `scratch` to be transposed, 16 keys at a time (the second 16 only if there
+// are so many).
+__device__ __forceinline__ void q8_tree_tile(const Q8Args& a, const Q8Ws& ws, int head, int s0, int tn,
+                                             uint32_t scratch, const intx8 (&q)[2][2], int qe,
+                                             Q8Rows& rt, uint32_t word) {
+  const int lane = threadIdx.x & (kWave - 1);
+  const int h = lane >> 5, lr = lane & 15;
+  const uint32_t row_bytes = uint32_t(a.hkv) * kD * 2;
+  const uint64_t vh = uniform64(reinterpret_cast<uint64_t>(a.v_new) + uint64_t(uint32_t(s0)) * row_bytes +
+                                uint32_t(head) * (kD * 2));
+  const auto copy_v = [&](int g) {
     uint32_t o[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const int row = 8 * j + (lane >> 3);
-      o[j] = uint32_t(min(row, tn - 1) * kD + (((lane & 7) ^ q8_swz(row)) << 4));
+      // (LDS: 256-byte rows, 16-byte chunk c of row r at place c ^ swz_pattern(r))
+      const int row = 4 * j + (lane >> 4);
+      o[j] = uint32_t(min(16 * g + row, tn - 1)) * row_bytes + uint32_t((lr ^ swz_pattern(row)) << 4);
     }
-    q8_copy_part(lds, kb, vb, o[0], o[1], o[2], o[3], scale);
-  }
-  is.t += 1;
-  is.sent += 1;
-}
-
-template <int kFmt>
-__device__ __forceinline__ bf16x8 widen8(uint32_t lo, uint32_t hi) {
-  bf16x2 a, b, c, d;
-  if (kFmt == ECHO_KV_E4M3) {
-    a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false);
-    b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, true);
-    c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, false);
-    d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true);
-  } else {
-    a = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(lo, 1.0f, false);
-    b = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(lo, 1.0f, true);
-    c = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(hi, 1.0f, false);
-    d = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(hi, 1.0f, true);
-  }
-  return as_bf16x8(make_uint4(__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b),
-                              __builtin_bit_cast(uint32_t, c), __builtin_bit_cast(uint32_t, d)));
-}
-
-// Maximum and sum over the four lanes of a row (l, l ^ 16, l ^ 32, l ^ 48).
-__device__ __forceinline__ float quad_max(float v) {
-  const uint32_t u = __float_as_uint(v);
-  const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
-  v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
-  const uint32_t w = __float_as_uint(v);
-  const auto b = __builtin_amdgcn_permlane32_swap(w, w, false, false);
-  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
-}
-__device__ __forceinline__ float quad_sum(float v) {
-  const uint32_t u = __float_as_uint(v);
-  const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
-  v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
-  const uint32_t w = __float_as_uint(v);
-  const auto b = __builtin_amdgcn_permlane32_swap(w, w, false, false);
-  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
-}
-
-// 16 rows: O^T (lane: dims 16 dt + 4 (lane / 16) + i of row lane % 16) and the softmax's
-// state, of which each of the row's four lanes has its share of the sums.
-struct Q8Rows {
-  floatx4 o[8];
-  float m;      // reference maximum (log2 units)
-  float l, lq;  // sums of the weights, and of the weights as multiplied with V
-  float mgrow;  // a logit above it raises the reference
-};
-
-// What a tile's products take: K and V^T fragments.  K fragment kk (0..3) of 16 keys: lane
-// holds dims 64 (kk >> 1) + 16 (lane / 16) + 8 (kk & 1) .. + 7 of key lane % 16 (the
-// order of dims that two 16-byte reads give; Q is loaded in the same).  V^T
-// fragment dt: dim 16 dt + lane % 16 of keys 4 (lane / 16) + 0..3 and the same + 16: the
-// order in which S^T leaves the keys in the lanes.
-
-// Scores to weights: S^T of 16 rows (two subtiles of 16 keys), c = softmax factor x K
-// scale, lvs = log2 of V's scale, which the weights take along (ivs takes it out of
-// the sums again).  word: bit k set iff the row sees key k.
-__device__ __forceinline__ bf16x8 q8_softmax(floatx4 s0, floatx4 s1, Q8Rows& rt, bool masked,
-                                             uint32_t word, float c, float lvs, float ivs) {
-  float sv[8] = {s0[0], s0[1], s0[2], s0[3], s1[0], s1[1], s1[2], s1[3]};
-  if (masked) {
-    const uint32_t w = word >> (4 * ((threadIdx.x & (kWave - 1)) >> 4));
+    q8_copy4(scratch, vh, o);
+  };
+  copy_v(0);
+  const size_t krow = size_t(s0 + min(lane & 31, tn - 1)) * a.hkv + head;
+  const uint8_t* kp = ws.ks + krow * kSplitBytes + 32 * h;
+  const int ke = ws.ke[krow];
+  floatx16 s[1] = {};
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-      sv[e] = ((w >> (16 * (e >> 2) + (e & 3))) & 1u) ? sv[e] : -__builtin_inff();
-  }
-  const float lmt = fmaxf(fmaxf(fmaxf(sv[0], sv[1]), fmaxf(sv[2], sv[3])),
-                          fmaxf(fmaxf(sv[4], sv[5]), fmaxf(sv[6], sv[7]))) * c;
-  // the reference is raised only when a logit exceeds it by more than 2^8, so that
-  // weights stay <= 256
-  if (__ballot(lmt > rt.mgrow) != 0ull) {
-    const float mt = quad_max(lmt);
-    const bool grow = mt > rt.mgrow;
-    const float alpha = grow ? __builtin_amdgcn_exp2f(rt.m - mt) : 1.0f;  // 0 from -inf
-    rt.l *= alpha;
-    rt.lq *= alpha;
+  for (int j = 0; j < 2; ++j) {
+    const intx8 kh = q8_half(kp + 64 * j), kl = q8_half(kp + kD + 64 * j);
 #pragma unroll
-    for (int dt = 0; dt < 8; ++dt) rt.o[dt] *= alpha;
-    rt.m = grow ? mt : rt.m;
-    rt.mgrow = rt.m + kRescaleSlack;
-  }
-  const float off = lvs - (rt.m == -__builtin_inff() ? 0.0f : rt.m);
-  float sum = 0.0f;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    sv[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sv[e], c, off));
-    sum += sv[e];
-  }
-  uint4 pk;
-  pk.x = pack_bf16x2(sv[0], sv[1]);
-  pk.y = pack_bf16x2(sv[2], sv[3]);
-  pk.z = pack_bf16x2(sv[4], sv[5]);
-  pk.w = pack_bf16x2(sv[6], sv[7]);
-  const float used = add_bf16x2(pk.w, add_bf16x2(pk.z, add_bf16x2(pk.y, add_bf16x2(pk.x, 0.0f))));
-  rt.l = __builtin_fmaf(sum, ivs, rt.l);
-  rt.lq = __builtin_fmaf(used, ivs, rt.lq);
-  return as_bf16x8(pk);
-}
-
-// One tile against MT row tiles.  kf(s2, kk), vf(dt): its fragments.
-template <int MT, typename KF, typename VF>
-__device__ __forceinline__ void q8_tile(const KF& kf, const VF& vf, const bf16x8 (*qf)[4],
-                                        Q8Rows* rt, bool masked, const uint32_t* word, float c,
-                                        float lvs, float ivs) {
-  floatx4 st[MT][2];
-#pragma unroll
-  for (int s2 = 0; s2 < 2; ++s2)
-#pragma unroll
-    for (int kk = 0; kk < 4; ++kk) {
-      const bf16x8 f = kf(s2, kk);
-#pragma unroll
-      for (int i = 0; i < MT; ++i)
-        st[i][s2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-            f, qf[i][kk], kk == 0 ? floatx4{0.f, 0.f, 0.f, 0.f} : st[i][s2], 0, 0, 0);
-    }
-  bf16x8 pf[MT];
-#pragma unroll
-  for (int i = 0; i < MT; ++i)
-    pf[i] = q8_softmax(st[i][0], st[i][1], rt[i], masked, word[i], c, lvs, ivs);
-#pragma unroll
-  for (int dt = 0; dt < 8; ++dt) {
-    const bf16x8 f = vf(dt);
-#pragma unroll
-    for (int i = 0; i < MT; ++i)
-      rt[i].o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, pf[i], rt[i].o[dt], 0, 0, 0);
-  }
-}
-
-// A tile of the tree's new keys (bfloat16, tn <= 32 of them from slot s0 on), read from
-// global memory; V goes through 4 KB of LDS to be transposed, 16 keys at a time.
-template <int MT>
-__device__ __forceinline__ void q8_tree_tile(const Q8Args& a, int head, int s0, int tn,
-                                             char* scratch, const bf16x8 (*qf)[4], Q8Rows* rt,
-                                             const uint32_t* word) {
-  const int lane = threadIdx.x & (kWave - 1);
-  const int lr = lane & 15, lg = lane >> 4;
-  const size_t row = size_t(a.hkv) * kD;
-  const uint16_t* kh = a.k_new + size_t(s0) * row + size_t(head) * kD;
-  const uint16_t* vh = a.v_new + size_t(s0) * row + size_t(head) * kD;
-  bf16x8 kfr[2][4];
-  uint4 vr[2][4];
-#pragma unroll
-  for (int s2 = 0; s2 < 2; ++s2) {
-    const uint16_t* p = kh + size_t(min(16 * s2 + lr, tn - 1)) * row + 16 * lg;
-#pragma unroll
-    for (int kk = 0; kk < 4; ++kk)
-      kfr[s2][kk] = as_bf16x8(
-          *reinterpret_cast<const uint4*>(p + 64 * (kk >> 1) + 8 * (kk & 1)));
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      vr[s2][j] = *reinterpret_cast<const uint4*>(
-          vh + size_t(min(16 * s2 + 4 * j + lg, tn - 1)) * row + 8 * lr);
-  }
-  shortx4 vt[2][8];
-#pragma unroll
-  for (int s2 = 0; s2 < 2; ++s2) {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int r16 = 4 * j + lg;
-      *reinterpret_cast<uint4*>(scratch + r16 * 256 + ((lr ^ swz_pattern(r16)) << 4)) = vr[s2][j];
-    }
-    q8_wait_lds();
-    const int key = 4 * lg + (lr >> 2);
-#pragma unroll
-    for (int dt = 0; dt < 8; ++dt) {
-      const int d = 16 * dt + 4 * (lr & 3);
-      vt[s2][dt] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-          (lds_shortx4_t*)(scratch + key * 256 + (((d >> 3) ^ swz_pattern(key)) << 4) +
-                           ((d & 4) << 1)));
-    }
-    q8_wait_lds();
-  }
-  q8_tile<MT>([&](int s2, int kk) { return kfr[s2][kk]; },
-              [&](int dt) {
-                return __builtin_bit_cast(bf16x8, __builtin_shufflevector(vt[0][dt], vt[1][dt], 0,
-                                                                          1, 2, 3, 4, 5, 6, 7));
-              },
-              qf, rt, true, word, a.scale2, 0.0f, 1.0f);
-}
-
-// The wave's tiles [lo, hi) of one unit, then its output or partial sums.
-template <int kFmt, int MT>
-__device__ __forceinline__ void q8_segment(const Q8Args& a, const Q8Ws& ws, const Q8Walk& w, int lo,
-                                           int hi, int range_hi, int b, char* lds_wave,
-                                           uint32_t ring, Q8Issue& is, int& done, uint32_t offa,
-                                           uint32_t offb, uint64_t scale_base, bool whole,
-                                           int part_slot) {
-  const int lane = threadIdx.x & (kWave - 1);
-  const int lr = lane & 15, lg = lane >> 4;
-  const int head = w.unit / w.q.passes;
-  const int row0 = (w.unit % w.q.passes) * w.q.rpp;
-  const int rows = min(w.q.rpp, w.q.nslots * a.G - row0);
-  bf16x8 qf[MT][4];
-  Q8Rows rt[MT];
-#pragma unroll
-  for (int i = 0; i < MT; ++i) {
-    const int ra = row0 + 16 * i + lr;
-    const int slot = w.q.q0 + ra / a.G;
-    const uint16_t* p = a.q + (size_t(slot) * a.hq + size_t(head) * a.G + ra % a.G) * kD + 16 * lg;
-#pragma unroll
-    for (int kk = 0; kk < 4; ++kk) {
-      uint4 v = make_uint4(0, 0, 0, 0);
-      if (16 * i + lr < rows) v = *reinterpret_cast<const uint4*>(p + 64 * (kk >> 1) + 8 * (kk & 1));
-      qf[i][kk] = as_bf16x8(v);
-    }
-#pragma unroll
-    for (int dt = 0; dt < 8; ++dt) rt[i].o[dt] = floatx4{0.f, 0.f, 0.f, 0.f};
-    rt[i].m = -__builtin_inff();
-    rt[i].l = 0.0f;
-    rt[i].lq = 0.0f;
-    rt[i].mgrow = -__builtin_inff();
-  }
-  wait_vm<0>();  // no load that the compiler knows of is in flight in the loops below
-
-  int t = lo;
-  for (; t < hi && t - w.u0 < w.q.ntail; ++t) {
-    const int lt = t - w.u0;
-    const int tn = min(kTileKeys, w.q.nslots - lt * kTileKeys);
-    uint32_t word[MT];
-#pragma unroll
-    for (int i = 0; i < MT; ++i) {
-      const int rho = 16 * i + lr;
-      const int slot = w.q.q0 + (row0 + rho) / a.G;
-      word[i] = rho < rows && lt < a.W ? a.tree_mask[size_t(slot) * a.W + lt] : 0u;
-      if (tn < kTileKeys) word[i] &= (1u << tn) - 1u;
-    }
-    q8_tree_tile<MT>(a, head, w.q.q0 + lt * kTileKeys, tn, lds_wave + kQ8Stages * kQ8StageBytes, qf,
-                     rt, word);
+    for (int n = 0; n < 4; ++n)
+      s[0] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
+          n & 1 ? kl : kh, q[n >> 1][j], s[0], 0, 0, 0, n & 1 ? ke - 4 : ke, 0, n & 2 ? qe - 4 : qe);
   }
   wait_vm<0>();
-
-  const int kswz = q8_swz(lr);  // rows 16 apart: the same but for bit 2
-  const int vkey = 4 * lg + ((lr >> 1) & 3) + ((lr >> 3) << 4);
-  const int vswz = q8_swz(vkey);
-  for (; t < hi; ++t) {
-    q8_wait<kQ8Stages>(is.sent - done - 1);
-    const char* stg = lds_wave + (done & (kQ8Stages - 1)) * kQ8StageBytes;
-    uint4 kr[2][2];
-    intx2 vr[8];
+  asm volatile("" ::: "memory");
+  // V^T of a 16-key group: keys 4 h + 0..3 and the same + 8 of dims 32 dt + lane % 32
+  const int vrow = 4 * h + (lr >> 2);
+  const uint32_t vt = scratch + uint32_t(vrow * 256 + ((lr & 1) << 3));
+  const uint32_t chunk = uint32_t((2 * ((lane >> 4) & 1) + ((lr & 3) >> 1)) ^ swz_pattern(vrow));
+  shortx4 v[2][4][2];
+  const auto read_v = [&](int g) {
 #pragma unroll
-    for (int s2 = 0; s2 < 2; ++s2)
+    for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+      for (int k = 0; k < 2; ++k)  // (8 rows on: bit 1 of the pattern)
+        v[g][dt][k] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (lds_shortx4_t*)(lds_at(vt + ((chunk ^ uint32_t(4 * dt) ^ uint32_t(2 * k)) << 4)) + 2048 * k));
+    q8_wait_lds();
+  };
+  read_v(0);
+  if (tn > 16) {  // uniform
+    copy_v(1);
+    wait_vm<0>();
+    asm volatile("" ::: "memory");
+    read_v(1);
+  } else {
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt) v[1][dt][0] = v[1][dt][1] = shortx4{0, 0, 0, 0};
+  }
+  q8_mask(s[0], word);
+  const float c[1] = {a.scale2}, lvs[1] = {0.0f};
+  q8_values<1>(
+      [&](int g, int dt) {
+        return __builtin_bit_cast(uint4, __builtin_shufflevector(v[g][dt][0], v[g][dt][1], 0, 1, 2, 3,
+                                                                 4, 5, 6, 7));
+      },
+      s, rt, c, lvs);
+}
+
+// The ring's first copies.
+__device__ __forceinline__ void q8_prime(Q8Table& tb, const Q8Args& a, uint32_t ring, uint32_t offs) {
+  q8_send(tb, tb.k_sent, a.k_pages, ring, offs);
+  q8_send(tb, tb.v_sent, a.v_pages, ring + kQ8Slot, offs);
+}
+
+// A wave's steps [lo, hi) of one unit, then its output or partial sums.
+//
+// S^T = K Q^T of a cached tile takes its bytes as they are:
+// v_mfma_f32_32x32x64_f8f6f4 with Q as the sum of two e4m3 numbers (see q8_split).  That
+// is as many cycles as bfloat16 products, and no conversion of K.  P V stays in
+// bfloat16: weights as two 8-bit numbers would cost more instructions than V's
+// conversion.
+template <int kFmt>
+__device__ __forceinline__ void q8_segment(const Q8Args& a, const Q8Ws& ws, const Q8Walk& w, int lo,
+                                           int hi, int range_hi, int b, int k, int member,
+                                           uint32_t ring, Q8Table& tb, uint32_t offs, bool whole,
+                                           int part_slot) {
+  const int lane = threadIdx.x & (kWave - 1);
+  const int h = lane >> 5;
+  const int head = w.unit / w.q.passes;
+  const int row0 = (w.unit % w.q.passes * k + member) * w.q.rpp;
+  const int rows = min(w.q.rpp, w.q.nslots * a.G - row0);  // (0 or less: none)
+  intx8 q[2][2];  // [hi, lo][half of the dims]
+  int qe;
+  Q8Rows rt;
+  int t = lo;
+  {
+    // (a row past the last one computes the last one again, to be dropped)
+    const int ra = min(row0 + min(lane & 31, w.q.rpp - 1), w.q.nslots * a.G - 1);
+    const int slot = w.q.q0 + ra / a.G;
+    const size_t row = size_t(slot) * a.hq + size_t(head) * a.G + ra % a.G;
+    const uint8_t* p = ws.qs + row * kSplitBytes + 32 * h;
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) q[n][j] = q8_half(p + kD * n + 64 * j);
+    qe = ws.qe[row];
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt) rt.o[dt] = floatx16{};
+    rt.m = -__builtin_inff();
+    rt.l = 0.0f;
+    rt.lq = 0.0f;
+    rt.mgrow = -__builtin_inff();
+    for (; t < hi && t - w.u0 < w.ntail(); ++t) {
+      const int lt = t - w.u0;
+      const int tn = min(kTileKeys, w.q.nslots - lt * kTileKeys);
+      uint32_t word = lt < a.W ? a.tree_mask[size_t(slot) * a.W + lt] : 0u;
+      if (tn < kTileKeys) word &= (1u << tn) - 1u;
+      q8_tree_tile(a, ws, head, w.q.q0 + lt * kTileKeys, tn, ring + 2 * kQ8Slot, q, qe, rt, word);
+    }
+  }
+  wait_vm<0>();  // no load that the compiler knows of is in flight in the loop
+
+  for (; t < hi; ++t) {
+    if (tb.done == tb.known) {  // the table is used up, and the ring empty
+      q8_fill(tb, a, ws, w, t, range_hi);
+      q8_prime(tb, a, ring, offs);
+    }
+    const int i = (2 * tb.done) & (kWave - 1);
+    // K.  (The copies go K, V, K, V: behind this step's K comes its V.)
+    q8_wait(tb.v_sent > tb.done);
+    uint4v kr[2][2][2];  // [tile][half of the dims][chunk]
+    const uint32_t ka = ring + k_offset(offs);
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
 #pragma unroll
       for (int j = 0; j < 2; ++j)
-        kr[s2][j] = *reinterpret_cast<const uint4*>(
-            stg + (16 * s2 + lr) * kD + (((4 * j + lg) ^ kswz ^ (s2 << 2)) << 4));
 #pragma unroll
-    for (int dt = 0; dt < 8; ++dt)
-      vr[dt] = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
-          (lds_intx2_t*)(const_cast<char*>(stg) + kBlockBytes + vkey * kD + ((dt ^ vswz) << 4) +
-                         ((lr & 1) << 3)));
-    const float2 scales = *reinterpret_cast<const float2*>(stg + kQ8ScaleOff);
+        for (int e = 0; e < 2; ++e)
+          kr[n][j][e] = *(lds_uint4_t*)(lds_at(ka ^ uint32_t(64 * j + 16 * e)) + kBlockBytes * n);
     q8_wait_lds();
-    ++done;
-    // the stage is in registers: refill it while the tile is multiplied
-    q8_send(is, a, ws, range_hi, ring, offa, offb, scale_base);
-    const int tn = w.q.P - (t - w.u0 - w.q.ntail) * kTileKeys;
-    const bool masked = tn < kTileKeys;
-    uint32_t word[MT];
+    // it is in registers: refill its place while it is multiplied
+    q8_send(tb, tb.k_sent, a.k_pages, ring, offs);
+    floatx16 s[2] = {};
 #pragma unroll
-    for (int i = 0; i < MT; ++i) word[i] = masked ? (1u << tn) - 1u : 0xFFFFFFFFu;
-    q8_tile<MT>(
-        [&](int s2, int kk) {
-          const uint4& v = kr[s2][kk >> 1];
-          return kk & 1 ? widen8<kFmt>(v.z, v.w) : widen8<kFmt>(v.x, v.y);
+    for (int n = 0; n < 8; ++n) {
+      const int term = n >> 2, j = (n >> 1) & 1, tile = n & 1;
+      s[tile] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
+          __builtin_bit_cast(intx8, __builtin_shufflevector(kr[tile][j][0], kr[tile][j][1], 0, 1, 2, 3,
+                                                            4, 5, 6, 7)),
+          q[term][j], s[tile], kFmt == ECHO_KV_E4M3 ? 0 : 1, 0, 0, 127, 0, term ? qe - 4 : qe);
+    }
+    const int tn1 = lane_of(tb.tokens, i + 1);
+    if (tn1 < kTileKeys) {
+      const int tn0 = lane_of(tb.tokens, i);
+      q8_mask(s[0], tn0 < kTileKeys ? (1u << tn0) - 1u : 0xFFFFFFFFu);
+      q8_mask(s[1], (1u << tn1) - 1u);
+    }
+    // V.  (Behind it comes K of the next step.)
+    q8_wait(tb.k_sent > tb.done + 1);
+    intx2 vr[4][4];  // [16-key group][32 dims]
+    const uint32_t va = ring + kQ8Slot + v_offset(offs);
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+#pragma unroll
+      for (int dt = 0; dt < 4; ++dt)
+        vr[g][dt] = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+            (lds_intx2_t*)(lds_at(va ^ uint32_t(dt << 5)) + 16 * kD * g));
+    q8_wait_lds();
+    q8_send(tb, tb.v_sent, a.v_pages, ring + kQ8Slot, offs);
+    tb.done += 1;
+    const float c[2] = {lane_of(tb.c, i), lane_of(tb.c, i + 1)};
+    const float lvs[2] = {lane_of(tb.lvs, i), lane_of(tb.lvs, i + 1)};
+    q8_values<2>(
+        [&](int g, int dt) {
+          const uint32_t x = uint32_t(vr[g][dt][0]), y = uint32_t(vr[g][dt][1]);
+          return make_uint4(widen2<kFmt>(x, false), widen2<kFmt>(x, true), widen2<kFmt>(y, false),
+                            widen2<kFmt>(y, true));
         },
-        [&](int dt) { return widen8<kFmt>(uint32_t(vr[dt][0]), uint32_t(vr[dt][1])); }, qf, rt,
-        masked, word, a.scale2 * scales.x, __builtin_amdgcn_logf(scales.y),
-        __builtin_amdgcn_rcpf(scales.y));
+        s, rt, c, lvs);
   }
 
+  int rho = lane & 31;  // (opaque: the output's addresses are formed here, not kept in registers)
+  asm volatile("" : "+v"(rho));
+  const float L = pair_sum(rt.l);
+  const float Lq = pair_sum(rt.lq);
+  if (whole) {
+    if (rho < rows) {
+      const int ra = row0 + rho;
+      const size_t orow = size_t(w.q.q0 + ra / a.G) * a.hq + size_t(head) * a.G + ra % a.G;
+      const float inv = Lq > 0.0f ? 1.0f / Lq : 0.0f;
+      uint16_t* po = a.out + orow * kD + 4 * h;
 #pragma unroll
-  for (int i = 0; i < MT; ++i) {
-    const float L = quad_sum(rt[i].l);
-    const float Lq = quad_sum(rt[i].lq);
-    const int rho = 16 * i + lr;
-    if (whole) {
-      if (rho < rows) {
-        const int ra = row0 + rho;
-        const size_t orow = size_t(w.q.q0 + ra / a.G) * a.hq + size_t(head) * a.G + ra % a.G;
-        const float inv = Lq > 0.0f ? 1.0f / Lq : 0.0f;
+      for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
-        for (int dt = 0; dt < 8; ++dt) {
-          const floatx4 v = rt[i].o[dt] * inv;
-          *reinterpret_cast<uint2*>(a.out + orow * kD + 16 * dt + 4 * lg) =
-              make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+        for (int r = 0; r < 16; r += 4)
+          *reinterpret_cast<uint2*>(po + 32 * dt + 2 * r) =
+              make_uint2(pack_bf16x2(rt.o[dt][r] * inv, rt.o[dt][r + 1] * inv),
+                         pack_bf16x2(rt.o[dt][r + 2] * inv, rt.o[dt][r + 3] * inv));
+      if (a.lse != nullptr && h == 0)
+        a.lse[orow] = L > 0.0f ? (rt.m + log2f(L)) * kLn2 : -__builtin_inff();
+    }
+  } else {
+    float mx = 0.0f;
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, fabsf(rt.o[dt][r]));
+    mx = pair_max(mx);
+    const int e = mx > 0.0f ? __builtin_amdgcn_frexp_expf(mx) - 15 : 0;
+    if (rho < rows) {
+      const float sc = __builtin_amdgcn_ldexpf(1.0f, -e);
+      const size_t prow = (size_t(b) * 2 + part_slot) * kQ8Rows + rho;
+#pragma unroll
+      for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+        for (int r = 0; r < 16; r += 8) {  // (dims as q8_combine takes them)
+          halfx8 v;
+#pragma unroll
+          for (int k = 0; k < 8; ++k) v[k] = static_cast<_Float16>(rt.o[dt][r + k] * sc);
+          *reinterpret_cast<halfx8*>(ws.part_o + prow * kD + 32 * dt + 2 * r + 8 * h) = v;
         }
-        if (a.lse != nullptr && lg == 0)
-          a.lse[orow] = L > 0.0f ? (rt[i].m + log2f(L)) * kLn2 : -__builtin_inff();
-      }
-    } else {
-      float mx = 0.0f;
-#pragma unroll
-      for (int dt = 0; dt < 8; ++dt)
-#pragma unroll
-        for (int c = 0; c < 4; ++c) mx = fmaxf(mx, fabsf(rt[i].o[dt][c]));
-      mx = quad_max(mx);
-      const int e = mx > 0.0f ? __builtin_amdgcn_frexp_expf(mx) - 15 : 0;
-      if (rho < rows) {
-        const float sc = __builtin_amdgcn_ldexpf(1.0f, -e);
-        const size_t prow = (size_t(b) * 2 + part_slot) * kQ8Rows + rho;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const halfx4 a0 = __builtin_convertvector(rt[i].o[2 * j] * sc, halfx4);
-          const halfx4 a1 = __builtin_convertvector(rt[i].o[2 * j + 1] * sc, halfx4);
-          *reinterpret_cast<halfx8*>(ws.part_o + prow * kD + part_dim(32 * j + 4 * lg)) =
-              halfx8{a0[0], a0[1], a0[2], a0[3], a1[0], a1[1], a1[2], a1[3]};
-        }
-        if (lg == 0)
-          *reinterpret_cast<floatx4*>(ws.part_ml + prow * 4) = floatx4{rt[i].m, L, Lq, float(e)};
-      }
+      if (h == 0)
+        *reinterpret_cast<floatx4*>(ws.part_ml + prow * 4) = floatx4{rt.m, L, Lq, float(e)};
     }
   }
 }
 
 template <int kFmt>
-__global__ __launch_bounds__(kQ8Waves * kWave, 1) void q8_main_kernel(Q8Args a, Q8Ws ws) {
+__global__ __launch_bounds__(kQ8Waves * kWave) __attribute__((amdgpu_waves_per_eu(2, 2))) void
+q8_main_kernel(Q8Args a, Q8Ws ws) {
   __shared__ __attribute__((aligned(1024))) char smem[kQ8Waves * kQ8WaveLds];
   const int wid = wave_id();
   const int b = __builtin_amdgcn_readfirstlane(int(blockIdx.x) * kQ8Waves + wid);
   const Q8Start st = load_start(ws.starts, b);
   if (st.lo >= st.hi) return;  // (no barrier in this kernel: the waves are independent)
   const int lane = threadIdx.x & (kWave - 1);
-  char* lds_wave = smem + wid * kQ8WaveLds;
   const uint32_t ring = __builtin_amdgcn_readfirstlane(
-      uint32_t(reinterpret_cast<uintptr_t>((lds_void_t*)lds_wave)));
-  // rows 0-7 of a tile (and 24-31), rows 8-15 (and 16-23): see q8_swz
-  const uint32_t offa = uint32_t((lane >> 3) * kD + (((lane & 7) ^ (lane >> 4)) << 4));
-  const uint32_t offb = offa ^ 64u;
-  const uint64_t scale_base =
-      lane == 0 ? reinterpret_cast<uint64_t>(a.k_scale) : reinterpret_cast<uint64_t>(a.v_scale);
+      uint32_t(reinterpret_cast<uintptr_t>((lds_void_t*)(smem + wid * kQ8WaveLds))));
+  const uint32_t offs = q8_lane_offsets();
   Q8Walk w;
   w.q = st.q;
-  w.r = st.r;
+  w.req = st.req;
   w.unit = st.unit;
   w.u0 = st.q.tile0 + st.unit * st.q.tpu;
-  Q8Issue is;
-  is.w = w;
-  is.t = st.lo;
-  is.sent = 0;
-#pragma unroll 1
-  for (int k = 0; k < kQ8Stages; ++k) q8_send(is, a, ws, st.hi, ring, offa, offb, scale_base);
-  int done = 0;
+  Q8Table tb = {};
+  tb.alone = st.k == 1;
+  q8_fill(tb, a, ws, w, st.lo, st.hi);
+  q8_prime(tb, a, ring, offs);
   while (true) {
     const int lo = max(st.lo, w.u0), hi = min(st.hi, w.u0 + w.q.tpu);
     const bool whole = w.u0 >= st.lo && w.u0 + w.q.tpu <= st.hi;
     const int slot = w.u0 >= st.lo ? 1 : 0;
-    const int rows = min(w.q.rpp, w.q.nslots * a.G - (w.unit % w.q.passes) * w.q.rpp);
-    const auto seg = [&](auto mt) {
-      q8_segment<kFmt, decltype(mt)::value>(a, ws, w, lo, hi, st.hi, b, lds_wave, ring, is, done,
-                                            offa, offb, scale_base, whole, slot);
-    };
-    if (rows <= 16) seg(std::integral_constant<int, 1>{});
-    else if (rows <= 32) seg(std::integral_constant<int, 2>{});
-    else if (rows <= 48) seg(std::integral_constant<int, 3>{});
-    else seg(std::integral_constant<int, 4>{});
+    q8_segment<kFmt>(a, ws, w, lo, hi, st.hi, b, st.k, st.member, ring, tb, offs, whole, slot);
     if (hi >= st.hi) break;
     q8_next_unit(w, a, ws);
   }
 }
 
 // ------------------------------------------------------------- combine ----
-// Workgroup (b, y): rows 16 y .. 16 y + 15 of the unit that is cut first at wave b's
-// range (if any); a thread has 8 dims of a row.  Parts in the order of the waves.
+// Workgroup (b, y): rows 16 y .. 16 y + 15 that wave b has of the unit that is cut first
+// at its range (if any); a thread has 8 dims of a row.  Parts in the order of the gangs.
 __global__ __launch_bounds__(256) void q8_combine_kernel(Q8Args a, Q8Ws ws) {
   const int b = blockIdx.x;
   const Q8Start st = load_start(ws.starts, b);
   if (st.cut_last == 0) return;
   const int head = st.unit / st.q.passes;
-  const int row0 = (st.unit % st.q.passes) * st.q.rpp;
+  const int row0 = (st.unit % st.q.passes * st.k + st.member) * st.q.rpp;
   const int rows = min(st.q.rpp, st.q.nslots * a.G - row0);
   const int rho = blockIdx.y * 16 + threadIdx.x / 16;
   if (rho >= rows) return;
-  const int piece = threadIdx.x & 15;  // 8 halves of the partial: dims as in part_dim
-  const int np = st.cut_last - b + 2;
+  const int piece = threadIdx.x & 15;  // 8 halves of the partial
+  const int np = st.cut_last - st.gang + 2;
   const auto prow = [&](int i) {
-    return (size_t(b - 1 + i) * 2 + (i == 0 ? 1 : 0)) * kQ8Rows + size_t(rho);
+    const int wave = q8_wave_of(st.gang - 1 + i, st.k, st.wg0, st.nwg) + st.member;
+    return (size_t(wave) * 2 + (i == 0 ? 1 : 0)) * kQ8Rows + size_t(rho);
   };
   float M = -__builtin_inff();
   for (int i = 0; i < np; ++i) M = fmaxf(M, ws.part_ml[prow(i) * 4]);
@@ -789,11 +1032,11 @@ __global__ __launch_bounds__(256) void q8_combine_kernel(Q8Args a, Q8Ws ws) {
   const int ra = row0 + rho;
   const size_t orow = size_t(st.q.q0 + ra / a.G) * a.hq + size_t(head) * a.G + ra % a.G;
   const float inv = Lq > 0.0f ? 1.0f / Lq : 0.0f;
-  // halves 0-3: dims 32 (piece / 4) + 4 (piece % 4) + i, halves 4-7: the same + 16
-  uint16_t* po = a.out + orow * kD + 32 * (piece >> 2) + 4 * (piece & 3);
+  // piece 4 dt + 2 k + h holds dims 32 dt + 16 k + 4 h + 0..3 and the same + 8
+  uint16_t* po = a.out + orow * kD + 32 * (piece >> 2) + 16 * ((piece >> 1) & 1) + 4 * (piece & 1);
   *reinterpret_cast<uint2*>(po) =
       make_uint2(pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv));
-  *reinterpret_cast<uint2*>(po + 16) =
+  *reinterpret_cast<uint2*>(po + 8) =
       make_uint2(pack_bf16x2(acc[4] * inv, acc[5] * inv), pack_bf16x2(acc[6] * inv, acc[7] * inv));
   if (a.lse != nullptr && piece == 0)
     a.lse[orow] = L > 0.0f ? (M + log2f(L)) * kLn2 : -__builtin_inff();
@@ -803,18 +1046,16 @@ __global__ __launch_bounds__(256) void q8_combine_kernel(Q8Args a, Q8Ws ws) {
 
 size_t attn_q8_workspace_bytes(int32_t R, int32_t max_rows, int32_t hq, int32_t hkv,
                                int32_t max_pages) {
-  (void)max_rows;
-  (void)hq;
-  (void)hkv;
   size_t n = 0;
-  q8_layout(nullptr, R, max_pages, q8_waves(), &n);
+  q8_layout(nullptr, R, max_rows, hq, hkv, max_pages, q8_waves(), &n);
   return n;
 }
 
 int32_t launch_tree_verify_attn_q8(const AttnQ8Args& x, hipStream_t stream) {
   (void)hipGetLastError();
   const int nw = q8_waves();
-  const Q8Ws ws = q8_layout(x.workspace, x.R, x.max_pages, nw, nullptr);
+  const Q8Ws ws = q8_layout(x.workspace, x.R, x.max_rows, x.hq, x.cache.hkv, x.max_pages,
+                            nw, nullptr);
   Q8Args a;
   a.q = x.q;
   a.k_new = x.k_new;
@@ -847,8 +1088,10 @@ int32_t launch_tree_verify_attn_q8(const AttnQ8Args& x, hipStream_t stream) {
     hipLaunchKernelGGL(q8_pages_kernel, dim3(unsigned(a.R), unsigned(chunks)), dim3(kPageChunk), 0,
                        stream, a, ws.bad);
   }
-  hipLaunchKernelGGL(q8_plan_kernel, dim3(1), dim3(kPlanThreads),
-                     (size_t(a.R) + 1) * sizeof(int32_t), stream, a, ws, nw, chunks);
+  const long long split = (long long)a.max_rows * (a.hq + a.hkv);
+  hipLaunchKernelGGL(q8_plan_kernel, dim3(unsigned(1 + (split + kPlanRows - 1) / kPlanRows)),
+                     dim3(kPlanThreads),
+                     2 * size_t(a.R) * sizeof(int32_t), stream, a, ws, nw, chunks);
   hipLaunchKernelGGL(x.cache.format == ECHO_KV_E4M3 ? q8_main_kernel<ECHO_KV_E4M3>
                                                     : q8_main_kernel<ECHO_KV_E5M2>,
                      dim3(unsigned(nw / kQ8Waves)), dim3(kQ8Waves * kWave), 0, stream, a, ws);

@@ -42,6 +42,8 @@ def _attn(**kw):
 @pytest.mark.parametrize("bad,code", BAD_CACHE + [
     (dict(R=0), INVALID), (dict(R=4096), UNSUPPORTED), (dict(max_rows=-1), INVALID), (dict(hq=6), INVALID),
     (dict(mask_words=0), INVALID), (dict(max_pages=0), INVALID), (dict(max_pages=1 << 26), UNSUPPORTED),
+    (dict(R=4000, max_pages=1 << 20, ws_bytes=1 << 60), UNSUPPORTED),
+    (dict(num_pages=(1 << 25) - 1, page_size=32, hkv=512, hq=512), UNSUPPORTED),
     (dict(max_rows=1 << 23), UNSUPPORTED), (dict(scale=0.0), INVALID), (dict(scale=float("nan")), INVALID),
     (dict(scale=float("inf")), INVALID), (dict(q=None), INVALID), (dict(k_new=None), INVALID),
     (dict(v_new=P(8)), INVALID), (dict(q=P(8)), INVALID), (dict(out=P(264)), INVALID),
