@@ -3,20 +3,20 @@
 // for large block tables:
 //
 //   q8_pages    checks the page ids (small tables: the plan does).
-//   q8_plan     one workgroup.  A unit is one KV head of one request with up to 48 of
-//               its rows (verify slots x query heads of the GQA group); its tiles
-//               are first the tree's (32 new keys each), then the prefix's, one
-//               32-token block each.  The tiles of all units are cut into equal
-//               contiguous ranges, one per wave of the main kernel: a head's blocks
-//               lie in one piece, so nothing is gained by waves that read the heads
-//               of the same tokens side by side, and one head's keys are spread over
-//               as many waves as they can feed.
-//   q8_main     persistent, one workgroup of eight independent waves per CU.  A wave
-//               copies its tiles HBM -> LDS into a ring of its own with direct-to-LDS
-//               loads, converts a tile to bfloat16 (exact) and multiplies it with
-//               all rows of the unit: S^T = K Q^T and O^T = V^T P^T on
-//               v_mfma_f32_16x16x32_bf16 with an online softmax in base 2.  The K
-//               scale goes into the softmax's factor, the V scale into its exponent.
+//   q8_plan     one workgroup plans, the others split the rows of Q and of the new keys.
+//               A unit is one KV head of one request with up to 32, 64 or 128 of its
+//               rows (verify slots x query heads of the GQA group); its steps are first
+//               the tree's (32 new keys each), then the prefix's, two 32-token blocks
+//               each.  The steps of all units are cut into equal contiguous ranges: a
+//               head's blocks lie in one piece, so nothing is gained by waves that read
+//               the heads of the same tokens side by side, and one head's keys are
+//               spread over as many waves as they can feed.
+//   q8_main     persistent, two workgroups of four independent waves per CU.  A wave has
+//               32 rows.  It copies its tiles HBM -> LDS into slots of its own with
+//               direct-to-LDS loads: S^T = K Q^T on the cache's bytes, O^T += V^T P^T
+//               with V widened to bfloat16 (exact), an online softmax in base 2 between
+//               them.  The K scale goes into the softmax's factor, the V scale into its
+//               exponent.
 //   q8_combine  merges the partial sums of units that several waves share.
 //
 // Softmax statistics and sums are fp32.  The weights p are rounded to bfloat16 for
@@ -44,10 +44,11 @@ static_assert(kQ8Wgs * kQ8Waves * kQ8WaveLds <= 160 * 1024, "gfx950 LDS per CU")
 constexpr int kQ8Copies = 8;       // copy instructions per step and tensor
 constexpr int kSplitBytes = 2 * kD;               // a row as two 8-bit numbers per dim
 // What a step costs a workgroup that has 4, 2 or 1 gangs at work, relative to each other.
-constexpr double kQ8Cost1 = 1.4, kQ8Cost2 = 2.2, kQ8Cost4 = 4.0;
+constexpr float kQ8Cost1 = 1.4f, kQ8Cost2 = 2.2f, kQ8Cost4 = 4.0f;
 constexpr int kPlanThreads = 1024;
 constexpr int kPlanRows = kPlanThreads / 16;      // rows that a workgroup beside the plan's splits
-constexpr int kPlanPages = 8 * kPlanThreads;      // block-table entries the plan checks itself
+constexpr int kPlanBatch = 16;     // block-table entries per thread and round trip
+constexpr int kPlanPages = 2 * kPlanBatch * kPlanThreads;  // entries that the plan checks itself
 
 typedef int intx2 __attribute__((ext_vector_type(2)));
 typedef int intx8 __attribute__((ext_vector_type(8)));
@@ -68,11 +69,11 @@ constexpr int kQ8Classes = 3;  // k = 1 << class
 
 // One request as the plan shapes it, in the list of its class: Hkv * passes units (unit =
 // head * passes + pass) of tpu steps each, from step tile0 of the class on; gang member
-// m has rows rpp (k pass + m) .. of a head.
+// m has rows 32 (k pass + m) .. of a head, as far as there are so many.
 struct Q8Req {
   int32_t tile0, tpu;
   int32_t q0, nslots;
-  int32_t P, r, passes, rpp;
+  int32_t P, r, passes, pad;
 };
 
 // A wave's range of steps and where it starts (req: place in the class's list).
@@ -129,6 +130,8 @@ __host__ __device__ inline int q8_page_chunks(int max_pages) {
   return (max_pages + kPageChunk - 1) / kPageChunk;
 }
 
+// Whether the plan checks the page ids itself, with loads issued beside those of the
+// requests' fields (a launch of their own costs 3-5 us).
 __host__ inline bool q8_plan_checks(int R, int max_pages) {
   return (long long)R * max_pages <= kPlanPages;
 }
@@ -182,23 +185,19 @@ __global__ __launch_bounds__(kPageChunk) void q8_pages_kernel(Q8Args a, int32_t*
 }
 
 // ---------------------------------------------------------------- plan ----
-// The request's shape and class (-1: nothing to do).
-__device__ __forceinline__ Q8Req shape_of(const Q8Args& a, int r, bool ok, int& cls) {
+// The request's shape and class (-1: nothing to do), given that its fields are in range.
+__device__ __forceinline__ Q8Req shape_of(int r, int q0, int nslots, int P, int G, int& cls) {
   Q8Req s = {};
-  cls = -1;
-  if (!ok) return s;
-  s.q0 = a.q_offsets[r];
-  s.nslots = a.q_offsets[r + 1] - s.q0;
-  s.P = a.prefix_len[r];
+  s.q0 = q0;
+  s.nslots = nslots;
+  s.P = P;
   s.r = r;
-  const int rows = s.nslots * a.G;
-  if (rows == 0) return s;
-  cls = rows <= kQ8Rows ? 0 : rows <= 2 * kQ8Rows ? 1 : 2;
-  const int k = 1 << cls;
-  s.passes = (rows + k * kQ8Rows - 1) / (k * kQ8Rows);
-  s.rpp = (rows + k * s.passes - 1) / (k * s.passes);
-  s.tpu = (s.nslots + kTileKeys - 1) / kTileKeys +
-          int(((long long)s.P + kQ8StepKeys - 1) / kQ8StepKeys);
+  const int rows = nslots * G;
+  cls = rows == 0 ? -1 : rows <= kQ8Rows ? 0 : rows <= 2 * kQ8Rows ? 1 : 2;
+  const int unit = kQ8Rows << max(cls, 0);
+  s.passes = (rows + unit - 1) / unsigned(unit);
+  s.tpu = (nslots + kTileKeys - 1) / kTileKeys +
+          int((unsigned(P) + kQ8StepKeys - 1) / kQ8StepKeys);
   return s;
 }
 
@@ -239,161 +238,187 @@ __device__ __forceinline__ void q8_split(const uint16_t* rows, uint8_t* split, i
   if (lane16 == 0) exps[r] = e;
 }
 
-// Workgroup 0 plans; the others split the query rows and the new keys.
-__global__ __launch_bounds__(kPlanThreads) void q8_plan_kernel(Q8Args a, Q8Ws ws, int nw_max,
-                                                               int chunks) {
-  extern __shared__ int32_t s_tile0[];  // [R] first step of each listed request, [R] the request
-  __shared__ uint8_t s_bad[ECHO_MAX_REQUESTS + 1];
-  __shared__ long long s_total[kQ8Classes][kPlanThreads / kWave];
-  __shared__ int2 s_scan[kPlanThreads / kWave + 1];
-  int32_t* s_req = s_tile0 + a.R;
-  const int tid = threadIdx.x;
-  if (blockIdx.x > 0) {
-    const long long r = (long long)(blockIdx.x - 1) * kPlanRows + tid / 16;
-    const long long nq = (long long)a.max_rows * a.hq, nk = (long long)a.max_rows * a.hkv;
-    if (r < nq) q8_split(a.q, ws.qs, ws.qe, r, tid & 15);
-    else if (r - nq < nk) q8_split(a.k_new, ws.ks, ws.ke, r - nq, tid & 15);
-    return;
-  }
+// The plan, on one workgroup.  It runs once, so that its time is the fetching of its code and
+// a few round trips: loops instead of unrolled copies, a wave per class for the scans.
+__device__ __forceinline__ void q8_plan(const Q8Args& a, const Q8Ws& ws, int nw, int chunks,
+                                        int32_t* s_mem) {
+  __shared__ int8_t s_cls[ECHO_MAX_REQUESTS + 1];  // class of each request (-1: none, -2: bad)
+  __shared__ int s_n[kQ8Classes + 1], s_T[kQ8Classes + 1], s_wg[kQ8Classes + 1];
+  __shared__ long long s_T64[kQ8Classes];
+  const int tid = threadIdx.x, lane = tid & (kWave - 1), wid = wave_id();
   const int R = a.R;
-  int bits = 0;
+  int32_t* s_tile0 = s_mem;      // [R] first step of each listed request (before: steps of request r)
+  int32_t* s_req = s_mem + R;    // [R] the request (before: pages of request r)
+  int32_t* s_steps = s_mem + 2 * R;  // [R] steps of request r
   // requests whose offsets, length or pages cannot be used
   const bool own = chunks == 0;
-  int pg[8];
-  if (own) {  // every load in flight at once
-    const long long total = (long long)R * a.max_pages;
+  const int entries = own ? R * a.max_pages : 0;
+  int pg[kPlanBatch];
+  if (own) {  // (every load in flight at once)
 #pragma unroll
-    for (int k = 0; k < 8; ++k)
-      pg[k] = a.block_table[min((long long)tid + k * kPlanThreads, total - 1)];
+    for (int k = 0; k < kPlanBatch; ++k)
+      pg[k] = a.block_table[min(tid + k * kPlanThreads, entries - 1)];
   }
+#pragma unroll 1
   for (int r = tid; r < R; r += kPlanThreads) {
-    const int q0 = a.q_offsets[r], q1 = a.q_offsets[r + 1];
-    bool bad = !(q0 >= 0 && q1 >= q0 && q1 <= a.max_rows) || prefix_pages(a.prefix_len[r], a) < 0;
+    const int q0 = a.q_offsets[r], q1 = a.q_offsets[r + 1], P = a.prefix_len[r];
+    const int np = prefix_pages(P, a);
+    bool bad = !(q0 >= 0 && q1 >= q0 && q1 <= a.max_rows) || np < 0;
     for (int c = 0; c < chunks; ++c) bad = bad || ws.bad[size_t(r) * chunks + c] != 0;
-    s_bad[r] = bad ? 1 : 0;
+    int cls = -2;
+    long long steps = 0;
+    if (!bad) {
+      const Q8Req s = shape_of(r, q0, q1 - q0, P, a.G, cls);
+      steps = (long long)a.hkv * s.passes * s.tpu;
+    }
+    s_cls[r] = int8_t(cls);
+    s_req[r] = np;
+    // (offsets that overlap may ask for any number: 2^31 - 1 stands for more)
+    s_steps[r] = int(min(steps, 0x7FFFFFFFll));
   }
   __syncthreads();
   if (own) {
-    const long long total = (long long)R * a.max_pages;
+    const int mp = a.max_pages, dr = kPlanThreads / mp, dc = kPlanThreads % mp;
+    int r = tid / mp, c = tid % mp;  // entry tid + 1024 k is page c of request r
+#pragma unroll 1
+    for (int base = 0; base < entries; base += kPlanBatch * kPlanThreads) {
+      if (base > 0) {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const long long e = (long long)tid + k * kPlanThreads;
-      if (e < total && (pg[k] < 0 || pg[k] >= a.num_pages)) {
-        const int r = int(e / a.max_pages), c = int(e % a.max_pages);
-        if (c < prefix_pages(a.prefix_len[r], a)) s_bad[r] = 1;
+        for (int k = 0; k < kPlanBatch; ++k)
+          pg[k] = a.block_table[min(base + tid + k * kPlanThreads, entries - 1)];
+      }
+#pragma unroll
+      for (int k = 0; k < kPlanBatch; ++k) {
+        if (r < R && (pg[k] < 0 || pg[k] >= a.num_pages) && c < s_req[r]) s_cls[r] = -2;
+        r += dr;
+        c += dc;
+        r += c >= mp ? 1 : 0;
+        c -= c >= mp ? mp : 0;
       }
     }
     __syncthreads();
   }
-  // requests and steps of every class; 64-bit and capped, as offsets that overlap may ask
-  // for any number
-  long long mine[kQ8Classes] = {};  // steps, and requests above bit 48
-  for (int r = tid; r < R; r += kPlanThreads) {
-    if (s_bad[r]) bits |= ECHO_DATA_BAD_OFFSETS;
-    int cls;
-    const Q8Req s = shape_of(a, r, !s_bad[r], cls);
-    for (int c = 0; c < kQ8Classes; ++c)
-      if (c == cls) mine[c] += min((long long)a.hkv * s.passes * s.tpu, 1ll << 32) + (1ll << 48);
-  }
-#pragma unroll
-  for (int c = 0; c < kQ8Classes; ++c) {
-    for (int d = kWave / 2; d > 0; d >>= 1) mine[c] += __shfl_xor(mine[c], d);
-    if ((tid & (kWave - 1)) == 0) s_total[c][tid / kWave] = mine[c];
+  // requests and steps of every class: wave c counts class c
+  if (wid < kQ8Classes) {
+    int n = 0, bits = 0;
+    long long T = 0;
+#pragma unroll 1
+    for (int r = lane; r - lane < R; r += kWave) {
+      const int cls = r < R ? s_cls[r] : -1;
+      if (cls == -2) bits = ECHO_DATA_BAD_OFFSETS;
+      if (cls == wid) {
+        n += 1;
+        T += s_steps[r];
+      }
+    }
+#pragma unroll 1
+    for (int d = kWave / 2; d > 0; d >>= 1) {
+      n += __shfl_xor(n, d);
+      T += __shfl_xor(T, d);
+    }
+    if (lane == 0) {
+      s_n[wid] = n;
+      s_T64[wid] = T;
+    }
+    if (wid == 0) wave_status_or(a.status, bits);
   }
   __syncthreads();
-  long long T[kQ8Classes], all = 0;
-  int count[kQ8Classes];
-#pragma unroll
-  for (int c = 0; c < kQ8Classes; ++c) {
-    long long x = 0;
-    for (int k = 0; k < kPlanThreads / kWave; ++k) x += s_total[c][k];
-    count[c] = int(x >> 48);
-    T[c] = x & ((1ll << 48) - 1);
-    all += T[c];
+  const bool fits = s_T64[0] + s_T64[1] + s_T64[2] <= 0x7FFFFFFFll;
+  if (!fits && tid == 0) status_or(a.status, ECHO_DATA_BAD_OFFSETS);
+  // its list of requests; thread 1023 finds the classes' workgroups: by cost, at least one
+  // where there is work
+  if (fits && wid < kQ8Classes) {
+    int run_n = 0, run_t = 0;
+#pragma unroll 1
+    for (int c = 0; c < wid; ++c) run_n += s_n[c];
+#pragma unroll 1
+    for (int r = lane; r - lane < R; r += kWave) {
+      const bool in = r < R && s_cls[r] == wid;
+      const uint64_t who = __ballot(in);
+      const int steps = in ? s_steps[r] : 0;
+      const int inc = wave_inclusive_sum(steps);
+      if (in) {
+        const int at = run_n + lanes_below(who);
+        s_tile0[at] = run_t + inc - steps;
+        s_req[at] = r;
+      }
+      run_n += __popcll(who);
+      run_t += __builtin_amdgcn_readlane(inc, kWave - 1);
+    }
   }
-  if (all > 0x7FFFFFFFll) {
-    bits |= ECHO_DATA_BAD_OFFSETS;
-    all = 0;
-  }
-  wave_status_or(a.status, bits);
-  for (int b = tid; b < nw_max; b += kPlanThreads) ws.starts[b].lo = ws.starts[b].hi = ws.starts[b].cut_last = 0;
-  if (all == 0) return;
-  // the workgroups of each class: by cost, at least one where there is work
-  const int wgs = nw_max / kQ8Waves;
-  int wg0[kQ8Classes], nwg[kQ8Classes];
-  {
-    const double cost[kQ8Classes] = {kQ8Cost1 * double(T[0]), kQ8Cost2 * double(T[1]),
-                                     kQ8Cost4 * double(T[2])};
-    const double total = cost[0] + cost[1] + cost[2];
-    int left = wgs, need = (T[0] > 0) + (T[1] > 0) + (T[2] > 0);
-    int at = 0;
-#pragma unroll
+  if (tid == kPlanThreads - 1) {
+    const int wgs = nw / kQ8Waves;
+    const float cost[kQ8Classes] = {kQ8Cost1 * float(s_T64[0]), kQ8Cost2 * float(s_T64[1]),
+                                    kQ8Cost4 * float(s_T64[2])};
+    const float per = float(wgs) / (cost[0] + cost[1] + cost[2]);
+    int left = wgs, need = 0;
+    for (int c = 0; c < kQ8Classes; ++c) need += cost[c] > 0.0f ? 1 : 0;
     for (int c = 0; c < kQ8Classes; ++c) {
       int n = 0;
-      if (T[c] > 0) {
+      if (cost[c] > 0.0f) {
         need -= 1;
-        n = need == 0 ? left : min(max(int(wgs * cost[c] / total + 0.5), 1), left - need);
+        n = need == 0 ? left : min(max(int(per * cost[c] + 0.5f), 1), left - need);
       }
-      wg0[c] = at;
-      nwg[c] = n;
-      at += n;
+      s_wg[c] = wgs - left;
+      s_T[c] = fits ? int(s_T64[c]) : 0;
       left -= n;
     }
-  }
-  // the classes' lists of requests
-  int run_n[kQ8Classes] = {0, count[0], count[0] + count[1]}, run_t[kQ8Classes] = {};
-  for (int base = 0; base < R; base += kPlanThreads) {
-    const int r = base + tid;
-    Q8Req s = {};
-    int cls = -1;
-    if (r < R) s = shape_of(a, r, !s_bad[r], cls);
-    const int steps = a.hkv * s.passes * s.tpu;
-#pragma unroll
-    for (int c = 0; c < kQ8Classes; ++c) {
-      int n_tot, t_tot;
-      const int2 ex = block_exclusive_sum2<kPlanThreads>(
-          make_int2(c == cls ? 1 : 0, c == cls ? steps : 0), s_scan, &n_tot, &t_tot);
-      if (c == cls) {
-        s.tile0 = run_t[c] + ex.y;
-        s_tile0[run_n[c] + ex.x] = s.tile0;
-        s_req[run_n[c] + ex.x] = r;
-        ws.reqs[run_n[c] + ex.x] = s;
-      }
-      run_n[c] += n_tot;
-      run_t[c] += t_tot;
-    }
+    s_wg[kQ8Classes] = wgs;
   }
   __syncthreads();
-  int first = 0;
-#pragma unroll
-  for (int c = 0; c < kQ8Classes; ++c) {
-    if (T[c] > 0) {
-      const int k = 1 << c;
-      const long long gangs = (long long)nwg[c] * (kQ8Waves / k);
-      const int ng = int(T[c] < gangs ? T[c] : gangs);
-      const DivBy by_t(T[c]), by_n(ng);
-      for (int x = tid; x < ng * k; x += kPlanThreads) {
-        Q8Start st = {};
-        st.gang = x >> c;
-        st.member = x & (k - 1);
-        st.k = k;
-        st.wg0 = wg0[c];
-        st.nwg = nwg[c];
-        st.lo = int(range_lo(T[c], st.gang, by_n));
-        st.hi = int(range_lo(T[c], st.gang + 1, by_n));
-        st.req = first + upper_bound_idx(s_tile0 + first, count[c], st.lo);
-        int cls;
-        st.q = shape_of(a, s_req[st.req], true, cls);
-        st.q.tile0 = s_tile0[st.req];
-        st.unit = (st.lo - st.q.tile0) / st.q.tpu;
+  // every wave's start, and the listed requests' shapes
+  const auto shape_at = [&](int at) {
+    const int r = s_req[at];
+    const int q0 = a.q_offsets[r];
+    int cls;
+    Q8Req s = shape_of(r, q0, a.q_offsets[r + 1] - q0, a.prefix_len[r], a.G, cls);
+    s.tile0 = s_tile0[at];
+    return s;
+  };
+  const int listed = fits ? s_n[0] + s_n[1] + s_n[2] : 0;
+#pragma unroll 1
+  for (int x = tid; x < max(nw, listed); x += kPlanThreads) {
+    if (x < listed) ws.reqs[x] = shape_at(x);
+    if (x >= nw) continue;
+    const int g = x / kQ8Waves, slot = x % kQ8Waves;
+    int c = 0, first = 0;
+    while (g >= s_wg[c + 1]) first += s_n[c++];  // (s_wg[kQ8Classes] is past every g)
+    Q8Start st = {};
+    const int T = s_T[c];
+    if (T > 0) {
+      st.k = 1 << c;
+      st.wg0 = s_wg[c];
+      st.nwg = s_wg[c + 1] - st.wg0;
+      st.gang = g - st.wg0 + (slot >> c) * st.nwg;
+      st.member = slot & (st.k - 1);
+      const int ng = min(T, st.nwg * (kQ8Waves >> c));
+      if (st.gang < ng) {
+        const DivBy by_n(ng);
+        st.lo = int(range_lo(T, st.gang, by_n));
+        st.hi = int(range_lo(T, st.gang + 1, by_n));
+        st.req = first + upper_bound_idx(s_tile0 + first, s_n[c], st.lo);
+        st.q = shape_at(st.req);
+        st.unit = (st.lo - st.q.tile0) / unsigned(st.q.tpu);
         const int u0 = st.q.tile0 + st.unit * st.q.tpu;
-        if (u0 < st.lo && int(range_lo(T[c], st.gang - 1, by_n)) <= u0)
-          st.cut_last = range_of((long long)u0 + st.q.tpu - 1, T[c], ng, by_t);
-        ws.starts[q8_wave_of(st.gang, k, wg0[c], nwg[c]) + st.member] = st;
+        if (u0 < st.lo && int(range_lo(T, st.gang - 1, by_n)) <= u0)
+          st.cut_last = range_of((long long)u0 + st.q.tpu - 1, T, ng, DivBy(T));
       }
     }
-    first += count[c];
+    ws.starts[x] = st;
   }
+}
+
+// Workgroup 0 plans; the others split the query rows and the new keys.
+__global__ __launch_bounds__(kPlanThreads) void q8_plan_kernel(Q8Args a, Q8Ws ws, int nw, int chunks) {
+  extern __shared__ int32_t s_mem[];  // 3 R words
+  if (blockIdx.x > 0) {
+    const long long r = (long long)(blockIdx.x - 1) * kPlanRows + threadIdx.x / 16;
+    const long long nq = (long long)a.max_rows * a.hq, nk = (long long)a.max_rows * a.hkv;
+    if (r < nq) q8_split(a.q, ws.qs, ws.qe, r, threadIdx.x & 15);
+    else if (r - nq < nk) q8_split(a.k_new, ws.ks, ws.ke, r - nq, threadIdx.x & 15);
+    return;
+  }
+  q8_plan(a, ws, nw, chunks, s_mem);
 }
 
 // ---------------------------------------------------------------- main ----
@@ -502,6 +527,11 @@ __device__ __forceinline__ void q8_next_unit(Q8Walk& w, const Q8Args& a, const Q
   w.u0 = w.q.tile0;
 }
 
+// The first of the member's rows of the unit.
+__device__ __forceinline__ int q8_row0(const Q8Walk& w, int k, int member) {
+  return (w.unit % w.q.passes * k + member) * kQ8Rows;
+}
+
 // What a wave knows of the next 32 steps of its range, tile i (two per step) in lane
 // i & 63: the block, the tokens it holds (32 or more: all), and what the softmax takes
 // of its scales.  A request's last step may have one tile: its second entry is that
@@ -514,7 +544,7 @@ struct Q8Table {
   int tokens;
   float c, lvs, ivs;  // softmax factor x K scale; log2 of the V scale, and its reciprocal
   int known, k_sent, v_sent, done;
-  bool alone;
+  int k, member;      // of the wave's gang
 };
 
 // Fills the table from step t of the unit at w on.
@@ -528,6 +558,8 @@ __device__ __forceinline__ void q8_fill(Q8Table& tb, const Q8Args& a, const Q8Ws
     const int end = min(hi, w.u0 + w.q.tpu);
     const int p0 = w.u0 + w.ntail();
     t = max(t, min(end, p0));
+    // (a member without rows of this unit takes none of its steps)
+    if (q8_row0(w, tb.k, tb.member) >= w.q.nslots * a.G) t = end;
     const int m = min((kWave - n) / 2, end - t);
     if (lane >= n && lane < n + 2 * m) {
       key = (t - p0) * kQ8StepKeys + (lane - n) * kTileKeys;
@@ -596,7 +628,7 @@ __device__ __forceinline__ void q8_send(const Q8Table& tb, int& sent, const uint
   const int tn1 = lane_of(tb.tokens, i + 1);
   if (tn1 >= kTileKeys) {
     const uint32_t offa = copy_offset(offs);
-    q8_copy(lds, t0, t1, offa, offa ^ 64u, tb.alone);
+    q8_copy(lds, t0, t1, offa, offa ^ 64u, tb.k == 1);
   } else {
     const int lane = threadIdx.x & (kWave - 1);
     const int tn0 = lane_of(tb.tokens, i);
@@ -820,21 +852,20 @@ __device__ __forceinline__ void q8_prime(Q8Table& tb, const Q8Args& a, uint32_t 
 // conversion.
 template <int kFmt>
 __device__ __forceinline__ void q8_segment(const Q8Args& a, const Q8Ws& ws, const Q8Walk& w, int lo,
-                                           int hi, int range_hi, int b, int k, int member,
-                                           uint32_t ring, Q8Table& tb, uint32_t offs, bool whole,
-                                           int part_slot) {
+                                           int hi, int range_hi, int b, uint32_t ring, Q8Table& tb,
+                                           uint32_t offs, bool whole, int part_slot) {
   const int lane = threadIdx.x & (kWave - 1);
   const int h = lane >> 5;
   const int head = w.unit / w.q.passes;
-  const int row0 = (w.unit % w.q.passes * k + member) * w.q.rpp;
-  const int rows = min(w.q.rpp, w.q.nslots * a.G - row0);  // (0 or less: none)
+  const int row0 = q8_row0(w, tb.k, tb.member);
+  const int rows = min(kQ8Rows, w.q.nslots * a.G - row0);
   intx8 q[2][2];  // [hi, lo][half of the dims]
   int qe;
   Q8Rows rt;
   int t = lo;
   {
     // (a row past the last one computes the last one again, to be dropped)
-    const int ra = min(row0 + min(lane & 31, w.q.rpp - 1), w.q.nslots * a.G - 1);
+    const int ra = row0 + min(lane & 31, rows - 1);
     const int slot = w.q.q0 + ra / a.G;
     const size_t row = size_t(slot) * a.hq + size_t(head) * a.G + ra % a.G;
     const uint8_t* p = ws.qs + row * kSplitBytes + 32 * h;
@@ -982,20 +1013,24 @@ q8_main_kernel(Q8Args a, Q8Ws ws) {
   w.unit = st.unit;
   w.u0 = st.q.tile0 + st.unit * st.q.tpu;
   Q8Table tb = {};
-  tb.alone = st.k == 1;
+  tb.k = st.k;
+  tb.member = st.member;
   q8_fill(tb, a, ws, w, st.lo, st.hi);
   q8_prime(tb, a, ring, offs);
   while (true) {
     const int lo = max(st.lo, w.u0), hi = min(st.hi, w.u0 + w.q.tpu);
     const bool whole = w.u0 >= st.lo && w.u0 + w.q.tpu <= st.hi;
     const int slot = w.u0 >= st.lo ? 1 : 0;
-    q8_segment<kFmt>(a, ws, w, lo, hi, st.hi, b, st.k, st.member, ring, tb, offs, whole, slot);
+    if (q8_row0(w, tb.k, tb.member) < w.q.nslots * a.G)
+      q8_segment<kFmt>(a, ws, w, lo, hi, st.hi, b, ring, tb, offs, whole, slot);
     if (hi >= st.hi) break;
     q8_next_unit(w, a, ws);
   }
 }
 
 // ------------------------------------------------------------- combine ----
+constexpr int kQ8Parts = 8;  // partial sums per round trip
+
 // Workgroup (b, y): rows 16 y .. 16 y + 15 that wave b has of the unit that is cut first
 // at its range (if any); a thread has 8 dims of a row.  Parts in the order of the gangs.
 __global__ __launch_bounds__(256) void q8_combine_kernel(Q8Args a, Q8Ws ws) {
@@ -1003,8 +1038,8 @@ __global__ __launch_bounds__(256) void q8_combine_kernel(Q8Args a, Q8Ws ws) {
   const Q8Start st = load_start(ws.starts, b);
   if (st.cut_last == 0) return;
   const int head = st.unit / st.q.passes;
-  const int row0 = (st.unit % st.q.passes * st.k + st.member) * st.q.rpp;
-  const int rows = min(st.q.rpp, st.q.nslots * a.G - row0);
+  const int row0 = (st.unit % st.q.passes * st.k + st.member) * kQ8Rows;
+  const int rows = min(kQ8Rows, st.q.nslots * a.G - row0);
   const int rho = blockIdx.y * 16 + threadIdx.x / 16;
   if (rho >= rows) return;
   const int piece = threadIdx.x & 15;  // 8 halves of the partial
@@ -1013,22 +1048,38 @@ __global__ __launch_bounds__(256) void q8_combine_kernel(Q8Args a, Q8Ws ws) {
     const int wave = q8_wave_of(st.gang - 1 + i, st.k, st.wg0, st.nwg) + st.member;
     return (size_t(wave) * 2 + (i == 0 ? 1 : 0)) * kQ8Rows + size_t(rho);
   };
-  float M = -__builtin_inff();
-  for (int i = 0; i < np; ++i) M = fmaxf(M, ws.part_ml[prow(i) * 4]);
-  float L = 0.0f, Lq = 0.0f;
+  float M = -__builtin_inff(), L = 0.0f, Lq = 0.0f;
   float acc[8] = {};
-  if (M != -__builtin_inff())
-    for (int i = 0; i < np; ++i) {
-      const floatx4 ml = *reinterpret_cast<const floatx4*>(ws.part_ml + prow(i) * 4);
-      const halfx8 h = *reinterpret_cast<const halfx8*>(ws.part_o + prow(i) * kD + piece * 8);
-      if (ml[0] == -__builtin_inff()) continue;
-      const float wgt = __builtin_amdgcn_exp2f(ml[0] - M);
-      L = __builtin_fmaf(wgt, ml[1], L);
-      Lq = __builtin_fmaf(wgt, ml[2], Lq);
-      const float ws8 = wgt * __builtin_amdgcn_ldexpf(1.0f, int(ml[3]));
+  for (int i0 = 0; i0 < np; i0 += kQ8Parts) {  // (a batch's loads in one round trip)
+    floatx4 ml[kQ8Parts];
+    halfx8 h[kQ8Parts];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) acc[k] = __builtin_fmaf(ws8, float(h[k]), acc[k]);
+    for (int j = 0; j < kQ8Parts; ++j) {
+      const size_t at = prow(min(i0 + j, np - 1));
+      ml[j] = *reinterpret_cast<const floatx4*>(ws.part_ml + at * 4);
+      h[j] = *reinterpret_cast<const halfx8*>(ws.part_o + at * kD + piece * 8);
     }
+    float m = M;
+#pragma unroll
+    for (int j = 0; j < kQ8Parts; ++j)
+      if (i0 + j < np) m = fmaxf(m, ml[j][0]);
+    if (m == -__builtin_inff()) continue;
+    const float alpha = __builtin_amdgcn_exp2f(M - m);  // 0 from -inf
+    M = m;
+    L *= alpha;
+    Lq *= alpha;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) acc[k] *= alpha;
+#pragma unroll
+    for (int j = 0; j < kQ8Parts; ++j) {
+      const float wgt = i0 + j < np ? __builtin_amdgcn_exp2f(ml[j][0] - m) : 0.0f;
+      L = __builtin_fmaf(wgt, ml[j][1], L);
+      Lq = __builtin_fmaf(wgt, ml[j][2], Lq);
+      const float wo = wgt * __builtin_amdgcn_ldexpf(1.0f, int(ml[j][3]));
+#pragma unroll
+      for (int k = 0; k < 8; ++k) acc[k] = __builtin_fmaf(wo, float(h[j][k]), acc[k]);
+    }
+  }
   const int ra = row0 + rho;
   const size_t orow = size_t(st.q.q0 + ra / a.G) * a.hq + size_t(head) * a.G + ra % a.G;
   const float inv = Lq > 0.0f ? 1.0f / Lq : 0.0f;
@@ -1091,7 +1142,7 @@ int32_t launch_tree_verify_attn_q8(const AttnQ8Args& x, hipStream_t stream) {
   const long long split = (long long)a.max_rows * (a.hq + a.hkv);
   hipLaunchKernelGGL(q8_plan_kernel, dim3(unsigned(1 + (split + kPlanRows - 1) / kPlanRows)),
                      dim3(kPlanThreads),
-                     2 * size_t(a.R) * sizeof(int32_t), stream, a, ws, nw, chunks);
+                     3 * size_t(a.R) * sizeof(int32_t), stream, a, ws, nw, chunks);
   hipLaunchKernelGGL(x.cache.format == ECHO_KV_E4M3 ? q8_main_kernel<ECHO_KV_E4M3>
                                                     : q8_main_kernel<ECHO_KV_E5M2>,
                      dim3(unsigned(nw / kQ8Waves)), dim3(kQ8Waves * kWave), 0, stream, a, ws);
