@@ -12,9 +12,16 @@ namespace echo {
 namespace {
 
 constexpr int kStoreThreads = 256;
+// Rows per wave: as few as this many waves allow, up to a block's.  A wave with many rows
+// appends the runs that start in them one after another, 1.5 us each; a wave that starts
+// no run is a launch for nothing.  With eight heads, 1 | 8 | 32 rows per wave: 1024 single
+// tokens take 15.9 | 16.7 | 54 us (by the rule, 4: 11.9), 2048 prompt rows 21.8 | 10.5 |
+// 10.5 us (8), 40960 prompt rows 356 | 144 | 49 us (32).
+constexpr int kStoreWaves = 4096;
 constexpr int kCommitQ8Threads = 1024;
 
-// Wave -> (chunk of rows_per_wave rows, head, tensor), tensor fastest, then head.  The
+// Wave -> (chunk of rows_per_wave rows, tensor, head), head fastest: a workgroup's waves read
+// neighbouring heads of the same rows.  The
 // wave appends the runs that start in its chunk; a run ends within 32 rows.
 template <int kFmt>
 __global__ __launch_bounds__(kStoreThreads) void store_kv_q8_kernel(
@@ -25,7 +32,7 @@ __global__ __launch_bounds__(kStoreThreads) void store_kv_q8_kernel(
   const long long wave = (long long)blockIdx.x * (kStoreThreads / kWave) + threadIdx.x / kWave;
   const int per = 2 * c.hkv;
   const long long chunk = wave / per;
-  const int head = int(wave % per) >> 1, tensor = int(wave % per) & 1;
+  const int tensor = int(wave % per) >= c.hkv ? 1 : 0, head = int(wave % per) - tensor * c.hkv;
   const long long i0 = chunk * rows_per_wave;
   if (i0 >= T) return;  // uniform
   // the slots of the chunk's rows and of those that its last run may take in
@@ -134,7 +141,10 @@ int32_t launch_store_kv_q8(const uint16_t* k, const uint16_t* v, int64_t k_strid
                            int32_t* status, hipStream_t stream) {
   (void)hipGetLastError();
   const CacheQ8 c = cache_of(a);
-  const int rows_per_wave = num_rows <= 2048 ? 1 : kBlockTokens;
+  int rows_per_wave = 1;
+  while (rows_per_wave < kBlockTokens &&
+         (long long)num_rows * (2 * a.hkv) > (long long)rows_per_wave * kStoreWaves)
+    rows_per_wave *= 2;
   const long long waves =
       ((long long)num_rows + rows_per_wave - 1) / rows_per_wave * (2ll * a.hkv);
   const long long wgs = (waves + kStoreThreads / kWave - 1) / (kStoreThreads / kWave);

@@ -85,6 +85,13 @@ __device__ __forceinline__ uint32_t finite_mag2(uint32_t w) {
   return max(lo < 0x7F80u ? lo : 0u, hi < 0x7F80u ? hi : 0u);
 }
 
+// 16 bytes that are read once, past the caches' reuse order (prompts: 57 -> 54 us for 252 MB).
+__device__ __forceinline__ uint4 load_once(const uint4* p) {
+  typedef uint32_t uint4w __attribute__((ext_vector_type(4)));
+  const uint4w w = __builtin_nontemporal_load(reinterpret_cast<const uint4w*>(p));
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
 // One wave appends n rows (1..32) of a head to a block whose first o rows hold tokens
 // (o + n <= 32): the block's scale is the larger of the one it has (if o > 0) and the
 // one that the new rows need; where it grows, the o rows are scaled again.  Rows
@@ -99,7 +106,7 @@ __device__ __forceinline__ void append_block(const Src& src, int n, int o, uint8
   for (int j = 0; j < 8; ++j) {
     x[j] = make_uint4(0, 0, 0, 0);
     if (4 * j < n) {  // uniform
-      if (4 * j + row < n) x[j] = reinterpret_cast<const uint4*>(src(4 * j + row))[col];
+      if (4 * j + row < n) x[j] = load_once(reinterpret_cast<const uint4*>(src(4 * j + row)) + col);
     }
   }
   // the block's old bytes, should they need another scale, in the same round trip
