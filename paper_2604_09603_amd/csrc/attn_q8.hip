@@ -3,8 +3,7 @@
 // for large block tables:
 //
 //   q8_pages    checks the page ids (small tables: the plan does).
-//   q8_plan     one workgroup plans, the others split the rows of Q and of the new keys.
-//               A unit is one KV head of one request with up to 32, 64 or 128 of its
+//   q8_plan     one workgroup.  A unit is one KV head of one request with up to 32, 64 or 128 of its
 //               rows (verify slots x query heads of the GQA group); its steps are first
 //               the tree's (32 new keys each), then the prefix's, two 32-token blocks
 //               each.  The steps of all units are cut into equal contiguous ranges: a
@@ -13,9 +12,8 @@
 //               spread over as many waves as they can feed.
 //   q8_main     persistent, two workgroups of four independent waves per CU.  A wave has
 //               32 rows.  It copies its tiles HBM -> LDS into slots of its own with
-//               direct-to-LDS loads: S^T = K Q^T on the cache's bytes, O^T += V^T P^T
-//               with V widened to bfloat16 (exact), an online softmax in base 2 between
-//               them.  The K scale goes into the softmax's factor, the V scale into its
+//               direct-to-LDS loads: S^T = K Q^T and O^T += V^T P^T with K and V widened to
+//               bfloat16 (exact), an online softmax in base 2 between them.  The K scale goes into the softmax's factor, the V scale into its
 //               exponent.
 //   q8_combine  merges the partial sums of units that several waves share.
 //
@@ -42,11 +40,9 @@ constexpr int kQ8Scratch = 16 * kD * 2;           // 16 rows of bfloat16 V (tree
 constexpr int kQ8WaveLds = 2 * kQ8Slot + kQ8Scratch;  // K, V, scratch
 static_assert(kQ8Wgs * kQ8Waves * kQ8WaveLds <= 160 * 1024, "gfx950 LDS per CU");
 constexpr int kQ8Copies = 8;       // copy instructions per step and tensor
-constexpr int kSplitBytes = 2 * kD;               // a row as two 8-bit numbers per dim
 // What a step costs a workgroup that has 4, 2 or 1 gangs at work, relative to each other.
 constexpr float kQ8Cost1 = 1.4f, kQ8Cost2 = 2.2f, kQ8Cost4 = 4.0f;
 constexpr int kPlanThreads = 1024;
-constexpr int kPlanRows = kPlanThreads / 16;      // rows that a workgroup beside the plan's splits
 constexpr int kPlanBatch = 16;     // block-table entries per thread and round trip
 constexpr int kPlanPages = 2 * kPlanBatch * kPlanThreads;  // entries that the plan checks itself
 
@@ -98,10 +94,6 @@ struct Q8Ws {
   Q8Start* starts;   // [waves]
   Q8Req* reqs;       // [R], class by class
   int32_t* bad;      // [R][chunks] flags of q8_pages
-  uint8_t* qs;       // [max_rows][Hq] rows split in two 8-bit numbers: see q8_split
-  int32_t* qe;       // [max_rows][Hq] their scale exponents
-  uint8_t* ks;       // [max_rows][Hkv] the new keys, the same
-  int32_t* ke;
   float* part_ml;    // [waves][2][32][4]: max, sum, sum of the weights used, scale exponent
   _Float16* part_o;  // [waves][2][32][128]
 };
@@ -146,15 +138,6 @@ __host__ inline Q8Ws q8_layout(void* base, int R, int max_rows, int hq, int hkv,
   p += al(size_t(R) * sizeof(Q8Req));
   w.bad = reinterpret_cast<int32_t*>(p);
   if (!q8_plan_checks(R, max_pages)) p += al(size_t(R) * size_t(q8_page_chunks(max_pages)) * 4);
-  const size_t nq = size_t(max_rows) * size_t(hq), nk = size_t(max_rows) * size_t(hkv);
-  w.qs = reinterpret_cast<uint8_t*>(p);
-  p += al(nq * kSplitBytes);
-  w.qe = reinterpret_cast<int32_t*>(p);
-  p += al(nq * 4);
-  w.ks = reinterpret_cast<uint8_t*>(p);
-  p += al(nk * kSplitBytes);
-  w.ke = reinterpret_cast<int32_t*>(p);
-  p += al(nk * 4);
   w.part_ml = reinterpret_cast<float*>(p);
   p += al(size_t(nw) * 2 * kQ8Rows * 4 * sizeof(float));
   w.part_o = reinterpret_cast<_Float16*>(p);
@@ -201,47 +184,10 @@ __device__ __forceinline__ Q8Req shape_of(int r, int q0, int nslots, int P, int 
   return s;
 }
 
-// A row in bfloat16 as two e4m3 numbers per dim: x = 2^(e - 127) (hi + lo / 16), 2^(127 - e)
-// bringing the row's largest magnitude to [128, 256).  That holds a bfloat16's eight
-// bits exactly, and values below 2^-14 of the row's largest to 2^-22 of it.  A row is
-// stored as its 128 hi, then its 128 lo.  16 lanes per row, eight dims each.
-__device__ __forceinline__ void q8_split(const uint16_t* rows, uint8_t* split, int32_t* exps,
-                                         long long r, int lane16) {
-  const uint4 x = reinterpret_cast<const uint4*>(rows + r * kD)[lane16];
-  uint32_t m = max(max(finite_mag2(x.x), finite_mag2(x.y)), max(finite_mag2(x.z), finite_mag2(x.w)));
-#pragma unroll
-  for (int d = 8; d > 0; d >>= 1) m = max(m, uint32_t(__shfl_xor(int(m), d)));
-  // (m >> 7: the exponent's bits; a zero row takes any scale.  Both exponents, e and
-  // e - 4, and 2^(127 - e) are representable)
-  const int e = min(max(int(m >> 7) - 7, 7), 247);
-  const float s = __uint_as_float(uint32_t(254 - e) << 23);
-  const auto two = [&](uint32_t w, float (&y)[2]) {
-    y[0] = __uint_as_float(w << 16) * s;
-    y[1] = __uint_as_float(w & 0xFFFF0000u) * s;
-  };
-  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-  uint32_t hi[2], lo[2];
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    float a[2], b[2];
-    two(w[2 * h], a);
-    two(w[2 * h + 1], b);
-    hi[h] = encode4<ECHO_KV_E4M3>(a[0], a[1], b[0], b[1]);
-    const floatx2v c = __builtin_amdgcn_cvt_pk_f32_fp8(int(hi[h]), false);
-    const floatx2v d = __builtin_amdgcn_cvt_pk_f32_fp8(int(hi[h]), true);
-    lo[h] = encode4<ECHO_KV_E4M3>((a[0] - c[0]) * 16.0f, (a[1] - c[1]) * 16.0f, (b[0] - d[0]) * 16.0f,
-                                  (b[1] - d[1]) * 16.0f);
-  }
-  uint8_t* p = split + r * kSplitBytes;
-  reinterpret_cast<uint2*>(p)[lane16] = make_uint2(hi[0], hi[1]);
-  reinterpret_cast<uint2*>(p + kD)[lane16] = make_uint2(lo[0], lo[1]);
-  if (lane16 == 0) exps[r] = e;
-}
-
-// The plan, on one workgroup.  It runs once, so that its time is the fetching of its code and
-// a few round trips: loops instead of unrolled copies, a wave per class for the scans.
-__device__ __forceinline__ void q8_plan(const Q8Args& a, const Q8Ws& ws, int nw, int chunks,
-                                        int32_t* s_mem) {
+// One workgroup.  It runs once, so that its time is the fetching of its code and a few
+// round trips: loops instead of unrolled copies, a wave per class for the scans.
+__global__ __launch_bounds__(kPlanThreads) void q8_plan_kernel(Q8Args a, Q8Ws ws, int nw, int chunks) {
+  extern __shared__ int32_t s_mem[];  // 3 R words
   __shared__ int8_t s_cls[ECHO_MAX_REQUESTS + 1];  // class of each request (-1: none, -2: bad)
   __shared__ int s_n[kQ8Classes + 1], s_T[kQ8Classes + 1], s_wg[kQ8Classes + 1];
   __shared__ long long s_T64[kQ8Classes];
@@ -406,19 +352,6 @@ __device__ __forceinline__ void q8_plan(const Q8Args& a, const Q8Ws& ws, int nw,
     }
     ws.starts[x] = st;
   }
-}
-
-// Workgroup 0 plans; the others split the query rows and the new keys.
-__global__ __launch_bounds__(kPlanThreads) void q8_plan_kernel(Q8Args a, Q8Ws ws, int nw, int chunks) {
-  extern __shared__ int32_t s_mem[];  // 3 R words
-  if (blockIdx.x > 0) {
-    const long long r = (long long)(blockIdx.x - 1) * kPlanRows + threadIdx.x / 16;
-    const long long nq = (long long)a.max_rows * a.hq, nk = (long long)a.max_rows * a.hkv;
-    if (r < nq) q8_split(a.q, ws.qs, ws.qe, r, threadIdx.x & 15);
-    else if (r - nq < nk) q8_split(a.k_new, ws.ks, ws.ke, r - nq, threadIdx.x & 15);
-    return;
-  }
-  q8_plan(a, ws, nw, chunks, s_mem);
 }
 
 // ---------------------------------------------------------------- main ----
@@ -757,22 +690,20 @@ __device__ __forceinline__ void q8_values(const Frag& frag, floatx16 (&s)[NT], Q
     rt.lq = __builtin_fmaf(used[j][0] + used[j][1], ivs, rt.lq);
   }
 }
-#undef ECHO_FENCE
-
-// 32 bytes of a split row (p: dims 64 j + 32 (lane / 32) on).
-__device__ __forceinline__ intx8 q8_half(const uint8_t* p) {
-  const uint4v a = *reinterpret_cast<const uint4v*>(p);
-  const uint4v b = *reinterpret_cast<const uint4v*>(p + 16);
-  return __builtin_bit_cast(intx8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+// A row's 8 dims that the lane has in part n (of 8) of the product of Q and K: dims
+// 64 (n / 4) + 32 (lane / 32) + 8 (n % 4) on, so that the lane's cached bytes of a key
+// are two runs of 32.
+__device__ __forceinline__ bf16x8 q8_dims(const uint16_t* row, int n) {
+  const int h = (threadIdx.x & (kWave - 1)) >> 5;
+  return as_bf16x8(*reinterpret_cast<const uint4*>(row + 64 * (n >> 2) + 32 * h + 8 * (n & 3)));
 }
 
-// A tile of the tree's new keys (tn <= 32 of them from slot s0 on): K split in two 8-bit
-// numbers like Q, so that S^T is the sum of four products; V in bfloat16 through 4 KB
+// A tile of the tree's new keys (tn <= 32 of them from slot s0 on).  V goes through 4 KB
 // of LDS at `scratch` to be transposed, 16 keys at a time (the second 16 only if there
 // are so many).
-__device__ __forceinline__ void q8_tree_tile(const Q8Args& a, const Q8Ws& ws, int head, int s0, int tn,
-                                             uint32_t scratch, const intx8 (&q)[2][2], int qe,
-                                             Q8Rows& rt, uint32_t word) {
+__device__ __forceinline__ void q8_tree_tile(const Q8Args& a, int head, int s0, int tn,
+                                             uint32_t scratch, const bf16x8 (&q)[8], Q8Rows& rt,
+                                             uint32_t word) {
   const int lane = threadIdx.x & (kWave - 1);
   const int h = lane >> 5, lr = lane & 15;
   const uint32_t row_bytes = uint32_t(a.hkv) * kD * 2;
@@ -789,18 +720,11 @@ __device__ __forceinline__ void q8_tree_tile(const Q8Args& a, const Q8Ws& ws, in
     q8_copy4(scratch, vh, o);
   };
   copy_v(0);
-  const size_t krow = size_t(s0 + min(lane & 31, tn - 1)) * a.hkv + head;
-  const uint8_t* kp = ws.ks + krow * kSplitBytes + 32 * h;
-  const int ke = ws.ke[krow];
+  const uint16_t* kp = a.k_new + (size_t(s0 + min(lane & 31, tn - 1)) * a.hkv + head) * kD;
   floatx16 s[1] = {};
 #pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    const intx8 kh = q8_half(kp + 64 * j), kl = q8_half(kp + kD + 64 * j);
-#pragma unroll
-    for (int n = 0; n < 4; ++n)
-      s[0] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
-          n & 1 ? kl : kh, q[n >> 1][j], s[0], 0, 0, 0, n & 1 ? ke - 4 : ke, 0, n & 2 ? qe - 4 : qe);
-  }
+  for (int n = 0; n < 8; ++n)
+    s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(q8_dims(kp, n), q[n], s[0], 0, 0, 0);
   wait_vm<0>();
   asm volatile("" ::: "memory");
   // V^T of a 16-key group: keys 4 h + 0..3 and the same + 8 of dims 32 dt + lane % 32
@@ -845,11 +769,9 @@ __device__ __forceinline__ void q8_prime(Q8Table& tb, const Q8Args& a, uint32_t 
 
 // A wave's steps [lo, hi) of one unit, then its output or partial sums.
 //
-// S^T = K Q^T of a cached tile takes its bytes as they are:
-// v_mfma_f32_32x32x64_f8f6f4 with Q as the sum of two e4m3 numbers (see q8_split).  That
-// is as many cycles as bfloat16 products, and no conversion of K.  P V stays in
-// bfloat16: weights as two 8-bit numbers would cost more instructions than V's
-// conversion.
+// K is widened to bfloat16 between the products.  (v_mfma_f32_32x32x64_f8f6f4 would take its
+// bytes as they are and Q as the sum of two e4m3 numbers, in as many cycles, but it drops
+// what is below 2^-13 of the largest of its products.)
 template <int kFmt>
 __device__ __forceinline__ void q8_segment(const Q8Args& a, const Q8Ws& ws, const Q8Walk& w, int lo,
                                            int hi, int range_hi, int b, uint32_t ring, Q8Table& tb,
@@ -859,8 +781,7 @@ __device__ __forceinline__ void q8_segment(const Q8Args& a, const Q8Ws& ws, cons
   const int head = w.unit / w.q.passes;
   const int row0 = q8_row0(w, tb.k, tb.member);
   const int rows = min(kQ8Rows, w.q.nslots * a.G - row0);
-  intx8 q[2][2];  // [hi, lo][half of the dims]
-  int qe;
+  bf16x8 q[8];
   Q8Rows rt;
   int t = lo;
   {
@@ -868,12 +789,8 @@ __device__ __forceinline__ void q8_segment(const Q8Args& a, const Q8Ws& ws, cons
     const int ra = row0 + min(lane & 31, rows - 1);
     const int slot = w.q.q0 + ra / a.G;
     const size_t row = size_t(slot) * a.hq + size_t(head) * a.G + ra % a.G;
-    const uint8_t* p = ws.qs + row * kSplitBytes + 32 * h;
 #pragma unroll
-    for (int n = 0; n < 2; ++n)
-#pragma unroll
-      for (int j = 0; j < 2; ++j) q[n][j] = q8_half(p + kD * n + 64 * j);
-    qe = ws.qe[row];
+    for (int n = 0; n < 8; ++n) q[n] = q8_dims(a.q + row * kD, n);
 #pragma unroll
     for (int dt = 0; dt < 4; ++dt) rt.o[dt] = floatx16{};
     rt.m = -__builtin_inff();
@@ -885,7 +802,7 @@ __device__ __forceinline__ void q8_segment(const Q8Args& a, const Q8Ws& ws, cons
       const int tn = min(kTileKeys, w.q.nslots - lt * kTileKeys);
       uint32_t word = lt < a.W ? a.tree_mask[size_t(slot) * a.W + lt] : 0u;
       if (tn < kTileKeys) word &= (1u << tn) - 1u;
-      q8_tree_tile(a, ws, head, w.q.q0 + lt * kTileKeys, tn, ring + 2 * kQ8Slot, q, qe, rt, word);
+      q8_tree_tile(a, head, w.q.q0 + lt * kTileKeys, tn, ring + 2 * kQ8Slot, q, rt, word);
     }
   }
   wait_vm<0>();  // no load that the compiler knows of is in flight in the loop
@@ -911,14 +828,21 @@ __device__ __forceinline__ void q8_segment(const Q8Args& a, const Q8Ws& ws, cons
     // it is in registers: refill its place while it is multiplied
     q8_send(tb, tb.k_sent, a.k_pages, ring, offs);
     floatx16 s[2] = {};
+    const auto widen_k = [&](int x) {  // part x / 2 of tile x % 2
+      const uint4v c = kr[x & 1][x >> 3][(x >> 2) & 1];
+      const uint32_t lo = c[x & 2 ? 2 : 0], hi = c[x & 2 ? 3 : 1];
+      return as_bf16x8(make_uint4(widen2<kFmt>(lo, false), widen2<kFmt>(lo, true),
+                                  widen2<kFmt>(hi, false), widen2<kFmt>(hi, true)));
+    };
+    bf16x8 kf = widen_k(0);
 #pragma unroll
-    for (int n = 0; n < 8; ++n) {
-      const int term = n >> 2, j = (n >> 1) & 1, tile = n & 1;
-      s[tile] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
-          __builtin_bit_cast(intx8, __builtin_shufflevector(kr[tile][j][0], kr[tile][j][1], 0, 1, 2, 3,
-                                                            4, 5, 6, 7)),
-          q[term][j], s[tile], kFmt == ECHO_KV_E4M3 ? 0 : 1, 0, 0, 127, 0, term ? qe - 4 : qe);
+    for (int x = 0; x < 16; ++x) {
+      ECHO_FENCE();
+      s[x & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[x >> 1], s[x & 1], 0, 0, 0);
+      ECHO_FENCE();
+      if (x < 15) kf = widen_k(x + 1);
     }
+    ECHO_FENCE();
     const int tn1 = lane_of(tb.tokens, i + 1);
     if (tn1 < kTileKeys) {
       const int tn0 = lane_of(tb.tokens, i);
@@ -1027,6 +951,8 @@ q8_main_kernel(Q8Args a, Q8Ws ws) {
     q8_next_unit(w, a, ws);
   }
 }
+
+#undef ECHO_FENCE
 
 // ------------------------------------------------------------- combine ----
 constexpr int kQ8Parts = 8;  // partial sums per round trip
@@ -1139,9 +1065,7 @@ int32_t launch_tree_verify_attn_q8(const AttnQ8Args& x, hipStream_t stream) {
     hipLaunchKernelGGL(q8_pages_kernel, dim3(unsigned(a.R), unsigned(chunks)), dim3(kPageChunk), 0,
                        stream, a, ws.bad);
   }
-  const long long split = (long long)a.max_rows * (a.hq + a.hkv);
-  hipLaunchKernelGGL(q8_plan_kernel, dim3(unsigned(1 + (split + kPlanRows - 1) / kPlanRows)),
-                     dim3(kPlanThreads),
+  hipLaunchKernelGGL(q8_plan_kernel, dim3(1), dim3(kPlanThreads),
                      3 * size_t(a.R) * sizeof(int32_t), stream, a, ws, nw, chunks);
   hipLaunchKernelGGL(x.cache.format == ECHO_KV_E4M3 ? q8_main_kernel<ECHO_KV_E4M3>
                                                     : q8_main_kernel<ECHO_KV_E5M2>,

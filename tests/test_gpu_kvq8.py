@@ -562,6 +562,49 @@ def test_attention_skips_bad_requests(big):
     assert status == st.BAD_OFFSETS and np.isnan(out).all() and np.isnan(lse).all()
 
 
+@pytest.mark.parametrize("fmt", FMTS)
+def test_attention_scores_that_cancel(fmt):
+    """Two products of a score are large and cancel: what is left is still held in 32 bits."""
+    rng = np.random.default_rng(16)
+    c = _attn_case(rng, 8, 2, [1, 2, 1, 3], [1, 33, 2, 64], 32, fmt)
+    q = c["q"].astype(np.uint32).__lshift__(16).view(np.float32).copy()
+    q[..., 0] = q[..., 1] = 128.0
+    c["q"] = _bf(q)
+    top = 0x7E if fmt == kvq8.E4M3 else 0x78  # 448; 32768
+    c["cache"][0][..., 0], c["cache"][0][..., 1] = top, top | 0x80
+    c["mask"][[0, 3]] = 0
+    _log(f"[attn q8] scores that cancel fmt={fmt}")
+    _check_attn(c, *_run_attn(c))
+
+
+def test_attention_heads_of_every_size_in_one_batch():
+    """Requests with up to 32, 64, 128 and more rows per head side by side, some without work."""
+    rng = np.random.default_rng(17)
+    c = _attn_case(rng, 32, 2, [1, 2, 3, 0, 4, 5, 8, 9, 17, 1, 33], [700, 64, 333, 90, 1, 400, 31, 0, 129, 0, 95],
+                   64, kvq8.E4M3)
+    _log("[attn q8] heads of every size")
+    _check_attn(c, *_run_attn(c))
+
+
+@pytest.mark.parametrize("R,width", [(1024, 32), (1025, 32), (1024, 33), (4, 8300)])
+def test_attention_page_checks_of_every_size(R, width):
+    """Block tables just small enough for one workgroup's check, and just too large; bad ids in
+    the first, a middle and the last request."""
+    rng = np.random.default_rng(18)
+    plens = rng.integers(1, 34, R).tolist()
+    plens[0] = plens[R // 2] = plens[R - 1] = 64
+    c = _attn_case(rng, 2, 1, [1] * R, plens, 32, kvq8.E4M3)
+    pad = width - c["bt"].shape[1]
+    c["bt"] = np.pad(c["bt"], ((0, 0), (0, pad)), constant_values=-1)
+    c["bt"][0, 1] = -1
+    c["bt"][R // 2, 0] = c["cache"][0].shape[0]
+    c["bt"][R - 1, 1] = -2 ** 31
+    _log(f"[attn q8] page checks R={R} width={width}")
+    out, lse, status = _run_attn(c)
+    _check_attn(c, out, lse, status, st.BAD_OFFSETS)
+    assert np.isnan(lse[[0, R // 2, R - 1]]).all() and np.isfinite(lse[1]).all()
+
+
 def test_attention_without_lse_and_on_a_stream():
     import torch
     import paper_2604_09603_amd as pkg
