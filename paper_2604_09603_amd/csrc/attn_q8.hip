@@ -43,6 +43,7 @@ constexpr int kQ8Copies = 8;       // copy instructions per step and tensor
 // What a step costs a workgroup that has 4, 2 or 1 gangs at work, relative to each other.
 constexpr float kQ8Cost1 = 1.4f, kQ8Cost2 = 2.2f, kQ8Cost4 = 4.0f;
 constexpr int kPlanThreads = 1024;
+constexpr int kPlanWords = 6;      // words of LDS per request
 constexpr int kPlanBatch = 16;     // block-table entries per thread and round trip
 constexpr int kPlanPages = 2 * kPlanBatch * kPlanThreads;  // entries that the plan checks itself
 
@@ -58,18 +59,20 @@ typedef float floatx16 __attribute__((ext_vector_type(16)));
 __device__ __forceinline__ lds_char_t* lds_at(uint32_t x) { return (lds_char_t*)(uintptr_t(x)); }
 
 // A gang is the k waves (1, 2 or 4, of one workgroup) that take the same steps of a unit,
-// each with up to 32 of its rows: one copies the tiles from HBM, the others at about the
-// same time from the caches.  A request's k follows its rows per head; requests of
-// the same k form a class, whose steps are cut into equal ranges, one per gang.
+// each with 32 of its rows: one copies the tiles from HBM, the others at about the same
+// time from the caches.  A head's rows are dealt to gangs of four, and what is left to one of
+// one, two or (three) four waves: without the remainder's own gang, waves that have no
+// rows would be idle through its steps.  The requests with a part for gangs of k
+// waves form a class, whose steps are cut into equal ranges, one per gang.
 constexpr int kQ8Classes = 3;  // k = 1 << class
 
-// One request as the plan shapes it, in the list of its class: Hkv * passes units (unit =
-// head * passes + pass) of tpu steps each, from step tile0 of the class on; gang member
-// m has rows 32 (k pass + m) .. of a head, as far as there are so many.
+// A request's part in a class: Hkv * passes units (unit = head * passes + pass) of tpu steps
+// each, from step tile0 of the class on; gang member m has rows row0 + 32 (k pass + m) .. of
+// a head, as far as there are so many.
 struct Q8Req {
   int32_t tile0, tpu;
   int32_t q0, nslots;
-  int32_t P, r, passes, pad;
+  int32_t P, r, passes, row0;
 };
 
 // A wave's range of steps and where it starts (req: place in the class's list).
@@ -92,7 +95,7 @@ __device__ __forceinline__ int q8_wave_of(int g, int k, int wg0, int nwg) {
 
 struct Q8Ws {
   Q8Start* starts;   // [waves]
-  Q8Req* reqs;       // [R], class by class
+  Q8Req* reqs;       // [2 R], class by class
   int32_t* bad;      // [R][chunks] flags of q8_pages
   float* part_ml;    // [waves][2][32][4]: max, sum, sum of the weights used, scale exponent
   _Float16* part_o;  // [waves][2][32][128]
@@ -135,7 +138,7 @@ __host__ inline Q8Ws q8_layout(void* base, int R, int max_rows, int hq, int hkv,
   w.starts = reinterpret_cast<Q8Start*>(p);
   p += al(size_t(nw) * sizeof(Q8Start));
   w.reqs = reinterpret_cast<Q8Req*>(p);
-  p += al(size_t(R) * sizeof(Q8Req));
+  p += al(2 * size_t(R) * sizeof(Q8Req));
   w.bad = reinterpret_cast<int32_t*>(p);
   if (!q8_plan_checks(R, max_pages)) p += al(size_t(R) * size_t(q8_page_chunks(max_pages)) * 4);
   w.part_ml = reinterpret_cast<float*>(p);
@@ -168,34 +171,35 @@ __global__ __launch_bounds__(kPageChunk) void q8_pages_kernel(Q8Args a, int32_t*
 }
 
 // ---------------------------------------------------------------- plan ----
-// The request's shape and class (-1: nothing to do), given that its fields are in range.
-__device__ __forceinline__ Q8Req shape_of(int r, int q0, int nslots, int P, int G, int& cls) {
-  Q8Req s = {};
-  s.q0 = q0;
-  s.nslots = nslots;
-  s.P = P;
-  s.r = r;
-  const int rows = nslots * G;
-  cls = rows == 0 ? -1 : rows <= kQ8Rows ? 0 : rows <= 2 * kQ8Rows ? 1 : 2;
-  const int unit = kQ8Rows << max(cls, 0);
-  s.passes = (rows + unit - 1) / unsigned(unit);
-  s.tpu = (nslots + kTileKeys - 1) / kTileKeys +
-          int((unsigned(P) + kQ8StepKeys - 1) / kQ8StepKeys);
-  return s;
+// How often class c goes through the keys of a head with t tiles of 32 rows.
+__device__ __forceinline__ int q8_passes(int t, int c) {
+  const int rest = t & 3;
+  return c == 2 ? (t >> 2) + (rest == 3 ? 1 : 0) : rest == c + 1 ? 1 : 0;
+}
+
+__device__ __forceinline__ int q8_row_tiles(int nslots, int G) {
+  return int((unsigned(nslots) * unsigned(G) + kQ8Rows - 1) / kQ8Rows);
+}
+
+// Steps of a unit.
+__device__ __forceinline__ int q8_unit_steps(int nslots, int P) {
+  return (nslots + kTileKeys - 1) / kTileKeys +
+         int((unsigned(P) + kQ8StepKeys - 1) / kQ8StepKeys);
 }
 
 // One workgroup.  It runs once, so that its time is the fetching of its code and a few
 // round trips: loops instead of unrolled copies, a wave per class for the scans.
 __global__ __launch_bounds__(kPlanThreads) void q8_plan_kernel(Q8Args a, Q8Ws ws, int nw, int chunks) {
-  extern __shared__ int32_t s_mem[];  // 3 R words
-  __shared__ int8_t s_cls[ECHO_MAX_REQUESTS + 1];  // class of each request (-1: none, -2: bad)
+  extern __shared__ int32_t s_mem[];  // kPlanWords R
   __shared__ int s_n[kQ8Classes + 1], s_T[kQ8Classes + 1], s_wg[kQ8Classes + 1];
   __shared__ long long s_T64[kQ8Classes];
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wid = wave_id();
   const int R = a.R;
-  int32_t* s_tile0 = s_mem;      // [R] first step of each listed request (before: steps of request r)
-  int32_t* s_req = s_mem + R;    // [R] the request (before: pages of request r)
-  int32_t* s_steps = s_mem + 2 * R;  // [R] steps of request r
+  int32_t* s_tile0 = s_mem;               // [2 R] first steps of the classes' parts
+  int32_t* s_req = s_mem + 2 * R;         // [2 R] their requests
+  int32_t* s_steps = s_mem + 4 * R;       // [R] steps of a pass through request r
+  int32_t* s_tiles = s_mem + 5 * R;       // [R] its row tiles; -1: not to be used
+  int32_t* s_pages = s_mem;               // [R] its pages (before s_tile0)
   // requests whose offsets, length or pages cannot be used
   const bool own = chunks == 0;
   const int entries = own ? R * a.max_pages : 0;
@@ -211,16 +215,10 @@ __global__ __launch_bounds__(kPlanThreads) void q8_plan_kernel(Q8Args a, Q8Ws ws
     const int np = prefix_pages(P, a);
     bool bad = !(q0 >= 0 && q1 >= q0 && q1 <= a.max_rows) || np < 0;
     for (int c = 0; c < chunks; ++c) bad = bad || ws.bad[size_t(r) * chunks + c] != 0;
-    int cls = -2;
-    long long steps = 0;
-    if (!bad) {
-      const Q8Req s = shape_of(r, q0, q1 - q0, P, a.G, cls);
-      steps = (long long)a.hkv * s.passes * s.tpu;
-    }
-    s_cls[r] = int8_t(cls);
-    s_req[r] = np;
+    s_tiles[r] = bad ? -1 : q8_row_tiles(q1 - q0, a.G);
+    s_pages[r] = np;
     // (offsets that overlap may ask for any number: 2^31 - 1 stands for more)
-    s_steps[r] = int(min(steps, 0x7FFFFFFFll));
+    s_steps[r] = bad ? 0 : int(min((long long)a.hkv * q8_unit_steps(q1 - q0, P), 0x7FFFFFFFll));
   }
   __syncthreads();
   if (own) {
@@ -235,7 +233,7 @@ __global__ __launch_bounds__(kPlanThreads) void q8_plan_kernel(Q8Args a, Q8Ws ws
       }
 #pragma unroll
       for (int k = 0; k < kPlanBatch; ++k) {
-        if (r < R && (pg[k] < 0 || pg[k] >= a.num_pages) && c < s_req[r]) s_cls[r] = -2;
+        if (r < R && (pg[k] < 0 || pg[k] >= a.num_pages) && c < s_pages[r]) s_tiles[r] = -1;
         r += dr;
         c += dc;
         r += c >= mp ? 1 : 0;
@@ -250,11 +248,12 @@ __global__ __launch_bounds__(kPlanThreads) void q8_plan_kernel(Q8Args a, Q8Ws ws
     long long T = 0;
 #pragma unroll 1
     for (int r = lane; r - lane < R; r += kWave) {
-      const int cls = r < R ? s_cls[r] : -1;
-      if (cls == -2) bits = ECHO_DATA_BAD_OFFSETS;
-      if (cls == wid) {
+      const int tiles = r < R ? s_tiles[r] : 0;
+      if (tiles < 0) bits = ECHO_DATA_BAD_OFFSETS;
+      const int passes = tiles > 0 ? q8_passes(tiles, wid) : 0;
+      if (passes > 0) {
         n += 1;
-        T += s_steps[r];
+        T += (long long)s_steps[r] * passes;
       }
     }
 #pragma unroll 1
@@ -279,9 +278,11 @@ __global__ __launch_bounds__(kPlanThreads) void q8_plan_kernel(Q8Args a, Q8Ws ws
     for (int c = 0; c < wid; ++c) run_n += s_n[c];
 #pragma unroll 1
     for (int r = lane; r - lane < R; r += kWave) {
-      const bool in = r < R && s_cls[r] == wid;
+      const int tiles = r < R ? s_tiles[r] : 0;
+      const int passes = tiles > 0 ? q8_passes(tiles, wid) : 0;
+      const bool in = passes > 0;
       const uint64_t who = __ballot(in);
-      const int steps = in ? s_steps[r] : 0;
+      const int steps = in ? s_steps[r] * passes : 0;
       const int inc = wave_inclusive_sum(steps);
       if (in) {
         const int at = run_n + lanes_below(who);
@@ -312,19 +313,24 @@ __global__ __launch_bounds__(kPlanThreads) void q8_plan_kernel(Q8Args a, Q8Ws ws
     s_wg[kQ8Classes] = wgs;
   }
   __syncthreads();
-  // every wave's start, and the listed requests' shapes
-  const auto shape_at = [&](int at) {
+  // every wave's start, and the classes' lists
+  const auto part_at = [&](int at, int c) {
     const int r = s_req[at];
-    const int q0 = a.q_offsets[r];
-    int cls;
-    Q8Req s = shape_of(r, q0, a.q_offsets[r + 1] - q0, a.prefix_len[r], a.G, cls);
+    Q8Req s;
     s.tile0 = s_tile0[at];
+    s.q0 = a.q_offsets[r];
+    s.nslots = a.q_offsets[r + 1] - s.q0;
+    s.P = a.prefix_len[r];
+    s.r = r;
+    s.tpu = q8_unit_steps(s.nslots, s.P);
+    s.passes = q8_passes(s_tiles[r], c);
+    s.row0 = c == 2 ? 0 : (s_tiles[r] & ~3) * kQ8Rows;
     return s;
   };
   const int listed = fits ? s_n[0] + s_n[1] + s_n[2] : 0;
 #pragma unroll 1
   for (int x = tid; x < max(nw, listed); x += kPlanThreads) {
-    if (x < listed) ws.reqs[x] = shape_at(x);
+    if (x < listed) ws.reqs[x] = part_at(x, x < s_n[0] ? 0 : x < s_n[0] + s_n[1] ? 1 : 2);
     if (x >= nw) continue;
     const int g = x / kQ8Waves, slot = x % kQ8Waves;
     int c = 0, first = 0;
@@ -343,7 +349,7 @@ __global__ __launch_bounds__(kPlanThreads) void q8_plan_kernel(Q8Args a, Q8Ws ws
         st.lo = int(range_lo(T, st.gang, by_n));
         st.hi = int(range_lo(T, st.gang + 1, by_n));
         st.req = first + upper_bound_idx(s_tile0 + first, s_n[c], st.lo);
-        st.q = shape_at(st.req);
+        st.q = part_at(st.req, c);
         st.unit = (st.lo - st.q.tile0) / unsigned(st.q.tpu);
         const int u0 = st.q.tile0 + st.unit * st.q.tpu;
         if (u0 < st.lo && int(range_lo(T, st.gang - 1, by_n)) <= u0)
@@ -462,7 +468,7 @@ __device__ __forceinline__ void q8_next_unit(Q8Walk& w, const Q8Args& a, const Q
 
 // The first of the member's rows of the unit.
 __device__ __forceinline__ int q8_row0(const Q8Walk& w, int k, int member) {
-  return (w.unit % w.q.passes * k + member) * kQ8Rows;
+  return w.q.row0 + (w.unit % w.q.passes * k + member) * kQ8Rows;
 }
 
 // What a wave knows of the next 32 steps of its range, tile i (two per step) in lane
@@ -964,7 +970,7 @@ __global__ __launch_bounds__(256) void q8_combine_kernel(Q8Args a, Q8Ws ws) {
   const Q8Start st = load_start(ws.starts, b);
   if (st.cut_last == 0) return;
   const int head = st.unit / st.q.passes;
-  const int row0 = (st.unit % st.q.passes * st.k + st.member) * kQ8Rows;
+  const int row0 = st.q.row0 + (st.unit % st.q.passes * st.k + st.member) * kQ8Rows;
   const int rows = min(kQ8Rows, st.q.nslots * a.G - row0);
   const int rho = blockIdx.y * 16 + threadIdx.x / 16;
   if (rho >= rows) return;
@@ -1065,8 +1071,12 @@ int32_t launch_tree_verify_attn_q8(const AttnQ8Args& x, hipStream_t stream) {
     hipLaunchKernelGGL(q8_pages_kernel, dim3(unsigned(a.R), unsigned(chunks)), dim3(kPageChunk), 0,
                        stream, a, ws.bad);
   }
-  hipLaunchKernelGGL(q8_plan_kernel, dim3(1), dim3(kPlanThreads),
-                     3 * size_t(a.R) * sizeof(int32_t), stream, a, ws, nw, chunks);
+  const size_t lds = kPlanWords * size_t(a.R) * sizeof(int32_t);
+  if (lds > 60 * 1024 &&
+      hipFuncSetAttribute(reinterpret_cast<const void*>(q8_plan_kernel),
+                          hipFuncAttributeMaxDynamicSharedMemorySize, int(lds)) != hipSuccess)
+    return ECHO_ERR_HIP;
+  hipLaunchKernelGGL(q8_plan_kernel, dim3(1), dim3(kPlanThreads), lds, stream, a, ws, nw, chunks);
   hipLaunchKernelGGL(x.cache.format == ECHO_KV_E4M3 ? q8_main_kernel<ECHO_KV_E4M3>
                                                     : q8_main_kernel<ECHO_KV_E5M2>,
                      dim3(unsigned(nw / kQ8Waves)), dim3(kQ8Waves * kWave), 0, stream, a, ws);

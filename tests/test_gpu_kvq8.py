@@ -514,6 +514,16 @@ def test_attention_many_requests():
     _check_attn(c, *_run_attn(c))
 
 
+def test_attention_largest_batch():
+    """As many requests as a call takes, some with heads of more than 128 rows."""
+    rng = np.random.default_rng(19)
+    R = 4095
+    slots = [9 if r % 500 == 7 else 1 for r in range(R)]
+    c = _attn_case(rng, 16, 1, slots, rng.integers(0, 20, R).tolist(), 32, kvq8.E4M3)
+    _log("[attn q8] 4095 requests")
+    _check_attn(c, *_run_attn(c))
+
+
 @pytest.mark.parametrize("q_scale", [0.0, 30.0])
 def test_attention_flat_and_peaked_rows(q_scale):
     rng = np.random.default_rng(12)
