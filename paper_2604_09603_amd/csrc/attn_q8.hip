@@ -673,6 +673,8 @@ __device__ __forceinline__ void q8_values(const Frag& frag, floatx16 (&s)[NT], Q
     sum[j][1] += p1;
     pk[g & 1][i] = pack_bf16x2(p0, p1);
     used[j][i & 1] = add_bf16x2(pk[g & 1][i], used[j][i & 1]);
+    // (added here, not at the end)
+    asm volatile("" : "+v"(sum[j][0]), "+v"(sum[j][1]), "+v"(used[j][i & 1]));
   };
 #pragma unroll
   for (int i = 0; i < 4; ++i) two(0, i);
@@ -819,8 +821,9 @@ __device__ __forceinline__ void q8_segment(const Q8Args& a, const Q8Ws& ws, cons
       q8_prime(tb, a, ring, offs);
     }
     const int i = (2 * tb.done) & (kWave - 1);
-    // K.  (The copies go K, V, K, V: behind this step's K comes its V.)
-    q8_wait(tb.v_sent > tb.done);
+    // K and V of the step to registers; then their places are refilled while they are multiplied
+    wait_vm<0>();
+    asm volatile("" ::: "memory");  // the tiles' reads stay behind the wait
     uint4v kr[2][2][2];  // [tile][half of the dims][chunk]
     const uint32_t ka = ring + k_offset(offs);
 #pragma unroll
@@ -830,9 +833,18 @@ __device__ __forceinline__ void q8_segment(const Q8Args& a, const Q8Ws& ws, cons
 #pragma unroll
         for (int e = 0; e < 2; ++e)
           kr[n][j][e] = *(lds_uint4_t*)(lds_at(ka ^ uint32_t(64 * j + 16 * e)) + kBlockBytes * n);
+    intx2 vr[4][4];  // [16-key group][32 dims]
+    const uint32_t va = ring + kQ8Slot + v_offset(offs);
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+#pragma unroll
+      for (int dt = 0; dt < 4; ++dt)
+        vr[g][dt] = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+            (lds_intx2_t*)(lds_at(va ^ uint32_t(dt << 5)) + 16 * kD * g));
     q8_wait_lds();
-    // it is in registers: refill its place while it is multiplied
     q8_send(tb, tb.k_sent, a.k_pages, ring, offs);
+    q8_send(tb, tb.v_sent, a.v_pages, ring + kQ8Slot, offs);
+    tb.done += 1;
     floatx16 s[2] = {};
     const auto widen_k = [&](int x) {  // part x / 2 of tile x % 2
       const uint4v c = kr[x & 1][x >> 3][(x >> 2) & 1];
@@ -855,21 +867,11 @@ __device__ __forceinline__ void q8_segment(const Q8Args& a, const Q8Ws& ws, cons
       q8_mask(s[0], tn0 < kTileKeys ? (1u << tn0) - 1u : 0xFFFFFFFFu);
       q8_mask(s[1], (1u << tn1) - 1u);
     }
-    // V.  (Behind it comes K of the next step.)
-    q8_wait(tb.k_sent > tb.done + 1);
-    intx2 vr[4][4];  // [16-key group][32 dims]
-    const uint32_t va = ring + kQ8Slot + v_offset(offs);
-#pragma unroll
-    for (int g = 0; g < 4; ++g)
-#pragma unroll
-      for (int dt = 0; dt < 4; ++dt)
-        vr[g][dt] = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
-            (lds_intx2_t*)(lds_at(va ^ uint32_t(dt << 5)) + 16 * kD * g));
-    q8_wait_lds();
-    q8_send(tb, tb.v_sent, a.v_pages, ring + kQ8Slot, offs);
-    tb.done += 1;
     const float c[2] = {lane_of(tb.c, i), lane_of(tb.c, i + 1)};
     const float lvs[2] = {lane_of(tb.lvs, i), lane_of(tb.lvs, i + 1)};
+    // Without priorities the older of a SIMD's two waves goes first in every phase, and ends its
+    // range at 160 us where the other needs 222 (a long context); so both end near 206.
+    __builtin_amdgcn_s_setprio(1);
     q8_values<2>(
         [&](int g, int dt) {
           const uint32_t x = uint32_t(vr[g][dt][0]), y = uint32_t(vr[g][dt][1]);
@@ -877,6 +879,7 @@ __device__ __forceinline__ void q8_segment(const Q8Args& a, const Q8Ws& ws, cons
                             widen2<kFmt>(y, true));
         },
         s, rt, c, lvs);
+    __builtin_amdgcn_s_setprio(0);
   }
 
   int rho = lane & 31;  // (opaque: the output's addresses are formed here, not kept in registers)
