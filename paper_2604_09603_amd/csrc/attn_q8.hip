@@ -1,19 +1,21 @@
 // Tree-masked grouped-query verification attention over an 8-bit paged cache
-// (kvq8_device.h has the cache's layout).  Three launches, and one more before them
-// for large block tables:
+// (kvq8_device.h has the cache's layout).  Two launches, and one more before them for
+// large block tables:
 //
-//   q8_pages    checks the page ids (small tables: the plan does).
-//   q8_plan     one workgroup.  A unit is one KV head of one request with up to 32, 64 or 128 of its
-//               rows (verify slots x query heads of the GQA group); its steps are first
-//               the tree's (32 new keys each), then the prefix's, two 32-token blocks
-//               each.  The steps of all units are cut into equal contiguous ranges: a
-//               head's blocks lie in one piece, so nothing is gained by waves that read
-//               the heads of the same tokens side by side, and one head's keys are
-//               spread over as many waves as they can feed.
-//   q8_main     persistent, two workgroups of four independent waves per CU.  A wave has
-//               32 rows.  It copies its tiles HBM -> LDS into slots of its own with
-//               direct-to-LDS loads: S^T = K Q^T and O^T += V^T P^T with K and V widened to
-//               bfloat16 (exact), an online softmax in base 2 between them.  The K scale goes into the softmax's factor, the V scale into its
+//   q8_pages    checks the page ids (small tables: the main kernel's waves do).
+//   q8_main     persistent, two workgroups of four waves per CU.  A unit is one KV head of
+//               one request with up to 32, 64 or 128 of its rows (verify slots x query
+//               heads of the GQA group); its steps are first the tree's (32 new keys
+//               each), then the prefix's, two 32-token blocks each.  The steps of all
+//               units are cut into equal contiguous ranges: a head's blocks lie in one
+//               piece, so nothing is gained by waves that read the heads of the same
+//               tokens side by side, and one head's keys are spread over as many waves
+//               as they can feed.  Every workgroup finds its ranges by itself, from the
+//               requests' lengths.
+//               A wave has 32 rows.  It copies its tiles HBM -> LDS into slots of its own
+//               with direct-to-LDS loads: S^T = K Q^T and O^T += V^T P^T with K and V
+//               widened to bfloat16 (exact), an online softmax in base 2 between them.
+//               The K scale goes into the softmax's factor, the V scale into its
 //               exponent.
 //   q8_combine  merges the partial sums of units that several waves share.
 //
@@ -42,11 +44,8 @@ static_assert(kQ8Wgs * kQ8Waves * kQ8WaveLds <= 160 * 1024, "gfx950 LDS per CU")
 constexpr int kQ8Copies = 8;       // copy instructions per step and tensor
 // What a step costs a workgroup that has 4, 2 or 1 gangs at work, relative to each other.
 constexpr float kQ8Cost1 = 1.4f, kQ8Cost2 = 2.2f, kQ8Cost4 = 4.0f;
-constexpr int kPlanThreads = 1024;
-constexpr int kPlanWords = 6;      // words of LDS per request
-constexpr int kPlanBatch = 16;     // block-table entries per thread and round trip
-constexpr int kPlanPages = 2 * kPlanBatch * kPlanThreads;  // entries that the plan checks itself
-
+constexpr int kOwnPages = 512;     // block tables up to this wide are checked by the waves
+constexpr float kQ8MaxSteps = 1073741824.0f;  // 2^30: steps of a class
 typedef int intx2 __attribute__((ext_vector_type(2)));
 typedef int intx8 __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) intx2 lds_intx2_t;
@@ -69,33 +68,29 @@ constexpr int kQ8Classes = 3;  // k = 1 << class
 // A request's part in a class: Hkv * passes units (unit = head * passes + pass) of tpu steps
 // each, from step tile0 of the class on; gang member m has rows row0 + 32 (k pass + m) .. of
 // a head, as far as there are so many.
-struct Q8Req {
-  int32_t tile0, tpu;
-  int32_t q0, nslots;
-  int32_t P, r, passes, row0;
+struct Q8Part {
+  int tile0, tpu;
+  int q0, nslots;
+  int P, r, passes, row0;
 };
 
-// A wave's range of steps and where it starts (req: place in the class's list).
-// Gang g of the class is members m = 0 .. k - 1 at wave wave_of(g) + m.  cut_last: if the
-// range's first step lies inside a unit, and is the first range start that does, the
-// last gang of that unit (else 0): the unit's sums are merged from gangs gang - 1 ..
-// cut_last.
-struct Q8Start {
-  int32_t lo, hi, req, unit;
-  int32_t gang, cut_last, k, member;
-  int32_t wg0, nwg, pad[2];  // the class's workgroups
-  Q8Req q;
+// Where a wave's range begins inside a unit, and is the first that does: the unit's partial
+// sums are those of `parts` gangs from gang - 1 on (0: there is nothing to merge).  Gangs
+// go round the class's workgroups wg0 .. wg0 + nwg - 1, so that few of them spread
+// over the CUs.
+struct Q8Cut {
+  int32_t parts, gang, k, member;
+  int32_t wg0, nwg, q0, nslots;
+  int32_t head, row0, pad[2];
 };
-static_assert(sizeof(Q8Start) == 80, "20 words");
+static_assert(sizeof(Q8Cut) == 48, "12 words");
 
-// Gangs go round the class's workgroups, so that few of them spread over the CUs.
 __device__ __forceinline__ int q8_wave_of(int g, int k, int wg0, int nwg) {
   return (wg0 + g % nwg) * kQ8Waves + g / nwg * k;
 }
 
 struct Q8Ws {
-  Q8Start* starts;   // [waves]
-  Q8Req* reqs;       // [2 R], class by class
+  Q8Cut* cuts;       // [waves]
   int32_t* bad;      // [R][chunks] flags of q8_pages
   float* part_ml;    // [waves][2][32][4]: max, sum, sum of the weights used, scale exponent
   _Float16* part_o;  // [waves][2][32][128]
@@ -115,32 +110,25 @@ struct Q8Args {
   const uint32_t* tree_mask;
   long long num_pages;
   int page_shift, max_pages, W, R, max_rows, hq, hkv, G;
+  int chunks;        // flags of q8_pages per request, 0: the waves check
   float scale2;
   uint16_t* out;
   float* lse;
   int32_t* status;
 };
 
-__host__ __device__ inline int q8_page_chunks(int max_pages) {
-  return (max_pages + kPageChunk - 1) / kPageChunk;
+// Narrow tables need one or two loads a wave and request; a launch of its own costs 3-5 us.
+__host__ inline int q8_page_chunks(int max_pages) {
+  return max_pages <= kOwnPages ? 0 : (max_pages + kPageChunk - 1) / kPageChunk;
 }
 
-// Whether the plan checks the page ids itself, with loads issued beside those of the
-// requests' fields (a launch of their own costs 3-5 us).
-__host__ inline bool q8_plan_checks(int R, int max_pages) {
-  return (long long)R * max_pages <= kPlanPages;
-}
-
-__host__ inline Q8Ws q8_layout(void* base, int R, int max_rows, int hq, int hkv, int max_pages,
-                               int nw, size_t* bytes) {
+__host__ inline Q8Ws q8_layout(void* base, int R, int max_pages, int nw, size_t* bytes) {
   char* p = static_cast<char*>(base);
   Q8Ws w;
-  w.starts = reinterpret_cast<Q8Start*>(p);
-  p += al(size_t(nw) * sizeof(Q8Start));
-  w.reqs = reinterpret_cast<Q8Req*>(p);
-  p += al(2 * size_t(R) * sizeof(Q8Req));
+  w.cuts = reinterpret_cast<Q8Cut*>(p);
+  p += al(size_t(nw) * sizeof(Q8Cut));
   w.bad = reinterpret_cast<int32_t*>(p);
-  if (!q8_plan_checks(R, max_pages)) p += al(size_t(R) * size_t(q8_page_chunks(max_pages)) * 4);
+  p += al(size_t(R) * size_t(q8_page_chunks(max_pages)) * 4);
   w.part_ml = reinterpret_cast<float*>(p);
   p += al(size_t(nw) * 2 * kQ8Rows * 4 * sizeof(float));
   w.part_o = reinterpret_cast<_Float16*>(p);
@@ -170,7 +158,7 @@ __global__ __launch_bounds__(kPageChunk) void q8_pages_kernel(Q8Args a, int32_t*
   if (threadIdx.x == 0) bad_flags[size_t(r) * gridDim.y + c] = bad;
 }
 
-// ---------------------------------------------------------------- plan ----
+// -------------------------------------------------------------- ranges ----
 // How often class c goes through the keys of a head with t tiles of 32 rows.
 __device__ __forceinline__ int q8_passes(int t, int c) {
   const int rest = t & 3;
@@ -187,179 +175,6 @@ __device__ __forceinline__ int q8_unit_steps(int nslots, int P) {
          int((unsigned(P) + kQ8StepKeys - 1) / kQ8StepKeys);
 }
 
-// One workgroup.  It runs once, so that its time is the fetching of its code and a few
-// round trips: loops instead of unrolled copies, a wave per class for the scans.
-__global__ __launch_bounds__(kPlanThreads) void q8_plan_kernel(Q8Args a, Q8Ws ws, int nw, int chunks) {
-  extern __shared__ int32_t s_mem[];  // kPlanWords R
-  __shared__ int s_n[kQ8Classes + 1], s_T[kQ8Classes + 1], s_wg[kQ8Classes + 1];
-  __shared__ long long s_T64[kQ8Classes];
-  const int tid = threadIdx.x, lane = tid & (kWave - 1), wid = wave_id();
-  const int R = a.R;
-  int32_t* s_tile0 = s_mem;               // [2 R] first steps of the classes' parts
-  int32_t* s_req = s_mem + 2 * R;         // [2 R] their requests
-  int32_t* s_steps = s_mem + 4 * R;       // [R] steps of a pass through request r
-  int32_t* s_tiles = s_mem + 5 * R;       // [R] its row tiles; -1: not to be used
-  int32_t* s_pages = s_mem;               // [R] its pages (before s_tile0)
-  // requests whose offsets, length or pages cannot be used
-  const bool own = chunks == 0;
-  const int entries = own ? R * a.max_pages : 0;
-  int pg[kPlanBatch];
-  if (own) {  // (every load in flight at once)
-#pragma unroll
-    for (int k = 0; k < kPlanBatch; ++k)
-      pg[k] = a.block_table[min(tid + k * kPlanThreads, entries - 1)];
-  }
-#pragma unroll 1
-  for (int r = tid; r < R; r += kPlanThreads) {
-    const int q0 = a.q_offsets[r], q1 = a.q_offsets[r + 1], P = a.prefix_len[r];
-    const int np = prefix_pages(P, a);
-    bool bad = !(q0 >= 0 && q1 >= q0 && q1 <= a.max_rows) || np < 0;
-    for (int c = 0; c < chunks; ++c) bad = bad || ws.bad[size_t(r) * chunks + c] != 0;
-    s_tiles[r] = bad ? -1 : q8_row_tiles(q1 - q0, a.G);
-    s_pages[r] = np;
-    // (offsets that overlap may ask for any number: 2^31 - 1 stands for more)
-    s_steps[r] = bad ? 0 : int(min((long long)a.hkv * q8_unit_steps(q1 - q0, P), 0x7FFFFFFFll));
-  }
-  __syncthreads();
-  if (own) {
-    const int mp = a.max_pages, dr = kPlanThreads / mp, dc = kPlanThreads % mp;
-    int r = tid / mp, c = tid % mp;  // entry tid + 1024 k is page c of request r
-#pragma unroll 1
-    for (int base = 0; base < entries; base += kPlanBatch * kPlanThreads) {
-      if (base > 0) {
-#pragma unroll
-        for (int k = 0; k < kPlanBatch; ++k)
-          pg[k] = a.block_table[min(base + tid + k * kPlanThreads, entries - 1)];
-      }
-#pragma unroll
-      for (int k = 0; k < kPlanBatch; ++k) {
-        if (r < R && (pg[k] < 0 || pg[k] >= a.num_pages) && c < s_pages[r]) s_tiles[r] = -1;
-        r += dr;
-        c += dc;
-        r += c >= mp ? 1 : 0;
-        c -= c >= mp ? mp : 0;
-      }
-    }
-    __syncthreads();
-  }
-  // requests and steps of every class: wave c counts class c
-  if (wid < kQ8Classes) {
-    int n = 0, bits = 0;
-    long long T = 0;
-#pragma unroll 1
-    for (int r = lane; r - lane < R; r += kWave) {
-      const int tiles = r < R ? s_tiles[r] : 0;
-      if (tiles < 0) bits = ECHO_DATA_BAD_OFFSETS;
-      const int passes = tiles > 0 ? q8_passes(tiles, wid) : 0;
-      if (passes > 0) {
-        n += 1;
-        T += (long long)s_steps[r] * passes;
-      }
-    }
-#pragma unroll 1
-    for (int d = kWave / 2; d > 0; d >>= 1) {
-      n += __shfl_xor(n, d);
-      T += __shfl_xor(T, d);
-    }
-    if (lane == 0) {
-      s_n[wid] = n;
-      s_T64[wid] = T;
-    }
-    if (wid == 0) wave_status_or(a.status, bits);
-  }
-  __syncthreads();
-  const bool fits = s_T64[0] + s_T64[1] + s_T64[2] <= 0x7FFFFFFFll;
-  if (!fits && tid == 0) status_or(a.status, ECHO_DATA_BAD_OFFSETS);
-  // its list of requests; thread 1023 finds the classes' workgroups: by cost, at least one
-  // where there is work
-  if (fits && wid < kQ8Classes) {
-    int run_n = 0, run_t = 0;
-#pragma unroll 1
-    for (int c = 0; c < wid; ++c) run_n += s_n[c];
-#pragma unroll 1
-    for (int r = lane; r - lane < R; r += kWave) {
-      const int tiles = r < R ? s_tiles[r] : 0;
-      const int passes = tiles > 0 ? q8_passes(tiles, wid) : 0;
-      const bool in = passes > 0;
-      const uint64_t who = __ballot(in);
-      const int steps = in ? s_steps[r] * passes : 0;
-      const int inc = wave_inclusive_sum(steps);
-      if (in) {
-        const int at = run_n + lanes_below(who);
-        s_tile0[at] = run_t + inc - steps;
-        s_req[at] = r;
-      }
-      run_n += __popcll(who);
-      run_t += __builtin_amdgcn_readlane(inc, kWave - 1);
-    }
-  }
-  if (tid == kPlanThreads - 1) {
-    const int wgs = nw / kQ8Waves;
-    const float cost[kQ8Classes] = {kQ8Cost1 * float(s_T64[0]), kQ8Cost2 * float(s_T64[1]),
-                                    kQ8Cost4 * float(s_T64[2])};
-    const float per = float(wgs) / (cost[0] + cost[1] + cost[2]);
-    int left = wgs, need = 0;
-    for (int c = 0; c < kQ8Classes; ++c) need += cost[c] > 0.0f ? 1 : 0;
-    for (int c = 0; c < kQ8Classes; ++c) {
-      int n = 0;
-      if (cost[c] > 0.0f) {
-        need -= 1;
-        n = need == 0 ? left : min(max(int(per * cost[c] + 0.5f), 1), left - need);
-      }
-      s_wg[c] = wgs - left;
-      s_T[c] = fits ? int(s_T64[c]) : 0;
-      left -= n;
-    }
-    s_wg[kQ8Classes] = wgs;
-  }
-  __syncthreads();
-  // every wave's start, and the classes' lists
-  const auto part_at = [&](int at, int c) {
-    const int r = s_req[at];
-    Q8Req s;
-    s.tile0 = s_tile0[at];
-    s.q0 = a.q_offsets[r];
-    s.nslots = a.q_offsets[r + 1] - s.q0;
-    s.P = a.prefix_len[r];
-    s.r = r;
-    s.tpu = q8_unit_steps(s.nslots, s.P);
-    s.passes = q8_passes(s_tiles[r], c);
-    s.row0 = c == 2 ? 0 : (s_tiles[r] & ~3) * kQ8Rows;
-    return s;
-  };
-  const int listed = fits ? s_n[0] + s_n[1] + s_n[2] : 0;
-#pragma unroll 1
-  for (int x = tid; x < max(nw, listed); x += kPlanThreads) {
-    if (x < listed) ws.reqs[x] = part_at(x, x < s_n[0] ? 0 : x < s_n[0] + s_n[1] ? 1 : 2);
-    if (x >= nw) continue;
-    const int g = x / kQ8Waves, slot = x % kQ8Waves;
-    int c = 0, first = 0;
-    while (g >= s_wg[c + 1]) first += s_n[c++];  // (s_wg[kQ8Classes] is past every g)
-    Q8Start st = {};
-    const int T = s_T[c];
-    if (T > 0) {
-      st.k = 1 << c;
-      st.wg0 = s_wg[c];
-      st.nwg = s_wg[c + 1] - st.wg0;
-      st.gang = g - st.wg0 + (slot >> c) * st.nwg;
-      st.member = slot & (st.k - 1);
-      const int ng = min(T, st.nwg * (kQ8Waves >> c));
-      if (st.gang < ng) {
-        const DivBy by_n(ng);
-        st.lo = int(range_lo(T, st.gang, by_n));
-        st.hi = int(range_lo(T, st.gang + 1, by_n));
-        st.req = first + upper_bound_idx(s_tile0 + first, s_n[c], st.lo);
-        st.q = part_at(st.req, c);
-        st.unit = (st.lo - st.q.tile0) / unsigned(st.q.tpu);
-        const int u0 = st.q.tile0 + st.unit * st.q.tpu;
-        if (u0 < st.lo && int(range_lo(T, st.gang - 1, by_n)) <= u0)
-          st.cut_last = range_of((long long)u0 + st.q.tpu - 1, T, ng, DivBy(T));
-      }
-    }
-    ws.starts[x] = st;
-  }
-}
-
 // ---------------------------------------------------------------- main ----
 // A tile in LDS: 32 rows x 128 bytes per tensor.  The 16-byte chunk c of row r is at chunk
 // position c ^ f(r), with bits 2, 1, 3 of r as bits 0, 1, 2 of f: the 16 rows of which
@@ -368,13 +183,6 @@ __global__ __launch_bounds__(kPlanThreads) void q8_plan_kernel(Q8Args a, Q8Ws ws
 // sixteenths of the banks.
 __device__ __forceinline__ int q8_swz(int row) {
   return ((row >> 2) & 1) | (row & 2) | ((row >> 1) & 4);
-}
-
-// All copies but those of the youngest tensor of a step (one: it was sent) have landed.
-__device__ __forceinline__ void q8_wait(bool one) {  // uniform
-  if (one) wait_vm<kQ8Copies>();
-  else wait_vm<0>();
-  asm volatile("" ::: "memory");  // the tiles' reads stay behind the wait
 }
 
 // Every LDS read so far has its data (and stays ahead of what follows).
@@ -430,45 +238,255 @@ __device__ __forceinline__ void q8_copy4(uint32_t lds, uint64_t base, const uint
       : "memory", "scc");
 }
 
-__device__ __forceinline__ Q8Req load_req(const Q8Req* reqs, int r) {
-  const_i32_t* p = (const_i32_t*)(reqs + r);
-  int32_t w[8];
-#pragma unroll
-  for (int k = 0; k < 8; ++k) w[k] = p[k];
-  return __builtin_bit_cast(Q8Req, w);
+// What a lane knows of a request.  tiles: row tiles per head, -1: it cannot be used.
+struct Q8Look {
+  int q0, nslots, P, tiles, tpu;
+};
+__device__ __forceinline__ Q8Look q8_look(const Q8Args& a, int q0, int q1, int P) {
+  Q8Look x;
+  const bool ok = q0 >= 0 && q1 >= q0 && q1 <= a.max_rows && prefix_pages(P, a) >= 0;
+  x.q0 = q0;
+  x.nslots = ok ? q1 - q0 : 0;
+  x.P = ok ? P : 0;
+  x.tiles = ok ? q8_row_tiles(x.nslots, a.G) : -1;
+  x.tpu = q8_unit_steps(x.nslots, x.P);
+  return x;
+}
+__device__ __forceinline__ Q8Look q8_look(const Q8Args& a, int r) {
+  return q8_look(a, a.q_offsets[r], a.q_offsets[r + 1], a.prefix_len[r]);
 }
 
-__device__ __forceinline__ Q8Start load_start(const Q8Start* starts, int b) {
-  const_i32_t* p = (const_i32_t*)(starts + b);
-  int32_t w[20];
-#pragma unroll
-  for (int k = 0; k < 20; ++k) w[k] = p[k];
-  return __builtin_bit_cast(Q8Start, w);
-}
-
-// A place in the class's steps (wave-uniform): the unit and its first step.
+// Where a wave is in its class's steps: a unit (of part q), whose first step is u0.
 struct Q8Walk {
-  Q8Req q;
-  int req, unit, u0;
+  Q8Part q;
+  int unit, u0, cls;
+  bool bad;  // the request has pages that are not in the pool: no step of it is taken
   __device__ __forceinline__ int ntail() const { return (q.nslots + kTileKeys - 1) / kTileKeys; }
 };
 
+__device__ __forceinline__ int lane_of(int v, int i) { return __builtin_amdgcn_readlane(v, i); }
+__device__ __forceinline__ float lane_of(float v, int i) {
+  return __uint_as_float(uint32_t(__builtin_amdgcn_readlane(int(__float_as_uint(v)), i)));
+}
+
+// Puts w at the class's part of request r, which lane i has looked at, and checks its pages.
+__device__ __forceinline__ void q8_enter(Q8Walk& w, const Q8Args& a, const Q8Ws& ws, const Q8Look& x,
+                                         int i, int r, int tile0) {
+  const int lane = threadIdx.x & (kWave - 1);
+  w.q.tile0 = tile0;
+  w.q.tpu = lane_of(x.tpu, i);
+  w.q.q0 = lane_of(x.q0, i);
+  w.q.nslots = lane_of(x.nslots, i);
+  w.q.P = lane_of(x.P, i);
+  w.q.r = r;
+  const int tiles = lane_of(x.tiles, i);
+  w.q.passes = q8_passes(tiles, w.cls);
+  w.q.row0 = w.cls == 2 ? 0 : (tiles & ~3) * kQ8Rows;
+  w.unit = 0;
+  w.u0 = tile0;
+  const bool own = a.chunks == 0;
+  const int np = prefix_pages(w.q.P, a);
+  const int n = own ? np : (np + kPageChunk - 1) / kPageChunk;
+  const int32_t* e = own ? a.block_table + size_t(r) * size_t(a.max_pages)
+                         : ws.bad + size_t(r) * size_t(a.chunks);
+  bool bad = false;
+  for (int j = 0; j < n; j += 2 * kWave) {  // (two loads at a time)
+    const int e0 = e[min(j + lane, n - 1)], e1 = e[min(j + kWave + lane, n - 1)];
+    bad = bad || (own ? e0 < 0 || e0 >= a.num_pages || e1 < 0 || e1 >= a.num_pages : (e0 | e1) != 0);
+  }
+  w.bad = __ballot(bad) != 0ull;
+  if (w.bad && lane == 0) status_or(a.status, ECHO_DATA_BAD_OFFSETS);
+  asm volatile("");  // (the lanes meet here: what follows stays known to be uniform)
+}
+
 // (Only called where steps are left: there is a next unit.)
 __device__ __forceinline__ void q8_next_unit(Q8Walk& w, const Q8Args& a, const Q8Ws& ws) {
-  if (w.unit + 1 < a.hkv * w.q.passes) {
+  const int units = a.hkv * w.q.passes;
+  if (w.unit + 1 < units) {
     w.unit += 1;
     w.u0 += w.q.tpu;
     return;
   }
-  w.req = __builtin_amdgcn_readfirstlane(w.req + 1);
-  w.q = load_req(ws.reqs, w.req);
-  w.unit = 0;
-  w.u0 = w.q.tile0;
+  const int lane = threadIdx.x & (kWave - 1);
+  const int tile0 = w.q.tile0 + units * w.q.tpu;
+  for (int r = w.q.r + 1; r < a.R; r += kWave) {
+    Q8Look x = {};
+    if (r + lane < a.R) x = q8_look(a, r + lane);
+    const uint64_t in = __ballot(x.tiles > 0 && q8_passes(x.tiles, w.cls) > 0);
+    if (in != 0ull) {
+      const int i = __ffsll((unsigned long long)in) - 1;
+      q8_enter(w, a, ws, x, i, r + i, tile0);
+      return;
+    }
+  }
+}
+
+// T steps in n ranges (0 < n <= T): the first T % n have one step more than the others.
+struct Q8Cutter {
+  int each, more;
+  __device__ Q8Cutter(int T, int n) : each(int(unsigned(T) / unsigned(n))), more(T - each * n) {}
+  __device__ __forceinline__ int first(int g) const { return g * each + min(g, more); }
+  __device__ __forceinline__ int range_of(int t) const {
+    const int longer = more * (each + 1);
+    return t < longer ? int(unsigned(t) / unsigned(each + 1))
+                      : more + int(unsigned(t - longer) / unsigned(each));
+  }
+};
+
+struct Q8Range {
+  int lo, hi, k, member;
+};
+
+// The wave's range and where it starts; what the merge needs to know of it.  Every workgroup
+// counts the steps of all requests (thread t those of requests K t .. K t + K - 1): that is
+// a round trip, a scan and a search, where a launch for it took 10-15 us.  s: 13 KB of LDS.
+__device__ __forceinline__ Q8Range q8_begin(const Q8Args& a, const Q8Ws& ws, uint32_t* s, Q8Walk& w) {
+  constexpr int kThreads = kQ8Waves * kWave, kBatch = 4;
+  const int tid = threadIdx.x, lane = tid & (kWave - 1), wid = wave_id();
+  uint32_t* s_tot = s + kQ8Classes * kThreads;  // [waves][classes + 1]
+  const int K = (a.R + kThreads - 1) / kThreads;
+  uint32_t T[kQ8Classes] = {0u, 0u, 0u};
+  float all = 0.0f;  // (offsets that overlap may ask for any number of steps)
+  int bits = 0;
+#pragma unroll 1
+  for (int i = 0; i < K; i += kBatch) {
+    int q0[kBatch], q1[kBatch], P[kBatch];
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) {
+      const int r = min(tid * K + i + j, a.R - 1);
+      q0[j] = a.q_offsets[r];
+      q1[j] = a.q_offsets[r + 1];
+      P[j] = a.prefix_len[r];
+    }
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) {
+      if (i + j >= K || tid * K + i + j >= a.R) continue;
+      const Q8Look x = q8_look(a, q0[j], q1[j], P[j]);
+      if (x.tiles < 0) bits = ECHO_DATA_BAD_OFFSETS;
+      if (x.tiles <= 0) continue;
+      const uint32_t pass = uint32_t(a.hkv) * uint32_t(x.tpu);
+#pragma unroll
+      for (int c = 0; c < kQ8Classes; ++c) {
+        const int n = q8_passes(x.tiles, c);
+        T[c] += pass * uint32_t(n);
+        all += float(a.hkv) * float(x.tpu) * float(n);
+      }
+    }
+  }
+#pragma unroll
+  for (int d = 1; d < kWave; d *= 2) all += __shfl_xor(all, d);
+#pragma unroll
+  for (int c = 0; c < kQ8Classes; ++c) {
+    const uint32_t inc = uint32_t(wave_inclusive_sum(int(T[c])));
+    s[c * kThreads + tid] = inc - T[c];
+    if (lane == kWave - 1) s_tot[wid * (kQ8Classes + 1) + c] = inc;
+  }
+  if (lane == 0) s_tot[wid * (kQ8Classes + 1) + kQ8Classes] = __float_as_uint(all);
+  __syncthreads();
+  int tot[kQ8Classes] = {0, 0, 0};
+  all = 0.0f;
+#pragma unroll
+  for (int v = 0; v < kQ8Waves; ++v) {
+#pragma unroll
+    for (int c = 0; c < kQ8Classes; ++c)
+      tot[c] += __builtin_amdgcn_readfirstlane(int(s_tot[v * (kQ8Classes + 1) + c]));
+    all += __uint_as_float(s_tot[v * (kQ8Classes + 1) + kQ8Classes]);
+  }
+  // (all of it fits 31 bits, and so does each class; the sum's own rounding is far smaller)
+  if (!(__uint_as_float(uint32_t(__builtin_amdgcn_readfirstlane(int(__float_as_uint(all))))) <= kQ8MaxSteps)) {
+    tot[0] = tot[1] = tot[2] = 0;
+    bits = ECHO_DATA_BAD_OFFSETS;
+  }
+  if (blockIdx.x == 0) wave_status_or(a.status, bits);
+  // the workgroups of the classes: by cost, at least one where there is work
+  const int wgs = gridDim.x, g = blockIdx.x;
+  const float cost[kQ8Classes] = {kQ8Cost1 * float(tot[0]), kQ8Cost2 * float(tot[1]),
+                                  kQ8Cost4 * float(tot[2])};
+  const float per = float(wgs) / (cost[0] + cost[1] + cost[2]);
+  int left = wgs, need = 0, wg0 = 0, nwg = 0, cls = 0;
+#pragma unroll
+  for (int c = 0; c < kQ8Classes; ++c) need += tot[c] > 0 ? 1 : 0;
+#pragma unroll
+  for (int c = 0; c < kQ8Classes; ++c) {
+    int n = 0;
+    if (tot[c] > 0) {
+      need -= 1;
+      n = need == 0 ? left : min(max(int(per * cost[c] + 0.5f), 1), left - need);
+    }
+    if (g >= wgs - left && g < wgs - left + n) {
+      cls = c;
+      wg0 = wgs - left;
+      nwg = n;
+    }
+    left -= n;
+  }
+  cls = __builtin_amdgcn_readfirstlane(cls);
+  wg0 = __builtin_amdgcn_readfirstlane(wg0);
+  nwg = __builtin_amdgcn_readfirstlane(nwg);
+  Q8Cut cut = {};
+  Q8Range x = {};
+  // the steps that each wave's threads counted, of the class
+  int part[kQ8Waves], all_steps = 0;
+#pragma unroll
+  for (int v = 0; v < kQ8Waves; ++v) {
+    part[v] = __builtin_amdgcn_readfirstlane(int(s_tot[v * (kQ8Classes + 1) + cls]));
+    all_steps += part[v];
+  }
+  const int gangs = min(all_steps, nwg * (kQ8Waves >> cls));
+  cut.k = 1 << cls;
+  cut.member = wid & (cut.k - 1);
+  cut.wg0 = wg0;
+  cut.nwg = nwg;
+  cut.gang = g - wg0 + (wid >> cls) * nwg;
+  if (nwg > 0 && cut.gang < gangs) {  // (no workgroups: no steps that can be taken)
+    const Q8Cutter ranges(all_steps, gangs);
+    x.lo = ranges.first(cut.gang);
+    x.hi = ranges.first(cut.gang + 1);
+    x.k = cut.k;
+    x.member = cut.member;
+    w.cls = cls;
+    // the last thread whose requests' steps start at lo or before: of four in each lane
+    const uint4 v = reinterpret_cast<const uint4*>(s + cls * kThreads)[lane];
+    const auto offset = [&](int u) {
+      int o = 0;
+#pragma unroll
+      for (int v = 0; v + 1 < kQ8Waves; ++v) o += u > v ? part[v] : 0;
+      return o;
+    };
+    const int o = offset(lane / (kWave / kQ8Waves));
+    const int th = __popcll(__ballot(int(v.x) + o <= x.lo)) + __popcll(__ballot(int(v.y) + o <= x.lo)) +
+                   __popcll(__ballot(int(v.z) + o <= x.lo)) + __popcll(__ballot(int(v.w) + o <= x.lo)) - 1;
+    const int start = __builtin_amdgcn_readfirstlane(int(s[cls * kThreads + th])) + offset(th / kWave);
+    // and which of them it is
+    Q8Look q = {};
+    if (lane < K && th * K + lane < a.R) q = q8_look(a, th * K + lane);
+    const int steps = q.tiles > 0 ? a.hkv * q.tpu * q8_passes(q.tiles, cls) : 0;
+    const int end = start + wave_inclusive_sum(steps);
+    const int i = __ffsll((unsigned long long)__ballot(end > x.lo)) - 1;
+    q8_enter(w, a, ws, q, i, th * K + i, lane_of(end - steps, i));
+    w.unit = int(unsigned(x.lo - w.q.tile0) / unsigned(w.q.tpu));
+    w.u0 = w.q.tile0 + w.unit * w.q.tpu;
+    if (w.u0 < x.lo && ranges.first(cut.gang - 1) <= w.u0 && !w.bad) {
+      cut.parts = ranges.range_of(w.u0 + w.q.tpu - 1) - cut.gang + 2;
+      cut.q0 = w.q.q0;
+      cut.nslots = w.q.nslots;
+      cut.head = w.unit / w.q.passes;
+      cut.row0 = w.q.row0 + (w.unit % w.q.passes * cut.k + cut.member) * kQ8Rows;
+    }
+  }
+  if (lane == 0) ws.cuts[g * kQ8Waves + wid] = cut;
+  __syncthreads();  // the tiles take this memory
+  return x;
 }
 
 // The first of the member's rows of the unit.
 __device__ __forceinline__ int q8_row0(const Q8Walk& w, int k, int member) {
   return w.q.row0 + (w.unit % w.q.passes * k + member) * kQ8Rows;
+}
+
+// Whether the member has rows of the unit, of a request that can be used.
+__device__ __forceinline__ bool q8_has_rows(const Q8Walk& w, const Q8Args& a, int k, int member) {
+  return !w.bad && q8_row0(w, k, member) < w.q.nslots * a.G;
 }
 
 // What a wave knows of the next 32 steps of its range, tile i (two per step) in lane
@@ -498,7 +516,7 @@ __device__ __forceinline__ void q8_fill(Q8Table& tb, const Q8Args& a, const Q8Ws
     const int p0 = w.u0 + w.ntail();
     t = max(t, min(end, p0));
     // (a member without rows of this unit takes none of its steps)
-    if (q8_row0(w, tb.k, tb.member) >= w.q.nslots * a.G) t = end;
+    if (!q8_has_rows(w, a, tb.k, tb.member)) t = end;
     const int m = min((kWave - n) / 2, end - t);
     if (lane >= n && lane < n + 2 * m) {
       key = (t - p0) * kQ8StepKeys + (lane - n) * kTileKeys;
@@ -522,11 +540,6 @@ __device__ __forceinline__ void q8_fill(Q8Table& tb, const Q8Args& a, const Q8Ws
     tb.lvs = __builtin_amdgcn_logf(vs);
     tb.ivs = __builtin_amdgcn_rcpf(vs);
   }
-}
-
-__device__ __forceinline__ int lane_of(int v, int i) { return __builtin_amdgcn_readlane(v, i); }
-__device__ __forceinline__ float lane_of(float v, int i) {
-  return __uint_as_float(uint32_t(__builtin_amdgcn_readlane(int(__float_as_uint(v)), i)));
 }
 
 // The lane's LDS and copy offsets in one register (three would be reloaded from memory in
@@ -934,17 +947,12 @@ q8_main_kernel(Q8Args a, Q8Ws ws) {
   __shared__ __attribute__((aligned(1024))) char smem[kQ8Waves * kQ8WaveLds];
   const int wid = wave_id();
   const int b = __builtin_amdgcn_readfirstlane(int(blockIdx.x) * kQ8Waves + wid);
-  const Q8Start st = load_start(ws.starts, b);
-  if (st.lo >= st.hi) return;  // (no barrier in this kernel: the waves are independent)
-  const int lane = threadIdx.x & (kWave - 1);
+  Q8Walk w = {};
+  const Q8Range st = q8_begin(a, ws, reinterpret_cast<uint32_t*>(smem), w);
+  if (st.lo >= st.hi) return;  // (no barrier after this: the waves are independent)
   const uint32_t ring = __builtin_amdgcn_readfirstlane(
       uint32_t(reinterpret_cast<uintptr_t>((lds_void_t*)(smem + wid * kQ8WaveLds))));
   const uint32_t offs = q8_lane_offsets();
-  Q8Walk w;
-  w.q = st.q;
-  w.req = st.req;
-  w.unit = st.unit;
-  w.u0 = st.q.tile0 + st.unit * st.q.tpu;
   Q8Table tb = {};
   tb.k = st.k;
   tb.member = st.member;
@@ -954,7 +962,7 @@ q8_main_kernel(Q8Args a, Q8Ws ws) {
     const int lo = max(st.lo, w.u0), hi = min(st.hi, w.u0 + w.q.tpu);
     const bool whole = w.u0 >= st.lo && w.u0 + w.q.tpu <= st.hi;
     const int slot = w.u0 >= st.lo ? 1 : 0;
-    if (q8_row0(w, tb.k, tb.member) < w.q.nslots * a.G)
+    if (q8_has_rows(w, a, tb.k, tb.member))
       q8_segment<kFmt>(a, ws, w, lo, hi, st.hi, b, ring, tb, offs, whole, slot);
     if (hi >= st.hi) break;
     q8_next_unit(w, a, ws);
@@ -966,19 +974,25 @@ q8_main_kernel(Q8Args a, Q8Ws ws) {
 // ------------------------------------------------------------- combine ----
 constexpr int kQ8Parts = 8;  // partial sums per round trip
 
+__device__ __forceinline__ Q8Cut load_cut(const Q8Cut* cuts, int b) {
+  const_i32_t* p = (const_i32_t*)(cuts + b);
+  int32_t w[12];
+#pragma unroll
+  for (int i = 0; i < 12; ++i) w[i] = p[i];
+  return __builtin_bit_cast(Q8Cut, w);
+}
+
 // Workgroup (b, y): rows 16 y .. 16 y + 15 that wave b has of the unit that is cut first
 // at its range (if any); a thread has 8 dims of a row.  Parts in the order of the gangs.
 __global__ __launch_bounds__(256) void q8_combine_kernel(Q8Args a, Q8Ws ws) {
   const int b = blockIdx.x;
-  const Q8Start st = load_start(ws.starts, b);
-  if (st.cut_last == 0) return;
-  const int head = st.unit / st.q.passes;
-  const int row0 = st.q.row0 + (st.unit % st.q.passes * st.k + st.member) * kQ8Rows;
-  const int rows = min(kQ8Rows, st.q.nslots * a.G - row0);
+  const Q8Cut st = load_cut(ws.cuts, b);
+  if (st.parts == 0) return;
+  const int rows = min(kQ8Rows, st.nslots * a.G - st.row0);
   const int rho = blockIdx.y * 16 + threadIdx.x / 16;
   if (rho >= rows) return;
   const int piece = threadIdx.x & 15;  // 8 halves of the partial
-  const int np = st.cut_last - st.gang + 2;
+  const int np = st.parts;
   const auto prow = [&](int i) {
     const int wave = q8_wave_of(st.gang - 1 + i, st.k, st.wg0, st.nwg) + st.member;
     return (size_t(wave) * 2 + (i == 0 ? 1 : 0)) * kQ8Rows + size_t(rho);
@@ -1015,8 +1029,8 @@ __global__ __launch_bounds__(256) void q8_combine_kernel(Q8Args a, Q8Ws ws) {
       for (int k = 0; k < 8; ++k) acc[k] = __builtin_fmaf(wo, float(h[j][k]), acc[k]);
     }
   }
-  const int ra = row0 + rho;
-  const size_t orow = size_t(st.q.q0 + ra / a.G) * a.hq + size_t(head) * a.G + ra % a.G;
+  const int ra = st.row0 + rho;
+  const size_t orow = size_t(st.q0 + ra / a.G) * a.hq + size_t(st.head) * a.G + ra % a.G;
   const float inv = Lq > 0.0f ? 1.0f / Lq : 0.0f;
   // piece 4 dt + 2 k + h holds dims 32 dt + 16 k + 4 h + 0..3 and the same + 8
   uint16_t* po = a.out + orow * kD + 32 * (piece >> 2) + 16 * ((piece >> 1) & 1) + 4 * (piece & 1);
@@ -1033,15 +1047,14 @@ __global__ __launch_bounds__(256) void q8_combine_kernel(Q8Args a, Q8Ws ws) {
 size_t attn_q8_workspace_bytes(int32_t R, int32_t max_rows, int32_t hq, int32_t hkv,
                                int32_t max_pages) {
   size_t n = 0;
-  q8_layout(nullptr, R, max_rows, hq, hkv, max_pages, q8_waves(), &n);
+  q8_layout(nullptr, R, max_pages, q8_waves(), &n);
   return n;
 }
 
 int32_t launch_tree_verify_attn_q8(const AttnQ8Args& x, hipStream_t stream) {
   (void)hipGetLastError();
   const int nw = q8_waves();
-  const Q8Ws ws = q8_layout(x.workspace, x.R, x.max_rows, x.hq, x.cache.hkv, x.max_pages,
-                            nw, nullptr);
+  const Q8Ws ws = q8_layout(x.workspace, x.R, x.max_pages, nw, nullptr);
   Q8Args a;
   a.q = x.q;
   a.k_new = x.k_new;
@@ -1068,18 +1081,10 @@ int32_t launch_tree_verify_attn_q8(const AttnQ8Args& x, hipStream_t stream) {
   a.out = x.out;
   a.lse = x.lse;
   a.status = x.status;
-  int chunks = 0;
-  if (!q8_plan_checks(a.R, a.max_pages)) {
-    chunks = q8_page_chunks(a.max_pages);
-    hipLaunchKernelGGL(q8_pages_kernel, dim3(unsigned(a.R), unsigned(chunks)), dim3(kPageChunk), 0,
+  a.chunks = q8_page_chunks(a.max_pages);
+  if (a.chunks > 0)
+    hipLaunchKernelGGL(q8_pages_kernel, dim3(unsigned(a.R), unsigned(a.chunks)), dim3(kPageChunk), 0,
                        stream, a, ws.bad);
-  }
-  const size_t lds = kPlanWords * size_t(a.R) * sizeof(int32_t);
-  if (lds > 60 * 1024 &&
-      hipFuncSetAttribute(reinterpret_cast<const void*>(q8_plan_kernel),
-                          hipFuncAttributeMaxDynamicSharedMemorySize, int(lds)) != hipSuccess)
-    return ECHO_ERR_HIP;
-  hipLaunchKernelGGL(q8_plan_kernel, dim3(1), dim3(kPlanThreads), lds, stream, a, ws, nw, chunks);
   hipLaunchKernelGGL(x.cache.format == ECHO_KV_E4M3 ? q8_main_kernel<ECHO_KV_E4M3>
                                                     : q8_main_kernel<ECHO_KV_E5M2>,
                      dim3(unsigned(nw / kQ8Waves)), dim3(kQ8Waves * kWave), 0, stream, a, ws);
