@@ -44,6 +44,10 @@ static_assert(kQ8Wgs * kQ8Waves * kQ8WaveLds <= 160 * 1024, "gfx950 LDS per CU")
 constexpr int kQ8Copies = 8;       // copy instructions per step and tensor
 // What a step costs a workgroup that has 4, 2 or 1 gangs at work, relative to each other.
 constexpr float kQ8Cost1 = 1.4f, kQ8Cost2 = 2.2f, kQ8Cost4 = 4.0f;
+// Entering a unit (its rows of Q, the way out of the last one) takes as long as this many steps.
+constexpr int kQ8Enter = 1;
+// Of 32 steps that two gangs on the same CU share, the older workgroup's gets this many.
+constexpr int kQ8Older = 18;
 constexpr int kOwnPages = 512;     // block tables up to this wide are checked by the waves
 constexpr float kQ8MaxSteps = 1073741824.0f;  // 2^30: steps of a class
 typedef int intx2 __attribute__((ext_vector_type(2)));
@@ -76,8 +80,8 @@ struct Q8Part {
 
 // Where a wave's range begins inside a unit, and is the first that does: the unit's partial
 // sums are those of `parts` gangs from gang - 1 on (0: there is nothing to merge).  Gangs
-// go round the class's workgroups wg0 .. wg0 + nwg - 1, so that few of them spread
-// over the CUs.
+// go round the class's places wg0 .. wg0 + nwg - 1, so that few of them spread over the
+// CUs.
 struct Q8Cut {
   int32_t parts, gang, k, member;
   int32_t wg0, nwg, q0, nslots;
@@ -85,8 +89,14 @@ struct Q8Cut {
 };
 static_assert(sizeof(Q8Cut) == 48, "12 words");
 
-__device__ __forceinline__ int q8_wave_of(int g, int k, int wg0, int nwg) {
-  return (wg0 + g % nwg) * kQ8Waves + g / nwg * k;
+// Workgroups b and b + half the grid share a CU (no result depends on it): places 2 b and
+// 2 b + 1, so that a class has as many of the older as of the younger.
+__device__ __forceinline__ int q8_place(int b, int wgs) {
+  return b < wgs / 2 ? 2 * b : 2 * (b - wgs / 2) + 1;
+}
+__device__ __forceinline__ int q8_wave_of(int g, int k, int wg0, int nwg, int wgs) {
+  const int place = wg0 + g % nwg;
+  return ((place & 1) * (wgs / 2) + (place >> 1)) * kQ8Waves + g / nwg * k;
 }
 
 struct Q8Ws {
@@ -111,6 +121,7 @@ struct Q8Args {
   long long num_pages;
   int page_shift, max_pages, W, R, max_rows, hq, hkv, G;
   int chunks;        // flags of q8_pages per request, 0: the waves check
+  int wgs;           // workgroups of the main kernel (even)
   float scale2;
   uint16_t* out;
   float* lse;
@@ -169,9 +180,9 @@ __device__ __forceinline__ int q8_row_tiles(int nslots, int G) {
   return int((unsigned(nslots) * unsigned(G) + kQ8Rows - 1) / kQ8Rows);
 }
 
-// Steps of a unit.
+// Steps of a unit: those of entering it (nothing is done in them), the tree's, the prefix's.
 __device__ __forceinline__ int q8_unit_steps(int nslots, int P) {
-  return (nslots + kTileKeys - 1) / kTileKeys +
+  return kQ8Enter + (nslots + kTileKeys - 1) / kTileKeys +
          int((unsigned(P) + kQ8StepKeys - 1) / kQ8StepKeys);
 }
 
@@ -261,7 +272,10 @@ struct Q8Walk {
   Q8Part q;
   int unit, u0, cls;
   bool bad;  // the request has pages that are not in the pool: no step of it is taken
-  __device__ __forceinline__ int ntail() const { return (q.nslots + kTileKeys - 1) / kTileKeys; }
+  // steps before the prefix's
+  __device__ __forceinline__ int head() const {
+    return kQ8Enter + (q.nslots + kTileKeys - 1) / kTileKeys;
+  }
 };
 
 __device__ __forceinline__ int lane_of(int v, int i) { return __builtin_amdgcn_readlane(v, i); }
@@ -321,15 +335,27 @@ __device__ __forceinline__ void q8_next_unit(Q8Walk& w, const Q8Args& a, const Q
   }
 }
 
-// T steps in n ranges (0 < n <= T): the first T % n have one step more than the others.
+// T > 0 steps in ranges, of which two make a pair (one of its own if T = 1): pairs of equal
+// size but for one step, and the first of two has kQ8Older / 32 of the pair's steps.
+// No range before the last is empty.
 struct Q8Cutter {
-  int each, more;
-  __device__ Q8Cutter(int T, int n) : each(int(unsigned(T) / unsigned(n))), more(T - each * n) {}
-  __device__ __forceinline__ int first(int g) const { return g * each + min(g, more); }
+  int n, each, more;
+  __device__ Q8Cutter(int T, int gangs) : n(max(min(gangs, T) / 2, 1)) {
+    each = int(unsigned(T) / unsigned(n));
+    more = T - each * n;
+  }
+  __device__ __forceinline__ int pair_at(int p) const { return p * each + min(p, more); }
+  __device__ __forceinline__ int first(int g) const {
+    const int p = g >> 1, lo = pair_at(p);
+    if ((g & 1) == 0) return lo;
+    const int len = each + (p < more ? 1 : 0);
+    return lo + min((len * kQ8Older + 16) / 32, max(len - 1, 1));
+  }
   __device__ __forceinline__ int range_of(int t) const {
     const int longer = more * (each + 1);
-    return t < longer ? int(unsigned(t) / unsigned(each + 1))
-                      : more + int(unsigned(t - longer) / unsigned(each));
+    const int p = t < longer ? int(unsigned(t) / unsigned(each + 1))
+                             : more + int(unsigned(t - longer) / unsigned(each));
+    return 2 * p + (t >= first(2 * p + 1) ? 1 : 0);
   }
 };
 
@@ -339,11 +365,14 @@ struct Q8Range {
 
 // The wave's range and where it starts; what the merge needs to know of it.  Every workgroup
 // counts the steps of all requests (thread t those of requests K t .. K t + K - 1): that is
-// a round trip, a scan and a search, where a launch for it took 10-15 us.  s: 13 KB of LDS.
+// a round trip, a scan and a search, where a launch for it took 10-15 us.  s: 3.1 KB and 8
+// bytes a request, of LDS.
 __device__ __forceinline__ Q8Range q8_begin(const Q8Args& a, const Q8Ws& ws, uint32_t* s, Q8Walk& w) {
   constexpr int kThreads = kQ8Waves * kWave, kBatch = 4;
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wid = wave_id();
   uint32_t* s_tot = s + kQ8Classes * kThreads;  // [waves][classes + 1]
+  int* s_q = reinterpret_cast<int*>(s_tot + kQ8Waves * (kQ8Classes + 1));  // [R + 1] offsets
+  int* s_P = s_q + a.R + 1;                                                // [R] lengths
   const int K = (a.R + kThreads - 1) / kThreads;
   uint32_t T[kQ8Classes] = {0u, 0u, 0u};
   float all = 0.0f;  // (offsets that overlap may ask for any number of steps)
@@ -360,7 +389,11 @@ __device__ __forceinline__ Q8Range q8_begin(const Q8Args& a, const Q8Ws& ws, uin
     }
 #pragma unroll
     for (int j = 0; j < kBatch; ++j) {
-      if (i + j >= K || tid * K + i + j >= a.R) continue;
+      const int r = tid * K + i + j;
+      if (i + j >= K || r >= a.R) continue;
+      s_q[r] = q0[j];
+      s_P[r] = P[j];
+      if (r + 1 == a.R) s_q[r + 1] = q1[j];
       const Q8Look x = q8_look(a, q0[j], q1[j], P[j]);
       if (x.tiles < 0) bits = ECHO_DATA_BAD_OFFSETS;
       if (x.tiles <= 0) continue;
@@ -398,8 +431,8 @@ __device__ __forceinline__ Q8Range q8_begin(const Q8Args& a, const Q8Ws& ws, uin
     bits = ECHO_DATA_BAD_OFFSETS;
   }
   if (blockIdx.x == 0) wave_status_or(a.status, bits);
-  // the workgroups of the classes: by cost, at least one where there is work
-  const int wgs = gridDim.x, g = blockIdx.x;
+  // the workgroups of the classes, in pairs: by cost, at least one where there is work
+  const int wgs = a.wgs, g = q8_place(blockIdx.x, wgs);
   const float cost[kQ8Classes] = {kQ8Cost1 * float(tot[0]), kQ8Cost2 * float(tot[1]),
                                   kQ8Cost4 * float(tot[2])};
   const float per = float(wgs) / (cost[0] + cost[1] + cost[2]);
@@ -411,7 +444,7 @@ __device__ __forceinline__ Q8Range q8_begin(const Q8Args& a, const Q8Ws& ws, uin
     int n = 0;
     if (tot[c] > 0) {
       need -= 1;
-      n = need == 0 ? left : min(max(int(per * cost[c] + 0.5f), 1), left - need);
+      n = need == 0 ? left : min(max(2 * int(0.5f * per * cost[c] + 0.5f), 2), left - 2 * need);
     }
     if (g >= wgs - left && g < wgs - left + n) {
       cls = c;
@@ -432,16 +465,17 @@ __device__ __forceinline__ Q8Range q8_begin(const Q8Args& a, const Q8Ws& ws, uin
     part[v] = __builtin_amdgcn_readfirstlane(int(s_tot[v * (kQ8Classes + 1) + cls]));
     all_steps += part[v];
   }
-  const int gangs = min(all_steps, nwg * (kQ8Waves >> cls));
+  const Q8Cutter ranges(max(all_steps, 1), nwg * (kQ8Waves >> cls));
   cut.k = 1 << cls;
   cut.member = wid & (cut.k - 1);
   cut.wg0 = wg0;
   cut.nwg = nwg;
   cut.gang = g - wg0 + (wid >> cls) * nwg;
-  if (nwg > 0 && cut.gang < gangs) {  // (no workgroups: no steps that can be taken)
-    const Q8Cutter ranges(all_steps, gangs);
+  if (all_steps > 0 && cut.gang < 2 * ranges.n) {
     x.lo = ranges.first(cut.gang);
     x.hi = ranges.first(cut.gang + 1);
+  }
+  if (x.lo < x.hi) {
     x.k = cut.k;
     x.member = cut.member;
     w.cls = cls;
@@ -459,7 +493,8 @@ __device__ __forceinline__ Q8Range q8_begin(const Q8Args& a, const Q8Ws& ws, uin
     const int start = __builtin_amdgcn_readfirstlane(int(s[cls * kThreads + th])) + offset(th / kWave);
     // and which of them it is
     Q8Look q = {};
-    if (lane < K && th * K + lane < a.R) q = q8_look(a, th * K + lane);
+    const int rl = th * K + lane;
+    if (lane < K && rl < a.R) q = q8_look(a, s_q[rl], s_q[rl + 1], s_P[rl]);
     const int steps = q.tiles > 0 ? a.hkv * q.tpu * q8_passes(q.tiles, cls) : 0;
     const int end = start + wave_inclusive_sum(steps);
     const int i = __ffsll((unsigned long long)__ballot(end > x.lo)) - 1;
@@ -474,7 +509,7 @@ __device__ __forceinline__ Q8Range q8_begin(const Q8Args& a, const Q8Ws& ws, uin
       cut.row0 = w.q.row0 + (w.unit % w.q.passes * cut.k + cut.member) * kQ8Rows;
     }
   }
-  if (lane == 0) ws.cuts[g * kQ8Waves + wid] = cut;
+  if (lane == 0) ws.cuts[blockIdx.x * kQ8Waves + wid] = cut;
   __syncthreads();  // the tiles take this memory
   return x;
 }
@@ -499,48 +534,11 @@ __device__ __forceinline__ bool q8_has_rows(const Q8Walk& w, const Q8Args& a, in
 struct Q8Table {
   uint32_t blk;
   int tokens;
-  float c, lvs, ivs;  // softmax factor x K scale; log2 of the V scale, and its reciprocal
+  float c, lvs;       // softmax factor x K scale; log2 of the V scale
   int known, k_sent, v_sent, done;
   int k, member;      // of the wave's gang
+  bool raw;           // c and lvs are still the scales (which may be on their way)
 };
-
-// Fills the table from step t of the unit at w on.
-__device__ __forceinline__ void q8_fill(Q8Table& tb, const Q8Args& a, const Q8Ws& ws, Q8Walk w, int t,
-                                        int hi) {
-  const int lane = threadIdx.x & (kWave - 1);
-  int n = 0;  // lanes filled
-  uint32_t entry = 0, head = 0;
-  int key = 0, tokens = 0;
-  while (n < kWave && t < hi) {  // uniform
-    const int end = min(hi, w.u0 + w.q.tpu);
-    const int p0 = w.u0 + w.ntail();
-    t = max(t, min(end, p0));
-    // (a member without rows of this unit takes none of its steps)
-    if (!q8_has_rows(w, a, tb.k, tb.member)) t = end;
-    const int m = min((kWave - n) / 2, end - t);
-    if (lane >= n && lane < n + 2 * m) {
-      key = (t - p0) * kQ8StepKeys + (lane - n) * kTileKeys;
-      tokens = max(w.q.P - key, 0);
-      if (tokens == 0) key -= kTileKeys;
-      entry = uint32_t(w.q.r) * uint32_t(a.max_pages) + uint32_t(key >> a.page_shift);
-      head = uint32_t(w.unit / w.q.passes);
-    }
-    n += 2 * m;
-    t += m;
-    if (t >= end && t < hi) q8_next_unit(w, a, ws);
-  }
-  tb.known += n / 2;
-  if (lane < n) {
-    const uint32_t page = uint32_t(a.block_table[entry]);
-    tb.blk = ((page * uint32_t(a.hkv) + head) << (a.page_shift - 5)) +
-             (uint32_t(key & ((1 << a.page_shift) - 1)) >> 5);
-    tb.tokens = tokens;
-    const float ks = a.k_scale[tb.blk], vs = a.v_scale[tb.blk];
-    tb.c = a.scale2 * ks;
-    tb.lvs = __builtin_amdgcn_logf(vs);
-    tb.ivs = __builtin_amdgcn_rcpf(vs);
-  }
-}
 
 // The lane's LDS and copy offsets in one register (three would be reloaded from memory in
 // the main loop, behind every copy in flight).
@@ -599,6 +597,57 @@ __device__ __forceinline__ void q8_send(const Q8Table& tb, int& sent, const uint
   sent += 1;
 }
 
+// Fills the table from step t of the unit at w on, and sends for the first step's tiles; the
+// scales come in the same round trip, beside Q and the tree's keys if a unit begins.
+__device__ __forceinline__ void q8_fill(Q8Table& tb, const Q8Args& a, const Q8Ws& ws, Q8Walk w, int t,
+                                        int hi, uint32_t ring, uint32_t offs) {
+  const int lane = threadIdx.x & (kWave - 1);
+  int n = 0;  // lanes filled
+  uint32_t entry = 0, head = 0;
+  int key = 0, tokens = 0;
+  while (n < kWave && t < hi) {  // uniform
+    const int end = min(hi, w.u0 + w.q.tpu);
+    const int p0 = w.u0 + w.head();
+    t = max(t, min(end, p0));
+    // (a member without rows of this unit takes none of its steps)
+    if (!q8_has_rows(w, a, tb.k, tb.member)) t = end;
+    const int m = min((kWave - n) / 2, end - t);
+    if (lane >= n && lane < n + 2 * m) {
+      key = (t - p0) * kQ8StepKeys + (lane - n) * kTileKeys;
+      tokens = max(w.q.P - key, 0);
+      if (tokens == 0) key -= kTileKeys;
+      entry = uint32_t(w.q.r) * uint32_t(a.max_pages) + uint32_t(key >> a.page_shift);
+      head = uint32_t(w.unit / w.q.passes);
+    }
+    n += 2 * m;
+    t += m;
+    if (t >= end && t < hi) q8_next_unit(w, a, ws);
+  }
+  tb.known += n / 2;
+  float ks = 1.0f, vs = 1.0f;
+  if (lane < n) {
+    const uint32_t page = uint32_t(a.block_table[entry]);
+    tb.blk = ((page * uint32_t(a.hkv) + head) << (a.page_shift - 5)) +
+             (uint32_t(key & ((1 << a.page_shift) - 1)) >> 5);
+    tb.tokens = tokens;
+    ks = a.k_scale[tb.blk];
+    vs = a.v_scale[tb.blk];
+  }
+  q8_send(tb, tb.k_sent, a.k_pages, ring, offs);
+  q8_send(tb, tb.v_sent, a.v_pages, ring + kQ8Slot, offs);
+  tb.c = ks;
+  tb.lvs = vs;
+  tb.raw = true;
+}
+
+// The scales' values, once they are there, become what the softmax takes.
+__device__ __forceinline__ void q8_scales(Q8Table& tb, const Q8Args& a) {
+  tb.c *= a.scale2;
+  tb.lvs = __builtin_amdgcn_logf(tb.lvs);
+  tb.raw = false;
+}
+
+
 // Two bytes (the upper two of w if hi) as bfloat16 (exact).
 template <int kFmt>
 __device__ __forceinline__ uint32_t widen2(uint32_t w, bool hi) {  // hi: a constant
@@ -652,10 +701,11 @@ __device__ __forceinline__ void q8_mask(floatx16& s, uint32_t word) {
     s[r] = ((w >> (8 * (r >> 2) + (r & 3))) & 1u) ? s[r] : -__builtin_inff();
 }
 
-__device__ __forceinline__ float max16(const floatx16& s) {
-  const float a = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(s[4], s[5]));
-  const float b = fmaxf(fmaxf(fmaxf(s[6], s[7]), fmaxf(s[8], s[9])), fmaxf(s[10], s[11]));
-  return fmaxf(fmaxf(a, b), fmaxf(fmaxf(s[12], s[13]), fmaxf(s[14], s[15])));
+__device__ __forceinline__ float max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
+__device__ __forceinline__ float max16(const floatx16& s) {  // (eight instructions)
+  const float a = max3(s[0], s[1], s[2]), b = max3(s[3], s[4], s[5]), c = max3(s[6], s[7], s[8]);
+  const float d = max3(s[9], s[10], s[11]), e = max3(s[12], s[13], s[14]);
+  return fmaxf(max3(a, b, s[15]), max3(c, d, e));
 }
 
 #define ECHO_FENCE() __builtin_amdgcn_sched_barrier(0)
@@ -782,12 +832,6 @@ __device__ __forceinline__ void q8_tree_tile(const Q8Args& a, int head, int s0, 
       s, rt, c, lvs);
 }
 
-// The ring's first copies.
-__device__ __forceinline__ void q8_prime(Q8Table& tb, const Q8Args& a, uint32_t ring, uint32_t offs) {
-  q8_send(tb, tb.k_sent, a.k_pages, ring, offs);
-  q8_send(tb, tb.v_sent, a.v_pages, ring + kQ8Slot, offs);
-}
-
 // A wave's steps [lo, hi) of one unit, then its output or partial sums.
 //
 // K is widened to bfloat16 between the products.  (v_mfma_f32_32x32x64_f8f6f4 would take its
@@ -818,20 +862,21 @@ __device__ __forceinline__ void q8_segment(const Q8Args& a, const Q8Ws& ws, cons
     rt.l = 0.0f;
     rt.lq = 0.0f;
     rt.mgrow = -__builtin_inff();
-    for (; t < hi && t - w.u0 < w.ntail(); ++t) {
-      const int lt = t - w.u0;
+    for (t = max(t, min(hi, w.u0 + kQ8Enter)); t < hi && t - w.u0 < w.head(); ++t) {
+      const int lt = t - w.u0 - kQ8Enter;
       const int tn = min(kTileKeys, w.q.nslots - lt * kTileKeys);
       uint32_t word = lt < a.W ? a.tree_mask[size_t(slot) * a.W + lt] : 0u;
       if (tn < kTileKeys) word &= (1u << tn) - 1u;
       q8_tree_tile(a, head, w.q.q0 + lt * kTileKeys, tn, ring + 2 * kQ8Slot, q, rt, word);
     }
   }
+  if (tb.raw) q8_scales(tb, a);  // uniform
   wait_vm<0>();  // no load that the compiler knows of is in flight in the loop
 
   for (; t < hi; ++t) {
     if (tb.done == tb.known) {  // the table is used up, and the ring empty
-      q8_fill(tb, a, ws, w, t, range_hi);
-      q8_prime(tb, a, ring, offs);
+      q8_fill(tb, a, ws, w, t, range_hi, ring, offs);
+      q8_scales(tb, a);
     }
     const int i = (2 * tb.done) & (kWave - 1);
     // K and V of the step to registers; then their places are refilled while they are multiplied
@@ -945,6 +990,7 @@ template <int kFmt>
 __global__ __launch_bounds__(kQ8Waves * kWave) __attribute__((amdgpu_waves_per_eu(2, 2))) void
 q8_main_kernel(Q8Args a, Q8Ws ws) {
   __shared__ __attribute__((aligned(1024))) char smem[kQ8Waves * kQ8WaveLds];
+  static_assert(4096 + 8 * (ECHO_MAX_REQUESTS + 1) <= sizeof(smem), "the requests fit");
   const int wid = wave_id();
   const int b = __builtin_amdgcn_readfirstlane(int(blockIdx.x) * kQ8Waves + wid);
   Q8Walk w = {};
@@ -956,8 +1002,7 @@ q8_main_kernel(Q8Args a, Q8Ws ws) {
   Q8Table tb = {};
   tb.k = st.k;
   tb.member = st.member;
-  q8_fill(tb, a, ws, w, st.lo, st.hi);
-  q8_prime(tb, a, ring, offs);
+  q8_fill(tb, a, ws, w, st.lo, st.hi, ring, offs);
   while (true) {
     const int lo = max(st.lo, w.u0), hi = min(st.hi, w.u0 + w.q.tpu);
     const bool whole = w.u0 >= st.lo && w.u0 + w.q.tpu <= st.hi;
@@ -994,7 +1039,7 @@ __global__ __launch_bounds__(256) void q8_combine_kernel(Q8Args a, Q8Ws ws) {
   const int piece = threadIdx.x & 15;  // 8 halves of the partial
   const int np = st.parts;
   const auto prow = [&](int i) {
-    const int wave = q8_wave_of(st.gang - 1 + i, st.k, st.wg0, st.nwg) + st.member;
+    const int wave = q8_wave_of(st.gang - 1 + i, st.k, st.wg0, st.nwg, a.wgs) + st.member;
     return (size_t(wave) * 2 + (i == 0 ? 1 : 0)) * kQ8Rows + size_t(rho);
   };
   float M = -__builtin_inff(), L = 0.0f, Lq = 0.0f;
@@ -1081,6 +1126,7 @@ int32_t launch_tree_verify_attn_q8(const AttnQ8Args& x, hipStream_t stream) {
   a.out = x.out;
   a.lse = x.lse;
   a.status = x.status;
+  a.wgs = nw / kQ8Waves;
   a.chunks = q8_page_chunks(a.max_pages);
   if (a.chunks > 0)
     hipLaunchKernelGGL(q8_pages_kernel, dim3(unsigned(a.R), unsigned(a.chunks)), dim3(kPageChunk), 0,
