@@ -41,7 +41,7 @@ constexpr int kQ8Slot = 2 * kBlockBytes;          // one tensor's tiles of a ste
 constexpr int kQ8Scratch = 16 * kD * 2;           // 16 rows of bfloat16 V (tree tiles)
 constexpr int kQ8WaveLds = 2 * kQ8Slot + kQ8Scratch;  // K, V, scratch
 static_assert(kQ8Wgs * kQ8Waves * kQ8WaveLds <= 160 * 1024, "gfx950 LDS per CU");
-constexpr int kQ8Copies = 8;       // copy instructions per step and tensor
+constexpr int kGangSlots = 4;      // slots of a gang of four waves, which share their tiles
 // What a step costs a workgroup that has 4, 2 or 1 gangs at work, relative to each other.
 constexpr float kQ8Cost1 = 1.4f, kQ8Cost2 = 2.2f, kQ8Cost4 = 4.0f;
 // Entering a unit (its rows of Q, the way out of the last one) takes as long as this many steps.
@@ -272,6 +272,7 @@ struct Q8Walk {
   Q8Part q;
   int unit, u0, cls;
   bool bad;  // the request has pages that are not in the pool: no step of it is taken
+  bool met;  // this or an earlier one had
   // steps before the prefix's
   __device__ __forceinline__ int head() const {
     return kQ8Enter + (q.nslots + kTileKeys - 1) / kTileKeys;
@@ -309,8 +310,7 @@ __device__ __forceinline__ void q8_enter(Q8Walk& w, const Q8Args& a, const Q8Ws&
     bad = bad || (own ? e0 < 0 || e0 >= a.num_pages || e1 < 0 || e1 >= a.num_pages : (e0 | e1) != 0);
   }
   w.bad = __ballot(bad) != 0ull;
-  if (w.bad && lane == 0) status_or(a.status, ECHO_DATA_BAD_OFFSETS);
-  asm volatile("");  // (the lanes meet here: what follows stays known to be uniform)
+  w.met |= w.bad;
 }
 
 // (Only called where steps are left: there is a next unit.)
@@ -535,7 +535,8 @@ struct Q8Table {
   uint32_t blk;
   int tokens;
   float c, lvs;       // softmax factor x K scale; log2 of the V scale
-  int known, k_sent, v_sent, done;
+  int known, k_sent, v_sent, done;  // (a gang of four: k_sent for both)
+  bool more;          // the range has steps past the table's
   int k, member;      // of the wave's gang
   bool raw;           // c and lvs are still the scales (which may be on their way)
 };
@@ -547,14 +548,16 @@ struct Q8Table {
 //             the order in which S^T leaves them in the lanes), dims 32 dt + lane % 32: the
 //             lane supplies half of one key's 16-byte chunk 2 dt + (lane / 16) % 2, an
 //             exclusive-or of bits 5 and 6
-//   copies    rows 0-7 of a tile (and 16-23); the other rows have bit 6 flipped
-__device__ __forceinline__ uint32_t q8_lane_offsets() {
+//   copies    eight rows of a tile from row_of_copy on (rows 0-7, and 16-23; the other
+//             rows have bit 6 flipped)
+__device__ __forceinline__ uint32_t q8_lane_offsets(int row_of_copy) {
   const int lane = threadIdx.x & (kWave - 1);
   const int row = lane & 31, h = lane >> 5, i = lane & 15;
   const int vkey = 4 * h + ((i >> 1) & 3) + ((i >> 3) << 3);
   const uint32_t k = uint32_t(row * kD + (((2 * h) ^ q8_swz(row)) << 4));
   const uint32_t v = uint32_t(vkey * kD + ((((lane >> 4) & 1) ^ q8_swz(vkey)) << 4) + ((i & 1) << 3));
-  const uint32_t c = uint32_t((lane >> 3) * kD + (((lane & 7) ^ q8_swz(lane >> 3)) << 4));
+  const int crow = row_of_copy + (lane >> 3);
+  const uint32_t c = uint32_t(crow * kD + (((lane & 7) ^ q8_swz(crow)) << 4));
   return (k >> 4) | (v << 8) | (c << 16);  // k a multiple of 16 and v of 8 below 2^12 (2^11)
 }
 __device__ __forceinline__ uint32_t q8_opaque(uint32_t x) {  // (not kept unpacked)
@@ -597,23 +600,62 @@ __device__ __forceinline__ void q8_send(const Q8Table& tb, int& sent, const uint
   sent += 1;
 }
 
-// Fills the table from step t of the unit at w on, and sends for the first step's tiles; the
-// scales come in the same round trip, beside Q and the tree's keys if a unit begins.
+// The wave's quarter (eight rows of each tile) of the next step's tiles, for its gang of four.
+__device__ __forceinline__ void q8_send_gang(Q8Table& tb, const Q8Args& a, uint32_t ring, uint32_t offs) {
+  if (tb.k_sent >= tb.known) return;  // uniform
+  const int i = (2 * tb.k_sent) & (kWave - 1);
+  const uint64_t b0 = uint64_t(uint32_t(lane_of(int(tb.blk), i))) * kBlockBytes;
+  const uint64_t b1 = uint64_t(uint32_t(lane_of(int(tb.blk), i + 1))) * kBlockBytes;
+  const uint64_t k = reinterpret_cast<uint64_t>(a.k_pages), v = reinterpret_cast<uint64_t>(a.v_pages);
+  const uint32_t c = copy_offset(offs);
+  const int row = int(c) / kD;
+  const uint32_t in_row = c & (kD - 1);
+  const auto offset = [&](int tokens) {  // (rows past the tile's tokens: the last one again)
+    return uint32_t(min(row, min(max(tokens, 1), kTileKeys) - 1) * kD) + in_row;
+  };
+  const uint32_t o0 = offset(lane_of(tb.tokens, i)), o1 = offset(lane_of(tb.tokens, i + 1));
+  const uint32_t lds = ring + uint32_t((tb.k_sent & (kGangSlots - 1)) * 2 * kQ8Slot + tb.member * 1024);
+  uint32_t saved;
+  asm volatile(
+      "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %4 nt\n\t"
+      "s_add_u32 m0, m0, 0x1000\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %3, %5 nt\n\t"
+      "s_add_u32 m0, m0, 0x1000\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %6 nt\n\t"
+      "s_add_u32 m0, m0, 0x1000\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %3, %7 nt\n\t"
+      "s_mov_b32 m0, %0"
+      : "=&s"(saved)
+      : "s"(lds), "v"(o0), "v"(o1), "s"(k + b0), "s"(k + b1), "s"(v + b0), "s"(v + b1)
+      : "memory", "scc");
+  tb.k_sent += 1;
+}
+
+// Fills the table behind what it still holds, given that step t of the unit at w is the next to
+// be taken, and sends for the first steps' tiles; the scales come in the same round trip, the
+// first time beside Q and the tree's keys if a unit begins.
+template <bool kGang>
 __device__ __forceinline__ void q8_fill(Q8Table& tb, const Q8Args& a, const Q8Ws& ws, Q8Walk w, int t,
                                         int hi, uint32_t ring, uint32_t offs) {
   const int lane = threadIdx.x & (kWave - 1);
-  int n = 0;  // lanes filled
+  const bool first = tb.known == 0;
+  int skip = tb.known - tb.done;  // steps that it holds
+  const int room = kWave - 2 * skip;
+  const int pos = (lane - 2 * tb.known) & (kWave - 1);  // the lane's place in what is filled
+  int n = 0;                                            // lanes filled
   uint32_t entry = 0, head = 0;
   int key = 0, tokens = 0;
-  while (n < kWave && t < hi) {  // uniform
+  while (n < room && t < hi) {  // uniform
     const int end = min(hi, w.u0 + w.q.tpu);
     const int p0 = w.u0 + w.head();
     t = max(t, min(end, p0));
-    // (a member without rows of this unit takes none of its steps)
-    if (!q8_has_rows(w, a, tb.k, tb.member)) t = end;
-    const int m = min((kWave - n) / 2, end - t);
-    if (lane >= n && lane < n + 2 * m) {
-      key = (t - p0) * kQ8StepKeys + (lane - n) * kTileKeys;
+    // (a wave without rows of this unit takes none of its steps, unless its gang counts on it)
+    if (kGang ? w.bad : !q8_has_rows(w, a, tb.k, tb.member)) t = end;
+    if (kGang) {
+      const int held = min(skip, end - t);
+      skip -= held;
+      t += held;
+    }
+    const int m = min((room - n) / 2, end - t);
+    if (pos >= n && pos < n + 2 * m) {
+      key = (t - p0) * kQ8StepKeys + (pos - n) * kTileKeys;
       tokens = max(w.q.P - key, 0);
       if (tokens == 0) key -= kTileKeys;
       entry = uint32_t(w.q.r) * uint32_t(a.max_pages) + uint32_t(key >> a.page_shift);
@@ -624,8 +666,9 @@ __device__ __forceinline__ void q8_fill(Q8Table& tb, const Q8Args& a, const Q8Ws
     if (t >= end && t < hi) q8_next_unit(w, a, ws);
   }
   tb.known += n / 2;
+  tb.more = t < hi;
   float ks = 1.0f, vs = 1.0f;
-  if (lane < n) {
+  if (pos < n) {
     const uint32_t page = uint32_t(a.block_table[entry]);
     tb.blk = ((page * uint32_t(a.hkv) + head) << (a.page_shift - 5)) +
              (uint32_t(key & ((1 << a.page_shift) - 1)) >> 5);
@@ -633,11 +676,20 @@ __device__ __forceinline__ void q8_fill(Q8Table& tb, const Q8Args& a, const Q8Ws
     ks = a.k_scale[tb.blk];
     vs = a.v_scale[tb.blk];
   }
-  q8_send(tb, tb.k_sent, a.k_pages, ring, offs);
-  q8_send(tb, tb.v_sent, a.v_pages, ring + kQ8Slot, offs);
-  tb.c = ks;
-  tb.lvs = vs;
-  tb.raw = true;
+  if (kGang) {
+    for (int j = tb.k_sent - tb.done; j < kGangSlots - 1; ++j) q8_send_gang(tb, a, ring, offs);
+  } else {
+    q8_send(tb, tb.k_sent, a.k_pages, ring, offs);
+    q8_send(tb, tb.v_sent, a.v_pages, ring + kQ8Slot, offs);
+  }
+  if (first) {
+    tb.c = ks;
+    tb.lvs = vs;
+    tb.raw = true;
+  } else if (pos < n) {
+    tb.c = a.scale2 * ks;
+    tb.lvs = __builtin_amdgcn_logf(vs);
+  }
 }
 
 // The scales' values, once they are there, become what the softmax takes.
@@ -646,7 +698,6 @@ __device__ __forceinline__ void q8_scales(Q8Table& tb, const Q8Args& a) {
   tb.lvs = __builtin_amdgcn_logf(tb.lvs);
   tb.raw = false;
 }
-
 
 // Two bytes (the upper two of w if hi) as bfloat16 (exact).
 template <int kFmt>
@@ -837,10 +888,10 @@ __device__ __forceinline__ void q8_tree_tile(const Q8Args& a, int head, int s0, 
 // K is widened to bfloat16 between the products.  (v_mfma_f32_32x32x64_f8f6f4 would take its
 // bytes as they are and Q as the sum of two e4m3 numbers, in as many cycles, but it drops
 // what is below 2^-13 of the largest of its products.)
-template <int kFmt>
+template <int kFmt, bool kGang>
 __device__ __forceinline__ void q8_segment(const Q8Args& a, const Q8Ws& ws, const Q8Walk& w, int lo,
-                                           int hi, int range_hi, int b, uint32_t ring, Q8Table& tb,
-                                           uint32_t offs, bool whole, int part_slot) {
+                                           int hi, int range_hi, int b, uint32_t ring, uint32_t scratch,
+                                           Q8Table& tb, uint32_t offs, bool whole, int part_slot) {
   const int lane = threadIdx.x & (kWave - 1);
   const int h = lane >> 5;
   const int head = w.unit / w.q.passes;
@@ -848,8 +899,8 @@ __device__ __forceinline__ void q8_segment(const Q8Args& a, const Q8Ws& ws, cons
   const int rows = min(kQ8Rows, w.q.nslots * a.G - row0);
   bf16x8 q[8];
   Q8Rows rt;
-  int t = lo;
-  {
+  int t = max(lo, min(hi, w.u0 + kQ8Enter));
+  if (!kGang || rows > 0) {  // uniform
     // (a row past the last one computes the last one again, to be dropped)
     const int ra = row0 + min(lane & 31, rows - 1);
     const int slot = w.q.q0 + ra / a.G;
@@ -862,28 +913,46 @@ __device__ __forceinline__ void q8_segment(const Q8Args& a, const Q8Ws& ws, cons
     rt.l = 0.0f;
     rt.lq = 0.0f;
     rt.mgrow = -__builtin_inff();
-    for (t = max(t, min(hi, w.u0 + kQ8Enter)); t < hi && t - w.u0 < w.head(); ++t) {
+    for (; t < hi && t - w.u0 < w.head(); ++t) {
       const int lt = t - w.u0 - kQ8Enter;
       const int tn = min(kTileKeys, w.q.nslots - lt * kTileKeys);
       uint32_t word = lt < a.W ? a.tree_mask[size_t(slot) * a.W + lt] : 0u;
       if (tn < kTileKeys) word &= (1u << tn) - 1u;
-      q8_tree_tile(a, head, w.q.q0 + lt * kTileKeys, tn, ring + 2 * kQ8Slot, q, rt, word);
+      q8_tree_tile(a, head, w.q.q0 + lt * kTileKeys, tn, scratch, q, rt, word);
     }
   }
+  if (kGang) t = max(t, min(hi, w.u0 + w.head()));
   if (tb.raw) q8_scales(tb, a);  // uniform
   wait_vm<0>();  // no load that the compiler knows of is in flight in the loop
 
   for (; t < hi; ++t) {
-    if (tb.done == tb.known) {  // the table is used up, and the ring empty
-      q8_fill(tb, a, ws, w, t, range_hi, ring, offs);
-      q8_scales(tb, a);
-    }
     const int i = (2 * tb.done) & (kWave - 1);
+    uint32_t tiles = ring;
+    if (kGang) {
+      if (tb.more && tb.k_sent == tb.known) q8_fill<true>(tb, a, ws, w, t, range_hi, ring, offs);
+      // the wave's quarter of the step has landed (up to two steps are behind it), and the others'
+      const int behind = tb.k_sent - tb.done - 1;
+      if (behind >= 2) wait_vm<8>();
+      else if (behind == 1) wait_vm<4>();
+      else wait_vm<0>();
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      tiles += uint32_t((tb.done & (kGangSlots - 1)) * 2 * kQ8Slot);
+      if (rows <= 0) {
+        q8_send_gang(tb, a, ring, offs);
+        tb.done += 1;
+        continue;
+      }
+    } else {
+      // (the table is used up, and the ring empty)
+      if (tb.done == tb.known) q8_fill<false>(tb, a, ws, w, t, range_hi, ring, offs);
+      wait_vm<0>();
+      asm volatile("" ::: "memory");  // the tiles' reads stay behind the wait
+    }
     // K and V of the step to registers; then their places are refilled while they are multiplied
-    wait_vm<0>();
-    asm volatile("" ::: "memory");  // the tiles' reads stay behind the wait
     uint4v kr[2][2][2];  // [tile][half of the dims][chunk]
-    const uint32_t ka = ring + k_offset(offs);
+    const uint32_t ka = tiles + k_offset(offs);
 #pragma unroll
     for (int n = 0; n < 2; ++n)
 #pragma unroll
@@ -892,7 +961,7 @@ __device__ __forceinline__ void q8_segment(const Q8Args& a, const Q8Ws& ws, cons
         for (int e = 0; e < 2; ++e)
           kr[n][j][e] = *(lds_uint4_t*)(lds_at(ka ^ uint32_t(64 * j + 16 * e)) + kBlockBytes * n);
     intx2 vr[4][4];  // [16-key group][32 dims]
-    const uint32_t va = ring + kQ8Slot + v_offset(offs);
+    const uint32_t va = tiles + kQ8Slot + v_offset(offs);
 #pragma unroll
     for (int g = 0; g < 4; ++g)
 #pragma unroll
@@ -900,8 +969,13 @@ __device__ __forceinline__ void q8_segment(const Q8Args& a, const Q8Ws& ws, cons
         vr[g][dt] = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
             (lds_intx2_t*)(lds_at(va ^ uint32_t(dt << 5)) + 16 * kD * g));
     q8_wait_lds();
-    q8_send(tb, tb.k_sent, a.k_pages, ring, offs);
-    q8_send(tb, tb.v_sent, a.v_pages, ring + kQ8Slot, offs);
+    if (kGang) {
+      // (into the last step's slot: the others have read it, or they had not come to the barrier)
+      q8_send_gang(tb, a, ring, offs);
+    } else {
+      q8_send(tb, tb.k_sent, a.k_pages, ring, offs);
+      q8_send(tb, tb.v_sent, a.v_pages, ring + kQ8Slot, offs);
+    }
     tb.done += 1;
     floatx16 s[2] = {};
     const auto widen_k = [&](int x) {  // part x / 2 of tile x % 2
@@ -940,6 +1014,7 @@ __device__ __forceinline__ void q8_segment(const Q8Args& a, const Q8Ws& ws, cons
     __builtin_amdgcn_s_setprio(0);
   }
 
+  if (kGang && rows <= 0) return;
   int rho = lane & 31;  // (opaque: the output's addresses are formed here, not kept in registers)
   asm volatile("" : "+v"(rho));
   const float L = pair_sum(rt.l);
@@ -984,6 +1059,27 @@ __device__ __forceinline__ void q8_segment(const Q8Args& a, const Q8Ws& ws, cons
         *reinterpret_cast<floatx4*>(ws.part_ml + prow * 4) = floatx4{rt.m, L, Lq, float(e)};
     }
   }
+  asm volatile("");  // (the lanes meet here: what follows stays known to be uniform)
+}
+
+// A wave's range.
+template <int kFmt, bool kGang>
+__device__ __forceinline__ void q8_range(const Q8Args& a, const Q8Ws& ws, const Q8Range& st, Q8Walk& w,
+                                         int b, uint32_t ring, uint32_t scratch) {
+  const uint32_t offs = q8_lane_offsets(kGang ? 8 * st.member : 0);
+  Q8Table tb = {};
+  tb.k = st.k;
+  tb.member = st.member;
+  q8_fill<kGang>(tb, a, ws, w, st.lo, st.hi, ring, offs);
+  while (true) {
+    const int lo = max(st.lo, w.u0), hi = min(st.hi, w.u0 + w.q.tpu);
+    const bool whole = w.u0 >= st.lo && w.u0 + w.q.tpu <= st.hi;
+    const int slot = w.u0 >= st.lo ? 1 : 0;
+    if (kGang ? !w.bad : q8_has_rows(w, a, tb.k, tb.member))
+      q8_segment<kFmt, kGang>(a, ws, w, lo, hi, st.hi, b, ring, scratch, tb, offs, whole, slot);
+    if (hi >= st.hi) break;
+    q8_next_unit(w, a, ws);
+  }
 }
 
 template <int kFmt>
@@ -991,27 +1087,22 @@ __global__ __launch_bounds__(kQ8Waves * kWave) __attribute__((amdgpu_waves_per_e
 q8_main_kernel(Q8Args a, Q8Ws ws) {
   __shared__ __attribute__((aligned(1024))) char smem[kQ8Waves * kQ8WaveLds];
   static_assert(4096 + 8 * (ECHO_MAX_REQUESTS + 1) <= sizeof(smem), "the requests fit");
+  static_assert(kGangSlots * 2 * kQ8Slot + kQ8Waves * kQ8Scratch == sizeof(smem), "a gang's LDS");
   const int wid = wave_id();
   const int b = __builtin_amdgcn_readfirstlane(int(blockIdx.x) * kQ8Waves + wid);
   Q8Walk w = {};
   const Q8Range st = q8_begin(a, ws, reinterpret_cast<uint32_t*>(smem), w);
-  if (st.lo >= st.hi) return;  // (no barrier after this: the waves are independent)
-  const uint32_t ring = __builtin_amdgcn_readfirstlane(
-      uint32_t(reinterpret_cast<uintptr_t>((lds_void_t*)(smem + wid * kQ8WaveLds))));
-  const uint32_t offs = q8_lane_offsets();
-  Q8Table tb = {};
-  tb.k = st.k;
-  tb.member = st.member;
-  q8_fill(tb, a, ws, w, st.lo, st.hi, ring, offs);
-  while (true) {
-    const int lo = max(st.lo, w.u0), hi = min(st.hi, w.u0 + w.q.tpu);
-    const bool whole = w.u0 >= st.lo && w.u0 + w.q.tpu <= st.hi;
-    const int slot = w.u0 >= st.lo ? 1 : 0;
-    if (q8_has_rows(w, a, tb.k, tb.member))
-      q8_segment<kFmt>(a, ws, w, lo, hi, st.hi, b, ring, tb, offs, whole, slot);
-    if (hi >= st.hi) break;
-    q8_next_unit(w, a, ws);
+  if (st.lo >= st.hi) return;
+  const uint32_t base = __builtin_amdgcn_readfirstlane(
+      uint32_t(reinterpret_cast<uintptr_t>((lds_void_t*)smem)));
+  if (st.k == kQ8Waves) {
+    q8_range<kFmt, true>(a, ws, st, w, b, base,
+                         base + uint32_t(kGangSlots * 2 * kQ8Slot + wid * kQ8Scratch));
+  } else {
+    const uint32_t ring = base + uint32_t(wid * kQ8WaveLds);  // (no barrier: independent waves)
+    q8_range<kFmt, false>(a, ws, st, w, b, ring, ring + 2 * kQ8Slot);
   }
+  if (w.met && (threadIdx.x & (kWave - 1)) == 0) status_or(a.status, ECHO_DATA_BAD_OFFSETS);
 }
 
 #undef ECHO_FENCE
