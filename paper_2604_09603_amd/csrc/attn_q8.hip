@@ -42,8 +42,10 @@ constexpr int kQ8Scratch = 16 * kD * 2;           // 16 rows of bfloat16 V (tree
 constexpr int kQ8WaveLds = 2 * kQ8Slot + kQ8Scratch;  // K, V, scratch
 static_assert(kQ8Wgs * kQ8Waves * kQ8WaveLds <= 160 * 1024, "gfx950 LDS per CU");
 constexpr int kGangSlots = 4;      // slots of a gang of four waves, which share their tiles
-// What a step costs a workgroup that has 4, 2 or 1 gangs at work, relative to each other.
-constexpr float kQ8Cost1 = 1.4f, kQ8Cost2 = 2.2f, kQ8Cost4 = 4.0f;
+// What a step costs a workgroup that has 4, 2 or 1 gangs at work, relative to each other: between
+// the ratios of their products (1, 2, 4) and those of their copies (4 : 2 : 1 gangs, so 1, 1, 1).
+// 235B-shaped trees of 1 to 12 slots: 1, 2, 4 took 8 us more, 1, 1.5, 2.5 took 2 us more.
+constexpr float kQ8Cost1 = 1.4f, kQ8Cost2 = 2.2f, kQ8Cost4 = 3.6f;
 // Entering a unit (its rows of Q, the way out of the last one) takes as long as this many steps.
 constexpr int kQ8Enter = 1;
 // Of 32 steps that two gangs on the same CU share, the older workgroup's gets this many.
@@ -128,7 +130,9 @@ struct Q8Args {
   int32_t* status;
 };
 
-// Narrow tables need one or two loads a wave and request; a launch of its own costs 3-5 us.
+// Narrow tables need a few loads a wave and request; a launch of its own costs 2 us, which wide
+// ones are worth (waves | launch: 64 pages 20.2 | 22.6 us, 512 pages 45.5 | 47.6, 2048 pages
+// 115 | 111).
 __host__ inline int q8_page_chunks(int max_pages) {
   return max_pages <= kOwnPages ? 0 : (max_pages + kPageChunk - 1) / kPageChunk;
 }
@@ -1001,8 +1005,8 @@ __device__ __forceinline__ void q8_segment(const Q8Args& a, const Q8Ws& ws, cons
     }
     const float c[2] = {lane_of(tb.c, i), lane_of(tb.c, i + 1)};
     const float lvs[2] = {lane_of(tb.lvs, i), lane_of(tb.lvs, i + 1)};
-    // Without priorities the older of a SIMD's two waves goes first in every phase, and ends its
-    // range at 160 us where the other needs 222 (a long context); so both end near 206.
+    // Without priorities the older of a SIMD's two waves goes first in every phase, and the other
+    // ends its range long after it (a long context: 231 us without, 225 with).
     __builtin_amdgcn_s_setprio(1);
     q8_values<2>(
         [&](int g, int dt) {
