@@ -161,7 +161,7 @@ __device__ __forceinline__ int prefix_pages(long long P, const Q8Args& a) {
 }
 
 __global__ __launch_bounds__(kPageChunk) void q8_pages_kernel(Q8Args a, int32_t* bad_flags) {
-  const int r = blockIdx.x, c = blockIdx.y;
+  const int c = blockIdx.x, r = blockIdx.y;
   const int np = prefix_pages(a.prefix_len[r], a);
   const int e = c * kPageChunk + int(threadIdx.x);
   int bad = 0;
@@ -170,7 +170,7 @@ __global__ __launch_bounds__(kPageChunk) void q8_pages_kernel(Q8Args a, int32_t*
     bad = pg < 0 || pg >= a.num_pages;
   }
   bad = __syncthreads_or(bad);
-  if (threadIdx.x == 0) bad_flags[size_t(r) * gridDim.y + c] = bad;
+  if (threadIdx.x == 0) bad_flags[size_t(r) * gridDim.x + c] = bad;
 }
 
 // -------------------------------------------------------------- ranges ----
@@ -288,6 +288,22 @@ __device__ __forceinline__ float lane_of(float v, int i) {
   return __uint_as_float(uint32_t(__builtin_amdgcn_readlane(int(__float_as_uint(v)), i)));
 }
 
+// What tells whether a request's pages are in the pool: its page ids, or q8_pages' flags.
+struct Q8Pages {
+  const int32_t* e;
+  int n;
+  bool own;
+  __device__ Q8Pages(const Q8Args& a, const Q8Ws& ws, int r, int P) : own(a.chunks == 0) {
+    const int np = prefix_pages(P, a);
+    n = own ? np : (np + kPageChunk - 1) / kPageChunk;
+    e = own ? a.block_table + size_t(r) * size_t(a.max_pages) : ws.bad + size_t(r) * size_t(a.chunks);
+  }
+  __device__ __forceinline__ bool bad(const Q8Args& a, int i) const {  // (past n: the last again)
+    const int v = e[min(i, n - 1)];
+    return own ? v < 0 || v >= a.num_pages : v != 0;
+  }
+};
+
 // Puts w at the class's part of request r, which lane i has looked at, and checks its pages.
 __device__ __forceinline__ void q8_enter(Q8Walk& w, const Q8Args& a, const Q8Ws& ws, const Q8Look& x,
                                          int i, int r, int tile0) {
@@ -303,16 +319,10 @@ __device__ __forceinline__ void q8_enter(Q8Walk& w, const Q8Args& a, const Q8Ws&
   w.q.row0 = w.cls == 2 ? 0 : (tiles & ~3) * kQ8Rows;
   w.unit = 0;
   w.u0 = tile0;
-  const bool own = a.chunks == 0;
-  const int np = prefix_pages(w.q.P, a);
-  const int n = own ? np : (np + kPageChunk - 1) / kPageChunk;
-  const int32_t* e = own ? a.block_table + size_t(r) * size_t(a.max_pages)
-                         : ws.bad + size_t(r) * size_t(a.chunks);
+  const Q8Pages pages(a, ws, r, w.q.P);
   bool bad = false;
-  for (int j = 0; j < n; j += 2 * kWave) {  // (two loads at a time)
-    const int e0 = e[min(j + lane, n - 1)], e1 = e[min(j + kWave + lane, n - 1)];
-    bad = bad || (own ? e0 < 0 || e0 >= a.num_pages || e1 < 0 || e1 >= a.num_pages : (e0 | e1) != 0);
-  }
+  for (int j = 0; j < pages.n; j += 2 * kWave)  // (two loads at a time)
+    bad |= pages.bad(a, j + lane) | pages.bad(a, j + kWave + lane);
   w.bad = __ballot(bad) != 0ull;
   w.met |= w.bad;
 }
@@ -399,7 +409,13 @@ __device__ __forceinline__ Q8Range q8_begin(const Q8Args& a, const Q8Ws& ws, uin
       s_P[r] = P[j];
       if (r + 1 == a.R) s_q[r + 1] = q1[j];
       const Q8Look x = q8_look(a, q0[j], q1[j], P[j]);
-      if (x.tiles < 0) bits = ECHO_DATA_BAD_OFFSETS;
+      if (x.tiles < 0 && blockIdx.x == 0) bits = ECHO_DATA_BAD_OFFSETS;
+      if (x.tiles == 0 && r % int(gridDim.x) == int(blockIdx.x)) {
+        // nothing to do, but its pages count for the status
+        const Q8Pages pages(a, ws, r, x.P);
+        for (int e = 0; e < pages.n; ++e)
+          if (pages.bad(a, e)) bits = ECHO_DATA_BAD_OFFSETS;
+      }
       if (x.tiles <= 0) continue;
       const uint32_t pass = uint32_t(a.hkv) * uint32_t(x.tpu);
 #pragma unroll
@@ -434,7 +450,7 @@ __device__ __forceinline__ Q8Range q8_begin(const Q8Args& a, const Q8Ws& ws, uin
     tot[0] = tot[1] = tot[2] = 0;
     bits = ECHO_DATA_BAD_OFFSETS;
   }
-  if (blockIdx.x == 0) wave_status_or(a.status, bits);
+  wave_status_or(a.status, bits);
   // the workgroups of the classes, in pairs: by cost, at least one where there is work
   const int wgs = a.wgs, g = q8_place(blockIdx.x, wgs);
   const float cost[kQ8Classes] = {kQ8Cost1 * float(tot[0]), kQ8Cost2 * float(tot[1]),
@@ -1224,7 +1240,7 @@ int32_t launch_tree_verify_attn_q8(const AttnQ8Args& x, hipStream_t stream) {
   a.wgs = nw / kQ8Waves;
   a.chunks = q8_page_chunks(a.max_pages);
   if (a.chunks > 0)
-    hipLaunchKernelGGL(q8_pages_kernel, dim3(unsigned(a.R), unsigned(a.chunks)), dim3(kPageChunk), 0,
+    hipLaunchKernelGGL(q8_pages_kernel, dim3(unsigned(a.chunks), unsigned(a.R)), dim3(kPageChunk), 0,
                        stream, a, ws.bad);
   hipLaunchKernelGGL(x.cache.format == ECHO_KV_E4M3 ? q8_main_kernel<ECHO_KV_E4M3>
                                                     : q8_main_kernel<ECHO_KV_E5M2>,

@@ -9,9 +9,8 @@
 //
 // Both are bound by latency: the 16 bytes a request and the 4 bytes a page of the first
 // fit in the caches, and the second writes 8 bytes a row.  128 requests that take a token
-// each: 6.8 us, of which three dependent round trips to memory (lengths, stack, tables) and
-// their barriers are most; 256 requests with
-// prompts of up to 2048 rows: 7.6 and 4.0 us.
+// each: 6.8 us, most of it three dependent round trips to memory (lengths, stack, tables)
+// and their barriers; 256 requests with prompts of up to 2048 rows: 7.6 and 4.0 us.
 #include "echo_device.h"
 #include "echo_internal.h"
 

@@ -615,6 +615,27 @@ def test_attention_page_checks_of_every_size(R, width):
     assert np.isnan(lse[[0, R // 2, R - 1]]).all() and np.isfinite(lse[1]).all()
 
 
+@pytest.mark.parametrize("width", [4, 600])
+def test_attention_pages_of_requests_without_slots_count(width):
+    """A request that has nothing to verify writes nothing, but its missing page is reported."""
+    rng = np.random.default_rng(20)
+    c = _attn_case(rng, 8, 2, [2, 0, 1], [40, 70, 33], 32, kvq8.E4M3)
+    c["bt"] = np.pad(c["bt"], ((0, 0), (0, width - c["bt"].shape[1])), constant_values=-1)
+    _log(f"[attn q8] no slots, width={width}")
+    _check_attn(c, *_run_attn(c))
+    c["bt"][1, 2] = -1
+    _check_attn(c, *_run_attn(c), st.BAD_OFFSETS)
+
+
+def test_attention_widest_block_table():
+    """One request whose row of the block table has 20 million entries."""
+    rng = np.random.default_rng(21)
+    c = _attn_case(rng, 4, 2, [2], [77], 32, kvq8.E4M3)
+    c["bt"] = np.pad(c["bt"], ((0, 0), (0, 20_000_000)), constant_values=-1)
+    _log("[attn q8] 20 million entries")
+    _check_attn(c, *_run_attn(c))
+
+
 def test_attention_without_lse_and_on_a_stream():
     import torch
     import paper_2604_09603_amd as pkg
