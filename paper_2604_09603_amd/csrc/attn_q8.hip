@@ -48,7 +48,9 @@ constexpr int kGangSlots = 4;      // slots of a gang of four waves, which share
 constexpr float kQ8Cost1 = 1.4f, kQ8Cost2 = 2.2f, kQ8Cost4 = 3.6f;
 // Entering a unit (its rows of Q, the way out of the last one) takes as long as this many steps.
 constexpr int kQ8Enter = 1;
-// Of 32 steps that two gangs on the same CU share, the older workgroup's gets this many.
+// Of 32 steps that two gangs on the same CU share, the older workgroup's gets this many (17 in a
+// class of gangs of four, which are bound by their products): its loads and products go
+// first.  With these shares both end their ranges within a few us of each other.
 constexpr int kQ8Older = 18;
 constexpr int kOwnPages = 512;     // block tables up to this wide are checked by the waves
 constexpr float kQ8MaxSteps = 1073741824.0f;  // 2^30: steps of a class
@@ -350,11 +352,11 @@ __device__ __forceinline__ void q8_next_unit(Q8Walk& w, const Q8Args& a, const Q
 }
 
 // T > 0 steps in ranges, of which two make a pair (one of its own if T = 1): pairs of equal
-// size but for one step, and the first of two has kQ8Older / 32 of the pair's steps.
+// size but for one step, and the first of two has older / 32 of the pair's steps.
 // No range before the last is empty.
 struct Q8Cutter {
-  int n, each, more;
-  __device__ Q8Cutter(int T, int gangs) : n(max(min(gangs, T) / 2, 1)) {
+  int n, each, more, older;
+  __device__ Q8Cutter(int T, int gangs, int older_) : n(max(min(gangs, T) / 2, 1)), older(older_) {
     each = int(unsigned(T) / unsigned(n));
     more = T - each * n;
   }
@@ -363,7 +365,7 @@ struct Q8Cutter {
     const int p = g >> 1, lo = pair_at(p);
     if ((g & 1) == 0) return lo;
     const int len = each + (p < more ? 1 : 0);
-    return lo + min((len * kQ8Older + 16) / 32, max(len - 1, 1));
+    return lo + min((len * older + 16) / 32, max(len - 1, 1));
   }
   __device__ __forceinline__ int range_of(int t) const {
     const int longer = more * (each + 1);
@@ -485,7 +487,7 @@ __device__ __forceinline__ Q8Range q8_begin(const Q8Args& a, const Q8Ws& ws, uin
     part[v] = __builtin_amdgcn_readfirstlane(int(s_tot[v * (kQ8Classes + 1) + cls]));
     all_steps += part[v];
   }
-  const Q8Cutter ranges(max(all_steps, 1), nwg * (kQ8Waves >> cls));
+  const Q8Cutter ranges(max(all_steps, 1), nwg * (kQ8Waves >> cls), kQ8Older - (cls == 2 ? 1 : 0));
   cut.k = 1 << cls;
   cut.member = wid & (cut.k - 1);
   cut.wg0 = wg0;
