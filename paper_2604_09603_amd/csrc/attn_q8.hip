@@ -19,6 +19,19 @@
 //               exponent.
 //   q8_combine  merges the partial sums of units that several waves share.
 //
+// What bounds it.  Few rows per head: HBM.  64 requests decoding over 1024-8192 tokens (32
+// query and 8 KV heads, 604 MB) take 90 us in the main kernel, 6.7 TB/s, and 5 us in the
+// merge; the 10 us until the first tiles are there (lengths, page ids, scales and tiles are
+// dependent round trips) are most of the rest.  Many rows: the vector instructions.  A step
+// of 64 keys and 32 rows takes 32 matrix products (1044 cycles) and about 400 other vector
+// instructions (1700 cycles: 128 conversions, 32 exponentials of two each, 96 products,
+// sums and roundings of the weights), which share a SIMD's issue; with trees of 13 slots on
+// average (16 rows each) over 16384-32768 tokens, 79 us of products, the main kernel takes
+// 210 us, 64% of it issuing vector instructions.  128 trees of 3 slots on average (617 MB) are
+// between the two: 132 us and 9 in the merge.  Units of 32 rows because a 32x32x16 product
+// leaves room for five vector instructions, where 16x16x32 leaves two for the same work;
+// two waves per SIMD, so that one's softmax runs beside the other's products.
+//
 // Softmax statistics and sums are fp32.  The weights p are rounded to bfloat16 for
 // the product with V (at most 2^-8 each) and the output is divided by the sum of the
 // weights used, so that it stays a convex combination of V rows; the output's own
@@ -216,14 +229,14 @@ __device__ __forceinline__ void q8_wait_lds() {
 #define ECHO_Q8_COPY(POL)                                                              \
   "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\t"                                 \
   "global_load_lds_dwordx4 %2, %4" POL "\n\t"                                          \
-  "global_load_lds_dwordx4 %3, %4 offset:1024" POL "\n\t"                              \
-  "global_load_lds_dwordx4 %2, %4 offset:2048" POL "\n\t"                              \
-  "global_load_lds_dwordx4 %3, %4 offset:3072" POL "\n\t"                              \
+  "global_load_lds_dwordx4 %3, %4 offset:0x400" POL "\n\t"                              \
+  "global_load_lds_dwordx4 %2, %4 offset:0x800" POL "\n\t"                              \
+  "global_load_lds_dwordx4 %3, %4 offset:0xc00" POL "\n\t"                              \
   "s_add_u32 m0, m0, 0x1000\n\ts_nop 0\n\t"                                            \
   "global_load_lds_dwordx4 %2, %5" POL "\n\t"                                          \
-  "global_load_lds_dwordx4 %3, %5 offset:1024" POL "\n\t"                              \
-  "global_load_lds_dwordx4 %2, %5 offset:2048" POL "\n\t"                              \
-  "global_load_lds_dwordx4 %3, %5 offset:3072" POL "\n\t"                              \
+  "global_load_lds_dwordx4 %3, %5 offset:0x400" POL "\n\t"                              \
+  "global_load_lds_dwordx4 %2, %5 offset:0x800" POL "\n\t"                              \
+  "global_load_lds_dwordx4 %3, %5 offset:0xc00" POL "\n\t"                              \
   "s_mov_b32 m0, %0"
 __device__ __forceinline__ void q8_copy(uint32_t lds, uint64_t tile0, uint64_t tile1, uint32_t offa,
                                         uint32_t offb, bool alone) {
@@ -1140,7 +1153,8 @@ __device__ __forceinline__ Q8Cut load_cut(const Q8Cut* cuts, int b) {
   return __builtin_bit_cast(Q8Cut, w);
 }
 
-// Workgroup (b, y): rows 16 y .. 16 y + 15 that wave b has of the unit that is cut first
+// (4 us for 16 partial sums, 9-10 us for 2900 of them, 25 MB: latency and the launch, then their
+// bytes.)  Workgroup (b, y): rows 16 y .. 16 y + 15 that wave b has of the unit that is cut first
 // at its range (if any); a thread has 8 dims of a row.  Parts in the order of the gangs.
 __global__ __launch_bounds__(256) void q8_combine_kernel(Q8Args a, Q8Ws ws) {
   const int b = blockIdx.x;
