@@ -314,15 +314,16 @@ struct Q8Pages {
     e = own ? a.block_table + size_t(r) * size_t(a.max_pages) : ws.bad + size_t(r) * size_t(a.chunks);
   }
   __device__ __forceinline__ bool bad(const Q8Args& a, int i) const {  // (past n: the last again)
-    const int v = e[min(i, n - 1)];
+    return bad_value(a, at(i));
+  }
+  __device__ __forceinline__ int at(int i) const { return e[min(i, n - 1)]; }
+  __device__ __forceinline__ bool bad_value(const Q8Args& a, int v) const {
     return own ? v < 0 || v >= a.num_pages : v != 0;
   }
 };
 
-// Puts w at the class's part of request r, which lane i has looked at, and checks its pages.
-__device__ __forceinline__ void q8_enter(Q8Walk& w, const Q8Args& a, const Q8Ws& ws, const Q8Look& x,
-                                         int i, int r, int tile0) {
-  const int lane = threadIdx.x & (kWave - 1);
+// Puts w at the class's part of request r, which lane i has looked at.
+__device__ __forceinline__ void q8_enter(Q8Walk& w, const Q8Look& x, int i, int r, int tile0) {
   w.q.tile0 = tile0;
   w.q.tpu = lane_of(x.tpu, i);
   w.q.q0 = lane_of(x.q0, i);
@@ -334,9 +335,13 @@ __device__ __forceinline__ void q8_enter(Q8Walk& w, const Q8Args& a, const Q8Ws&
   w.q.row0 = w.cls == 2 ? 0 : (tiles & ~3) * kQ8Rows;
   w.unit = 0;
   w.u0 = tile0;
-  const Q8Pages pages(a, ws, r, w.q.P);
-  bool bad = false;
-  for (int j = 0; j < pages.n; j += 2 * kWave)  // (two loads at a time)
+}
+
+// Checks the pages of w's request, from place j of what tells it on.
+__device__ __forceinline__ void q8_check(Q8Walk& w, const Q8Args& a, const Q8Pages& pages, bool bad,
+                                         int j) {
+  const int lane = threadIdx.x & (kWave - 1);
+  for (; j < pages.n; j += 2 * kWave)  // (two loads at a time)
     bad |= pages.bad(a, j + lane) | pages.bad(a, j + kWave + lane);
   w.bad = __ballot(bad) != 0ull;
   w.met |= w.bad;
@@ -358,7 +363,8 @@ __device__ __forceinline__ void q8_next_unit(Q8Walk& w, const Q8Args& a, const Q
     const uint64_t in = __ballot(x.tiles > 0 && q8_passes(x.tiles, w.cls) > 0);
     if (in != 0ull) {
       const int i = __ffsll((unsigned long long)in) - 1;
-      q8_enter(w, a, ws, x, i, r + i, tile0);
+      q8_enter(w, x, i, r + i, tile0);
+      q8_check(w, a, Q8Pages(a, ws, r + i, w.q.P), false, 0);
       return;
     }
   }
@@ -389,10 +395,11 @@ struct Q8Cutter {
 };
 
 struct Q8Range {
-  int lo, hi, k, member;
+  Q8Cutter ranges;  // of the class
+  int lo, hi, k, member, gang, wg0, nwg;
 };
 
-// The wave's range and where it starts; what the merge needs to know of it.  Every workgroup
+// The wave's range and where it starts (its request's pages are not checked).  Every workgroup
 // counts the steps of all requests (thread t those of requests K t .. K t + K - 1): that is
 // a round trip, a scan and a search, where a launch for it took 10-15 us.  s: 3.1 KB and 8
 // bytes a request, of LDS.
@@ -441,8 +448,13 @@ __device__ __forceinline__ Q8Range q8_begin(const Q8Args& a, const Q8Ws& ws, uin
       }
     }
   }
+  // (a sum that could matter is rare)
+  if (__ballot(all > kQ8MaxSteps / kThreads) != 0ull) {
 #pragma unroll
-  for (int d = 1; d < kWave; d *= 2) all += __shfl_xor(all, d);
+    for (int d = 1; d < kWave; d *= 2) all += __shfl_xor(all, d);
+  } else {
+    all = 0.0f;
+  }
 #pragma unroll
   for (int c = 0; c < kQ8Classes; ++c) {
     const uint32_t inc = uint32_t(wave_inclusive_sum(int(T[c])));
@@ -460,7 +472,8 @@ __device__ __forceinline__ Q8Range q8_begin(const Q8Args& a, const Q8Ws& ws, uin
       tot[c] += __builtin_amdgcn_readfirstlane(int(s_tot[v * (kQ8Classes + 1) + c]));
     all += __uint_as_float(s_tot[v * (kQ8Classes + 1) + kQ8Classes]);
   }
-  // (all of it fits 31 bits, and so does each class; the sum's own rounding is far smaller)
+  // (then all of it fits 31 bits: four waves that pass have less than 2^30 between them, and the
+  // sum's own rounding is far smaller)
   if (!(__uint_as_float(uint32_t(__builtin_amdgcn_readfirstlane(int(__float_as_uint(all))))) <= kQ8MaxSteps)) {
     tot[0] = tot[1] = tot[2] = 0;
     bits = ECHO_DATA_BAD_OFFSETS;
@@ -491,8 +504,6 @@ __device__ __forceinline__ Q8Range q8_begin(const Q8Args& a, const Q8Ws& ws, uin
   cls = __builtin_amdgcn_readfirstlane(cls);
   wg0 = __builtin_amdgcn_readfirstlane(wg0);
   nwg = __builtin_amdgcn_readfirstlane(nwg);
-  Q8Cut cut = {};
-  Q8Range x = {};
   // the steps that each wave's threads counted, of the class
   int part[kQ8Waves], all_steps = 0;
 #pragma unroll
@@ -500,19 +511,13 @@ __device__ __forceinline__ Q8Range q8_begin(const Q8Args& a, const Q8Ws& ws, uin
     part[v] = __builtin_amdgcn_readfirstlane(int(s_tot[v * (kQ8Classes + 1) + cls]));
     all_steps += part[v];
   }
-  const Q8Cutter ranges(max(all_steps, 1), nwg * (kQ8Waves >> cls), kQ8Older - (cls == 2 ? 1 : 0));
-  cut.k = 1 << cls;
-  cut.member = wid & (cut.k - 1);
-  cut.wg0 = wg0;
-  cut.nwg = nwg;
-  cut.gang = g - wg0 + (wid >> cls) * nwg;
-  if (all_steps > 0 && cut.gang < 2 * ranges.n) {
-    x.lo = ranges.first(cut.gang);
-    x.hi = ranges.first(cut.gang + 1);
+  Q8Range x = {Q8Cutter(max(all_steps, 1), nwg * (kQ8Waves >> cls), kQ8Older - (cls == 2 ? 1 : 0)),
+               0, 0, 1 << cls, wid & ((1 << cls) - 1), g - wg0 + (wid >> cls) * nwg, wg0, nwg};
+  if (all_steps > 0 && x.gang < 2 * x.ranges.n) {
+    x.lo = x.ranges.first(x.gang);
+    x.hi = x.ranges.first(x.gang + 1);
   }
   if (x.lo < x.hi) {
-    x.k = cut.k;
-    x.member = cut.member;
     w.cls = cls;
     // the last thread whose requests' steps start at lo or before: of four in each lane
     const uint4 v = reinterpret_cast<const uint4*>(s + cls * kThreads)[lane];
@@ -533,18 +538,10 @@ __device__ __forceinline__ Q8Range q8_begin(const Q8Args& a, const Q8Ws& ws, uin
     const int steps = q.tiles > 0 ? a.hkv * q.tpu * q8_passes(q.tiles, cls) : 0;
     const int end = start + wave_inclusive_sum(steps);
     const int i = __ffsll((unsigned long long)__ballot(end > x.lo)) - 1;
-    q8_enter(w, a, ws, q, i, th * K + i, lane_of(end - steps, i));
+    q8_enter(w, q, i, th * K + i, lane_of(end - steps, i));
     w.unit = int(unsigned(x.lo - w.q.tile0) / unsigned(w.q.tpu));
     w.u0 = w.q.tile0 + w.unit * w.q.tpu;
-    if (w.u0 < x.lo && ranges.first(cut.gang - 1) <= w.u0 && !w.bad) {
-      cut.parts = ranges.range_of(w.u0 + w.q.tpu - 1) - cut.gang + 2;
-      cut.q0 = w.q.q0;
-      cut.nslots = w.q.nslots;
-      cut.head = w.unit / w.q.passes;
-      cut.row0 = w.q.row0 + (w.unit % w.q.passes * cut.k + cut.member) * kQ8Rows;
-    }
   }
-  if (lane == 0) ws.cuts[blockIdx.x * kQ8Waves + wid] = cut;
   __syncthreads();  // the tiles take this memory
   return x;
 }
@@ -557,6 +554,23 @@ __device__ __forceinline__ int q8_row0(const Q8Walk& w, int k, int member) {
 // Whether the member has rows of the unit, of a request that can be used.
 __device__ __forceinline__ bool q8_has_rows(const Q8Walk& w, const Q8Args& a, int k, int member) {
   return !w.bad && q8_row0(w, k, member) < w.q.nslots * a.G;
+}
+
+// What the merge has to know of the wave's range, w being where it starts.
+__device__ __forceinline__ Q8Cut q8_cut(const Q8Walk& w, const Q8Range& x) {
+  Q8Cut c = {};
+  if (!w.bad && w.u0 < x.lo && x.ranges.first(x.gang - 1) <= w.u0)
+    c.parts = x.ranges.range_of(w.u0 + w.q.tpu - 1) - x.gang + 2;
+  c.gang = x.gang;
+  c.k = x.k;
+  c.member = x.member;
+  c.wg0 = x.wg0;
+  c.nwg = x.nwg;
+  c.q0 = w.q.q0;
+  c.nslots = w.q.nslots;
+  c.head = w.unit / w.q.passes;
+  c.row0 = q8_row0(w, x.k, x.member);
+  return c;
 }
 
 // What a wave knows of the next 32 steps of its range, tile i (two per step) in lane
@@ -608,6 +622,7 @@ __device__ __forceinline__ uint32_t copy_offset(uint32_t p) { return (q8_opaque(
 // multiplied (they are masked).
 __device__ __forceinline__ void q8_send(const Q8Table& tb, int& sent, const uint8_t* pages,
                                         uint32_t lds, uint32_t offs) {
+  sent = __builtin_amdgcn_readfirstlane(sent);
   if (sent >= tb.known) return;  // uniform
   const int i = (2 * sent) & (kWave - 1);
   const uint64_t base = reinterpret_cast<uint64_t>(pages);
@@ -637,8 +652,9 @@ __device__ __forceinline__ void q8_send(const Q8Table& tb, int& sent, const uint
 
 // The wave's quarter (eight rows of each tile) of the next step's tiles, for its gang of four.
 __device__ __forceinline__ void q8_send_gang(Q8Table& tb, const Q8Args& a, uint32_t ring, uint32_t offs) {
-  if (tb.k_sent >= tb.known) return;  // uniform
-  const int i = (2 * tb.k_sent) & (kWave - 1);
+  const int sent = __builtin_amdgcn_readfirstlane(tb.k_sent);
+  if (sent >= tb.known) return;  // uniform
+  const int i = (2 * sent) & (kWave - 1);
   const uint64_t b0 = uint64_t(uint32_t(lane_of(int(tb.blk), i))) * kBlockBytes;
   const uint64_t b1 = uint64_t(uint32_t(lane_of(int(tb.blk), i + 1))) * kBlockBytes;
   const uint64_t k = reinterpret_cast<uint64_t>(a.k_pages), v = reinterpret_cast<uint64_t>(a.v_pages);
@@ -649,7 +665,7 @@ __device__ __forceinline__ void q8_send_gang(Q8Table& tb, const Q8Args& a, uint3
     return uint32_t(min(row, min(max(tokens, 1), kTileKeys) - 1) * kD) + in_row;
   };
   const uint32_t o0 = offset(lane_of(tb.tokens, i)), o1 = offset(lane_of(tb.tokens, i + 1));
-  const uint32_t lds = ring + uint32_t((tb.k_sent & (kGangSlots - 1)) * 2 * kQ8Slot + tb.member * 1024);
+  const uint32_t lds = ring + uint32_t((sent & (kGangSlots - 1)) * 2 * kQ8Slot + tb.member * 1024);
   uint32_t saved;
   asm volatile(
       "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %4 nt\n\t"
@@ -660,24 +676,26 @@ __device__ __forceinline__ void q8_send_gang(Q8Table& tb, const Q8Args& a, uint3
       : "=&s"(saved)
       : "s"(lds), "v"(o0), "v"(o1), "s"(k + b0), "s"(k + b1), "s"(v + b0), "s"(v + b1)
       : "memory", "scc");
-  tb.k_sent += 1;
+  tb.k_sent = sent + 1;
 }
 
-// Fills the table behind what it still holds, given that step t of the unit at w is the next to
-// be taken, and sends for the first steps' tiles; the scales come in the same round trip, the
-// first time beside Q and the tree's keys if a unit begins.
+// What the table's lanes take next.
+struct Q8Next {
+  int n, pos;  // lanes to be filled; the lane's place among them
+  uint32_t entry, head;
+  int key, tokens;
+};
+
+// What follows the table's steps, given that step t of the unit at w is the next to be taken.
 template <bool kGang>
-__device__ __forceinline__ void q8_fill(Q8Table& tb, const Q8Args& a, const Q8Ws& ws, Q8Walk w, int t,
-                                        int hi, uint32_t ring, uint32_t offs) {
+__device__ __forceinline__ Q8Next q8_next_steps(Q8Table& tb, const Q8Args& a, const Q8Ws& ws, Q8Walk w,
+                                                int t, int hi) {
   const int lane = threadIdx.x & (kWave - 1);
-  const bool first = tb.known == 0;
   int skip = tb.known - tb.done;  // steps that it holds
   const int room = kWave - 2 * skip;
-  const int pos = (lane - 2 * tb.known) & (kWave - 1);  // the lane's place in what is filled
-  int n = 0;                                            // lanes filled
-  uint32_t entry = 0, head = 0;
-  int key = 0, tokens = 0;
-  while (n < room && t < hi) {  // uniform
+  Q8Next x = {};
+  x.pos = (lane - 2 * tb.known) & (kWave - 1);
+  while (x.n < room && t < hi) {  // uniform
     const int end = min(hi, w.u0 + w.q.tpu);
     const int p0 = w.u0 + w.head();
     t = max(t, min(end, p0));
@@ -688,26 +706,34 @@ __device__ __forceinline__ void q8_fill(Q8Table& tb, const Q8Args& a, const Q8Ws
       skip -= held;
       t += held;
     }
-    const int m = min((room - n) / 2, end - t);
-    if (pos >= n && pos < n + 2 * m) {
-      key = (t - p0) * kQ8StepKeys + (pos - n) * kTileKeys;
-      tokens = max(w.q.P - key, 0);
-      if (tokens == 0) key -= kTileKeys;
-      entry = uint32_t(w.q.r) * uint32_t(a.max_pages) + uint32_t(key >> a.page_shift);
-      head = uint32_t(w.unit / w.q.passes);
+    const int m = min((room - x.n) / 2, end - t);
+    if (x.pos >= x.n && x.pos < x.n + 2 * m) {
+      x.key = (t - p0) * kQ8StepKeys + (x.pos - x.n) * kTileKeys;
+      x.tokens = max(w.q.P - x.key, 0);
+      if (x.tokens == 0) x.key -= kTileKeys;
+      x.entry = uint32_t(w.q.r) * uint32_t(a.max_pages) + uint32_t(x.key >> a.page_shift);
+      x.head = uint32_t(w.unit / w.q.passes);
     }
-    n += 2 * m;
+    x.n += 2 * m;
     t += m;
     if (t >= end && t < hi) q8_next_unit(w, a, ws);
   }
-  tb.known += n / 2;
   tb.more = t < hi;
+  return x;
+}
+
+// Fills the table with them (page: the lane's) and sends for the first steps' tiles; the scales
+// come in the same round trip, the first time beside Q and the tree's keys if a unit begins.
+template <bool kGang>
+__device__ __forceinline__ void q8_fill(Q8Table& tb, const Q8Args& a, const Q8Next& x, uint32_t page,
+                                        uint32_t ring, uint32_t offs) {
+  const bool first = tb.known == 0;
+  tb.known += x.n / 2;
   float ks = 1.0f, vs = 1.0f;
-  if (pos < n) {
-    const uint32_t page = uint32_t(a.block_table[entry]);
-    tb.blk = ((page * uint32_t(a.hkv) + head) << (a.page_shift - 5)) +
-             (uint32_t(key & ((1 << a.page_shift) - 1)) >> 5);
-    tb.tokens = tokens;
+  if (x.pos < x.n) {
+    tb.blk = ((page * uint32_t(a.hkv) + x.head) << (a.page_shift - 5)) +
+             (uint32_t(x.key & ((1 << a.page_shift) - 1)) >> 5);
+    tb.tokens = x.tokens;
     ks = a.k_scale[tb.blk];
     vs = a.v_scale[tb.blk];
   }
@@ -721,10 +747,16 @@ __device__ __forceinline__ void q8_fill(Q8Table& tb, const Q8Args& a, const Q8Ws
     tb.c = ks;
     tb.lvs = vs;
     tb.raw = true;
-  } else if (pos < n) {
+  } else if (x.pos < x.n) {
     tb.c = a.scale2 * ks;
     tb.lvs = __builtin_amdgcn_logf(vs);
   }
+}
+template <bool kGang>
+__device__ __forceinline__ void q8_refill(Q8Table& tb, const Q8Args& a, const Q8Ws& ws, const Q8Walk& w,
+                                          int t, int hi, uint32_t ring, uint32_t offs) {
+  const Q8Next x = q8_next_steps<kGang>(tb, a, ws, w, t, hi);
+  q8_fill<kGang>(tb, a, x, x.pos < x.n ? uint32_t(a.block_table[x.entry]) : 0u, ring, offs);
 }
 
 // The scales' values, once they are there, become what the softmax takes.
@@ -961,10 +993,12 @@ __device__ __forceinline__ void q8_segment(const Q8Args& a, const Q8Ws& ws, cons
   wait_vm<0>();  // no load that the compiler knows of is in flight in the loop
 
   for (; t < hi; ++t) {
+    tb.done = __builtin_amdgcn_readfirstlane(tb.done);  // (uniform, which the compiler loses)
+    tb.known = __builtin_amdgcn_readfirstlane(tb.known);
     const int i = (2 * tb.done) & (kWave - 1);
     uint32_t tiles = ring;
     if (kGang) {
-      if (tb.more && tb.k_sent == tb.known) q8_fill<true>(tb, a, ws, w, t, range_hi, ring, offs);
+      if (tb.more && tb.k_sent == tb.known) q8_refill<true>(tb, a, ws, w, t, range_hi, ring, offs);
       // the wave's quarter of the step has landed (up to two steps are behind it), and the others'
       const int behind = tb.k_sent - tb.done - 1;
       if (behind >= 2) wait_vm<8>();
@@ -981,7 +1015,7 @@ __device__ __forceinline__ void q8_segment(const Q8Args& a, const Q8Ws& ws, cons
       }
     } else {
       // (the table is used up, and the ring empty)
-      if (tb.done == tb.known) q8_fill<false>(tb, a, ws, w, t, range_hi, ring, offs);
+      if (tb.done == tb.known) q8_refill<false>(tb, a, ws, w, t, range_hi, ring, offs);
       wait_vm<0>();
       asm volatile("" ::: "memory");  // the tiles' reads stay behind the wait
     }
@@ -1105,7 +1139,28 @@ __device__ __forceinline__ void q8_range(const Q8Args& a, const Q8Ws& ws, const 
   Q8Table tb = {};
   tb.k = st.k;
   tb.member = st.member;
-  q8_fill<kGang>(tb, a, ws, w, st.lo, st.hi, ring, offs);
+  // the first steps' page ids in one round trip with those that the check takes
+  const int lane = threadIdx.x & (kWave - 1);
+  const Q8Pages pages(a, ws, w.q.r, w.q.P);
+  int e[2] = {0, 0};
+  if (pages.n > 0) {
+    e[0] = pages.at(lane);
+    e[1] = pages.at(kWave + lane);
+  }
+  Q8Next x;
+  uint32_t page;
+#pragma unroll 1
+  for (bool checked = false;; checked = true) {
+    x = q8_next_steps<kGang>(tb, a, ws, w, st.lo, st.hi);
+    page = x.pos < x.n ? uint32_t(a.block_table[x.entry]) : 0u;
+    if (checked) break;
+    q8_check(w, a, pages, pages.n > 0 && (pages.bad_value(a, e[0]) || pages.bad_value(a, e[1])),
+             2 * kWave);
+    if (!w.bad) break;
+  }
+  q8_fill<kGang>(tb, a, x, page, ring, offs);
+  const Q8Cut cut = q8_cut(w, st);
+  if (lane == 0) ws.cuts[b] = cut;
   while (true) {
     const int lo = max(st.lo, w.u0), hi = min(st.hi, w.u0 + w.q.tpu);
     const bool whole = w.u0 >= st.lo && w.u0 + w.q.tpu <= st.hi;
@@ -1127,7 +1182,10 @@ q8_main_kernel(Q8Args a, Q8Ws ws) {
   const int b = __builtin_amdgcn_readfirstlane(int(blockIdx.x) * kQ8Waves + wid);
   Q8Walk w = {};
   const Q8Range st = q8_begin(a, ws, reinterpret_cast<uint32_t*>(smem), w);
-  if (st.lo >= st.hi) return;
+  if (st.lo >= st.hi) {
+    if ((threadIdx.x & (kWave - 1)) == 0) ws.cuts[b] = Q8Cut{};
+    return;
+  }
   const uint32_t base = __builtin_amdgcn_readfirstlane(
       uint32_t(reinterpret_cast<uintptr_t>((lds_void_t*)smem)));
   if (st.k == kQ8Waves) {
