@@ -235,6 +235,29 @@ def test_store_long_prompts(T):
         assert np.array_equal(dev[2 + i].cpu().numpy(), want[2 + i])
 
 
+@pytest.mark.parametrize("T", [256, 257, 600, 1025, 2050, 4097, 9000])
+def test_store_rows_per_wave(T):
+    """Every number of rows that a wave takes (eight heads: 1 at 256 rows, 32 from 4097 on), with
+    runs that begin and end at any row of its chunk."""
+    rng = np.random.default_rng(T)
+    hkv, ps = 8, 64
+    lens, starts = [], []
+    while sum(lens) < T:
+        n = int(rng.choice([1, 1, 2, 7, 31, 33, 64, 200]))
+        lens.append(min(n, T - sum(lens)))
+        starts.append(int(rng.integers(0, 70)))
+    slots, pages, _ = _slots_of(lens, starts, ps, rng)
+    k, v = _values(rng, T, hkv, 128), _values(rng, T, hkv, 128)
+    cache = _empty_cache(rng, pages, hkv, ps)
+    dev = [_dev(a) for a in cache]
+    _log(f"[store] rows per wave, T={T}")
+    _store(_dev(k), _dev(v), _dev(slots), kvq8.E5M2, dev, ps)
+    *want, _ = kvq8.store_kv(k, v, slots, kvq8.E5M2, *cache)
+    for i in range(2):
+        _same_bytes(dev[i].cpu().numpy(), want[i], kvq8.E5M2, f"tensor {i}")
+        assert np.array_equal(dev[2 + i].cpu().numpy(), want[2 + i])
+
+
 # ---- commit ---------------------------------------------------------------
 
 @pytest.mark.parametrize("fmt", FMTS)
@@ -656,6 +679,38 @@ def test_attention_without_lse_and_on_a_stream():
     for bufs, _ in runs:
         got = bufs[0].float().cpu().numpy()
         assert np.array_equal(got, ref, equal_nan=True)
+
+
+def test_two_captured_calls_share_a_workspace():
+    """Graphs of two batches with one workspace, replayed in turn: each replay is its eager call."""
+    import torch
+    import paper_2604_09603_amd as pkg
+    rng = np.random.default_rng(22)
+    batches = [_attn_case(rng, 32, 2, [1, 9, 3], [500, 40, 999], 64, kvq8.E4M3),
+               _attn_case(rng, 8, 8, [1] * 5, [10, 300, 0, 77, 1], 32, kvq8.E5M2)]
+    bufs = [_attn_buffers(c) for c in batches]
+    ws = max((b[2] for b in bufs), key=lambda w: w.numel())
+    args = [_attn_args(c, b[0], b[1], ws, b[3]) for c, b in zip(batches, bufs)]
+    _log("[attn q8] two graphs")
+
+    def fetch(b):
+        torch.cuda.synchronize()
+        return b[0].view(torch.int16).cpu().numpy(), b[1].view(torch.int32).cpu().numpy()
+
+    eager, graphs = [], []
+    for a, b in zip(args, bufs):
+        pkg.echo_tree_verify_attn_paged_q8(*a)
+        eager.append(fetch(b))
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            pkg.echo_tree_verify_attn_paged_q8(*a)
+    for i in (0, 1, 1, 0, 1, 0):
+        for b in bufs:
+            b[0].fill_(float("nan"))
+            b[1].fill_(float("nan"))
+        graphs[i].replay()
+        for x, y in zip(fetch(bufs[i]), eager[i]):
+            assert np.array_equal(x, y), i
 
 
 def test_offsets_past_32_bits():
