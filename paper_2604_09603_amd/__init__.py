@@ -51,6 +51,7 @@ EXPORTS = [
 GATE_SCRATCH_BYTES = 8 << 20
 
 _lib = None
+_raw_stream = _device = None  # the current stream's handle, and the current device: set by load()
 
 _P = ctypes.c_void_p
 _I32 = ctypes.c_int32
@@ -115,7 +116,7 @@ class EchoError(RuntimeError):
 
 def load(path: str = LIB_PATH) -> ctypes.CDLL:
     """Load libecho (once).  Raises if it has not been built."""
-    global _lib
+    global _lib, _raw_stream, _device
     if _lib is not None:
         return _lib
     if not os.path.exists(path):
@@ -123,7 +124,8 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
                         "`python -m paper_2604_09603_amd.build` (there is no CPU fallback)")
     # torch ships its own HIP runtime under the same soname; load it first so that the
     # library and torch's streams and allocations share one runtime instance
-    import torch  # noqa: F401
+    import torch
+    _raw_stream, _device = torch._C._cuda_getCurrentRawStream, torch.cuda.current_device
     lib = ctypes.CDLL(path)
     for name, (res, args) in _SIGS.items():
         fn = getattr(lib, name)
@@ -141,8 +143,7 @@ def _ptr(t):
 
 def _stream(stream):
     if stream is None:  # the current one; its handle alone is 2.4 us cheaper than its object
-        import torch
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+        return _raw_stream(_device())
     return stream.cuda_stream
 
 
@@ -427,13 +428,13 @@ def echo_store_kv_q8(k, v, slot_map, num_rows, hkv, head_dim, kv_format, k_pages
     """Quantise rows into an 8-bit paged KV cache at the slots of a slot map.  Device tensors;
     k and v are [num_rows, Hkv, 128] bf16 bits whose rows may be strided (parts of one
     projection's output), slot_map int64."""
-    for t in (k, v):
-        if t.stride(-1) != 1 or (hkv > 1 and t.stride(-2) != head_dim):
-            raise ValueError("the heads of a row of k and v must be contiguous")
+    ks, vs = k.stride(), v.stride()
+    if ks[-1] != 1 or vs[-1] != 1 or (hkv > 1 and (ks[-2] != head_dim or vs[-2] != head_dim)):
+        raise ValueError("the heads of a row of k and v must be contiguous")
     # (the stride of a dimension of size 1 says nothing)
-    strides = [t.stride(0) if t.shape[0] > 1 else hkv * head_dim for t in (k, v)]
     code = load().echo_store_kv_q8(
-        _ptr(k), _ptr(v), *strides, _ptr(slot_map), num_rows, hkv, head_dim,
+        _ptr(k), _ptr(v), ks[0] if k.shape[0] > 1 else hkv * head_dim,
+        vs[0] if v.shape[0] > 1 else hkv * head_dim, _ptr(slot_map), num_rows, hkv, head_dim,
         kv_format, _ptr(k_pages), _ptr(v_pages), _ptr(k_scale), _ptr(v_scale), k_pages.shape[0],
         page_size, _ptr(status), _stream(stream))
     if check:
