@@ -54,6 +54,10 @@ __global__ __launch_bounds__(kTableThreads) void build_tables_kernel(TablesArgs 
   int32_t* s_held = s_mem;            // R: pages held before
   int32_t* s_give = s_mem + R;        // R + 1: pages given back by the requests before, and by all
   int32_t* s_take = s_give + (R + 1); // R + 1: pages wanted by the requests before, and by all
+  int32_t* s_off = s_take + (R + 1);  // R + 1: row offsets (map)
+  const int before = *a.num_free;     // (in the round trip of the lengths, as the offsets)
+  if (map)
+    for (int r = tid; r <= R; r += kTableThreads) s_off[r] = a.row_offsets[r];
   if (tid == 0) s_last = 0;
   int bits = 0;
   int give_run = 0, take_run = 0;
@@ -86,7 +90,6 @@ __global__ __launch_bounds__(kTableThreads) void build_tables_kernel(TablesArgs 
     s_give[R] = give_run;
     s_take[R] = take_run;
   }
-  const int before = *a.num_free;
   const bool stack_ok = before >= 0 && before <= a.max_free && give_run <= a.max_free - before;
   if (!stack_ok) bits |= ECHO_DATA_BAD_OFFSETS;
   const int gives = stack_ok ? give_run : 0;
@@ -136,7 +139,7 @@ __global__ __launch_bounds__(kTableThreads) void build_tables_kernel(TablesArgs 
     };
     for (int i = tid; i < a.max_rows; i += kTableThreads) {
       bool missing;
-      a.slot_map[i] = slot_of(a, page_shift, i, a.row_offsets, held, missing);
+      a.slot_map[i] = slot_of(a, page_shift, i, s_off, held, missing);
       if (missing) bits |= ECHO_DATA_NO_PAGES;
     }
   }
@@ -169,8 +172,13 @@ int32_t launch_build_block_tables(const TablesArgs& a, hipStream_t stream) {
   while ((1 << page_shift) < a.page_size) ++page_shift;
   const bool map = a.slot_map != nullptr && a.max_rows > 0;
   const bool fused = map && a.max_rows <= kFusedRows;
-  hipLaunchKernelGGL(build_tables_kernel, dim3(1), dim3(kTableThreads),
-                     (3 * size_t(a.R) + 2) * sizeof(int32_t), stream, a, page_shift, fused);
+  const size_t lds = (3 * size_t(a.R) + 2 + (fused ? size_t(a.R) + 1 : 0)) * sizeof(int32_t);
+  if (lds > 60 * 1024 && hipFuncSetAttribute(reinterpret_cast<const void*>(build_tables_kernel),
+                                             hipFuncAttributeMaxDynamicSharedMemorySize,
+                                             int(lds)) != hipSuccess)
+    return ECHO_ERR_HIP;
+  hipLaunchKernelGGL(build_tables_kernel, dim3(1), dim3(kTableThreads), lds, stream, a, page_shift,
+                     fused);
   if (map && !fused)
     hipLaunchKernelGGL(slot_map_kernel, dim3(unsigned((a.max_rows + kMapThreads - 1) / kMapThreads)),
                        dim3(kMapThreads), (size_t(a.R) + 1) * sizeof(int32_t), stream, a,

@@ -365,6 +365,21 @@ def test_tables_match_oracle(R, most, ps, free, rows, pad, alias):
     _same_tables(got, want)
 
 
+@pytest.mark.parametrize("R,most,ps,free,rows,pad", [
+    (128, 9, 64, 300, 2000, 48), (128, 9, 64, 300, 2000, 49), (4095, 2, 16, 3000, 2000, 11),
+    (4095, 2, 16, 3000, 0, 1)])
+def test_tables_and_slots_in_one_launch_or_two(R, most, ps, free, rows, pad):
+    """The longest slot map that the tables' launch writes and the shortest of a launch of its own;
+    the largest batch in one launch."""
+    rng = np.random.default_rng(R + rows + pad)
+    c = _tables_case(rng, R, most, ps, free, rows)
+    _log(f"[tables] R={R} rows={rows}+{pad}")
+    got = _run_tables(c, R, ps, rows + pad, False)
+    want = kvq8.build_block_tables(c["want"], ps, c["bt"], c["held"], c["stack"], c["free"], c["ro"],
+                                   c["start"], rows + pad)
+    _same_tables(got, want)
+
+
 @pytest.mark.parametrize("rows", [20, 5000])
 def test_tables_bad_requests_keep_what_they_have(rows):
     rng = np.random.default_rng(rows)
