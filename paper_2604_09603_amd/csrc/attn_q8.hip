@@ -38,8 +38,6 @@
 // rounding to bfloat16 is as large, so the residuals of the weights are not
 // multiplied.  Partial sums are stored as fp16 with a power-of-two scale per row
 // (at most 2^-11 of the row's largest).
-#include <type_traits>
-
 #include "attn_core.h"
 #include "kvq8_device.h"
 
@@ -66,9 +64,9 @@ constexpr int kQ8Enter = 1;
 // first.  With these shares both end their ranges within a few us of each other.
 constexpr int kQ8Older = 18;
 constexpr int kOwnPages = 512;     // block tables up to this wide are checked by the waves
-constexpr float kQ8MaxSteps = 1073741824.0f;  // 2^30: steps of a class
+constexpr float kQ8MaxSteps = 1073741824.0f;  // 2^30: steps of a call
+
 typedef int intx2 __attribute__((ext_vector_type(2)));
-typedef int intx8 __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) intx2 lds_intx2_t;
 typedef uint32_t uint4v __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) const uint4v lds_uint4_t;
@@ -79,7 +77,8 @@ typedef float floatx16 __attribute__((ext_vector_type(16)));
 __device__ __forceinline__ lds_char_t* lds_at(uint32_t x) { return (lds_char_t*)(uintptr_t(x)); }
 
 // A gang is the k waves (1, 2 or 4, of one workgroup) that take the same steps of a unit,
-// each with 32 of its rows: one copies the tiles from HBM, the others at about the same
+// each with 32 of its rows.  Four share their tiles in LDS (each copies a quarter of them,
+// with a barrier per step); of two one copies them from HBM, the other at about the same
 // time from the caches.  A head's rows are dealt to gangs of four, and what is left to one of
 // one, two or (three) four waves: without the remainder's own gang, waves that have no
 // rows would be idle through its steps.  The requests with a part for gangs of k
@@ -577,7 +576,7 @@ __device__ __forceinline__ Q8Cut q8_cut(const Q8Walk& w, const Q8Range& x) {
 // i & 63: the block, the tokens it holds (32 or more: all), and what the softmax takes
 // of its scales.  A request's last step may have one tile: its second entry is that
 // block again, without tokens.  One vector of loads instead of scalar ones for every
-// tile; the ring runs empty once in 32 steps for it.  Steps [.., known) are in the
+// tile; once in 32 steps the ring runs empty for it (a gang of four's does not).  Steps [.., known) are in the
 // table; K of those below k_sent and V of those below v_sent have been copied, and
 // those below `done` multiplied.
 struct Q8Table {

@@ -9,8 +9,9 @@
 //
 // Both are bound by latency: the 16 bytes a request and the 4 bytes a page of the first
 // fit in the caches, and the second writes 8 bytes a row.  128 requests that take a token
-// each: 6.8 us, most of it three dependent round trips to memory (lengths, stack, tables)
-// and their barriers; 256 requests with prompts of up to 2048 rows: 7.6 and 4.0 us.
+// each: 5.8 us, most of it the launch and three dependent round trips to memory (lengths,
+// stack, tables) with their barriers; 256 requests with prompts of up to 2048 rows: 7.4 and
+// 4.0 us.
 #include "echo_device.h"
 #include "echo_internal.h"
 
@@ -20,8 +21,8 @@ namespace {
 constexpr int kTableThreads = 1024;
 constexpr int kMapThreads = 256;
 // Slot maps up to this long need no second launch.  With 128 requests, here | in a launch of
-// its own: 512 rows 6.6 | 7.7 us, 2048 rows 8.3 | 7.8 (and a launch less for the host), 4096
-// rows 11.4 | 7.8, 32768 rows 60 | 8.0.
+// its own: 512 rows 6.2 | 7.7 us, 2048 rows 7.5 | 7.8 (and a launch less for the host), 4096
+// rows 9.8 | 7.9, 32768 rows 42 | 7.9.
 constexpr int kFusedRows = 2 * kTableThreads;
 
 // The slot of row i, or -1: rows past the last request's, and those whose page their
