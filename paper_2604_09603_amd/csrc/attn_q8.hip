@@ -20,7 +20,7 @@
 //   q8_combine  merges the partial sums of units that several waves share.
 //
 // What bounds it.  Few rows per head: HBM.  64 requests decoding over 1024-8192 tokens (32
-// query and 8 KV heads, 604 MB) take 90 us in the main kernel, 6.7 TB/s, and 5 us in the
+// query and 8 KV heads, 604 MB) take 91 us in the main kernel, 6.7 TB/s, and 5 us in the
 // merge; the 10 us until the first tiles are there (lengths, page ids, scales and tiles are
 // dependent round trips) are most of the rest.  Many rows: the vector instructions.  A step
 // of 64 keys and 32 rows takes 32 matrix products (1044 cycles) and about 400 other vector
@@ -28,7 +28,7 @@
 // sums and roundings of the weights), which share a SIMD's issue; with trees of 13 slots on
 // average (16 rows each) over 16384-32768 tokens, 79 us of products, the main kernel takes
 // 210 us, 64% of it issuing vector instructions.  128 trees of 3 slots on average (617 MB) are
-// between the two: 132 us and 9 in the merge.  Units of 32 rows because a 32x32x16 product
+// between the two: 132 us and 8 in the merge.  Units of 32 rows because a 32x32x16 product
 // leaves room for five vector instructions, where 16x16x32 leaves two for the same work;
 // two waves per SIMD, so that one's softmax runs beside the other's products.
 //
@@ -95,13 +95,13 @@ struct Q8Part {
 };
 
 // Where a wave's range begins inside a unit, and is the first that does: the unit's partial
-// sums are those of `parts` gangs from gang - 1 on (0: there is nothing to merge).  Gangs
-// go round the class's places wg0 .. wg0 + nwg - 1, so that few of them spread over the
-// CUs.
+// sums are those of `parts` gangs from the one before on (0: there is nothing to merge).
+// Gangs go round the class's places wg0 .. wg0 + nwg - 1, so that few of them spread over
+// the CUs: the one before has place wg0 + at and is that workgroup's gang number `slot`.
 struct Q8Cut {
-  int32_t parts, gang, k, member;
-  int32_t wg0, nwg, q0, nslots;
-  int32_t head, row0, pad[2];
+  int32_t parts, at, slot, k;
+  int32_t wg0, nwg, member, q0;
+  int32_t nslots, head, row0, pad;
 };
 static_assert(sizeof(Q8Cut) == 48, "12 words");
 
@@ -110,9 +110,8 @@ static_assert(sizeof(Q8Cut) == 48, "12 words");
 __device__ __forceinline__ int q8_place(int b, int wgs) {
   return b < wgs / 2 ? 2 * b : 2 * (b - wgs / 2) + 1;
 }
-__device__ __forceinline__ int q8_wave_of(int g, int k, int wg0, int nwg, int wgs) {
-  const int place = wg0 + g % nwg;
-  return ((place & 1) * (wgs / 2) + (place >> 1)) * kQ8Waves + g / nwg * k;
+__device__ __forceinline__ int q8_first_wave(int place, int wgs) {
+  return ((place & 1) * (wgs / 2) + (place >> 1)) * kQ8Waves;
 }
 
 struct Q8Ws {
@@ -560,7 +559,9 @@ __device__ __forceinline__ Q8Cut q8_cut(const Q8Walk& w, const Q8Range& x) {
   Q8Cut c = {};
   if (!w.bad && w.u0 < x.lo && x.ranges.first(x.gang - 1) <= w.u0)
     c.parts = x.ranges.range_of(w.u0 + w.q.tpu - 1) - x.gang + 2;
-  c.gang = x.gang;
+  const int before = max(x.gang - 1, 0);
+  c.slot = int(unsigned(before) / unsigned(x.nwg));
+  c.at = before - c.slot * x.nwg;
   c.k = x.k;
   c.member = x.member;
   c.wg0 = x.wg0;
@@ -1210,8 +1211,8 @@ __device__ __forceinline__ Q8Cut load_cut(const Q8Cut* cuts, int b) {
   return __builtin_bit_cast(Q8Cut, w);
 }
 
-// (4 us for 16 partial sums, 9-10 us for 2900 of them, 25 MB: latency and the launch, then their
-// bytes.)  Workgroup (b, y): rows 16 y .. 16 y + 15 that wave b has of the unit that is cut first
+// (3.7 us for a few partial sums, 8 us for 2900 of them, 25 MB: latency and the launch, then their
+// bytes; four at a time took 0.5 us more.)  Workgroup (b, y): rows 16 y .. 16 y + 15 that wave b has of the unit that is cut first
 // at its range (if any); a thread has 8 dims of a row.  Parts in the order of the gangs.
 __global__ __launch_bounds__(256) void q8_combine_kernel(Q8Args a, Q8Ws ws) {
   const int b = blockIdx.x;
@@ -1221,26 +1222,31 @@ __global__ __launch_bounds__(256) void q8_combine_kernel(Q8Args a, Q8Ws ws) {
   const int rho = blockIdx.y * 16 + threadIdx.x / 16;
   if (rho >= rows) return;
   const int piece = threadIdx.x & 15;  // 8 halves of the partial
-  const int np = st.parts;
-  const auto prow = [&](int i) {
-    const int wave = q8_wave_of(st.gang - 1 + i, st.k, st.wg0, st.nwg, a.wgs) + st.member;
-    return (size_t(wave) * 2 + (i == 0 ? 1 : 0)) * kQ8Rows + size_t(rho);
-  };
   float M = -__builtin_inff(), L = 0.0f, Lq = 0.0f;
   float acc[8] = {};
-  for (int i0 = 0; i0 < np; i0 += kQ8Parts) {  // (a batch's loads in one round trip)
+  int at = st.at, slot = st.slot, half = 1;  // (the first part is the end of its wave's range)
+  for (int i0 = 0; i0 < st.parts; i0 += kQ8Parts) {  // (a batch's loads in one round trip)
     floatx4 ml[kQ8Parts];
     halfx8 h[kQ8Parts];
 #pragma unroll
     for (int j = 0; j < kQ8Parts; ++j) {
-      const size_t at = prow(min(i0 + j, np - 1));
-      ml[j] = *reinterpret_cast<const floatx4*>(ws.part_ml + at * 4);
-      h[j] = *reinterpret_cast<const halfx8*>(ws.part_o + at * kD + piece * 8);
+      ml[j] = floatx4{-__builtin_inff(), 0.0f, 0.0f, 0.0f};
+      h[j] = halfx8{};
+      if (i0 + j < st.parts) {  // uniform
+        const int wave = q8_first_wave(st.wg0 + at, a.wgs) + slot * st.k + st.member;
+        const size_t row = (size_t(wave) * 2 + half) * kQ8Rows + size_t(rho);
+        ml[j] = *reinterpret_cast<const floatx4*>(ws.part_ml + row * 4);
+        h[j] = *reinterpret_cast<const halfx8*>(ws.part_o + row * kD + piece * 8);
+      }
+      half = 0;
+      at += 1;
+      slot += at == st.nwg ? 1 : 0;
+      at = at == st.nwg ? 0 : at;
     }
     float m = M;
 #pragma unroll
     for (int j = 0; j < kQ8Parts; ++j)
-      if (i0 + j < np) m = fmaxf(m, ml[j][0]);
+      m = fmaxf(m, ml[j][0]);
     if (m == -__builtin_inff()) continue;
     const float alpha = __builtin_amdgcn_exp2f(M - m);  // 0 from -inf
     M = m;
@@ -1250,7 +1256,7 @@ __global__ __launch_bounds__(256) void q8_combine_kernel(Q8Args a, Q8Ws ws) {
     for (int k = 0; k < 8; ++k) acc[k] *= alpha;
 #pragma unroll
     for (int j = 0; j < kQ8Parts; ++j) {
-      const float wgt = i0 + j < np ? __builtin_amdgcn_exp2f(ml[j][0] - m) : 0.0f;
+      const float wgt = __builtin_amdgcn_exp2f(ml[j][0] - m);  // 0 from -inf
       L = __builtin_fmaf(wgt, ml[j][1], L);
       Lq = __builtin_fmaf(wgt, ml[j][2], Lq);
       const float wo = wgt * __builtin_amdgcn_ldexpf(1.0f, int(ml[j][3]));
