@@ -402,7 +402,7 @@ struct Q8Range {
 // a round trip, a scan and a search, where a launch for it took 10-15 us.  s: 3.1 KB and 8
 // bytes a request, of LDS.
 __device__ __forceinline__ Q8Range q8_begin(const Q8Args& a, const Q8Ws& ws, uint32_t* s, Q8Walk& w) {
-  constexpr int kThreads = kQ8Waves * kWave, kBatch = 4;
+  constexpr int kThreads = kQ8Waves * kWave, kBatch = 2;
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wid = wave_id();
   uint32_t* s_tot = s + kQ8Classes * kThreads;  // [waves][classes + 1]
   int* s_q = reinterpret_cast<int*>(s_tot + kQ8Waves * (kQ8Classes + 1));  // [R + 1] offsets
@@ -481,7 +481,7 @@ __device__ __forceinline__ Q8Range q8_begin(const Q8Args& a, const Q8Ws& ws, uin
   const int wgs = a.wgs, g = q8_place(blockIdx.x, wgs);
   const float cost[kQ8Classes] = {kQ8Cost1 * float(tot[0]), kQ8Cost2 * float(tot[1]),
                                   kQ8Cost4 * float(tot[2])};
-  const float per = float(wgs) / (cost[0] + cost[1] + cost[2]);
+  const float per = float(wgs) * __builtin_amdgcn_rcpf(cost[0] + cost[1] + cost[2]);
   int left = wgs, need = 0, wg0 = 0, nwg = 0, cls = 0;
 #pragma unroll
   for (int c = 0; c < kQ8Classes; ++c) need += tot[c] > 0 ? 1 : 0;
