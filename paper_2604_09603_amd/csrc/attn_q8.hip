@@ -40,31 +40,19 @@
 // (at most 2^-11 of the row's largest).
 #include "attn_core.h"
 #include "kvq8_device.h"
+#include "q8_ranges.h"
 
 namespace echo {
 namespace {
 
-constexpr int kQ8Rows = 32;        // rows per unit
-constexpr int kQ8Waves = 4;        // waves per workgroup
+static_assert(kQ8TreeKeys == kTileKeys, "a step of the tree is a tile");
 constexpr int kQ8Wgs = 2;          // workgroups per CU: two waves per SIMD
-constexpr int kQ8StepKeys = 64;    // keys per step of the main loop: two tiles
 constexpr int kQ8Slot = 2 * kBlockBytes;          // one tensor's tiles of a step
 constexpr int kQ8Scratch = 16 * kD * 2;           // 16 rows of bfloat16 V (tree tiles)
 constexpr int kQ8WaveLds = 2 * kQ8Slot + kQ8Scratch;  // K, V, scratch
 static_assert(kQ8Wgs * kQ8Waves * kQ8WaveLds <= 160 * 1024, "gfx950 LDS per CU");
 constexpr int kGangSlots = 4;      // slots of a gang of four waves, which share their tiles
-// What a step costs a workgroup that has 4, 2 or 1 gangs at work, relative to each other: between
-// the ratios of their products (1, 2, 4) and those of their copies (4 : 2 : 1 gangs, so 1, 1, 1).
-// 235B-shaped trees of 1 to 12 slots: 1, 2, 4 took 8 us more, 1, 1.5, 2.5 took 2 us more.
-constexpr float kQ8Cost1 = 1.4f, kQ8Cost2 = 2.2f, kQ8Cost4 = 3.6f;
-// Entering a unit (its rows of Q, the way out of the last one) takes as long as this many steps.
-constexpr int kQ8Enter = 1;
-// Of 32 steps that two gangs on the same CU share, the older workgroup's gets this many (17 in a
-// class of gangs of four, which are bound by their products): its loads and products go
-// first.  With these shares both end their ranges within a few us of each other.
-constexpr int kQ8Older = 18;
 constexpr int kOwnPages = 512;     // block tables up to this wide are checked by the waves
-constexpr float kQ8MaxSteps = 1073741824.0f;  // 2^30: steps of a call
 
 typedef int intx2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) intx2 lds_intx2_t;
@@ -83,7 +71,6 @@ __device__ __forceinline__ lds_char_t* lds_at(uint32_t x) { return (lds_char_t*)
 // one, two or (three) four waves: without the remainder's own gang, waves that have no
 // rows would be idle through its steps.  The requests with a part for gangs of k
 // waves form a class, whose steps are cut into equal ranges, one per gang.
-constexpr int kQ8Classes = 3;  // k = 1 << class
 
 // A request's part in a class: Hkv * passes units (unit = head * passes + pass) of tpu steps
 // each, from step tile0 of the class on; gang member m has rows row0 + 32 (k pass + m) .. of
@@ -104,15 +91,6 @@ struct Q8Cut {
   int32_t nslots, head, row0, pad;
 };
 static_assert(sizeof(Q8Cut) == 48, "12 words");
-
-// Workgroups b and b + half the grid share a CU (no result depends on it): places 2 b and
-// 2 b + 1, so that a class has as many of the older as of the younger.
-__device__ __forceinline__ int q8_place(int b, int wgs) {
-  return b < wgs / 2 ? 2 * b : 2 * (b - wgs / 2) + 1;
-}
-__device__ __forceinline__ int q8_first_wave(int place, int wgs) {
-  return ((place & 1) * (wgs / 2) + (place >> 1)) * kQ8Waves;
-}
 
 struct Q8Ws {
   Q8Cut* cuts;       // [waves]
@@ -184,23 +162,6 @@ __global__ __launch_bounds__(kPageChunk) void q8_pages_kernel(Q8Args a, int32_t*
   }
   bad = __syncthreads_or(bad);
   if (threadIdx.x == 0) bad_flags[size_t(r) * gridDim.x + c] = bad;
-}
-
-// -------------------------------------------------------------- ranges ----
-// How often class c goes through the keys of a head with t tiles of 32 rows.
-__device__ __forceinline__ int q8_passes(int t, int c) {
-  const int rest = t & 3;
-  return c == 2 ? (t >> 2) + (rest == 3 ? 1 : 0) : rest == c + 1 ? 1 : 0;
-}
-
-__device__ __forceinline__ int q8_row_tiles(int nslots, int G) {
-  return int((unsigned(nslots) * unsigned(G) + kQ8Rows - 1) / kQ8Rows);
-}
-
-// Steps of a unit: those of entering it (nothing is done in them), the tree's, the prefix's.
-__device__ __forceinline__ int q8_unit_steps(int nslots, int P) {
-  return kQ8Enter + (nslots + kTileKeys - 1) / kTileKeys +
-         int((unsigned(P) + kQ8StepKeys - 1) / kQ8StepKeys);
 }
 
 // ---------------------------------------------------------------- main ----
@@ -368,35 +329,7 @@ __device__ __forceinline__ void q8_next_unit(Q8Walk& w, const Q8Args& a, const Q
   }
 }
 
-// T > 0 steps in ranges, of which two make a pair (one of its own if T = 1): pairs of equal
-// size but for one step, and the first of two has older / 32 of the pair's steps.
-// No range before the last is empty.
-struct Q8Cutter {
-  int n, each, more, older;
-  __device__ Q8Cutter(int T, int gangs, int older_) : n(max(min(gangs, T) / 2, 1)), older(older_) {
-    each = int(unsigned(T) / unsigned(n));
-    more = T - each * n;
-  }
-  __device__ __forceinline__ int pair_at(int p) const { return p * each + min(p, more); }
-  __device__ __forceinline__ int first(int g) const {
-    const int p = g >> 1, lo = pair_at(p);
-    if ((g & 1) == 0) return lo;
-    const int len = each + (p < more ? 1 : 0);
-    return lo + min((len * older + 16) / 32, max(len - 1, 1));
-  }
-  __device__ __forceinline__ int range_of(int t) const {
-    const int longer = more * (each + 1);
-    const int p = t < longer ? int(unsigned(t) / unsigned(each + 1))
-                             : more + int(unsigned(t - longer) / unsigned(each));
-    return 2 * p + (t >= first(2 * p + 1) ? 1 : 0);
-  }
-};
-
-struct Q8Range {
-  Q8Cutter ranges;  // of the class
-  int lo, hi, k, member, gang, wg0, nwg;
-};
-
+// -------------------------------------------------------------- ranges ----
 // The wave's range and where it starts (its request's pages are not checked).  Every workgroup
 // counts the steps of all requests (thread t those of requests K t .. K t + K - 1): that is
 // a round trip, a scan and a search, where a launch for it took 10-15 us.  s: 3.1 KB and 8
@@ -408,8 +341,7 @@ __device__ __forceinline__ Q8Range q8_begin(const Q8Args& a, const Q8Ws& ws, uin
   int* s_q = reinterpret_cast<int*>(s_tot + kQ8Waves * (kQ8Classes + 1));  // [R + 1] offsets
   int* s_P = s_q + a.R + 1;                                                // [R] lengths
   const int K = (a.R + kThreads - 1) / kThreads;
-  uint32_t T[kQ8Classes] = {0u, 0u, 0u};
-  float all = 0.0f;  // (offsets that overlap may ask for any number of steps)
+  Q8Steps T;
   int bits = 0;
 #pragma unroll 1
   for (int i = 0; i < K; i += kBatch) {
@@ -437,16 +369,11 @@ __device__ __forceinline__ Q8Range q8_begin(const Q8Args& a, const Q8Ws& ws, uin
           if (pages.bad(a, e)) bits = ECHO_DATA_BAD_OFFSETS;
       }
       if (x.tiles <= 0) continue;
-      const uint32_t pass = uint32_t(a.hkv) * uint32_t(x.tpu);
-#pragma unroll
-      for (int c = 0; c < kQ8Classes; ++c) {
-        const int n = q8_passes(x.tiles, c);
-        T[c] += pass * uint32_t(n);
-        all += float(a.hkv) * float(x.tpu) * float(n);
-      }
+      T.add(a.hkv, x.tiles, x.tpu);
     }
   }
   // (a sum that could matter is rare)
+  float all = T.all;
   if (__ballot(all > kQ8MaxSteps / kThreads) != 0ull) {
 #pragma unroll
     for (int d = 1; d < kWave; d *= 2) all += __shfl_xor(all, d);
@@ -455,8 +382,8 @@ __device__ __forceinline__ Q8Range q8_begin(const Q8Args& a, const Q8Ws& ws, uin
   }
 #pragma unroll
   for (int c = 0; c < kQ8Classes; ++c) {
-    const uint32_t inc = uint32_t(wave_inclusive_sum(int(T[c])));
-    s[c * kThreads + tid] = inc - T[c];
+    const uint32_t inc = uint32_t(wave_inclusive_sum(int(T.of[c])));
+    s[c * kThreads + tid] = inc - T.of[c];
     if (lane == kWave - 1) s_tot[wid * (kQ8Classes + 1) + c] = inc;
   }
   if (lane == 0) s_tot[wid * (kQ8Classes + 1) + kQ8Classes] = __float_as_uint(all);
@@ -470,51 +397,25 @@ __device__ __forceinline__ Q8Range q8_begin(const Q8Args& a, const Q8Ws& ws, uin
       tot[c] += __builtin_amdgcn_readfirstlane(int(s_tot[v * (kQ8Classes + 1) + c]));
     all += __uint_as_float(s_tot[v * (kQ8Classes + 1) + kQ8Classes]);
   }
-  // (then all of it fits 31 bits: four waves that pass have less than 2^30 between them, and the
-  // sum's own rounding is far smaller)
-  if (!(__uint_as_float(uint32_t(__builtin_amdgcn_readfirstlane(int(__float_as_uint(all))))) <= kQ8MaxSteps)) {
-    tot[0] = tot[1] = tot[2] = 0;
+  // (what passes fits 31 bits: four waves that are not summed have less than 2^30 between them, and
+  // the sum's own rounding is far smaller)
+  if (q8_refuses(__uint_as_float(uint32_t(__builtin_amdgcn_readfirstlane(int(__float_as_uint(all))))), tot))
     bits = ECHO_DATA_BAD_OFFSETS;
-  }
   wave_status_or(a.status, bits);
-  // the workgroups of the classes, in pairs: by cost, at least one where there is work
-  const int wgs = a.wgs, g = q8_place(blockIdx.x, wgs);
-  const float cost[kQ8Classes] = {kQ8Cost1 * float(tot[0]), kQ8Cost2 * float(tot[1]),
-                                  kQ8Cost4 * float(tot[2])};
-  const float per = float(wgs) * __builtin_amdgcn_rcpf(cost[0] + cost[1] + cost[2]);
-  int left = wgs, need = 0, wg0 = 0, nwg = 0, cls = 0;
-#pragma unroll
-  for (int c = 0; c < kQ8Classes; ++c) need += tot[c] > 0 ? 1 : 0;
-#pragma unroll
-  for (int c = 0; c < kQ8Classes; ++c) {
-    int n = 0;
-    if (tot[c] > 0) {
-      need -= 1;
-      n = need == 0 ? left : min(max(2 * int(0.5f * per * cost[c] + 0.5f), 2), left - 2 * need);
-    }
-    if (g >= wgs - left && g < wgs - left + n) {
-      cls = c;
-      wg0 = wgs - left;
-      nwg = n;
-    }
-    left -= n;
-  }
-  cls = __builtin_amdgcn_readfirstlane(cls);
-  wg0 = __builtin_amdgcn_readfirstlane(wg0);
-  nwg = __builtin_amdgcn_readfirstlane(nwg);
+  const int g = q8_place(blockIdx.x, a.wgs);
+  const float per =
+      float(a.wgs) * __builtin_amdgcn_rcpf(q8_cost(tot, 0) + q8_cost(tot, 1) + q8_cost(tot, 2));
+  Q8Share share = q8_share(tot, a.wgs, per, g);
+  share.cls = __builtin_amdgcn_readfirstlane(share.cls);
+  share.wg0 = __builtin_amdgcn_readfirstlane(share.wg0);
+  share.nwg = __builtin_amdgcn_readfirstlane(share.nwg);
+  const int cls = share.cls;
   // the steps that each wave's threads counted, of the class
-  int part[kQ8Waves], all_steps = 0;
+  int part[kQ8Waves];
 #pragma unroll
-  for (int v = 0; v < kQ8Waves; ++v) {
+  for (int v = 0; v < kQ8Waves; ++v)
     part[v] = __builtin_amdgcn_readfirstlane(int(s_tot[v * (kQ8Classes + 1) + cls]));
-    all_steps += part[v];
-  }
-  Q8Range x = {Q8Cutter(max(all_steps, 1), nwg * (kQ8Waves >> cls), kQ8Older - (cls == 2 ? 1 : 0)),
-               0, 0, 1 << cls, wid & ((1 << cls) - 1), g - wg0 + (wid >> cls) * nwg, wg0, nwg};
-  if (all_steps > 0 && x.gang < 2 * x.ranges.n) {
-    x.lo = x.ranges.first(x.gang);
-    x.hi = x.ranges.first(x.gang + 1);
-  }
+  const Q8Range x = q8_range_at(share, cls == 0 ? tot[0] : cls == 1 ? tot[1] : tot[2], g, wid);
   if (x.lo < x.hi) {
     w.cls = cls;
     // the last thread whose requests' steps start at lo or before: of four in each lane
