@@ -420,6 +420,7 @@ int32_t echo_commit_kv(const int32_t* q_offsets, const int32_t* accept_len,
  *         values stay the same unless they become subnormal.
  * The tokens behind the appended ones are left as they are.  Readers take any
  * positive finite scale from 2^-60 to 2^60, not only powers of two.
+ * Limits of all calls: num_pages * page_size < 2^31, at most 2^20 KV heads.
  */
 
 /*
@@ -439,12 +440,12 @@ int32_t echo_commit_kv(const int32_t* q_offsets, const int32_t* accept_len,
  *   lse      [max_rows][Hq]       float (nullable), natural log; -inf with out = 0
  *                                 for a row that sees no key
  * All other arguments, the skipped requests (ECHO_DATA_BAD_OFFSETS) and the
- * limits are those of echo_tree_verify_attn_paged; further limits: fewer than
- * 2^32 blocks (num_pages * Hkv * page_size / 32), R * max_pages_per_request <
- * 2^31, and fewer than 2^30 steps of 64 keys over all requests, KV heads and
- * groups of 128 rows of a head (offsets that ask for more: nothing is computed,
- * ECHO_DATA_BAD_OFFSETS).  k_scale and v_scale are 4-byte aligned, q, k_new,
- * v_new, out and the pages 16-byte aligned.  Deterministic.
+ * limits are those of echo_tree_verify_attn_paged; further limits: at most 2^19
+ * KV heads, fewer than 2^32 blocks (num_pages * Hkv * page_size / 32),
+ * R * max_pages_per_request < 2^31, and fewer than 2^30 steps of 64 keys over all
+ * requests, KV heads and groups of 128 rows of a head (offsets that ask for more:
+ * nothing is computed, ECHO_DATA_BAD_OFFSETS).  k_scale and v_scale are 4-byte
+ * aligned, q, k_new, v_new, out and the pages 16-byte aligned.  Deterministic.
  * The workspace: echo_tree_verify_attn_paged_q8_workspace_size.
  */
 int32_t echo_tree_verify_attn_paged_q8(

@@ -551,7 +551,8 @@ int32_t echo_tree_verify_attn_paged_q8(
                                    const_cast<float*>(v_scale), num_pages, page_size, num_kv_heads,
                                    head_dim, &a.cache);
   if (rc != ECHO_OK) return rc;
-  if (R > ECHO_MAX_REQUESTS) return ECHO_ERR_UNSUPPORTED;
+  // (32 rows of the new values, of 256 bytes a head, are addressed with 32-bit offsets)
+  if (R > ECHO_MAX_REQUESTS || num_kv_heads > (1 << 19)) return ECHO_ERR_UNSUPPORTED;
   if (int64_t(max_pages_per_request) * page_size >= (int64_t(1) << 31)) return ECHO_ERR_UNSUPPORTED;
   if (int64_t(max_rows) * num_q_heads >= (int64_t(1) << 26)) return ECHO_ERR_UNSUPPORTED;
   // (32-bit numbers of the cache's blocks and of the tables' entries)
