@@ -429,8 +429,8 @@ int32_t echo_commit_kv(const int32_t* q_offsets, const int32_t* accept_len,
  * With one slot per request it is plain decoding.  Scores, softmax and sums
  * are fp32; the cached bytes enter the products exactly, their scales in fp32;
  * each probability is rounded to bf16 for the product with V (2^-8) and the
- * output divided by the sum of the weights used; the merge of rows that are
- * split between waves rounds partial sums to fp16 (2^-11 of the row's largest).
+ * output divided by the sum of the weights used; rows that are split between
+ * waves are merged from fp32 sums.
  * Cached values that are NaN or infinite, and such inputs, give unspecified
  * outputs for the rows of their request; bytes past a request's prefix are not
  * used, whatever they hold.

@@ -20,7 +20,7 @@
 //   q8_combine  merges the partial sums of units that several waves share.
 //
 // What bounds it.  Few rows per head: HBM.  64 requests decoding over 1024-8192 tokens (32
-// query and 8 KV heads, 604 MB) take 91 us in the main kernel, 6.7 TB/s, and 5 us in the
+// query and 8 KV heads, 604 MB) take 91 us in the main kernel, 6.7 TB/s, and 6 us in the
 // merge; the 10 us until the first tiles are there (lengths, page ids, scales and tiles are
 // dependent round trips) are most of the rest.  Many rows: the vector instructions.  A step
 // of 64 keys and 32 rows takes 32 matrix products (1044 cycles) and about 400 other vector
@@ -28,7 +28,7 @@
 // sums and roundings of the weights), which share a SIMD's issue; with trees of 13 slots on
 // average (16 rows each) over 16384-32768 tokens, 79 us of products, the main kernel takes
 // 210 us, 64% of it issuing vector instructions.  128 trees of 3 slots on average (617 MB) are
-// between the two: 132 us and 8 in the merge.  Units of 32 rows because a 32x32x16 product
+// between the two: 140 us and 11 in the merge.  Units of 32 rows because a 32x32x16 product
 // leaves room for five vector instructions, where 16x16x32 leaves two for the same work;
 // two waves per SIMD, so that one's softmax runs beside the other's products.
 //
@@ -36,8 +36,7 @@
 // the product with V (at most 2^-8 each) and the output is divided by the sum of the
 // weights used, so that it stays a convex combination of V rows; the output's own
 // rounding to bfloat16 is as large, so the residuals of the weights are not
-// multiplied.  Partial sums are stored as fp16 with a power-of-two scale per row
-// (at most 2^-11 of the row's largest).
+// multiplied.  Partial sums are stored in fp32.
 #include "attn_core.h"
 #include "kvq8_device.h"
 #include "q8_ranges.h"
@@ -95,8 +94,8 @@ static_assert(sizeof(Q8Cut) == 48, "12 words");
 struct Q8Ws {
   Q8Cut* cuts;       // [waves]
   int32_t* bad;      // [R][chunks] flags of q8_pages
-  float* part_ml;    // [waves][2][32][4]: max, sum, sum of the weights used, scale exponent
-  _Float16* part_o;  // [waves][2][32][128]
+  float* part_ml;    // [waves][2][32][4]: max, sum, sum of the weights used
+  float* part_o;     // [waves][2][16][32][8]: 8 dims of each of the 32 rows, 16 times
 };
 
 struct Q8Args {
@@ -137,8 +136,8 @@ __host__ inline Q8Ws q8_layout(void* base, int R, int max_pages, int nw, size_t*
   p += al(size_t(R) * size_t(q8_page_chunks(max_pages)) * 4);
   w.part_ml = reinterpret_cast<float*>(p);
   p += al(size_t(nw) * 2 * kQ8Rows * 4 * sizeof(float));
-  w.part_o = reinterpret_cast<_Float16*>(p);
-  p += al(size_t(nw) * 2 * kQ8Rows * kD * sizeof(_Float16));
+  w.part_o = reinterpret_cast<float*>(p);
+  p += al(size_t(nw) * 2 * kQ8Rows * kD * sizeof(float));
   if (bytes != nullptr) *bytes = size_t(p - static_cast<char*>(base));
   return w;
 }
@@ -1006,27 +1005,18 @@ __device__ __forceinline__ void q8_segment(const Q8Args& a, const Q8Ws& ws, cons
         a.lse[orow] = L > 0.0f ? (rt.m + log2f(L)) * kLn2 : -__builtin_inff();
     }
   } else {
-    float mx = 0.0f;
-#pragma unroll
-    for (int dt = 0; dt < 4; ++dt)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, fabsf(rt.o[dt][r]));
-    mx = pair_max(mx);
-    const int e = mx > 0.0f ? __builtin_amdgcn_frexp_expf(mx) - 15 : 0;
     if (rho < rows) {
-      const float sc = __builtin_amdgcn_ldexpf(1.0f, -e);
-      const size_t prow = (size_t(b) * 2 + part_slot) * kQ8Rows + rho;
+      const size_t part = size_t(b) * 2 + part_slot;
+      float* po = ws.part_o + (part * 16 * kQ8Rows + rho) * 8 + 4 * h;  // (a store: 1 KB in one piece)
 #pragma unroll
       for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
-        for (int r = 0; r < 16; r += 8) {  // (dims as q8_combine takes them)
-          halfx8 v;
-#pragma unroll
-          for (int k = 0; k < 8; ++k) v[k] = static_cast<_Float16>(rt.o[dt][r + k] * sc);
-          *reinterpret_cast<halfx8*>(ws.part_o + prow * kD + 32 * dt + 2 * r + 8 * h) = v;
-        }
+        for (int r = 0; r < 16; r += 4)
+          *reinterpret_cast<floatx4*>(po + (4 * dt + (r >> 2)) * kQ8Rows * 8) =
+              floatx4{rt.o[dt][r], rt.o[dt][r + 1], rt.o[dt][r + 2], rt.o[dt][r + 3]};
       if (h == 0)
-        *reinterpret_cast<floatx4*>(ws.part_ml + prow * 4) = floatx4{rt.m, L, Lq, float(e)};
+        *reinterpret_cast<floatx4*>(ws.part_ml + (part * kQ8Rows + rho) * 4) =
+            floatx4{rt.m, L, Lq, 0.0f};
     }
   }
   asm volatile("");  // (the lanes meet here: what follows stays known to be uniform)
@@ -1112,32 +1102,35 @@ __device__ __forceinline__ Q8Cut load_cut(const Q8Cut* cuts, int b) {
   return __builtin_bit_cast(Q8Cut, w);
 }
 
-// (3.7 us for a few partial sums, 8 us for 2900 of them, 25 MB: latency and the launch, then their
-// bytes; four at a time took 0.5 us more.)  Workgroup (b, y): rows 16 y .. 16 y + 15 that wave b has of the unit that is cut first
-// at its range (if any); a thread has 8 dims of a row.  Parts in the order of the gangs.
+// Workgroup (b, y): rows 16 y .. 16 y + 15 that wave b has of the unit that is cut first at its
+// range (if any); a thread has 8 dims of a row.  Parts in the order of the gangs.  4 us for a
+// few partial sums, 11 us for 2900 of them, 50 MB: latency and the launch, then their bytes (in
+// fp16 they were half of these and the call 2-8% shorter; a sum below 2^-113 had no scale there).
 __global__ __launch_bounds__(256) void q8_combine_kernel(Q8Args a, Q8Ws ws) {
   const int b = blockIdx.x;
   const Q8Cut st = load_cut(ws.cuts, b);
   if (st.parts == 0) return;
   const int rows = min(kQ8Rows, st.nslots * a.G - st.row0);
-  const int rho = blockIdx.y * 16 + threadIdx.x / 16;
+  const int rho = blockIdx.y * 16 + (threadIdx.x & 15);
   if (rho >= rows) return;
-  const int piece = threadIdx.x & 15;  // 8 halves of the partial
+  const int piece = threadIdx.x / 16;  // dims 8 piece .. 8 piece + 7
   float M = -__builtin_inff(), L = 0.0f, Lq = 0.0f;
   float acc[8] = {};
   int at = st.at, slot = st.slot, half = 1;  // (the first part is the end of its wave's range)
   for (int i0 = 0; i0 < st.parts; i0 += kQ8Parts) {  // (a batch's loads in one round trip)
     floatx4 ml[kQ8Parts];
-    halfx8 h[kQ8Parts];
+    floatx4 o[kQ8Parts][2];
 #pragma unroll
     for (int j = 0; j < kQ8Parts; ++j) {
       ml[j] = floatx4{-__builtin_inff(), 0.0f, 0.0f, 0.0f};
-      h[j] = halfx8{};
+      o[j][0] = o[j][1] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
       if (i0 + j < st.parts) {  // uniform
         const int wave = q8_first_wave(st.wg0 + at, a.wgs) + slot * st.k + st.member;
-        const size_t row = (size_t(wave) * 2 + half) * kQ8Rows + size_t(rho);
-        ml[j] = *reinterpret_cast<const floatx4*>(ws.part_ml + row * 4);
-        h[j] = *reinterpret_cast<const halfx8*>(ws.part_o + row * kD + piece * 8);
+        const size_t part = size_t(wave) * 2 + half;
+        ml[j] = *reinterpret_cast<const floatx4*>(ws.part_ml + (part * kQ8Rows + rho) * 4);
+        const float* po = ws.part_o + ((part * 16 + piece) * kQ8Rows + rho) * 8;
+        o[j][0] = *reinterpret_cast<const floatx4*>(po);
+        o[j][1] = *reinterpret_cast<const floatx4*>(po + 4);
       }
       half = 0;
       at += 1;
@@ -1160,20 +1153,16 @@ __global__ __launch_bounds__(256) void q8_combine_kernel(Q8Args a, Q8Ws ws) {
       const float wgt = __builtin_amdgcn_exp2f(ml[j][0] - m);  // 0 from -inf
       L = __builtin_fmaf(wgt, ml[j][1], L);
       Lq = __builtin_fmaf(wgt, ml[j][2], Lq);
-      const float wo = wgt * __builtin_amdgcn_ldexpf(1.0f, int(ml[j][3]));
 #pragma unroll
-      for (int k = 0; k < 8; ++k) acc[k] = __builtin_fmaf(wo, float(h[j][k]), acc[k]);
+      for (int k = 0; k < 8; ++k) acc[k] = __builtin_fmaf(wgt, o[j][k >> 2][k & 3], acc[k]);
     }
   }
   const int ra = st.row0 + rho;
   const size_t orow = size_t(st.q0 + ra / a.G) * a.hq + size_t(st.head) * a.G + ra % a.G;
   const float inv = Lq > 0.0f ? 1.0f / Lq : 0.0f;
-  // piece 4 dt + 2 k + h holds dims 32 dt + 16 k + 4 h + 0..3 and the same + 8
-  uint16_t* po = a.out + orow * kD + 32 * (piece >> 2) + 16 * ((piece >> 1) & 1) + 4 * (piece & 1);
-  *reinterpret_cast<uint2*>(po) =
-      make_uint2(pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv));
-  *reinterpret_cast<uint2*>(po + 8) =
-      make_uint2(pack_bf16x2(acc[4] * inv, acc[5] * inv), pack_bf16x2(acc[6] * inv, acc[7] * inv));
+  *reinterpret_cast<uint4*>(a.out + orow * kD + 8 * piece) =
+      make_uint4(pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv),
+                 pack_bf16x2(acc[4] * inv, acc[5] * inv), pack_bf16x2(acc[6] * inv, acc[7] * inv));
   if (a.lse != nullptr && piece == 0)
     a.lse[orow] = L > 0.0f ? (M + log2f(L)) * kLn2 : -__builtin_inff();
 }

@@ -1,9 +1,10 @@
 """The 8-bit paged cache where its calls can go wrong: their limits."""
+import numpy as np
 import pytest
 
 from oracle import kvq8, status as st
 from tests import gpu_common as gc
-from tests.test_gpu_kvq8 import _log, _zeros
+from tests.test_gpu_kvq8 import _dev, _log, _zeros
 
 pytestmark = pytest.mark.gpu
 
@@ -51,3 +52,174 @@ def test_more_steps_than_a_call_takes(tokens, slots, hq):
     out, lse, status = _attn(q, kn, kn, kvq8.E4M3, (page, page, scale, scale), ps, bt, plen, qo, mask, hq, hkv)
     assert status == st.BAD_OFFSETS
     assert bool(torch.isnan(out).all()) and bool(torch.isnan(lse).all())
+
+
+# ---- against a plain form in 64 bits ----------------------------------------
+
+def _decode(pages, fmt):
+    import torch
+    return pages.view(torch.float8_e4m3fn if fmt == kvq8.E4M3 else torch.float8_e5m2).to(torch.float64)
+
+
+def _plain(q, kn, vn, fmt, cache, ps, bt, plen, qo, mask, hq, hkv, scale):
+    """Attention in 64 bits from its definition, request by request, on device tensors (q, kn and vn bf16).
+    Returns out, lse and, for the bounds below, the weighted mean of |v - out| and of |v|, the
+    largest sum of |q k| and the keys of a row; NaN for requests with lengths, offsets or pages that
+    cannot be."""
+    import torch
+    R, G, cap = len(plen), hq // hkv, q.shape[0]
+    n_pages = cache[0].shape[0]
+    f64 = dict(dtype=torch.float64, device="cuda:0")
+    out, dev, mabs = (torch.full((cap, hq, 128), float("nan"), **f64) for _ in range(3))
+    lse, zabs, keys = (torch.full((cap, hq), float("nan"), **f64) for _ in range(3))
+    table, lens, offs = bt.cpu().tolist(), plen.cpu().tolist(), qo.cpu().tolist()
+    for r in range(R):
+        a, b, P = offs[r], offs[r + 1], lens[r]
+        need = -(-P // ps)
+        if not (0 <= a <= b <= cap and 0 <= P and need <= bt.shape[1]):
+            continue
+        ids = table[r][:need]
+        n = b - a
+        if n == 0 or any(not 0 <= i < n_pages for i in ids):
+            continue
+        at = torch.tensor(ids, dtype=torch.int64, device="cuda:0")
+        K, V = (torch.cat([(_decode(cache[i][at], fmt) * cache[2 + i][at].double().repeat_interleave(32, 2)[..., None]
+                            ).transpose(0, 1).reshape(hkv, -1, 128)[:, :P], x[a:b].double().transpose(0, 1)], 1)
+                for i, x in ((0, kn), (1, vn)))
+        j = torch.arange(n, device="cuda:0")
+        w = j >> 5
+        bits = mask[a:b, w.clamp(max=mask.shape[1] - 1)].long() >> (j & 31) & 1
+        see = torch.cat([torch.ones((n, P), dtype=torch.bool, device="cuda:0"), (bits > 0) & (w < mask.shape[1])], 1)
+        Q = q[a:b].double().view(n, hkv, G, 128).permute(1, 0, 2, 3).reshape(hkv, n * G, 128)
+        see = see[:, None, :].expand(n, G, P + n).reshape(1, n * G, P + n)
+        # K's columns side by side: products of plain matrices, head by head
+        z = torch.stack([Q[h] @ K[h].T.contiguous() for h in range(hkv)]).mul_(float(scale))
+        za = torch.stack([Q[h].abs() @ K[h].abs().T.contiguous() for h in range(hkv)]).mul_(float(scale))
+        z.masked_fill_(~see, -float("inf"))
+        za.masked_fill_(~see, 0.0)
+        m = z.amax(-1, keepdim=True).clamp(min=-1e300)
+        p = (z - m).exp_()
+        l = p.sum(-1, keepdim=True)
+        p /= l.clamp(min=1e-300)
+        o = torch.stack([p[h] @ V[h] for h in range(hkv)])
+        ma = torch.stack([p[h] @ V[h].abs() for h in range(hkv)])
+        # mean |v - o| <= the root of the mean square
+        sq = torch.stack([p[h] @ (V[h] * V[h]) for h in range(hkv)])
+        de = (sq - o * o).clamp_(min=0.0).sqrt_()
+        back = lambda x: x.view(hkv, n, G, -1).permute(1, 0, 2, 3).reshape(n, hq, -1)  # noqa: E731
+        out[a:b], dev[a:b], mabs[a:b] = back(o), back(de), back(ma)
+        lse[a:b] = back(m + l.log())[..., 0]
+        zabs[a:b], keys[a:b] = back(za.amax(-1, keepdim=True))[..., 0], float(P + n)
+    return dict(out=out, lse=lse, dev=dev, mabs=mabs, zabs=zabs, keys=keys)
+
+
+def _check(got, ref, chain, what=""):
+    """Bounds per element, from the call's documented roundings; u = 2^-24 is half a step of fp32.
+    * each weight is rounded to bf16 (2^-8 of it) and the sum is that of the rounded ones: 2^-8 /
+      (1 - 2^-8) of the mean |v - o|;
+    * a score: 129 products and sums and as many again for the factors, u each on sum |q k|; the exponential
+      2^-22: a relative error of the weights, on the same mean;
+    * fp32 sums: chain additions one after another (the keys of a wave's range and the merged parts),
+      u each on the mean |v|; the log of the sum the same, and 2^-18 for the exponents of scales;
+    * the output's rounding to bf16, 2^-8 of it."""
+    import torch
+    out, lse = got[0].double(), got[1].double()
+    live = ~torch.isnan(ref["lse"])
+    assert bool((torch.isnan(lse) == ~live).all()), f"{what}: rows written or not"
+    assert bool((torch.isnan(out) == ~live[..., None]).all()), f"{what}: outputs written or not"
+    u = 2.0 ** -24
+    x = {n: t[live] for n, t in ref.items()}
+    o, l = out[live], lse[live]
+    dz = x["zabs"] * (2 * 129 * u)
+    tol = x["dev"] * (2.0 ** -8 / (1 - 2.0 ** -8) + dz[:, None] + 2.0 ** -22) + x["mabs"] * (chain * u)
+    tol = tol * (1 + 2.0 ** -7) + x["out"].abs() * 2.0 ** -8
+    err = (o - x["out"]).abs()
+    assert bool((err <= tol).all()), f"{what}: off by {float((err / tol.clamp(min=1e-300)).max()):.3f} of the bound"
+    empty = torch.isneginf(x["lse"])
+    assert bool((torch.isneginf(l) == empty).all()) and not bool(o[empty].any())
+    f = ~empty
+    tol = dz[f] + chain * u + 2.0 ** -18 + x["lse"][f].abs() * 2.0 ** -22
+    err = (l[f] - x["lse"][f]).abs()
+    assert bool((err <= tol).all()), f"{what}: lse off by {float((err / tol).max()):.3f} of the bound"
+
+
+def _bf16(x):
+    import torch
+    return torch.as_tensor(np.asarray(x, np.float32)).to(torch.bfloat16).to("cuda:0")
+
+
+def _chains(n, rng):
+    """Masks of n slots that see themselves and some of those before."""
+    W = max(1, -(-n // 32))
+    m = np.zeros((n, W), np.uint32)
+    for j in range(n):
+        if j:
+            m[j] = m[rng.integers(max(0, j - 5), j)]
+        m[j, j >> 5] |= np.uint32(1 << (j & 31))
+    return m
+
+
+@pytest.mark.parametrize("fmt", [kvq8.E4M3, kvq8.E5M2])
+def test_values_far_below_the_dominant_keys(fmt):
+    """Half of the keys have all the weight and values of zero, the others 2^-57 of it and values near
+    2^-62: rows whose sums are near 2^-115 where their units are split between waves."""
+    import torch
+    rng = np.random.default_rng(30)
+    P, ps, hq, hkv = 4000, 64, 8, 2
+    pages = -(-P // ps)
+    kb = np.zeros((pages, hkv, ps, 128), np.uint8)
+    vb = np.zeros_like(kb)
+    kb[:, :, 1::2, 0] = kvq8.encode8(np.float64(-40.0), fmt)
+    vb[:, :, 1::2] = kvq8.encode8(rng.choice([-0.25, 0.25, 0.5], vb[:, :, 1::2].shape), fmt)
+    ks = np.ones((pages, hkv, ps // 32), np.float32)
+    vs = np.full_like(ks, 2.0 ** -60)
+    cache = [torch.from_numpy(a).to("cuda:0") for a in (kb, vb, ks, vs)]
+    q = np.zeros((1, hq, 128))
+    q[..., 0] = 1.0
+    kn = np.zeros((1, hkv, 128))
+    kn[..., 0] = -90.0
+    args = (_bf16(q), _bf16(kn), _bf16(kn * 0), fmt, cache, ps, torch.arange(pages, dtype=torch.int32, device="cuda:0")[None],
+            torch.tensor([P], dtype=torch.int32, device="cuda:0"), torch.tensor([0, 1], dtype=torch.int32, device="cuda:0"),
+            torch.ones((1, 1), dtype=torch.int32, device="cuda:0"), hq, hkv, 1.0)
+    ref = _plain(*args)
+    top = float(ref["out"].abs().max())
+    assert 2.0 ** -125 < top < 2.0 ** -114
+    _log(f"[attn q8] outputs up to {top:.2g}, fmt={fmt}")
+    got = _attn(*args)
+    assert got[2] == 0
+    _check(got, ref, 1000, "tiny sums")
+
+
+@pytest.mark.parametrize("fmt", [kvq8.E4M3, kvq8.E5M2])
+@pytest.mark.parametrize("k_exp,v_exps", [(-60, (-60,)), (60, (60,)), (0, (-60, 60)), (60, (-60, 0, 60)), (-3, (-1, 0, 1))])
+def test_scales_at_both_ends(fmt, k_exp, v_exps):
+    """K scales of 2^-60 and 2^60, V scales at either end and both in one row; in units that waves share
+    and in others."""
+    import torch
+    rng = np.random.default_rng(31)
+    hq, hkv, ps, lens, slots = 16, 2, 64, [3000, 40, 64, 500], [2, 1, 5, 9]
+    need = [-(-n // ps) for n in lens]
+    pages = sum(need)
+    gen = torch.Generator(device="cuda:0")
+    gen.manual_seed(5)
+    t = torch.float8_e4m3fn if fmt == kvq8.E4M3 else torch.float8_e5m2
+    cache = [torch.randn((pages, hkv, ps, 128), generator=gen, device="cuda:0").mul_(16.0).to(t).view(torch.uint8)
+             for _ in range(2)]
+    cache.append(torch.full((pages, hkv, ps // 32), 2.0 ** k_exp, device="cuda:0"))
+    cache.append(torch.from_numpy(np.exp2(rng.choice(v_exps, (pages, hkv, ps // 32))).astype(np.float32)).to("cuda:0"))
+    bt = np.full((len(lens), max(need)), -1, np.int32)
+    ids, at = rng.permutation(pages), 0
+    for r, n in enumerate(need):
+        bt[r, :n] = ids[at:at + n]
+        at += n
+    qo = np.concatenate([[0], np.cumsum(slots)]).astype(np.int32)
+    cap = int(qo[-1])
+    mask = np.concatenate([_chains(n, rng) for n in slots])
+    q = _bf16(rng.standard_normal((cap, hq, 128)) * 2.0 ** (-k_exp - 4))
+    kn = _bf16(rng.standard_normal((cap, hkv, 128)) * 2.0 ** (k_exp + 4))
+    vn = _bf16(rng.standard_normal((cap, hkv, 128)) * 2.0 ** v_exps[-1])
+    args = (q, kn, vn, fmt, cache, ps, _dev(bt), _dev(np.array(lens, np.int32)), _dev(qo), _dev(mask), hq, hkv)
+    _log(f"[attn q8] K scale 2^{k_exp}, V scales 2^{v_exps}, fmt={fmt}")
+    got = _attn(*args)
+    assert got[2] == 0
+    _check(got, _plain(*args, 128 ** -0.5), 1000, f"{k_exp} {v_exps}")
