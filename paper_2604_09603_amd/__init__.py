@@ -125,7 +125,9 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     # torch ships its own HIP runtime under the same soname; load it first so that the
     # library and torch's streams and allocations share one runtime instance
     import torch
-    _raw_stream, _device = torch._C._cuda_getCurrentRawStream, torch.cuda.current_device
+    # (a torch without GPU support has no streams, but the calls' refusals work there too)
+    _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    _device = torch.cuda.current_device
     lib = ctypes.CDLL(path)
     for name, (res, args) in _SIGS.items():
         fn = getattr(lib, name)
@@ -142,9 +144,12 @@ def _ptr(t):
 
 
 def _stream(stream):
-    if stream is None:  # the current one; its handle alone is 2.4 us cheaper than its object
+    if stream is not None:
+        return stream.cuda_stream
+    if _raw_stream is not None:  # the current one; its handle alone is 2.4 us cheaper than its object
         return _raw_stream(_device())
-    return stream.cuda_stream
+    import torch
+    return torch.cuda.current_stream().cuda_stream
 
 
 def _check(code: int, what: str):
