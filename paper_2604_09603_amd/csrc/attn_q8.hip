@@ -352,24 +352,34 @@ __device__ __forceinline__ Q8Range q8_begin(const Q8Args& a, const Q8Ws& ws, uin
       q1[j] = a.q_offsets[r + 1];
       P[j] = a.prefix_len[r];
     }
+    uint64_t idle[kBatch];  // lanes whose request has nothing to do, but whose pages count for the status
 #pragma unroll
     for (int j = 0; j < kBatch; ++j) {
       const int r = tid * K + i + j;
-      if (i + j >= K || r >= a.R) continue;
-      s_q[r] = q0[j];
-      s_P[r] = P[j];
-      if (r + 1 == a.R) s_q[r + 1] = q1[j];
-      const Q8Look x = q8_look(a, q0[j], q1[j], P[j]);
-      if (x.tiles < 0 && blockIdx.x == 0) bits = ECHO_DATA_BAD_OFFSETS;
-      if (x.tiles == 0 && r % int(gridDim.x) == int(blockIdx.x)) {
-        // nothing to do, but its pages count for the status
-        const Q8Pages pages(a, ws, r, x.P);
-        for (int e = 0; e < pages.n; ++e)
-          if (pages.bad(a, e)) bits = ECHO_DATA_BAD_OFFSETS;
+      const bool there = i + j < K && r < a.R;
+      Q8Look x = {};
+      x.tiles = -1;
+      if (there) {
+        s_q[r] = q0[j];
+        s_P[r] = P[j];
+        if (r + 1 == a.R) s_q[r + 1] = q1[j];
+        x = q8_look(a, q0[j], q1[j], P[j]);
+        if (x.tiles < 0 && blockIdx.x == 0) bits = ECHO_DATA_BAD_OFFSETS;
+        if (x.tiles > 0) T.add(a.hkv, x.tiles, x.tpu);
       }
-      if (x.tiles <= 0) continue;
-      T.add(a.hkv, x.tiles, x.tpu);
+      idle[j] = __ballot(x.tiles == 0 && r % int(gridDim.x) == int(blockIdx.x));
     }
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j)
+      while (idle[j] != 0ull) {  // uniform
+        const int l = __ffsll((unsigned long long)idle[j]) - 1;
+        idle[j] &= idle[j] - 1;
+        const Q8Pages pages(a, ws, (wid * kWave + l) * K + i + j, lane_of(P[j], l));
+        for (int e = 0; e < pages.n; e += 2 * kWave) {  // (two loads at a time)
+          const int v0 = pages.at(e + lane), v1 = pages.at(e + kWave + lane);
+          if (pages.bad_value(a, v0) || pages.bad_value(a, v1)) bits = ECHO_DATA_BAD_OFFSETS;
+        }
+      }
   }
   // (a sum that could matter is rare)
   float all = T.all;

@@ -1,4 +1,5 @@
-"""The 8-bit paged cache where its calls can go wrong: their limits."""
+"""The 8-bit paged cache where its calls can go wrong: limits, scales, page checks, long ranges, bad offsets.
+Attention is compared with a plain form in 64 bits."""
 import numpy as np
 import pytest
 
@@ -223,3 +224,59 @@ def test_scales_at_both_ends(fmt, k_exp, v_exps):
     got = _attn(*args)
     assert got[2] == 0
     _check(got, _plain(*args, 128 ** -0.5), 1000, f"{k_exp} {v_exps}")
+
+
+# ---- page checks --------------------------------------------------------------
+
+def _pool(pages, hkv, ps, fmt, seed, spare=1):
+    """Random pages and scales, with a page of memory behind them (as views): an id that is missed reads that."""
+    import torch
+    gen = torch.Generator(device="cuda:0")
+    gen.manual_seed(seed)
+    t, gain = (torch.float8_e4m3fn, 1.0) if fmt == kvq8.E4M3 else (torch.float8_e5m2, 2.0 ** 7)
+    n = pages + spare
+    c = [torch.randn((n, hkv, ps, 128), generator=gen, device="cuda:0").mul_(50.0 * gain).to(t).view(torch.uint8)[:pages]
+         for _ in range(2)]
+    return c + [torch.exp2(torch.randint(-9, -5, (n, hkv, ps // 32), generator=gen, device="cuda:0").float()).div_(gain)[:pages]
+                for _ in range(2)]
+
+
+def _new(cap, hq, hkv, seed, q_scale=1.0):
+    rng = np.random.default_rng(seed)
+    return (_bf16(rng.standard_normal((cap, hq, 128)) * q_scale), _bf16(rng.standard_normal((cap, hkv, 128))),
+            _bf16(rng.standard_normal((cap, hkv, 128))))
+
+
+def _skip(ref, rows):
+    for t in ref.values():
+        t[rows] = float("nan")
+    return ref
+
+
+@pytest.mark.parametrize("R", [3, 700])
+@pytest.mark.parametrize("width", [512, 513, 70000])
+def test_pages_of_paused_requests(width, R):
+    """Requests without slots and with up to 500 (70000) pages write nothing, but a bad id among their
+    pages is reported, at any place; one behind them is not."""
+    import torch
+    rng = np.random.default_rng(46)
+    ps, hq, hkv, pages = 32, 2, 1, 8
+    cache = _pool(pages, hkv, ps, kvq8.E5M2, 47)
+    n = 70000 if width == 70000 else 500
+    lens = rng.integers(0, 99, R).astype(np.int32)
+    slots = np.ones(R, np.int64)
+    paused = R // 2
+    slots[paused], lens[paused] = 0, n * ps - 3
+    qo = np.concatenate([[0], np.cumsum(slots)]).astype(np.int32)
+    q, kn, vn = _new(R - 1, hq, hkv, 48)
+    table = torch.zeros((R, width), dtype=torch.int32, device="cuda:0")
+    args = (q, kn, vn, kvq8.E5M2, cache, ps, table, _dev(lens), _dev(qo), _dev(np.ones((R - 1, 1), np.int32)), hq, hkv)
+    ref = _plain(*args, 128 ** -0.5)
+    for place in (None, 0, 1, 63, 64, 127, 128, 191, 256, n - 1, n):
+        if place is not None and place < width:
+            table[paused, place] = pages
+        _log(f"[attn q8] {R} requests, width {width}, a paused one's bad id at {place}")
+        got = _attn(*args)
+        assert got[2] == (0 if place in (None, n) else st.BAD_OFFSETS)
+        _check(got, ref, 100, f"place {place}")
+        table[paused] = 0
