@@ -253,6 +253,67 @@ def _skip(ref, rows):
     return ref
 
 
+@pytest.mark.parametrize("width", [512, 513])
+@pytest.mark.parametrize("at", [0, 63, 64, 127, 128, 255, 256, "last"])
+def test_page_checks_of_long_requests(width, at):
+    """An id past the pool at place `at` of a request's pages, for requests of 64 to 500 pages; the widest
+    table that the attention's waves check themselves, and one that has a launch of its own."""
+    rng = np.random.default_rng(40)
+    ps, hq, hkv = 32, 4, 1
+    need = [64, 65, 3, 128, 129, 256, 257, 500]
+    lens = [ps * n - int(rng.integers(0, ps)) for n in need]
+    slots = [1, 2, 1, 9, 1, 30, 2, 1]
+    pages = 600
+    cache = _pool(pages, hkv, ps, kvq8.E4M3, 41)
+    table = rng.integers(0, pages, (len(need), width)).astype(np.int32)
+    qo = np.concatenate([[0], np.cumsum(slots)]).astype(np.int32)
+    q, kn, vn = _new(int(qo[-1]), hq, hkv, 42)
+    mask = np.concatenate([_chains(n, rng) for n in slots])
+    args = (q, kn, vn, kvq8.E4M3, cache, ps, _dev(table), _dev(np.array(lens, np.int32)), _dev(qo), _dev(mask), hq, hkv)
+    ref = _plain(*args, 128 ** -0.5)
+    for r, n in enumerate(need):
+        place = n - 1 if at == "last" else at
+        if place >= n:
+            continue
+        bad = table.copy()
+        bad[r, place] = pages
+        bad[r, n:] = -1  # (behind the request's pages: not looked at)
+        _log(f"[attn q8] width {width}, request {r} of {n} pages, bad id at {place}")
+        got = _attn(*args[:6], _dev(bad), *args[7:])
+        assert got[2] == st.BAD_OFFSETS
+        _check(got, _skip({k: t.clone() for k, t in ref.items()}, slice(int(qo[r]), int(qo[r + 1]))), 1000, f"request {r}")
+
+
+def test_page_checks_of_later_requests_of_a_range():
+    """2000 requests over the same 130 pages: a wave's range holds several of them, and some have a bad id
+    at a place that each step of the check looks at.  (One request with a row for each, which sees the
+    prefix and itself, is the same computation.)"""
+    import torch
+    rng = np.random.default_rng(43)
+    R, ps, hq, hkv, n = 2000, 32, 2, 2, 130
+    P = ps * n - 5
+    cache = _pool(n, hkv, ps, kvq8.E4M3, 44)
+    q, kn, vn = _new(R, hq, hkv, 45)
+    order = rng.permutation(n).astype(np.int32)
+    ident = np.zeros((R, -(-R // 32)), np.uint32)
+    for r in range(R):
+        ident[r, r >> 5] = 1 << (r & 31)
+    i32 = dict(dtype=torch.int32, device="cuda:0")
+    ref = _plain(q, kn, vn, kvq8.E4M3, cache, ps, _dev(order[None]), torch.tensor([P], **i32),
+                 torch.tensor([0, R], **i32), _dev(ident), hq, hkv, 128 ** -0.5)
+    table = np.tile(order, (R, 1))
+    bad = rng.choice(R, 60, replace=False)
+    for i, r in enumerate(bad):
+        table[r, [0, 63, 64, 127, 128, 129][i % 6]] = n
+    for width in (n, 513):
+        wide = np.pad(table, ((0, 0), (0, width - n)), constant_values=-1)
+        _log(f"[attn q8] 2000 requests, width {width}")
+        got = _attn(q, kn, vn, kvq8.E4M3, cache, ps, _dev(wide), torch.full((R,), P, **i32),
+                    torch.arange(R + 1, **i32), torch.ones((R, 1), **i32), hq, hkv)
+        assert got[2] == st.BAD_OFFSETS
+        _check(got, _skip({k: t.clone() for k, t in ref.items()}, torch.from_numpy(bad).to("cuda:0")), 10000, f"width {width}")
+
+
 @pytest.mark.parametrize("R", [3, 700])
 @pytest.mark.parametrize("width", [512, 513, 70000])
 def test_pages_of_paused_requests(width, R):
