@@ -632,6 +632,12 @@ __device__ __forceinline__ Q8Next q8_next_steps(Q8Table& tb, const Q8Args& a, co
   return x;
 }
 
+// The softmax factor of a block.  Not 0, by which the scores of masked keys, -inf, are not to be
+// multiplied (the smallest normal number instead: a score is 0 with either).
+__device__ __forceinline__ float q8_factor(const Q8Args& a, float k_scale) {
+  return fmaxf(a.scale2 * k_scale, 1.17549435e-38f);
+}
+
 // Fills the table with them (page: the lane's) and sends for the first steps' tiles; the scales
 // come in the same round trip, the first time beside Q and the tree's keys if a unit begins.
 template <bool kGang>
@@ -658,7 +664,7 @@ __device__ __forceinline__ void q8_fill(Q8Table& tb, const Q8Args& a, const Q8Ne
     tb.lvs = vs;
     tb.raw = true;
   } else if (x.pos < x.n) {
-    tb.c = a.scale2 * ks;
+    tb.c = q8_factor(a, ks);
     tb.lvs = __builtin_amdgcn_logf(vs);
   }
 }
@@ -671,7 +677,7 @@ __device__ __forceinline__ void q8_refill(Q8Table& tb, const Q8Args& a, const Q8
 
 // The scales' values, once they are there, become what the softmax takes.
 __device__ __forceinline__ void q8_scales(Q8Table& tb, const Q8Args& a) {
-  tb.c *= a.scale2;
+  tb.c = q8_factor(a, tb.c);
   tb.lvs = __builtin_amdgcn_logf(tb.lvs);
   tb.raw = false;
 }

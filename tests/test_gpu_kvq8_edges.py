@@ -341,3 +341,29 @@ def test_pages_of_paused_requests(width, R):
         assert got[2] == (0 if place in (None, n) else st.BAD_OFFSETS)
         _check(got, ref, 100, f"place {place}")
         table[paused] = 0
+
+
+@pytest.mark.parametrize("sm_scale", [1e-30, 1e-40])
+def test_scores_that_vanish(sm_scale):
+    """sm_scale times a K scale below the smallest number: every score is 0, and keys past a prefix or
+    outside a row's mask still have no weight."""
+    import torch
+    rng = np.random.default_rng(50)
+    ps, hq, hkv, lens, slots = 64, 8, 2, [1, 70, 1000, 64, 33], [2, 1, 3, 40, 1]
+    need = [-(-n // ps) for n in lens]
+    cache = _pool(sum(need), hkv, ps, kvq8.E4M3, 51)
+    cache[2].fill_(2.0 ** -60)
+    table, at = np.full((len(lens), max(need)), -1, np.int32), 0
+    for r, n in enumerate(need):
+        table[r, :n] = np.arange(at, at + n)
+        at += n
+    qo = np.concatenate([[0], np.cumsum(slots)]).astype(np.int32)
+    q, kn, vn = _new(int(qo[-1]), hq, hkv, 52)
+    W = max(-(-n // 32) for n in slots)
+    mask = np.concatenate([np.pad(_chains(n, rng), ((0, 0), (0, W - max(1, -(-n // 32))))) for n in slots])
+    args = (q, kn, vn, kvq8.E4M3, cache, ps, _dev(table), _dev(np.array(lens, np.int32)), _dev(qo), _dev(mask), hq, hkv,
+            sm_scale)
+    _log(f"[attn q8] sm_scale {sm_scale}")
+    got = _attn(*args)
+    assert got[2] == 0
+    _check(got, _plain(*args), 1000, "vanishing scores")
