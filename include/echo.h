@@ -487,8 +487,8 @@ int32_t echo_store_kv_q8(const uint16_t* k, const uint16_t* v, int64_t k_stride,
  * echo_commit_kv_q8 -- echo_commit_kv into an 8-bit cache: each request's root
  * and accepted rows are appended at positions prefix_len[r], prefix_len[r] + 1,
  * ... and new_len[r] = prefix_len[r] + 1 + accept_len[r].  A request with a
- * missing page or a bad slot is left as it is (ECHO_DATA_BAD_OFFSETS) and one
- * without slots too: new_len[r] = prefix_len[r].
+ * missing page, a bad slot or a new length of 2^31 or more is left as it is
+ * (ECHO_DATA_BAD_OFFSETS) and one without slots too: new_len[r] = prefix_len[r].
  *   new_len  [R] int32, may be prefix_len itself
  *   page_size a power of two, >= 32; the other arguments as for echo_commit_kv
  */

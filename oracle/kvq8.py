@@ -129,7 +129,7 @@ def commit_kv_q8(q_offsets, accept_len, accept_slots, k_new, v_new, fmt, k_pages
             e = p // ps
             page = int(block_table[r, e]) if e < block_table.shape[1] else -1
             dest.append(page * ps + p % ps if 0 <= page < num_pages else -1)
-        if min(dest) < 0 or not all(0 <= s < k_new.shape[0] for s in slots):
+        if min(dest) < 0 or P + len(slots) >= 1 << 31 or not all(0 <= s < k_new.shape[0] for s in slots):
             status |= st.BAD_OFFSETS
             continue
         *cache, _ = store_kv(k_new[slots], v_new[slots], dest, fmt, *cache)

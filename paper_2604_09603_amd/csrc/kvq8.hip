@@ -98,7 +98,9 @@ __global__ __launch_bounds__(kCommitQ8Threads) void commit_kv_q8_kernel(
     const int s = tid == 0 ? q0 : accept_slots[size_t(r) * max_depth + (tid - 1)];
     const long long e = ((long long)P + tid) >> c.page_shift;
     const int page = e < max_pages ? block_table[size_t(r) * max_pages + size_t(e)] : -1;
-    if (s < 0 || s >= max_rows || page < 0 || page >= c.num_pages) atomicOr(&s_bad, 1);
+    // (the new length stays below 2^31: pages may be shared, so that a table's tokens can exceed the pool's)
+    if (s < 0 || s >= max_rows || page < 0 || page >= c.num_pages || P > 0x7FFFFFFE - tid)
+      atomicOr(&s_bad, 1);
     s_slot[tid] = s;
     s_page[tid] = page;
   }

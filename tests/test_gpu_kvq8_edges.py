@@ -367,3 +367,31 @@ def test_scores_that_vanish(sm_scale):
     got = _attn(*args)
     assert got[2] == 0
     _check(got, _plain(*args), 1000, "vanishing scores")
+
+
+# ---- commit -----------------------------------------------------------------
+
+@pytest.mark.parametrize("below,accepted", [(5, 4), (1, 0), (0, 0), (4, 4), (3, 4)])
+def test_commit_of_the_longest_requests(below, accepted):
+    """A request of 2^31 - 1 - below tokens, all in one shared page of 2^20: the last token that a length of 31
+    bits has is appended, a path that would go past it is not."""
+    import torch
+    import paper_2604_09603_amd as pkg
+    ps, depth, top = 1 << 20, 4, (1 << 31) - 1
+    P = top - below
+    fits = 1 + accepted <= below
+    gen = torch.Generator(device="cuda:0")
+    gen.manual_seed(60)
+    kn = torch.randn((depth + 1, 1, 128), generator=gen, device="cuda:0").abs_().add_(1.0).to(torch.bfloat16)
+    page = [torch.zeros((1, 1, ps, 128), dtype=torch.uint8, device="cuda:0") for _ in range(2)]
+    scale = [torch.ones((1, 1, ps // 32), device="cuda:0") for _ in range(2)]
+    status, new = _zeros(1), _zeros(1)
+    one = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda:0")  # noqa: E731
+    _log(f"[commit] {P} tokens and {1 + accepted} more")
+    pkg.echo_commit_kv_q8(one([0, depth + 1]), one([accepted]), one([[1, 2, 3, 4]]), depth, kn, kn, 1, depth + 1, 1, 128,
+                          kvq8.E4M3, *page, *scale, ps, _zeros(1, 2049), one([P]), new, status=status)
+    assert int(status.item()) == (0 if fits else st.BAD_OFFSETS)
+    assert int(new.item()) == (P + 1 + accepted if fits else P)
+    want = sorted((P + i) % ps for i in range(1 + accepted)) if fits else []
+    for t in page:
+        assert t[0, 0].any(-1).nonzero()[:, 0].tolist() == want
