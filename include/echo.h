@@ -528,7 +528,8 @@ int32_t echo_commit_kv_q8(const int32_t* q_offsets, const int32_t* accept_len,
  * row_offsets[r+1]) is token row_start[r] + i - row_offsets[r] of request r,
  * and slot_map[i] = page * page_size + token % page_size.  It is -1 where the
  * request does not hold that page (ECHO_DATA_NO_PAGES), and for the rows that no request
- * has, up to max_rows.
+ * has, up to max_rows.  Offsets that are negative, decrease or end past max_rows give no
+ * row a slot (ECHO_DATA_BAD_OFFSETS).
  *   row_offsets  [R+1] int32; row_start [R] int32; slot_map [max_rows] int64
  * The library does not look at the pages' ids.  R * max_pages_per_request < 2^31.
  */

@@ -245,7 +245,10 @@ def build_block_tables(want_len, page_size, block_table, num_held, free_pages, n
                     bt[r, j] = stack[top]
                 held[r] = need[r]
     slots = np.full(max_rows, -1, np.int64)
-    if row_offsets is not None:
+    if row_offsets is not None and (min(row_offsets) < 0 or max(row_offsets) > max_rows
+                                    or any(x > y for x, y in zip(row_offsets, row_offsets[1:]))):
+        status |= st.BAD_OFFSETS
+    elif row_offsets is not None:
         for r in range(R):
             have = int(held[r]) if 0 <= int(held[r]) <= most else 0
             for i in range(int(row_offsets[r]), min(int(row_offsets[r + 1]), max_rows)):

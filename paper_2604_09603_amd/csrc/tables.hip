@@ -25,6 +25,14 @@ constexpr int kMapThreads = 256;
 // rows 9.8 | 7.9, 32768 rows 42 | 7.9.
 constexpr int kFusedRows = 2 * kTableThreads;
 
+// Offset r of the rows; bad if it is not one of non-decreasing numbers in [0, max_rows].
+__device__ __forceinline__ int32_t row_offset(const TablesArgs& a, int r, bool& bad) {
+  const int32_t o = a.row_offsets[r];
+  const int32_t next = a.row_offsets[min(r + 1, a.R)];
+  bad |= o < 0 || next < o || next > a.max_rows;
+  return o;
+}
+
 // The slot of row i, or -1: rows past the last request's, and those whose page their
 // request does not hold (missing).  held(r): the pages of request r.
 template <typename Held>
@@ -34,9 +42,7 @@ __device__ __forceinline__ long long slot_of(const TablesArgs& a, int page_shift
   missing = false;
   if (i < row_offsets[0] || i >= row_offsets[a.R]) return -1;
   const int r = upper_bound_idx(row_offsets, a.R, int32_t(i));
-  const long long at = (long long)i - row_offsets[r];
-  if (at < 0 || i >= row_offsets[r + 1]) return -1;  // (offsets that decrease)
-  const long long pos = (long long)a.row_start[r] + at;
+  const long long pos = (long long)a.row_start[r] + i - row_offsets[r];
   const long long e = pos >> page_shift;
   missing = pos < 0 || e >= held(r);
   if (missing) return -1;
@@ -49,7 +55,7 @@ __global__ __launch_bounds__(kTableThreads) void build_tables_kernel(TablesArgs 
                                                                      bool map) {
   extern __shared__ int32_t s_mem[];
   __shared__ int2 s_scan[kTableThreads / kWave + 1];
-  __shared__ int s_last;
+  __shared__ int s_last, s_bad_rows;
   const int tid = threadIdx.x;
   const int R = a.R;
   int32_t* s_held = s_mem;            // R: pages held before
@@ -57,9 +63,10 @@ __global__ __launch_bounds__(kTableThreads) void build_tables_kernel(TablesArgs 
   int32_t* s_take = s_give + (R + 1); // R + 1: pages wanted by the requests before, and by all
   int32_t* s_off = s_take + (R + 1);  // R + 1: row offsets (map)
   const int before = *a.num_free;     // (in the round trip of the lengths, as the offsets)
+  bool bad_rows = false;
   if (map)
-    for (int r = tid; r <= R; r += kTableThreads) s_off[r] = a.row_offsets[r];
-  if (tid == 0) s_last = 0;
+    for (int r = tid; r <= R; r += kTableThreads) s_off[r] = row_offset(a, r, bad_rows);
+  if (tid == 0) s_last = s_bad_rows = 0;
   int bits = 0;
   int give_run = 0, take_run = 0;
   for (int base = 0; base < R; base += kTableThreads) {
@@ -87,6 +94,7 @@ __global__ __launch_bounds__(kTableThreads) void build_tables_kernel(TablesArgs 
     give_run += g_tot;
     take_run += t_tot;
   }
+  if (bad_rows) s_bad_rows = 1;
   if (tid == 0) {
     s_give[R] = give_run;
     s_take[R] = take_run;
@@ -131,6 +139,8 @@ __global__ __launch_bounds__(kTableThreads) void build_tables_kernel(TablesArgs 
   }
   if (map) {
     __syncthreads();
+    bad_rows = s_bad_rows != 0;  // then no row has a slot
+    if (bad_rows) bits |= ECHO_DATA_BAD_OFFSETS;
     const auto held = [&](int r) {
       const int take = s_take[r + 1] - s_take[r];
       const int h = s_held[r];
@@ -139,8 +149,8 @@ __global__ __launch_bounds__(kTableThreads) void build_tables_kernel(TablesArgs 
       return now <= a.max_pages ? now : 0;
     };
     for (int i = tid; i < a.max_rows; i += kTableThreads) {
-      bool missing;
-      a.slot_map[i] = slot_of(a, page_shift, i, s_off, held, missing);
+      bool missing = false;
+      a.slot_map[i] = bad_rows ? -1 : slot_of(a, page_shift, i, s_off, held, missing);
       if (missing) bits |= ECHO_DATA_NO_PAGES;
     }
   }
@@ -149,17 +159,24 @@ __global__ __launch_bounds__(kTableThreads) void build_tables_kernel(TablesArgs 
 
 __global__ __launch_bounds__(kMapThreads) void slot_map_kernel(TablesArgs a, int page_shift) {
   extern __shared__ int32_t s_off[];  // R + 1
-  for (int r = threadIdx.x; r <= a.R; r += kMapThreads) s_off[r] = a.row_offsets[r];
+  __shared__ bool s_bad[kMapThreads / kWave];
+  bool bad_rows = false;
+  for (int r = threadIdx.x; r <= a.R; r += kMapThreads) s_off[r] = row_offset(a, r, bad_rows);
+  const uint64_t bad_lanes = __ballot(bad_rows);
+  if ((threadIdx.x & (kWave - 1)) == 0) s_bad[threadIdx.x / kWave] = bad_lanes != 0ull;
   __syncthreads();
+  bad_rows = false;  // of any wave's: then no row has a slot
+#pragma unroll
+  for (int w = 0; w < kMapThreads / kWave; ++w) bad_rows |= s_bad[w];
   const int i = blockIdx.x * kMapThreads + threadIdx.x;
-  int bits = 0;
+  int bits = bad_rows ? ECHO_DATA_BAD_OFFSETS : 0;
   if (i < a.max_rows) {
     const auto held = [&](int r) {
       const int h = a.num_held_out[r];
       return h <= a.max_pages ? h : 0;
     };
-    bool missing;
-    a.slot_map[i] = slot_of(a, page_shift, i, s_off, held, missing);
+    bool missing = false;
+    a.slot_map[i] = bad_rows ? -1 : slot_of(a, page_shift, i, s_off, held, missing);
     if (missing) bits = ECHO_DATA_NO_PAGES;
   }
   wave_status_or(a.status, bits);
@@ -171,7 +188,7 @@ int32_t launch_build_block_tables(const TablesArgs& a, hipStream_t stream) {
   (void)hipGetLastError();
   int page_shift = 0;
   while ((1 << page_shift) < a.page_size) ++page_shift;
-  const bool map = a.slot_map != nullptr && a.max_rows > 0;
+  const bool map = a.slot_map != nullptr;
   const bool fused = map && a.max_rows <= kFusedRows;
   const size_t lds = (3 * size_t(a.R) + 2 + (fused ? size_t(a.R) + 1 : 0)) * sizeof(int32_t);
   if (lds > 60 * 1024 && hipFuncSetAttribute(reinterpret_cast<const void*>(build_tables_kernel),

@@ -395,3 +395,44 @@ def test_commit_of_the_longest_requests(below, accepted):
     want = sorted((P + i) % ps for i in range(1 + accepted)) if fits else []
     for t in page:
         assert t[0, 0].any(-1).nonzero()[:, 0].tolist() == want
+
+
+# ---- block tables -------------------------------------------------------------
+
+@pytest.mark.parametrize("max_rows", [60, 5000])
+@pytest.mark.parametrize("rows", [[0, 7, 5, 30], [-1, 3, 9, 20], [4, 9, 20, "past"], [0, 0, 0, "past"], [-9, -9, -9, -9],
+                                  ["past", 0, 1, 2], [0, 3, 9, "all"], [8, 8, 8, 8]])
+def test_row_offsets_that_cannot_be(rows, max_rows):
+    """Offsets that decrease, are negative or end past the slot map give no row a slot, and the status says
+    so, with the slots in the tables' launch and in one of their own; the pages are dealt all the same."""
+    from tests.test_gpu_kvq8 import _run_tables, _same_tables, _tables_case
+    rng = np.random.default_rng(70)
+    R, ps = 3, 32
+    c = _tables_case(rng, R, 4, ps, 9, 20)
+    c["ro"] = np.array([dict(past=max_rows + 1, all=max_rows).get(x, x) for x in rows], np.int32)
+    _log(f"[tables] row offsets {rows}, {max_rows} rows")
+    got = _run_tables(c, R, ps, max_rows, False)
+    want = kvq8.build_block_tables(c["want"], ps, c["bt"], c["held"], c["stack"], c["free"], c["ro"], c["start"], max_rows)
+    bad = "past" in rows or rows[0] < 0 or rows[2] < rows[1]
+    assert bool(got["status"] & st.BAD_OFFSETS) == bad
+    if bad:
+        assert np.all(got["slot_map"] == -1)
+    _same_tables(got, want)
+
+
+def test_row_offsets_without_rows():
+    """A slot map without rows: offsets that give requests rows end past it."""
+    import torch
+    import paper_2604_09603_amd as pkg
+    one = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda:0")  # noqa: E731
+    lib = pkg.load()
+    room = torch.full((4,), -7, dtype=torch.int64, device="cuda:0")
+    for offs, want in (((0, 0), 0), ((0, 1), st.BAD_OFFSETS)):
+        table, held, free, status = one(-1, -1), one(0), one(2), one(0)
+        stack, lens, rows, start = one(5, 6), one(40), one(*offs), one(0)
+        p = [t.data_ptr() for t in (lens, table, held, stack, free, rows, start, room, status)]
+        _log(f"[tables] no rows, offsets {offs}")
+        assert lib.echo_build_block_tables(p[0], 1, 32, p[1], 2, p[2], p[2], p[3], 2, p[4], p[4], p[5], p[6], 0, p[7], p[8],
+                                           torch.cuda.current_stream().cuda_stream) == pkg.OK
+        assert int(status.item()) == want and held.tolist() == [2] and table.tolist() == [6, 5]
+        assert room.tolist() == [-7] * 4
