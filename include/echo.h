@@ -446,7 +446,8 @@ int32_t echo_commit_kv(const int32_t* q_offsets, const int32_t* accept_len,
  * requests, KV heads and groups of 128 rows of a head (offsets that ask for more:
  * nothing is computed, ECHO_DATA_BAD_OFFSETS).  k_scale and v_scale are 4-byte
  * aligned, q, k_new, v_new, out and the pages 16-byte aligned.  Deterministic.
- * The workspace: echo_tree_verify_attn_paged_q8_workspace_size.
+ * The workspace: echo_tree_verify_attn_paged_q8_workspace_size; its bulk, 70 MB on 256
+ * CUs, is the same for every batch.
  */
 int32_t echo_tree_verify_attn_paged_q8(
     const uint16_t* q, const uint16_t* k_new, const uint16_t* v_new, int32_t kv_format,

@@ -529,8 +529,7 @@ size_t echo_tree_verify_attn_paged_q8_workspace_size(int32_t R, int32_t max_rows
   if (R < 1 || max_rows < 0 || num_q_heads < 1 || num_kv_heads < 1 ||
       head_dim != ECHO_HEAD_DIM || max_pages_per_request < 1)
     return 0;
-  return echo::attn_q8_workspace_bytes(R, max_rows, num_q_heads, num_kv_heads,
-                                       max_pages_per_request);
+  return echo::attn_q8_workspace_bytes(R, max_pages_per_request);
 }
 
 int32_t echo_tree_verify_attn_paged_q8(
@@ -563,8 +562,7 @@ int32_t echo_tree_verify_attn_paged_q8(
       !workspace)
     return ECHO_ERR_INVALID_ARG;
   if (!aligned256(workspace) ||
-      workspace_bytes < echo::attn_q8_workspace_bytes(R, max_rows, num_q_heads, num_kv_heads,
-                                                      max_pages_per_request))
+      workspace_bytes < echo::attn_q8_workspace_bytes(R, max_pages_per_request))
     return ECHO_ERR_WORKSPACE;
   const uintptr_t mis = reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(k_new) |
                         reinterpret_cast<uintptr_t>(v_new) | reinterpret_cast<uintptr_t>(out);

@@ -1185,8 +1185,8 @@ __global__ __launch_bounds__(256) void q8_combine_kernel(Q8Args a, Q8Ws ws) {
 
 }  // namespace
 
-size_t attn_q8_workspace_bytes(int32_t R, int32_t max_rows, int32_t hq, int32_t hkv,
-                               int32_t max_pages) {
+// Records and partial sums for every wave of the device, whatever the batch: 70 MB.
+size_t attn_q8_workspace_bytes(int32_t R, int32_t max_pages) {
   size_t n = 0;
   q8_layout(nullptr, R, max_pages, q8_waves(), &n);
   return n;

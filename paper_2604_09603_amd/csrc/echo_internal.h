@@ -154,8 +154,7 @@ struct AttnQ8Args {
   int32_t* status;
 };
 int32_t launch_tree_verify_attn_q8(const AttnQ8Args& a, hipStream_t stream);
-size_t attn_q8_workspace_bytes(int32_t R, int32_t max_rows, int32_t hq, int32_t hkv,
-                               int32_t max_pages);
+size_t attn_q8_workspace_bytes(int32_t R, int32_t max_pages);
 
 // Block tables from lengths (tables.hip); slot_map null: no slot map.
 struct TablesArgs {

@@ -28,13 +28,11 @@ template <>
 struct Fmt8<ECHO_KV_E4M3> {
   static constexpr float kMax = 448.0f;  // 1.75 * 2^8
   static constexpr int kMaxExp = 8;
-  static constexpr uint32_t kNan = 0x7Fu;
 };
 template <>
 struct Fmt8<ECHO_KV_E5M2> {
   static constexpr float kMax = 57344.0f;  // 1.75 * 2^15
   static constexpr int kMaxExp = 15;
-  static constexpr uint32_t kNan = 0x7Fu;
 };
 
 // Four values to four bytes, rounded to nearest even; beyond the largest value (an
