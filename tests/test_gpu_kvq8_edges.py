@@ -436,3 +436,133 @@ def test_row_offsets_without_rows():
                                            torch.cuda.current_stream().cuda_stream) == pkg.OK
         assert int(status.item()) == want and held.tolist() == [2] and table.tolist() == [6, 5]
         assert room.tolist() == [-7] * 4
+
+
+# ---- long ranges ----------------------------------------------------------------
+
+def _batch(lens, slots, hq, hkv, ps, fmt, seed, width=None, pool=None, head_scales=True):
+    """Requests over random pages of a pool (which they share), heads whose scores are flat and others whose few
+    largest have all the weight."""
+    rng = np.random.default_rng(seed)
+    need = [-(-int(n) // ps) for n in lens]
+    pages = pool or max(sum(need), 1)
+    cache = _pool(pages, hkv, ps, fmt, seed + 1)
+    table = np.full((len(need), width or max(max(need), 1)), -1, np.int32)
+    for r, n in enumerate(need):
+        table[r, :n] = rng.integers(0, pages, n)
+    qo = np.concatenate([[0], np.cumsum(slots)]).astype(np.int32)
+    cap = int(qo[-1])
+    scale = np.exp2(rng.integers(-1, 4, (cap, hq, 1))) if head_scales else 1.0
+    q = _bf16(rng.standard_normal((cap, hq, 128)) * scale)
+    kn, vn = (_bf16(rng.standard_normal((cap, hkv, 128))) for _ in range(2))
+    W = max(1, -(-max(slots) // 32))
+    mask = np.concatenate([np.zeros((0, W), np.uint32)] + [
+        np.pad(_chains(n, rng), ((0, 0), (0, W - max(1, -(-n // 32))))) for n in slots if n])
+    return [q, kn, vn, fmt, cache, ps, _dev(table), _dev(np.array(lens, np.int32)), _dev(qo), _dev(mask), hq, hkv]
+
+
+@pytest.mark.parametrize("fmt", [kvq8.E4M3, kvq8.E5M2])
+@pytest.mark.parametrize("R,slots,hq,kind", [(24, 1, 8, "waves alone"), (12, 5, 64, "gangs of two"), (6, 16, 64, "gangs of four"),
+                                             (6, 9, 64, "gangs of four, one without rows"),
+                                             (6, 20, 64, "gangs of four and waves alone"),
+                                             (5, 36, 64, "two passes of gangs of four and one of two")])
+def test_ranges_of_more_steps_than_a_table(R, slots, hq, kind, fmt):
+    """Ranges of 40 to 60 steps: what a wave knows of its steps, 32 of them, is filled again on the way."""
+    rng = np.random.default_rng(R)
+    lens = rng.integers(30000, 32769, R)
+    args = _batch(lens, [slots] * R, hq, 8, 64, fmt, 80 + slots, pool=700)
+    _log(f"[attn q8] {kind}, fmt={fmt}")
+    got = _attn(*args)
+    assert got[2] == 0
+    _check(got, _plain(*args, 128 ** -0.5), 5000, kind)
+
+
+@pytest.mark.parametrize("slots,kind", [(5, "a gang of four"), (3, "a gang of two")])
+def test_a_small_class_beside_a_large_one(slots, kind):
+    """One request whose heads take gangs of four (or of two) beside 900 whose rows are one wave's: its class has
+    two workgroups, and ranges of 45 (22) steps."""
+    R = 901
+    lens, n = np.full(R, 5600), [1] * R
+    n[500] = slots
+    lens[500] = 5600 * (1 if slots == 5 else 3)
+    args = _batch(lens, n, 16, 1, 64, kvq8.E4M3, 90, pool=900)
+    _log(f"[attn q8] {kind} beside 900 waves alone")
+    got = _attn(*args)
+    assert got[2] == 0
+    _check(got, _plain(*args, 128 ** -0.5), 64 * 100, kind)
+
+
+@pytest.mark.parametrize("width", [12, 600])
+@pytest.mark.parametrize("slots,hq", [((1,), 16), ((3, 5), 64), ((9, 12, 20), 64), ((0, 1, 2, 4, 9, 17), 64)])
+def test_many_short_requests_in_a_range(slots, hq, width):
+    """1500 requests of 0 to 700 tokens: a range goes through several of them and its table is filled across
+    their borders; every eighth has an id past the pool."""
+    rng = np.random.default_rng(100 + width + len(slots))
+    R, ps = 1500, 64
+    lens = rng.integers(0, 701, R)
+    lens[rng.random(R) < 0.1] = 0
+    args = _batch(lens, rng.choice(slots, R).tolist(), hq, 8, ps, kvq8.E4M3, 101, width=width, pool=64)
+    bad = args[6].cpu().numpy()
+    for r in range(3, R, 8):
+        if lens[r] > 0:
+            bad[r, int(rng.integers(0, -(-lens[r] // ps)))] = 64
+    args[6] = _dev(bad)
+    _log(f"[attn q8] 1500 requests of {slots} slots, width {width}")
+    got = _attn(*args)
+    assert got[2] == st.BAD_OFFSETS
+    _check(got, _plain(*args, 128 ** -0.5), 64 * 200, f"{slots}")
+
+
+# ---- offsets --------------------------------------------------------------------
+
+@pytest.mark.parametrize("width", [8, 600])
+@pytest.mark.parametrize("flaw", ["negative", "past the rows", "decreasing", "all"])
+def test_offsets_that_cannot_be(flaw, width):
+    """Requests whose rows are not the call's are left out, beside healthy ones of every size of gang."""
+    import torch
+    slots = [1, 3, 6, 2, 1, 9, 4, 1]
+    lens = [70, 200, 33, 0, 129, 300, 64, 5]
+    args = _batch(lens, slots, 16, 1, 64, kvq8.E4M3, 110, width=width)
+    qo = args[8].cpu().numpy().copy()
+    cap = int(qo[-1])
+    big = 2 ** 31 - 1
+    if flaw == "negative":
+        qo[0] = -1
+    elif flaw == "past the rows":
+        qo[-1] = cap + 1
+    elif flaw == "decreasing":
+        qo[3], qo[4] = big, qo[3]  # the third ends past the rows, the fourth begins there and ends before
+    else:
+        qo[0], qo[1], qo[4], qo[5], qo[-1] = -big - 1, 0, big, qo[4], -3
+    args[8] = _dev(qo)
+    _log(f"[attn q8] offsets {qo.tolist()}")
+    got = _attn(*args)
+    assert got[2] == st.BAD_OFFSETS
+    ref = _plain(*args, 128 ** -0.5)
+    assert 0 < int(torch.isnan(ref["lse"]).sum()) < cap * 16
+    _check(got, ref, 500, flaw)
+
+
+# ---- store ----------------------------------------------------------------------
+
+@pytest.mark.parametrize("T", [1023, 1024, 1025, 2048, 2049])
+def test_store_at_the_borders_of_rows_per_wave(T):
+    """With two heads, up to 1024 rows have waves of their own and up to 2048 share one with another: runs
+    that begin and end on either side of a wave's rows."""
+    from tests.test_gpu_kvq8 import _empty_cache, _same_bytes, _slots_of, _store, _values
+    rng = np.random.default_rng(T)
+    hkv, ps = 2, 64
+    lens, starts = [], []
+    while sum(lens) < T:
+        lens.append(min(int(rng.choice([1, 1, 2, 3, 33, 90])), T - sum(lens)))
+        starts.append(int(rng.integers(0, 70)))
+    slots, pages, _ = _slots_of(lens, starts, ps, rng)
+    k, v = _values(rng, T, hkv, 128), _values(rng, T, hkv, 128)
+    cache = _empty_cache(rng, pages, hkv, ps)
+    dev = [_dev(a) for a in cache]
+    _log(f"[store] {T} rows of two heads")
+    _store(_dev(k), _dev(v), _dev(slots), kvq8.E4M3, dev, ps)
+    *want, _ = kvq8.store_kv(k, v, slots, kvq8.E4M3, *cache)
+    for i in range(2):
+        _same_bytes(dev[i].cpu().numpy(), want[i], kvq8.E4M3, f"tensor {i}")
+        assert np.array_equal(dev[2 + i].cpu().numpy(), want[2 + i])
