@@ -566,3 +566,38 @@ def test_store_at_the_borders_of_rows_per_wave(T):
     for i in range(2):
         _same_bytes(dev[i].cpu().numpy(), want[i], kvq8.E4M3, f"tensor {i}")
         assert np.array_equal(dev[2 + i].cpu().numpy(), want[2 + i])
+
+
+@pytest.mark.parametrize("slots,hq", [(2, 4), (7, 16)])
+def test_one_request_of_64_million_tokens(slots, hq):
+    """A prefix that is one page of 2^20 tokens, 64 times: every wave fills its table again and again, and one
+    unit is merged from all waves' sums.  The same as one page whose keys have 64 times the weight."""
+    import torch
+    ps, times = 1 << 20, 64
+    cache = _pool(1, 1, ps, kvq8.E4M3, 120, spare=0)
+    q, kn, vn = _new(slots, hq, 1, 121, q_scale=4.0)
+    mask = _dev(_chains(slots, np.random.default_rng(122)))
+    i32 = dict(dtype=torch.int32, device="cuda:0")
+    _log(f"[attn q8] 2^26 tokens, {slots} slots")
+    got = _attn(q, kn, vn, kvq8.E4M3, cache, ps, _zeros(1, times), torch.tensor([ps * times], **i32),
+                torch.tensor([0, slots], **i32), mask, hq, 1)
+    assert got[2] == 0
+    K, V = (torch.cat([_decode(cache[i][0, 0], kvq8.E4M3) * cache[2 + i][0, 0].double().repeat_interleave(32)[:, None],
+                       x[:, 0].double()]) for i, x in ((0, kn), (1, vn)))
+    Q = q.double().view(slots * hq, 128) * 128 ** -0.5
+    j = torch.arange(slots, device="cuda:0")
+    see = (mask[:, j >> 5] >> (j & 31) & 1) > 0
+    z = Q @ K.T.contiguous()
+    za = Q.abs() @ K.abs().T.contiguous()
+    z[:, :ps] += float(np.log(times))
+    z[:, ps:].masked_fill_(~see.repeat_interleave(hq, 0), -float("inf"))
+    m = z.amax(-1, keepdim=True)
+    p = (z - m).exp_()
+    l = p.sum(-1, keepdim=True)
+    p /= l
+    o = p @ V
+    back = lambda x: x.view(slots, hq, -1)  # noqa: E731
+    ref = dict(out=back(o), lse=back(m + l.log())[..., 0], dev=back(((p @ (V * V)) - o * o).clamp_(min=0.0).sqrt_()),
+               mabs=back(p @ V.abs()), zabs=back(za.amax(-1, keepdim=True))[..., 0])
+    # a wave has 2^20 steps of 64 keys among 2048 waves (512 gangs of four), and as many parts
+    _check(got, ref, (1 << 20) * 64 // (2048 if slots * hq <= 32 else 512) * 1.15 + 2048, "2^26 tokens")
