@@ -737,7 +737,7 @@ __device__ __forceinline__ void run_segment(const MainArgs& a, const AttnWs& ws,
 #pragma unroll
         for (int c = 0; c < 4; ++c) mx = fmaxf(mx, fabsf(rt[i].o[dt][c]));
       mx = row_max4(mx);
-      e = mx > 0.0f ? __builtin_amdgcn_frexp_expf(mx) - 15 : 0;
+      e = mx > 0.0f ? max(__builtin_amdgcn_frexp_expf(mx) - 15, kPartMinExp) : 0;
     }
     const int rho = 16 * i + lr;
     if (rho < sm.rows) {

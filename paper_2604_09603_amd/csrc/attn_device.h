@@ -582,6 +582,10 @@ __host__ __device__ inline int part_dim(int d) {
   return (dt >> 1) * 32 + g * 8 + (dt & 1) * 4 + (d & 3);
 }
 
+// The smallest exponent of a partial row's scale: 2^126 is finite, 2^128 is not.  Rows below it
+// keep what the normal numbers have (2^-126 becomes 1).
+constexpr int kPartMinExp = -126;
+
 // Four dims of a partial row, back in the row's fp32 scale (e: its exponent).
 __device__ __forceinline__ floatx4 load_part_o(const AttnWs& ws, size_t prow, int d4, float e) {
   const halfx4 h = *reinterpret_cast<const halfx4*>(ws.part_o + prow * kD + part_dim(d4));

@@ -600,7 +600,7 @@ attn_wide_kernel(MainArgs a, AttnWs ws) {
 #pragma unroll
           for (int r = 0; r < 16; ++r) mx = fmaxf(mx, fabsf(o[dt][r]));
         mx = pair_max(mx);
-        const int e = mx > 0.0f ? __builtin_amdgcn_frexp_expf(mx) - 15 : 0;
+        const int e = mx > 0.0f ? max(__builtin_amdgcn_frexp_expf(mx) - 15, kPartMinExp) : 0;
         if (row_ok) {
           const float sc = __builtin_amdgcn_ldexpf(1.0f, -e);
           const int slot_id = lo < ud.tile_start ? 1 : 0;
