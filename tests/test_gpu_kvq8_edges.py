@@ -601,3 +601,98 @@ def test_one_request_of_64_million_tokens(slots, hq):
                mabs=back(p @ V.abs()), zabs=back(za.amax(-1, keepdim=True))[..., 0])
     # a wave has 2^20 steps of 64 keys among 2048 waves (512 gangs of four), and as many parts
     _check(got, ref, (1 << 20) * 64 // (2048 if slots * hq <= 32 else 512) * 1.15 + 2048, "2^26 tokens")
+
+
+# ---- other calls that the documentation allows --------------------------------------
+
+@pytest.mark.parametrize("slots,lens,hq,hkv", [([700, 1, 257], [1000, 64, 0], 4, 2), ([300], [31], 16, 1), ([1024, 33], [129, 2048], 8, 8)])
+def test_prompt_chunks(slots, lens, hq, hkv):
+    """Rows of a prompt over what is cached of it: a triangular mask of many words."""
+    args = _batch(lens, [1] * len(lens), hq, hkv, 64, kvq8.E4M3, 130, head_scales=False)
+    qo = np.concatenate([[0], np.cumsum(slots)]).astype(np.int32)
+    cap = int(qo[-1])
+    W = -(-max(slots) // 32)
+    mask = np.zeros((cap, W), np.uint32)
+    for r, n in enumerate(slots):
+        for j in range(n):
+            mask[qo[r] + j, :j >> 5] = 0xFFFFFFFF
+            mask[qo[r] + j, j >> 5] = (2 << (j & 31)) - 1
+    args[:3] = _new(cap, hq, hkv, 131, q_scale=2.0)
+    args[8], args[9] = _dev(qo), _dev(mask)
+    _log(f"[attn q8] prompt chunks of {slots} rows")
+    got = _attn(*args)
+    assert got[2] == 0
+    _check(got, _plain(*args, 128 ** -0.5), 4000, "chunks")
+
+
+def test_batch_of_paused_requests_only():
+    """No request has slots: nothing is written, and their pages are checked all the same."""
+    import torch
+    args = _batch([70, 0, 200], [0, 0, 0], 8, 2, 64, kvq8.E4M3, 140)
+    args[:3] = _new(5, 8, 2, 141)
+    args[9] = _zeros(5, 1)
+    for bad in (False, True):
+        if bad:
+            args[6][2, 1] = -1
+        _log(f"[attn q8] paused requests only, bad={bad}")
+        out, lse, status = _attn(*args)
+        assert status == (st.BAD_OFFSETS if bad else 0)
+        assert bool(torch.isnan(out).all()) and bool(torch.isnan(lse).all())
+
+
+@pytest.mark.parametrize("rows", [2000, 5000])
+def test_captured_tables_of_the_largest_batch(rows):
+    """4095 requests, whose offsets take more shared memory than a kernel has by itself, captured and replayed on
+    changing lengths with eager work between: every replay is the eager call."""
+    import torch
+    import paper_2604_09603_amd as pkg
+    rng = np.random.default_rng(150)
+    R, most, ps, free = 4095, 3, 16, 9000
+    held0 = rng.integers(0, most + 1, R).astype(np.int32)
+    total = int(held0.sum()) + free
+    perm = rng.permutation(total).astype(np.int32)
+    bt0, at = np.full((R, most), -1, np.int32), 0
+    for r in range(R):
+        bt0[r, :held0[r]] = perm[at:at + held0[r]]
+        at += int(held0[r])
+    stack0 = np.full(total, -5, np.int32)
+    stack0[:free] = perm[at:]
+    init = [_dev(x) for x in (held0, bt0, stack0, np.array([free], np.int32))]
+    held, bt, stack, nfree = (t.clone() for t in init)
+    n = rng.multinomial(rows, np.ones(R) / R)
+    ro = _dev(np.concatenate([[0], np.cumsum(n)]).astype(np.int32))
+    want, start, status = _zeros(R), _zeros(R), _zeros(1)
+    sm = torch.zeros(rows + 9, dtype=torch.int64, device="cuda:0")
+
+    def call():
+        pkg.echo_build_block_tables(want, R, ps, bt, held, held, stack, nfree, nfree, row_offsets=ro, row_start=start,
+                                    slot_map=sm, status=status)
+
+    def reset(seed):
+        g = np.random.default_rng(seed)
+        w = g.integers(0, most * ps + 1, R).astype(np.int32)
+        want.copy_(_dev(w))
+        start.copy_(_dev(np.maximum(0, w - n).astype(np.int32)))
+        for t, u in zip((held, bt, stack, nfree), init):
+            t.copy_(u)
+        sm.fill_(-77)
+        status.zero_()
+
+    def fetch():
+        torch.cuda.synchronize()
+        return [t.cpu().numpy() for t in (held, bt, stack, nfree, sm, status)]
+
+    eager = []
+    for seed in range(3):
+        reset(seed)
+        call()
+        eager.append(fetch())
+    graph = torch.cuda.CUDAGraph()
+    _log(f"[tables] 4095 requests captured, {rows} rows")
+    with torch.cuda.graph(graph):
+        call()
+    for i in (1, 0, 2, 1):
+        reset(i)
+        graph.replay()
+        for k, (a, b) in enumerate(zip(fetch(), eager[i])):
+            assert np.array_equal(a, b), (i, k)
