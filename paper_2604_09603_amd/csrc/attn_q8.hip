@@ -19,16 +19,17 @@
 //               exponent.
 //   q8_combine  merges the partial sums of units that several waves share.
 //
-// What bounds it.  Few rows per head: HBM.  64 requests decoding over 1024-8192 tokens (32
-// query and 8 KV heads, 604 MB) take 91 us in the main kernel, 6.7 TB/s, and 6 us in the
-// merge; the 10 us until the first tiles are there (lengths, page ids, scales and tiles are
+// What bounds it (medians of 60 launches; whole calls back to back are up to 5% shorter than their
+// kernels under the profiler).  Few rows per head: HBM.  64 requests decoding over 1024-8192
+// tokens (32 query and 8 KV heads, 604 MB) take 97 us in the main kernel, 6.2 TB/s, and 6 us in
+// the merge; the 10 us until the first tiles are there (lengths, page ids, scales and tiles are
 // dependent round trips) are most of the rest.  Many rows: the vector instructions.  A step
 // of 64 keys and 32 rows takes 32 matrix products (1044 cycles) and about 400 other vector
 // instructions (1700 cycles: 128 conversions, 32 exponentials of two each, 96 products,
 // sums and roundings of the weights), which share a SIMD's issue; with trees of 13 slots on
 // average (16 rows each) over 16384-32768 tokens, 79 us of products, the main kernel takes
-// 210 us, 64% of it issuing vector instructions.  128 trees of 3 slots on average (617 MB) are
-// between the two: 140 us and 11 in the merge.  Units of 32 rows because a 32x32x16 product
+// 234 us, 64% of it issuing vector instructions.  128 trees of 3 slots on average (617 MB) are
+// between the two: 145 us and 11 in the merge.  Units of 32 rows because a 32x32x16 product
 // leaves room for five vector instructions, where 16x16x32 leaves two for the same work;
 // two waves per SIMD, so that one's softmax runs beside the other's products.
 //
@@ -121,8 +122,8 @@ struct Q8Args {
 };
 
 // Narrow tables need a few loads a wave and request; a launch of its own costs 2 us, which wide
-// ones are worth (waves | launch: 64 pages 20.2 | 22.6 us, 512 pages 45.5 | 47.6, 2048 pages
-// 115 | 111).
+// ones are worth (64 requests of so many pages of 32 tokens, 8 heads, waves | launch: 64 pages
+// 32.0 | 34.0 us, 512 pages 133 | 134, 2048 pages 487 | 486).
 __host__ inline int q8_page_chunks(int max_pages) {
   return max_pages <= kOwnPages ? 0 : (max_pages + kPageChunk - 1) / kPageChunk;
 }
@@ -987,7 +988,7 @@ __device__ __forceinline__ void q8_segment(const Q8Args& a, const Q8Ws& ws, cons
     const float c[2] = {lane_of(tb.c, i), lane_of(tb.c, i + 1)};
     const float lvs[2] = {lane_of(tb.lvs, i), lane_of(tb.lvs, i + 1)};
     // Without priorities the older of a SIMD's two waves goes first in every phase, and the other
-    // ends its range long after it (a long context: 231 us without, 225 with).
+    // ends its range long after it (a long context: 239 us without, 229 with).
     __builtin_amdgcn_s_setprio(1);
     q8_values<2>(
         [&](int g, int dt) {

@@ -9,9 +9,9 @@
 //
 // A block's scale is the maximum over its new values, so a wave holds a whole block's new
 // rows in registers: they are read once, and written once as bytes.  Prompts are bound
-// by HBM: 40960 rows of eight heads, 252 MB, in 52.8 us, 4.8 TB/s (a large copy on the same
-// card moves 4.9-5.4).  Single tokens (128 rows of four heads: 4.3 us) and commits (128
-// requests: 4.7 us) are bound by latency: the slot, the row and the block's scale and bytes
+// by HBM: 40960 rows of eight heads, 252 MB, in 53.4 us a call back to back, 4.7 TB/s (a large copy
+// on the same card moves 4.4-5.3, by its size).  Single tokens (128 rows of four heads: 4.3 us
+// a kernel, median) and commits (128 requests: 5.0 us) are bound by latency: the slot, the row and the block's scale and bytes
 // are two or three dependent round trips.
 #include "kvq8_device.h"
 
@@ -21,9 +21,9 @@ namespace {
 constexpr int kStoreThreads = 256;
 // Rows per wave: as few as this many waves allow, up to a block's.  A wave with many rows
 // appends the runs that start in them one after another, 1.5 us each; a wave that starts
-// no run is a launch for nothing.  With eight heads, 1 | 8 | 32 rows per wave: 1024 single
-// tokens take 15.9 | 16.7 | 54 us (by the rule, 4: 11.9), 2048 prompt rows 21.8 | 10.5 |
-// 10.5 us (8), 40960 prompt rows 356 | 144 | 49 us (32).
+// no run is a launch for nothing.  With eight heads, 1 | 8 | 32 rows per wave, the same rows over
+// and over (so from the caches): 1024 single tokens take 16.2 | 17.4 | 55 us (by the rule, 4:
+// 13.3), 2048 prompt rows 22 | 10.6 | 8.8 us (8), 40960 prompt rows 356 | 143 | 51 us (32).
 constexpr int kStoreWaves = 4096;
 constexpr int kCommitQ8Threads = 1024;
 

@@ -9,9 +9,9 @@
 //
 // Both are bound by latency: the 16 bytes a request and the 4 bytes a page of the first
 // fit in the caches, and the second writes 8 bytes a row.  128 requests that take a token
-// each: 5.8 us, most of it the launch and three dependent round trips to memory (lengths,
+// each: 5.7 us, most of it the launch and three dependent round trips to memory (lengths,
 // stack, tables) with their barriers; 256 requests with prompts of up to 2048 rows: 7.4 and
-// 4.0 us.
+// 4.2 us (medians).
 #include "echo_device.h"
 #include "echo_internal.h"
 
@@ -21,8 +21,8 @@ namespace {
 constexpr int kTableThreads = 1024;
 constexpr int kMapThreads = 256;
 // Slot maps up to this long need no second launch.  With 128 requests, here | in a launch of
-// its own: 512 rows 6.2 | 7.7 us, 2048 rows 7.5 | 7.8 (and a launch less for the host), 4096
-// rows 9.8 | 7.9, 32768 rows 42 | 7.9.
+// its own (calls back to back): 512 rows 6.3 | 9.0 us, 2048 rows 7.5 | 9.0, 4096 rows
+// 9.6 | 9.0, 32768 rows 39 | 9.3.
 constexpr int kFusedRows = 2 * kTableThreads;
 
 // Offset r of the rows; bad if it is not one of non-decreasing numbers in [0, max_rows].
