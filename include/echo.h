@@ -382,9 +382,9 @@ int32_t echo_accept_logits(const int32_t* q_offsets, const int32_t* slot_parent,
  * positions prefix_len[r], prefix_len[r] + 1, ... (page layout as for
  * echo_tree_verify_attn_paged), and prefix_len[r] grows by 1 + accept_len[r]
  * (in place).  The caller provides the pages: if a position needs a page id
- * outside [0, num_pages), or a slot index is outside [0, max_rows), nothing
- * of that request is written (ECHO_DATA_BAD_OFFSETS).  Requests without slots
- * are left unchanged.
+ * outside [0, num_pages), a slot index is outside [0, max_rows), or the new
+ * length would be 2^31 or more, nothing of that request is written
+ * (ECHO_DATA_BAD_OFFSETS).  Requests without slots are left unchanged.
  *   accept_len [R], accept_slots [R][max_depth]  as written by echo_accept
  *   k_new, v_new [max_rows][Hkv][128] bf16; k_pages, v_pages as above
  *   page_size   any positive size; pointers 16-byte aligned

@@ -124,7 +124,7 @@ def commit_kv(q_offsets, accept_len, accept_slots, k_new, v_new, k_pages, v_page
             p = P + j
             e = p // page_size
             page = int(block_table[r, e]) if 0 <= e < block_table.shape[1] else -1
-            if page < 0 or page >= kp.shape[0]:
+            if page < 0 or page >= kp.shape[0] or p >= (1 << 31) - 1:
                 dest = None
                 break
             dest.append((page, p % page_size))

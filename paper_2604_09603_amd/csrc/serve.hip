@@ -261,7 +261,8 @@ __global__ __launch_bounds__(kCommitThreads) void commit_kv_kernel(
     const long long pos = (long long)P + j;
     const long long e = pos / page_size;
     const int page = e < max_pages ? block_table[size_t(r) * max_pages + size_t(e)] : -1;
-    if (s < 0 || s >= max_rows || page < 0 || page >= num_pages) atomicOr(&s_bad, 1);
+    // (the new length stays below 2^31)
+    if (s < 0 || s >= max_rows || page < 0 || page >= num_pages || pos >= 0x7FFFFFFF) atomicOr(&s_bad, 1);
     s_slot[j] = s;
     s_dst[j] = (long long)page * page_size + (pos % page_size);
   }

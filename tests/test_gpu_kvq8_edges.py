@@ -397,6 +397,32 @@ def test_commit_of_the_longest_requests(below, accepted):
         assert t[0, 0].any(-1).nonzero()[:, 0].tolist() == want
 
 
+def _one(x):
+    import torch
+    return torch.tensor(x, dtype=torch.int32, device="cuda:0")
+
+
+@pytest.mark.parametrize("below,accepted", [(5, 4), (1, 0), (0, 0), (4, 4)])
+def test_commit_of_the_longest_requests_in_bf16(below, accepted):
+    """The same with the bfloat16 cache."""
+    import torch
+    import paper_2604_09603_amd as pkg
+    ps, depth, top = 1 << 20, 4, (1 << 31) - 1
+    P = top - below
+    fits = 1 + accepted <= below
+    kn = torch.ones((depth + 1, 1, 128), dtype=torch.bfloat16, device="cuda:0")
+    page = [torch.zeros((1, ps, 1, 128), dtype=torch.bfloat16, device="cuda:0") for _ in range(2)]
+    status, length = _zeros(1), _one([P])
+    _log(f"[commit] bf16, {P} tokens and {1 + accepted} more")
+    pkg.echo_commit_kv(_one([0, depth + 1]), _one([accepted]), _one([[1, 2, 3, 4]]), depth, kn, kn, 1, depth + 1, 1,
+                       *page, ps, _zeros(1, 2049), length, status=status)
+    assert int(status.item()) == (0 if fits else st.BAD_OFFSETS)
+    assert int(length.item()) == (P + 1 + accepted if fits else P)
+    want = sorted((P + i) % ps for i in range(1 + accepted)) if fits else []
+    for t in page:
+        assert (t[0, :, 0] != 0).any(-1).nonzero()[:, 0].tolist() == want
+
+
 # ---- block tables -------------------------------------------------------------
 
 @pytest.mark.parametrize("max_rows", [60, 5000])
