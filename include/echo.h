@@ -74,6 +74,20 @@ typedef void* echo_stream_t; /* hipStream_t */
 #define ECHO_KV_E5M2 1   /* 8-bit float, 5 exponent bits, largest value 57344 (OCP) */
 #define ECHO_KV_BLOCK 32 /* tokens that share a scale (per head)                    */
 
+/* ---- rotary positions -------------------------------------------------- */
+#define ECHO_ROPE_HALF 0        /* pair i: dims i and i + rot_dim / 2               */
+#define ECHO_ROPE_INTERLEAVED 1 /* pair i: dims 2 i and 2 i + 1                     */
+#define ECHO_ROPE_MAX_DIM 1024  /* largest rotated part of a head                   */
+#define ECHO_ROPE_PLAIN 0       /* scalings of the frequencies:                     */
+#define ECHO_ROPE_LINEAR 1      /*   echo_rope_frequencies                          */
+#define ECHO_ROPE_BASE 2
+#define ECHO_ROPE_BANDS 3
+#define ECHO_ROPE_SMOOTH 4
+
+/* ---- latent cache ------------------------------------------------------ */
+#define ECHO_LATENT_DIM 512     /* the only supported latent dimension              */
+#define ECHO_LATENT_ROPE_DIM 64 /* the only supported rotated dimension beside it   */
+
 /*
  * echo_gate -- path scores and the global top-B selection.
  *
@@ -501,6 +515,115 @@ int32_t echo_commit_kv_q8(const int32_t* q_offsets, const int32_t* accept_len,
                           int64_t num_pages, int32_t page_size, const int32_t* block_table,
                           int32_t max_pages_per_request, const int32_t* prefix_len,
                           int32_t* new_len, int32_t* status, echo_stream_t stream);
+
+/*
+ * echo_rope -- rotary positions of queries and keys, in one launch: what
+ * echo_tree_verify_attn and its paged forms take as q, k_new and cached keys.
+ *
+ * Pair i of a head's rotated part, (a, b), becomes
+ *   scale * (a cos t - b sin t, b cos t + a sin t),  t = positions[row] * inv_freq[i]
+ * with t in 64 bits, cosine and sine (with the scale) and the products in fp32, rounded
+ * once to bf16.  The rotated part is what the pointers name: rot_dim dims of each
+ * head from q + row * q_row_stride + head * q_head_stride on.  A head's other dims
+ * take no part and are not copied.
+ *   q, k         bf16; strides in elements, rows or heads outermost, 0 for one that is
+ *                repeated.  Either may be left out (its number of heads 0)
+ *   q_out, k_out bf16; q and k themselves with the same strides (in place), or
+ *                memory that overlaps neither; rows and heads of their own
+ *   positions    [num_rows] int32 (echo_build_tree_mask's position_ids), of any sign:
+ *                negated frequencies turn back, and give the gradient of q and k
+ *   row_count    [1] int32 (nullable: all num_rows) how many rows exist, q_offsets + R
+ *                of a step; later rows are left untouched.  A count outside
+ *                [0, num_rows]: nothing is done (ECHO_DATA_BAD_OFFSETS)
+ *   rot_dim      even, 2 .. ECHO_ROPE_MAX_DIM
+ *   inv_freq     [rot_dim / 2] double, finite: a table of echo_rope_frequencies
+ *   scale        finite (ECHO_ERR_INVALID_ARG)
+ * Rows whose pointers are 16-byte aligned, strides multiples of 8 and rot_dim one of 16
+ * go 16 bytes at a time.
+ */
+int32_t echo_rope(const uint16_t* q, int64_t q_row_stride, int64_t q_head_stride, uint16_t* q_out,
+                  int64_t q_out_row_stride, int64_t q_out_head_stride, int32_t num_q_heads,
+                  const uint16_t* k, int64_t k_row_stride, int64_t k_head_stride, uint16_t* k_out,
+                  int64_t k_out_row_stride, int64_t k_out_head_stride, int32_t num_k_heads,
+                  const int32_t* positions, int32_t num_rows, const int32_t* row_count,
+                  int32_t rot_dim, int32_t layout, const double* inv_freq, float scale,
+                  int32_t* status, echo_stream_t stream);
+
+/*
+ * echo_rope_frequencies -- the table of inverse frequencies, on the HOST (both outputs
+ * are host memory; no GPU is used).  f_i = base^(-2 i / rot_dim), then by `scaling`:
+ *   ECHO_ROPE_PLAIN   as they are
+ *   ECHO_ROPE_LINEAR  f_i / factor (positions pressed together)
+ *   ECHO_ROPE_BASE    of the base base * factor^(rot_dim / (rot_dim - 2)): the longest
+ *                     wave is stretched by factor, the shortest is kept (rot_dim > 2)
+ *   ECHO_ROPE_BANDS   f_i / factor above the dim whose wave turns low_turns times within
+ *                     original_len positions, f_i below the one that turns high_turns
+ *                     times, a linear ramp over the dims between (whole ones); *scale is
+ *                     0.1 ln(factor) + 1 (factor > 1)
+ *   ECHO_ROPE_SMOOTH  f_i (s + (1 - s) / factor), s = (turns - low_turns) /
+ *                     (high_turns - low_turns) within [0, 1], turns those of f_i within
+ *                     original_len positions
+ *   base > 1, factor >= 1, all finite; for the last two original_len > 0 and
+ *   0 < low_turns < high_turns
+ *   inv_freq [rot_dim / 2], scale [1]: 1 but for ECHO_ROPE_BANDS
+ */
+int32_t echo_rope_frequencies(int32_t rot_dim, double base, int32_t scaling, double factor,
+                              double original_len, double low_turns, double high_turns,
+                              double* inv_freq, float* scale);
+
+/*
+ * The latent paged cache -- one row per token for all heads (latent attention):
+ *   pages [num_pages][page_size][576] bf16
+ * Dims 0-511 are the normalised latent vector, keys and values of every head (the
+ * heads' own projections are absorbed into the query and the output); dims 512-575
+ * are rotated and only the scores see them.  Page size, block tables and lengths are
+ * those of echo_tree_verify_attn_paged.  Limits of all calls: num_pages * page_size
+ * < 2^31; pages 16-byte aligned.
+ */
+
+/*
+ * echo_store_latent -- rows of the projection's output, normalised and rotated, into the
+ * latent cache at the slots of a slot map (prompts, or the token that each request
+ * decoded), beside a draft tree (latent_new, for echo_tree_verify_attn_latent), or both.
+ *
+ *   dims 0-511    x * rsqrt(mean(x^2) + eps) * norm_weight, in fp32, rounded once to bf16
+ *   dims 512-575  rotated as by echo_rope at positions[row]
+ *   kv           [num_rows] rows of 576 bf16, kv_stride elements apart (a multiple of 8, at
+ *                least 576); 16-byte aligned
+ *   norm_weight  [512] bf16, 16-byte aligned; null: dims 0-511 are copied
+ *   inv_freq     [32] double; null: dims 512-575 are copied (positions are not read)
+ *   row_count    as for echo_rope
+ *   latent_new   [num_rows][576] bf16 (nullable), 16-byte aligned; not kv itself
+ *   slot_map     [num_rows] int64 (nullable; then pages, num_pages and page_size are not
+ *                looked at): as echo_build_block_tables writes them.  A negative slot
+ *                leaves its row out of the cache; one of num_pages * page_size or more
+ *                does too, with ECHO_DATA_BAD_OFFSETS.  The same slot twice: unspecified
+ *                contents of that slot
+ * One of latent_new and slot_map has to be given.
+ */
+int32_t echo_store_latent(const uint16_t* kv, int64_t kv_stride, const uint16_t* norm_weight,
+                          float eps, const int32_t* positions, const double* inv_freq,
+                          float rope_scale, int32_t layout, int32_t num_rows,
+                          const int32_t* row_count, int32_t latent_dim, int32_t rope_dim,
+                          uint16_t* latent_new, const int64_t* slot_map, uint16_t* pages,
+                          int64_t num_pages, int32_t page_size, int32_t* status,
+                          echo_stream_t stream);
+
+/*
+ * echo_commit_latent -- echo_commit_kv_q8 for the latent cache: each request's root and
+ * accepted rows of latent_new are appended, and new_len[r] = prefix_len[r] + 1 +
+ * accept_len[r]; what leaves a request as it is, is the same.
+ *   latent_new [max_rows][576] bf16, 16-byte aligned
+ *   new_len    [R] int32, may be prefix_len itself
+ *   page_size  a power of two, >= 32
+ */
+int32_t echo_commit_latent(const int32_t* q_offsets, const int32_t* accept_len,
+                           const int32_t* accept_slots, int32_t max_depth,
+                           const uint16_t* latent_new, int32_t R, int32_t max_rows,
+                           int32_t latent_dim, int32_t rope_dim, uint16_t* pages,
+                           int64_t num_pages, int32_t page_size, const int32_t* block_table,
+                           int32_t max_pages_per_request, const int32_t* prefix_len,
+                           int32_t* new_len, int32_t* status, echo_stream_t stream);
 
 /*
  * echo_build_block_tables -- the pages of a batch from its lengths (block

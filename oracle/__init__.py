@@ -26,6 +26,8 @@ Stages (each module cites the passage it follows):
                verification attention over that paged cache.
 * ``kvq8``   -- the 8-bit paged cache (formats, block scales, writers, attention over
                it) and the block tables that give requests their pages.
+* ``latent`` -- rotary positions, the latent paged cache (its writers, and the tree
+               attention over it).
 * ``accept`` -- greedy (temperature 0) acceptance of the longest draft path
                matching the target argmax (Section 2, standard SD).
 
@@ -40,4 +42,4 @@ from .mask import build_tree_mask
 from .attn import tree_verify_attn
 from .accept import accept
 from .serve import target_argmax, accept_from_logits, tree_verify_attn_paged, commit_kv
-from . import kvq8
+from . import kvq8, latent

@@ -36,6 +36,14 @@ KV_E4M3 = 0
 KV_E5M2 = 1
 KV_BLOCK = 32
 
+ROPE_HALF = 0
+ROPE_INTERLEAVED = 1
+ROPE_MAX_DIM = 1024
+ROPE_SCALINGS = {"plain": 0, "linear": 1, "base": 2, "bands": 3, "smooth": 4}
+
+LATENT_DIM = 512
+LATENT_ROPE_DIM = 64
+
 EXPORTS = [
     "echo_gate", "echo_gate_workspace_size", "echo_gate_sparse", "echo_gate_sparse_workspace_size",
     "echo_gate_elastic", "echo_gate_elastic_workspace_size",
@@ -46,7 +54,8 @@ EXPORTS = [
     "echo_probe_stream_read", "echo_gate_noalloc", "echo_verify_step", "echo_status_string",
     "echo_version", "echo_tree_verify_attn_paged_q8",
     "echo_tree_verify_attn_paged_q8_workspace_size", "echo_store_kv_q8", "echo_commit_kv_q8",
-    "echo_build_block_tables",
+    "echo_build_block_tables", "echo_rope", "echo_rope_frequencies", "echo_store_latent",
+    "echo_commit_latent",
 ]
 GATE_SCRATCH_BYTES = 8 << 20
 
@@ -58,6 +67,7 @@ _I32 = ctypes.c_int32
 _I64 = ctypes.c_int64
 _SZ = ctypes.c_size_t
 _F32 = ctypes.c_float
+_F64 = ctypes.c_double
 
 _SIGS = {
     "echo_gate": (_I32, [_P, _P, _P, _I32, _I32, _I32, _P, _P, _P, _P, _SZ, _P, _P]),
@@ -105,6 +115,13 @@ _SIGS = {
                                  _P, _P, _I64, _I32, _P, _I32, _P, _P, _P, _P]),
     "echo_build_block_tables": (_I32, [_P, _I32, _I32, _P, _I32, _P, _P, _P, _I32, _P, _P, _P,
                                        _P, _I32, _P, _P, _P]),
+    "echo_rope": (_I32, [_P, _I64, _I64, _P, _I64, _I64, _I32, _P, _I64, _I64, _P, _I64, _I64,
+                         _I32, _P, _I32, _P, _I32, _I32, _P, _F32, _P, _P]),
+    "echo_rope_frequencies": (_I32, [_I32, _F64, _I32, _F64, _F64, _F64, _F64, _P, _P]),
+    "echo_store_latent": (_I32, [_P, _I64, _P, _F32, _P, _P, _F32, _I32, _I32, _P, _I32, _I32, _P,
+                                 _P, _P, _I64, _I32, _P, _P]),
+    "echo_commit_latent": (_I32, [_P, _P, _P, _I32, _P, _I32, _I32, _I32, _I32, _P, _I64, _I32,
+                                  _P, _I32, _P, _P, _P, _P]),
     "echo_status_string": (ctypes.c_char_p, [_I32]),
     "echo_version": (ctypes.c_char_p, []),
 }
@@ -476,4 +493,78 @@ def echo_build_block_tables(want_len, R, page_size, block_table, num_held, num_h
         _stream(stream))
     if check:
         _check(code, "echo_build_block_tables")
+    return code
+
+
+def _head_strides(t, rows, heads, rot_dim):
+    """Row and head strides of [rows, heads, rot_dim] (the stride of a dimension of size 1 says
+    nothing)."""
+    if t is None:
+        return 0, 0
+    s = t.stride()
+    if len(s) != 3 or s[-1] != 1 or t.shape[1] != heads or t.shape[2] != rot_dim or t.shape[0] < rows:
+        raise ValueError("q and k are [rows, heads, rot_dim] with contiguous dims")
+    return s[0] if t.shape[0] > 1 else heads * max(s[1], rot_dim), s[1] if heads > 1 else rot_dim
+
+
+def echo_rope(q, q_out, k, k_out, positions, num_rows, hq, hk, rot_dim, layout, inv_freq, scale,
+              row_count=None, status=None, stream=None, check=True):
+    """Rotary positions of queries and keys.  Device tensors; q and k (k may be None with hk 0)
+    are [rows, heads, rot_dim] bf16 bits, views of the rotated part of each head with any
+    strides; q_out may be q and k_out k; positions int32, inv_freq float64 [rot_dim / 2]."""
+    qr, qh = _head_strides(q, num_rows, hq, rot_dim)
+    qor, qoh = _head_strides(q_out, num_rows, hq, rot_dim)
+    kr, kh = _head_strides(k, num_rows, hk, rot_dim)
+    kor, koh = _head_strides(k_out, num_rows, hk, rot_dim)
+    code = load().echo_rope(_ptr(q), qr, qh, _ptr(q_out), qor, qoh, hq, _ptr(k), kr, kh, _ptr(k_out),
+                            kor, koh, hk, _ptr(positions), num_rows, _ptr(row_count), rot_dim, layout,
+                            _ptr(inv_freq), scale, _ptr(status), _stream(stream))
+    if check:
+        _check(code, "echo_rope")
+    return code
+
+
+def echo_rope_frequencies(rot_dim, base, scaling="plain", factor=1.0, original_len=0.0,
+                          low_turns=1.0, high_turns=32.0):
+    """Inverse frequencies of rotary positions (a list of rot_dim / 2 floats, for a float64 tensor)
+    and the factor on cosines and sines.  Computed on the host."""
+    f = (ctypes.c_double * max(int(rot_dim) // 2, 1))()
+    scale = ctypes.c_float()
+    _check(load().echo_rope_frequencies(rot_dim, base, ROPE_SCALINGS[scaling], factor, original_len,
+                                        low_turns, high_turns, ctypes.cast(f, _P),
+                                        ctypes.addressof(scale)), "echo_rope_frequencies")
+    return list(f), scale.value
+
+
+def echo_store_latent(kv, norm_weight, eps, positions, inv_freq, rope_scale, layout, num_rows,
+                      latent_dim, rope_dim, latent_new, slot_map, pages, page_size, row_count=None,
+                      status=None, stream=None, check=True):
+    """Normalise and rotate rows into the latent paged cache (slot_map, pages), beside a draft
+    tree (latent_new), or both.  Device tensors; kv is [num_rows, 576] bf16 bits whose rows may
+    be strided, norm_weight [512] bf16 bits or None, inv_freq float64 [32] or None, slot_map
+    int64."""
+    s = kv.stride()
+    if s[-1] != 1:
+        raise ValueError("the dims of a row of kv must be contiguous")
+    code = load().echo_store_latent(
+        _ptr(kv), s[0] if kv.shape[0] > 1 else latent_dim + rope_dim, _ptr(norm_weight), eps,
+        _ptr(positions), _ptr(inv_freq), rope_scale, layout, num_rows, _ptr(row_count), latent_dim,
+        rope_dim, _ptr(latent_new), _ptr(slot_map), _ptr(pages),
+        0 if pages is None else pages.shape[0], page_size, _ptr(status), _stream(stream))
+    if check:
+        _check(code, "echo_store_latent")
+    return code
+
+
+def echo_commit_latent(q_offsets, accept_len, accept_slots, max_depth, latent_new, R, max_rows,
+                       latent_dim, rope_dim, pages, page_size, block_table, prefix_len, new_len,
+                       status=None, stream=None, check=True):
+    """Append each request's root and accepted rows to its latent paged cache; new_len may be
+    prefix_len."""
+    code = load().echo_commit_latent(
+        _ptr(q_offsets), _ptr(accept_len), _ptr(accept_slots), max_depth, _ptr(latent_new), R,
+        max_rows, latent_dim, rope_dim, _ptr(pages), pages.shape[0], page_size, _ptr(block_table),
+        block_table.shape[1], _ptr(prefix_len), _ptr(new_len), _ptr(status), _stream(stream))
+    if check:
+        _check(code, "echo_commit_latent")
     return code

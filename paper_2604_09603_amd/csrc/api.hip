@@ -1,6 +1,8 @@
 // C ABI entry points: host-side argument checks, workspace sizing, launch.
 #include <hip/hip_runtime.h>
 
+#include <math.h>
+
 #include <mutex>
 #include <vector>
 
@@ -656,6 +658,176 @@ int32_t echo_build_block_tables(const int32_t* want_len, int32_t R, int32_t page
                            num_held_out, free_pages, max_free, num_free, num_free_out,
                            row_offsets, row_start, max_rows, slot_map, status};
   return echo::launch_build_block_tables(a, as_stream(stream));
+}
+
+}  // extern "C"
+
+extern "C" {
+
+int32_t echo_rope(const uint16_t* q, int64_t q_row_stride, int64_t q_head_stride, uint16_t* q_out,
+                  int64_t q_out_row_stride, int64_t q_out_head_stride, int32_t num_q_heads,
+                  const uint16_t* k, int64_t k_row_stride, int64_t k_head_stride, uint16_t* k_out,
+                  int64_t k_out_row_stride, int64_t k_out_head_stride, int32_t num_k_heads,
+                  const int32_t* positions, int32_t num_rows, const int32_t* row_count,
+                  int32_t rot_dim, int32_t layout, const double* inv_freq, float scale,
+                  int32_t* status, echo_stream_t stream) {
+  if (num_rows < 0 || num_q_heads < 0 || num_k_heads < 0 || rot_dim < 2 || rot_dim % 2 != 0)
+    return ECHO_ERR_INVALID_ARG;
+  if (layout != ECHO_ROPE_HALF && layout != ECHO_ROPE_INTERLEAVED) return ECHO_ERR_INVALID_ARG;
+  if (!isfinite(scale)) return ECHO_ERR_INVALID_ARG;
+  // (a workgroup numbers a row's pairs of all heads in 32 bits)
+  const int64_t heads = int64_t(num_q_heads) + num_k_heads;
+  if (rot_dim > ECHO_ROPE_MAX_DIM || heads > (1 << 16)) return ECHO_ERR_UNSUPPORTED;
+  if (num_rows == 0 || heads == 0) return ECHO_OK;
+  if (!positions || !inv_freq) return ECHO_ERR_INVALID_ARG;
+  if ((num_q_heads > 0 && (!q || !q_out)) || (num_k_heads > 0 && (!k || !k_out)))
+    return ECHO_ERR_INVALID_ARG;
+  const int64_t most = int64_t(1) << 31;
+  // inputs may repeat rows or heads (stride 0), outputs may not
+  const auto side = [&](const uint16_t* x, int64_t row, int64_t head, const uint16_t* y,
+                        int64_t out_row, int64_t out_head, int32_t n) -> int32_t {
+    if (row < 0 || head < 0 || out_row < 0 || out_head < 0) return ECHO_ERR_INVALID_ARG;
+    if (row >= most || head >= most || out_row >= most || out_head >= most)
+      return ECHO_ERR_UNSUPPORTED;
+    const bool apart = (n <= 1 || out_head >= rot_dim) && (num_rows <= 1 || out_row >= rot_dim);
+    const bool nested = n <= 1 || num_rows <= 1 ||
+                        out_row >= int64_t(n - 1) * out_head + rot_dim ||
+                        out_head >= int64_t(num_rows - 1) * out_row + rot_dim;
+    if (!apart || !nested) return ECHO_ERR_INVALID_ARG;
+    if (x == y && ((num_rows > 1 && row != out_row) || (n > 1 && head != out_head)))
+      return ECHO_ERR_INVALID_ARG;
+    return ECHO_OK;
+  };
+  int32_t rc = ECHO_OK;
+  if (num_q_heads > 0)
+    rc = side(q, q_row_stride, q_head_stride, q_out, q_out_row_stride, q_out_head_stride,
+              num_q_heads);
+  if (rc == ECHO_OK && num_k_heads > 0)
+    rc = side(k, k_row_stride, k_head_stride, k_out, k_out_row_stride, k_out_head_stride,
+              num_k_heads);
+  if (rc != ECHO_OK) return rc;
+  const echo::RopeArgs a{q, q_out, q_row_stride, q_head_stride, q_out_row_stride, q_out_head_stride,
+                         k, k_out, k_row_stride, k_head_stride, k_out_row_stride, k_out_head_stride,
+                         num_q_heads, num_k_heads, positions, num_rows, row_count, rot_dim, layout,
+                         inv_freq, scale, status};
+  return echo::launch_rope(a, as_stream(stream));
+}
+
+int32_t echo_rope_frequencies(int32_t rot_dim, double base, int32_t scaling, double factor,
+                              double original_len, double low_turns, double high_turns,
+                              double* inv_freq, float* scale) {
+  if (rot_dim < 2 || rot_dim % 2 != 0 || !inv_freq || !scale) return ECHO_ERR_INVALID_ARG;
+  if (rot_dim > ECHO_ROPE_MAX_DIM) return ECHO_ERR_UNSUPPORTED;
+  if (!(base > 1.0) || !isfinite(base) || !(factor >= 1.0) || !isfinite(factor))
+    return ECHO_ERR_INVALID_ARG;
+  if (scaling < ECHO_ROPE_PLAIN || scaling > ECHO_ROPE_SMOOTH) return ECHO_ERR_INVALID_ARG;
+  if (scaling == ECHO_ROPE_BASE && rot_dim < 4) return ECHO_ERR_INVALID_ARG;
+  const bool by_turns = scaling == ECHO_ROPE_BANDS || scaling == ECHO_ROPE_SMOOTH;
+  if (by_turns && (!(original_len > 0.0) || !isfinite(original_len) || !(low_turns > 0.0) ||
+                   !(high_turns > low_turns) || !isfinite(high_turns)))
+    return ECHO_ERR_INVALID_ARG;
+  const double two_pi = 6.283185307179586;
+  const double n = rot_dim;
+  if (scaling == ECHO_ROPE_BASE) base *= pow(factor, n / (n - 2.0));
+  double lo = 0.0, hi = 0.0;  // ECHO_ROPE_BANDS: the ramp's first and last dims (of pairs)
+  if (scaling == ECHO_ROPE_BANDS) {
+    const auto dim_of = [&](double turns) {
+      return n * log(original_len / (turns * two_pi)) / (2.0 * log(base));
+    };
+    lo = fmax(floor(dim_of(high_turns)), 0.0);
+    hi = fmin(ceil(dim_of(low_turns)), n - 1.0);
+  }
+  for (int32_t i = 0; i < rot_dim / 2; ++i) {
+    double f = pow(base, -2.0 * i / n);
+    if (scaling == ECHO_ROPE_LINEAR) f /= factor;
+    if (scaling == ECHO_ROPE_BANDS) {
+      const double ramp = fmin(fmax((i - lo) / fmax(hi - lo, 1e-3), 0.0), 1.0);
+      f = f / factor * ramp + f * (1.0 - ramp);
+    }
+    if (scaling == ECHO_ROPE_SMOOTH) {
+      const double turns = original_len * f / two_pi;
+      const double s = fmin(fmax((turns - low_turns) / (high_turns - low_turns), 0.0), 1.0);
+      f = f * s + f / factor * (1.0 - s);
+    }
+    inv_freq[i] = f;
+  }
+  *scale = scaling == ECHO_ROPE_BANDS ? float(0.1 * log(factor) + 1.0) : 1.0f;
+  return ECHO_OK;
+}
+
+}  // extern "C"
+
+namespace {
+// The latent cache's arguments: ECHO_OK with *c filled, or the error code.
+int32_t cache_latent_args(uint16_t* pages, int64_t num_pages, int32_t page_size,
+                          echo::LatentCacheArgs* c) {
+  if (num_pages < 1 || page_size < 1) return ECHO_ERR_INVALID_ARG;
+  if (page_size < 32 || (page_size & (page_size - 1)) != 0) return ECHO_ERR_UNSUPPORTED;
+  // (compared by division: num_pages is any 64-bit number)
+  if (num_pages >= (int64_t(1) << 31) / page_size) return ECHO_ERR_UNSUPPORTED;
+  if (!pages || (reinterpret_cast<uintptr_t>(pages) & 15u)) return ECHO_ERR_INVALID_ARG;
+  *c = echo::LatentCacheArgs{pages, num_pages, page_size};
+  return ECHO_OK;
+}
+bool latent_dims_ok(int32_t latent_dim, int32_t rope_dim) {
+  return latent_dim == ECHO_LATENT_DIM && rope_dim == ECHO_LATENT_ROPE_DIM;
+}
+}  // namespace
+
+extern "C" {
+
+int32_t echo_store_latent(const uint16_t* kv, int64_t kv_stride, const uint16_t* norm_weight,
+                          float eps, const int32_t* positions, const double* inv_freq,
+                          float rope_scale, int32_t layout, int32_t num_rows,
+                          const int32_t* row_count, int32_t latent_dim, int32_t rope_dim,
+                          uint16_t* latent_new, const int64_t* slot_map, uint16_t* pages,
+                          int64_t num_pages, int32_t page_size, int32_t* status,
+                          echo_stream_t stream) {
+  if (num_rows < 0) return ECHO_ERR_INVALID_ARG;
+  if (!latent_dims_ok(latent_dim, rope_dim)) return ECHO_ERR_UNSUPPORTED;
+  if (layout != ECHO_ROPE_HALF && layout != ECHO_ROPE_INTERLEAVED) return ECHO_ERR_INVALID_ARG;
+  if (norm_weight != nullptr && !(eps >= 0.0f && isfinite(eps))) return ECHO_ERR_INVALID_ARG;
+  if (inv_freq != nullptr && !isfinite(rope_scale)) return ECHO_ERR_INVALID_ARG;
+  if (num_rows == 0) return ECHO_OK;
+  if (!kv || (!latent_new && !slot_map) || (inv_freq != nullptr && !positions))
+    return ECHO_ERR_INVALID_ARG;
+  if (kv_stride < ECHO_LATENT_DIM + ECHO_LATENT_ROPE_DIM || (kv_stride & 7) != 0)
+    return ECHO_ERR_INVALID_ARG;
+  if (kv_stride >= (int64_t(1) << 31)) return ECHO_ERR_UNSUPPORTED;
+  if ((reinterpret_cast<uintptr_t>(kv) | reinterpret_cast<uintptr_t>(norm_weight) |
+       reinterpret_cast<uintptr_t>(latent_new)) & 15u)
+    return ECHO_ERR_INVALID_ARG;
+  echo::LatentCacheArgs c{nullptr, 0, 0};
+  if (slot_map != nullptr) {
+    const int32_t rc = cache_latent_args(pages, num_pages, page_size, &c);
+    if (rc != ECHO_OK) return rc;
+  }
+  const echo::StoreLatentArgs a{kv, kv_stride, norm_weight, eps, positions, inv_freq, rope_scale,
+                                layout, num_rows, row_count, latent_new, slot_map, c, status};
+  return echo::launch_store_latent(a, as_stream(stream));
+}
+
+int32_t echo_commit_latent(const int32_t* q_offsets, const int32_t* accept_len,
+                           const int32_t* accept_slots, int32_t max_depth,
+                           const uint16_t* latent_new, int32_t R, int32_t max_rows,
+                           int32_t latent_dim, int32_t rope_dim, uint16_t* pages,
+                           int64_t num_pages, int32_t page_size, const int32_t* block_table,
+                           int32_t max_pages_per_request, const int32_t* prefix_len,
+                           int32_t* new_len, int32_t* status, echo_stream_t stream) {
+  if (R < 1 || max_rows < 0 || max_pages_per_request < 1) return ECHO_ERR_INVALID_ARG;
+  if (max_depth < 1 || max_depth > ECHO_MAX_DEPTH || R > ECHO_MAX_REQUESTS ||
+      !latent_dims_ok(latent_dim, rope_dim))
+    return ECHO_ERR_UNSUPPORTED;
+  echo::LatentCacheArgs c;
+  const int32_t rc = cache_latent_args(pages, num_pages, page_size, &c);
+  if (rc != ECHO_OK) return rc;
+  if (!q_offsets || !accept_len || !accept_slots || !latent_new || !block_table || !prefix_len ||
+      !new_len)
+    return ECHO_ERR_INVALID_ARG;
+  if (reinterpret_cast<uintptr_t>(latent_new) & 15u) return ECHO_ERR_INVALID_ARG;
+  return echo::launch_commit_latent(q_offsets, accept_len, accept_slots, max_depth, latent_new, R,
+                                    max_rows, c, block_table, max_pages_per_request, prefix_len,
+                                    new_len, status, as_stream(stream));
 }
 
 }  // extern "C"

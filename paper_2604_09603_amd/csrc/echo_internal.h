@@ -176,6 +176,55 @@ struct TablesArgs {
 };
 int32_t launch_build_block_tables(const TablesArgs& a, hipStream_t stream);
 
+// Rotary positions (rope.hip): strides in elements; hk == 0: no keys.
+struct RopeArgs {
+  const uint16_t* q;
+  uint16_t* q_out;
+  long long q_row, q_head, q_out_row, q_out_head;
+  const uint16_t* k;
+  uint16_t* k_out;
+  long long k_row, k_head, k_out_row, k_out_head;
+  int32_t hq, hk;
+  const int32_t* positions;
+  int32_t num_rows;
+  const int32_t* row_count;
+  int32_t rot_dim, layout;
+  const double* inv_freq;
+  float scale;
+  int32_t* status;
+};
+int32_t launch_rope(const RopeArgs& a, hipStream_t stream);
+
+// The latent cache (latent.hip, attn_latent.hip): pages [num_pages][page_size][576].
+struct LatentCacheArgs {
+  uint16_t* pages;
+  int64_t num_pages;
+  int32_t page_size;
+};
+// norm_weight, inv_freq, latent_new and slot_map may be null.
+struct StoreLatentArgs {
+  const uint16_t* kv;
+  int64_t kv_stride;
+  const uint16_t* norm_weight;
+  float eps;
+  const int32_t* positions;
+  const double* inv_freq;
+  float scale;
+  int32_t layout, num_rows;
+  const int32_t* row_count;
+  uint16_t* latent_new;
+  const int64_t* slot_map;
+  LatentCacheArgs cache;
+  int32_t* status;
+};
+int32_t launch_store_latent(const StoreLatentArgs& a, hipStream_t stream);
+int32_t launch_commit_latent(const int32_t* q_offsets, const int32_t* accept_len,
+                             const int32_t* accept_slots, int32_t max_depth,
+                             const uint16_t* latent_new, int32_t R, int32_t max_rows,
+                             const LatentCacheArgs& c, const int32_t* block_table,
+                             int32_t max_pages, const int32_t* prefix_len, int32_t* new_len,
+                             int32_t* status, hipStream_t stream);
+
 // Fused step (front.hip): the end of the gate, flatten & pack and the attention plan
 // (contiguous cache) in one launch, after launch_gate_select_only (unless
 // front_gate_list is negative) and before launch_tree_verify_attn_main.

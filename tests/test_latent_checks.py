@@ -1,0 +1,150 @@
+"""Host-side refusals of the rotary and latent calls, and the tables of frequencies (no GPU
+needed)."""
+import ctypes
+import os
+
+import numpy as np
+import pytest
+
+import paper_2604_09603_amd as pkg
+from oracle import latent
+
+P = ctypes.c_void_p
+INVALID, UNSUPPORTED, WORKSPACE = pkg.ERR_INVALID_ARG, pkg.ERR_UNSUPPORTED, pkg.ERR_WORKSPACE
+NAN, INF = float("nan"), float("inf")
+
+
+@pytest.fixture(autouse=True)
+def _lib():
+    if not os.path.exists(pkg.LIB_PATH):
+        pytest.skip("libecho.so not built")
+
+
+def _rope(**kw):
+    a = dict(q=P(256), q_row=1024, q_head=128, q_out=P(512), q_out_row=1024, q_out_head=128, hq=8, k=P(256), k_row=256,
+             k_head=128, k_out=P(512), k_out_row=256, k_out_head=128, hk=2, positions=P(256), rows=4, row_count=None,
+             rot=128, layout=0, inv_freq=P(256), scale=1.0, status=None, stream=None)
+    a.update(kw)
+    return pkg.load().echo_rope(*a.values())
+
+
+@pytest.mark.parametrize("bad,code", [
+    (dict(rows=-1), INVALID), (dict(hq=-1), INVALID), (dict(hk=-1), INVALID), (dict(rot=0), INVALID),
+    (dict(rot=127), INVALID), (dict(rot=1026), UNSUPPORTED), (dict(rot=-2), INVALID), (dict(layout=2), INVALID),
+    (dict(layout=-1), INVALID), (dict(scale=NAN), INVALID), (dict(scale=INF), INVALID), (dict(positions=None), INVALID),
+    (dict(inv_freq=None), INVALID), (dict(q=None), INVALID), (dict(q_out=None), INVALID), (dict(k=None), INVALID),
+    (dict(k_out=None), INVALID), (dict(q_out_head=64), INVALID), (dict(q_out_row=100), INVALID),
+    (dict(q_out_row=512), INVALID), (dict(k_out_head=0), INVALID), (dict(q_row=-1024), INVALID),
+    (dict(q_head=-128), INVALID), (dict(q_row=1 << 31), UNSUPPORTED), (dict(k_out_head=1 << 31), UNSUPPORTED),
+    (dict(hq=1 << 16), UNSUPPORTED), (dict(q_out=P(256), q_row=2048), INVALID),
+    (dict(k_out=P(256), k_head=0), INVALID)])
+def test_rope_refuses(bad, code):
+    assert _rope(**bad) == code
+
+
+def test_rope_without_rows_or_heads_is_nothing():
+    assert _rope(rows=0, q=None, positions=None) == pkg.OK
+    assert _rope(hq=0, hk=0, inv_freq=None) == pkg.OK
+
+
+@pytest.mark.parametrize("rot", [2, 4, 64, 80, 128, 1024])
+@pytest.mark.parametrize("scaling", list(pkg.ROPE_SCALINGS))
+@pytest.mark.parametrize("base,factor,length,turns", [(10000.0, 40.0, 4096.0, (1.0, 32.0)),
+                                                      (500000.0, 8.0, 8192.0, (1.0, 4.0)),
+                                                      (10000.0, 1.0, 100.0, (0.5, 2.0))])
+def test_frequencies_match_the_oracle(rot, scaling, base, factor, length, turns):
+    if scaling == "base" and rot == 2:
+        with pytest.raises(pkg.EchoError):
+            pkg.echo_rope_frequencies(rot, base, scaling, factor)
+        return
+    f, s = pkg.echo_rope_frequencies(rot, base, scaling, factor, length, *turns)
+    want, ws = latent.frequencies(rot, base, scaling, factor, length, *turns)
+    # (powers and logarithms of two libraries, each within a few steps of 2^-52)
+    assert np.allclose(f, want, rtol=1e-13, atol=0) and s == np.float32(ws)
+
+
+def _freq(**kw):
+    f, s = (ctypes.c_double * 64)(), ctypes.c_float()
+    a = dict(rot=64, base=10000.0, scaling=4, factor=8.0, length=4096.0, low=1.0, high=4.0,
+             f=ctypes.cast(f, P), s=ctypes.addressof(s))
+    a.update(kw)
+    return pkg.load().echo_rope_frequencies(*a.values())
+
+
+@pytest.mark.parametrize("bad,code", [
+    (dict(rot=0), INVALID), (dict(rot=63), INVALID), (dict(rot=1026), UNSUPPORTED), (dict(base=1.0), INVALID),
+    (dict(base=NAN), INVALID), (dict(base=INF), INVALID), (dict(factor=0.5), INVALID), (dict(factor=NAN), INVALID),
+    (dict(factor=INF), INVALID), (dict(scaling=5), INVALID), (dict(scaling=-1), INVALID), (dict(length=0.0), INVALID),
+    (dict(length=NAN), INVALID), (dict(low=0.0), INVALID), (dict(high=1.0), INVALID), (dict(high=NAN), INVALID),
+    (dict(high=INF), INVALID), (dict(f=None), INVALID), (dict(s=None), INVALID), (dict(scaling=2, rot=2), INVALID)])
+def test_frequencies_refuse(bad, code):
+    assert _freq(**bad) == code
+
+
+CACHE = dict(pages=P(256), num_pages=8, page_size=64)
+BAD_CACHE = [(dict(pages=None), INVALID), (dict(pages=P(264)), INVALID), (dict(num_pages=0), INVALID),
+             (dict(num_pages=-1), INVALID), (dict(num_pages=1 << 62), UNSUPPORTED), (dict(num_pages=1 << 25), UNSUPPORTED),
+             (dict(page_size=0), INVALID), (dict(page_size=16), UNSUPPORTED), (dict(page_size=96), UNSUPPORTED),
+             (dict(page_size=-(1 << 31)), INVALID), (dict(latent_dim=256), UNSUPPORTED), (dict(rope_dim=32), UNSUPPORTED)]
+
+
+def _store(**kw):
+    a = dict(kv=P(256), stride=576, weight=P(256), eps=1e-6, positions=P(256), inv_freq=P(256), scale=1.0, layout=0,
+             rows=3, row_count=None, latent_dim=512, rope_dim=64, latent_new=None, slot_map=P(256), **CACHE, status=None,
+             stream=None)
+    a.update(kw)
+    return pkg.load().echo_store_latent(*a.values())
+
+
+@pytest.mark.parametrize("bad,code", BAD_CACHE + [
+    (dict(rows=-1), INVALID), (dict(kv=None), INVALID), (dict(kv=P(264)), INVALID), (dict(stride=568), INVALID),
+    (dict(stride=580), INVALID), (dict(stride=1 << 31), UNSUPPORTED), (dict(stride=-576), INVALID),
+    (dict(weight=P(8)), INVALID), (dict(eps=-1e-6), INVALID), (dict(eps=NAN), INVALID), (dict(eps=INF), INVALID),
+    (dict(positions=None), INVALID), (dict(scale=NAN), INVALID), (dict(layout=2), INVALID),
+    (dict(latent_new=P(264)), INVALID), (dict(slot_map=None), INVALID)])
+def test_store_refuses(bad, code):
+    assert _store(**bad) == code
+
+
+def test_store_without_rows_is_nothing():
+    assert _store(rows=0, kv=None, slot_map=None) == pkg.OK
+
+
+def _commit(**kw):
+    a = dict(q_offsets=P(256), accept_len=P(256), accept_slots=P(256), max_depth=4, latent_new=P(256), R=2, max_rows=4,
+             latent_dim=512, rope_dim=64, **CACHE, block_table=P(256), max_pages=4, prefix_len=P(256), new_len=P(256),
+             status=None, stream=None)
+    a.update(kw)
+    return pkg.load().echo_commit_latent(*a.values())
+
+
+@pytest.mark.parametrize("bad,code", BAD_CACHE + [
+    (dict(R=0), INVALID), (dict(R=4096), UNSUPPORTED), (dict(max_rows=-1), INVALID), (dict(max_depth=0), UNSUPPORTED),
+    (dict(max_depth=17), UNSUPPORTED), (dict(max_pages=0), INVALID), (dict(q_offsets=None), INVALID),
+    (dict(accept_len=None), INVALID), (dict(accept_slots=None), INVALID), (dict(latent_new=None), INVALID),
+    (dict(latent_new=P(258)), INVALID), (dict(block_table=None), INVALID), (dict(prefix_len=None), INVALID),
+    (dict(new_len=None), INVALID)])
+def test_commit_refuses(bad, code):
+    assert _commit(**bad) == code
+
+
+def test_constants_match_the_header():
+    with open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include",
+                           "echo.h")) as f:
+        text = f.read()
+    for name, v in [("ROPE_HALF", pkg.ROPE_HALF), ("ROPE_INTERLEAVED", pkg.ROPE_INTERLEAVED),
+                    ("ROPE_MAX_DIM", pkg.ROPE_MAX_DIM), ("LATENT_DIM", pkg.LATENT_DIM),
+                    ("LATENT_ROPE_DIM", pkg.LATENT_ROPE_DIM)]:
+        assert f"#define ECHO_{name} {v} " in text, name
+    for name, v in pkg.ROPE_SCALINGS.items():
+        assert f"#define ECHO_ROPE_{name.upper()} {v}" in text, name
+
+
+def test_binding_refuses_views_it_cannot_describe():
+    import torch
+    x = torch.zeros((4, 8, 64), dtype=torch.bfloat16)
+    f = torch.zeros(16, dtype=torch.float64)
+    call = lambda q: pkg.echo_rope(q, q, None, None, f, 4, 8, 0, 32, 0, f, 1.0)  # noqa: E731
+    for bad in (x, x[..., ::2], x[:2, :, :32], x[:, :4, :32], x[..., 0]):
+        with pytest.raises(ValueError):
+            call(bad)
