@@ -610,6 +610,43 @@ int32_t echo_store_latent(const uint16_t* kv, int64_t kv_stride, const uint16_t*
                           echo_stream_t stream);
 
 /*
+ * echo_tree_verify_attn_latent -- echo_tree_verify_attn_paged over a latent cache, in the
+ * absorbed form: all query heads read the request's rows, the cached ones and those of
+ * the tree's slots,
+ *   z_j = sm_scale * <q, row_j> over 576 dims,  out = softmax(z) row[0 .. 511]
+ * With one slot per request it is plain decoding.  Scores, softmax and sums are fp32;
+ * each probability is rounded to bf16 for the product with the rows (2^-8) and the
+ * output divided by the sum of the weights used; rows that are split between workgroups
+ * are merged from fp32 sums.
+ * Cached values that are NaN or infinite, and such inputs, give unspecified outputs for
+ * the rows of their request; rows past a request's prefix are not used, whatever they
+ * hold.
+ *   q          [max_rows][Hq][576] bf16: the query times the head's key projection, then
+ *              the rotated dims
+ *   latent_new [max_rows][576] bf16, as echo_store_latent writes them
+ *   out        [max_rows][Hq][512] bf16 (the value projection's input), rounded from fp32
+ *              (2^-8)
+ *   lse        [max_rows][Hq] float (nullable), natural log; -inf with out = 0 for a row
+ *              that sees no key
+ * q, latent_new and out 16-byte aligned.  A request whose offsets, length or pages cannot
+ * be is skipped (ECHO_DATA_BAD_OFFSETS; the pages of requests without slots are not
+ * looked at).  Limits: max_rows * Hq < 2^26, max_pages_per_request * page_size < 2^31.
+ * Deterministic.  The workspace: echo_tree_verify_attn_latent_workspace_size; its bulk,
+ * 135 MB on 256 CUs, is the same for every batch.
+ */
+int32_t echo_tree_verify_attn_latent(
+    const uint16_t* q, const uint16_t* latent_new, const uint16_t* pages, int64_t num_pages,
+    int32_t page_size, const int32_t* block_table, int32_t max_pages_per_request,
+    const int32_t* prefix_len, const int32_t* q_offsets, const uint32_t* tree_mask,
+    int32_t mask_words, int32_t R, int32_t max_rows, int32_t num_q_heads, int32_t latent_dim,
+    int32_t rope_dim, float sm_scale, uint16_t* out, float* lse, void* workspace,
+    size_t workspace_bytes, int32_t* status, echo_stream_t stream);
+size_t echo_tree_verify_attn_latent_workspace_size(int32_t R, int32_t max_rows,
+                                                   int32_t num_q_heads, int32_t latent_dim,
+                                                   int32_t rope_dim,
+                                                   int32_t max_pages_per_request);
+
+/*
  * echo_commit_latent -- echo_commit_kv_q8 for the latent cache: each request's root and
  * accepted rows of latent_new are appended, and new_len[r] = prefix_len[r] + 1 +
  * accept_len[r]; what leaves a request as it is, is the same.

@@ -55,7 +55,8 @@ EXPORTS = [
     "echo_version", "echo_tree_verify_attn_paged_q8",
     "echo_tree_verify_attn_paged_q8_workspace_size", "echo_store_kv_q8", "echo_commit_kv_q8",
     "echo_build_block_tables", "echo_rope", "echo_rope_frequencies", "echo_store_latent",
-    "echo_commit_latent",
+    "echo_commit_latent", "echo_tree_verify_attn_latent",
+    "echo_tree_verify_attn_latent_workspace_size",
 ]
 GATE_SCRATCH_BYTES = 8 << 20
 
@@ -120,6 +121,10 @@ _SIGS = {
     "echo_rope_frequencies": (_I32, [_I32, _F64, _I32, _F64, _F64, _F64, _F64, _P, _P]),
     "echo_store_latent": (_I32, [_P, _I64, _P, _F32, _P, _P, _F32, _I32, _I32, _P, _I32, _I32, _P,
                                  _P, _P, _I64, _I32, _P, _P]),
+    "echo_tree_verify_attn_latent": (_I32, [_P, _P, _P, _I64, _I32, _P, _I32, _P, _P, _P, _I32,
+                                            _I32, _I32, _I32, _I32, _I32, _F32, _P, _P, _P, _SZ,
+                                            _P, _P]),
+    "echo_tree_verify_attn_latent_workspace_size": (_SZ, [_I32, _I32, _I32, _I32, _I32, _I32]),
     "echo_commit_latent": (_I32, [_P, _P, _P, _I32, _P, _I32, _I32, _I32, _I32, _P, _I64, _I32,
                                   _P, _I32, _P, _P, _P, _P]),
     "echo_status_string": (ctypes.c_char_p, [_I32]),
@@ -553,6 +558,30 @@ def echo_store_latent(kv, norm_weight, eps, positions, inv_freq, rope_scale, lay
         0 if pages is None else pages.shape[0], page_size, _ptr(status), _stream(stream))
     if check:
         _check(code, "echo_store_latent")
+    return code
+
+
+def tree_verify_attn_latent_workspace_size(R, max_rows, hq, max_pages, latent_dim=LATENT_DIM,
+                                           rope_dim=LATENT_ROPE_DIM) -> int:
+    return int(load().echo_tree_verify_attn_latent_workspace_size(R, max_rows, hq, latent_dim,
+                                                                  rope_dim, max_pages))
+
+
+def echo_tree_verify_attn_latent(q, latent_new, pages, page_size, block_table, prefix_len,
+                                 q_offsets, tree_mask, mask_words, R, max_rows, hq, latent_dim,
+                                 rope_dim, sm_scale, out, lse, workspace, status=None,
+                                 stream=None, check=True):
+    """Verification attention over a latent paged cache (absorbed form).  Device tensors; q is
+    [max_rows, Hq, 576] bf16 bits, latent_new [max_rows, 576], pages [num_pages, page_size, 576],
+    out [max_rows, Hq, 512]."""
+    code = load().echo_tree_verify_attn_latent(
+        _ptr(q), _ptr(latent_new), _ptr(pages), pages.shape[0], page_size, _ptr(block_table),
+        block_table.shape[1], _ptr(prefix_len), _ptr(q_offsets), _ptr(tree_mask), mask_words, R,
+        max_rows, hq, latent_dim, rope_dim, float(sm_scale), _ptr(out), _ptr(lse),
+        _ptr(workspace), workspace.numel() * workspace.element_size(), _ptr(status),
+        _stream(stream))
+    if check:
+        _check(code, "echo_tree_verify_attn_latent")
     return code
 
 

@@ -33,6 +33,7 @@ FLAGS = [
 # The fused step's tail kernel holds the attention's combine and is built the
 # same way, so that its merges are the combine launch's to the bit.
 FILE_FLAGS = {
+    "attn_latent.hip": ["-mllvm", "--amdgpu-mfma-vgpr-form=1", "-fno-honor-nans"],
     "attn_q8.hip": ["-mllvm", "--amdgpu-mfma-vgpr-form=1", "-fno-honor-nans"],
     "attn.hip": ["-mllvm", "--amdgpu-mfma-vgpr-form=1", "-fno-honor-nans"],
     "tail.hip": ["-mllvm", "--amdgpu-mfma-vgpr-form=1", "-fno-honor-nans"],

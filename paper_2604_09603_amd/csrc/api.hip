@@ -807,6 +807,63 @@ int32_t echo_store_latent(const uint16_t* kv, int64_t kv_stride, const uint16_t*
   return echo::launch_store_latent(a, as_stream(stream));
 }
 
+size_t echo_tree_verify_attn_latent_workspace_size(int32_t R, int32_t max_rows,
+                                                   int32_t num_q_heads, int32_t latent_dim,
+                                                   int32_t rope_dim,
+                                                   int32_t max_pages_per_request) {
+  if (R < 1 || max_rows < 0 || num_q_heads < 1 || !latent_dims_ok(latent_dim, rope_dim) ||
+      max_pages_per_request < 1)
+    return 0;
+  return echo::attn_latent_workspace_bytes(R, max_pages_per_request);
+}
+
+int32_t echo_tree_verify_attn_latent(
+    const uint16_t* q, const uint16_t* latent_new, const uint16_t* pages, int64_t num_pages,
+    int32_t page_size, const int32_t* block_table, int32_t max_pages_per_request,
+    const int32_t* prefix_len, const int32_t* q_offsets, const uint32_t* tree_mask,
+    int32_t mask_words, int32_t R, int32_t max_rows, int32_t num_q_heads, int32_t latent_dim,
+    int32_t rope_dim, float sm_scale, uint16_t* out, float* lse, void* workspace,
+    size_t workspace_bytes, int32_t* status, echo_stream_t stream) {
+  if (R < 1 || max_rows < 0 || num_q_heads < 1 || mask_words < 1 || max_pages_per_request < 1)
+    return ECHO_ERR_INVALID_ARG;
+  if (!scale_ok(sm_scale)) return ECHO_ERR_INVALID_ARG;
+  if (!latent_dims_ok(latent_dim, rope_dim) || R > ECHO_MAX_REQUESTS) return ECHO_ERR_UNSUPPORTED;
+  echo::AttnLatentArgs a{};
+  const int32_t rc =
+      cache_latent_args(const_cast<uint16_t*>(pages), num_pages, page_size, &a.cache);
+  if (rc != ECHO_OK) return rc;
+  if (int64_t(max_pages_per_request) * page_size >= (int64_t(1) << 31) ||
+      int64_t(max_rows) * num_q_heads >= (int64_t(1) << 26))
+    return ECHO_ERR_UNSUPPORTED;
+  if (!q || !latent_new || !block_table || !prefix_len || !q_offsets || !tree_mask || !out ||
+      !workspace)
+    return ECHO_ERR_INVALID_ARG;
+  if (!aligned256(workspace) ||
+      workspace_bytes < echo::attn_latent_workspace_bytes(R, max_pages_per_request))
+    return ECHO_ERR_WORKSPACE;
+  if ((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(latent_new) |
+       reinterpret_cast<uintptr_t>(out)) & 15u)
+    return ECHO_ERR_INVALID_ARG;
+  if (max_rows == 0) return ECHO_OK;
+  a.q = q;
+  a.latent_new = latent_new;
+  a.block_table = block_table;
+  a.max_pages = max_pages_per_request;
+  a.prefix_len = prefix_len;
+  a.q_offsets = q_offsets;
+  a.tree_mask = tree_mask;
+  a.mask_words = mask_words;
+  a.R = R;
+  a.max_rows = max_rows;
+  a.hq = num_q_heads;
+  a.sm_scale = sm_scale;
+  a.out = out;
+  a.lse = lse;
+  a.workspace = workspace;
+  a.status = status;
+  return echo::launch_tree_verify_attn_latent(a, as_stream(stream));
+}
+
 int32_t echo_commit_latent(const int32_t* q_offsets, const int32_t* accept_len,
                            const int32_t* accept_slots, int32_t max_depth,
                            const uint16_t* latent_new, int32_t R, int32_t max_rows,

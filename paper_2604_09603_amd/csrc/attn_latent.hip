@@ -1,0 +1,704 @@
+// Tree-masked verification attention over a latent paged cache (latent.hip writes it): every
+// query head of a request reads the same rows of 576 values, all of a row as its key and
+// dims 0-511 as its value.  Two launches, and one more before them for large block tables:
+//
+//   latent_pages    checks the page ids (small tables: the main kernel's workgroups do).
+//   latent_main     persistent, one workgroup of four waves per CU.  A unit is up to 128 of a
+//                   request's rows (verify slots x heads, which lie one after another); its
+//                   tiles are 32 keys each, first the tree's, then the prefix's.  The tiles
+//                   of all units are cut into ranges of equal cost, one per workgroup, which
+//                   every workgroup finds by itself from the requests' lengths.
+//                   A tile is copied HBM -> LDS once and used twice.  S^T = K Q^T: each wave
+//                   has 32 (or 16) rows, its part of Q stays in registers.  The weights go
+//                   through LDS.  O^T += V^T P^T: each wave has 128 of the 512 dims for all
+//                   rows, so that a fragment of V serves all of them.
+//   latent_combine  merges the partial sums of units that several workgroups share.
+//
+// Softmax statistics and sums are fp32.  The weights p are rounded to bfloat16 for
+// the product with V (at most 2^-8 each) and the output is divided by the sum of the
+// weights used, so that it stays a convex combination of V rows; the output's own
+// rounding to bfloat16 is as large.  Partial sums are stored in fp32.
+#include "attn_core.h"
+
+namespace echo {
+namespace {
+
+constexpr int kLC = ECHO_LATENT_DIM, kLRow = ECHO_LATENT_DIM + ECHO_LATENT_ROPE_DIM;
+constexpr int kLRowBytes = kLRow * 2;          // 1152
+constexpr int kLWaves = 4;
+constexpr int kLThreads = kLWaves * kWave;
+constexpr int kLRows = 128;                    // rows of a unit
+constexpr int kLSteps = kLRow / 32;            // products along a row of K
+// A tile in LDS: nine blocks (64 dims) of 32 rows x 128 bytes.  The 16-byte chunk c of row r
+// is at chunk position c ^ f(r), with bits 2, 3, 1 of r as bits 0, 1, 2 of f: the 16 rows
+// of which a phase of a K read takes one chunk each, and the four rows of which half a
+// wave's transposed V read takes four chunks each, fall into 16 different sixteenths
+// of the banks.
+constexpr int kLBlock = kTileKeys * 128;       // 4 KB
+constexpr int kLTile = kLRowBytes * kTileKeys; // 36 KB
+constexpr int kLSlots = 4;
+constexpr int kLProb = kLRows * kTileKeys * 2; // the weights of a tile
+constexpr int kLStats = 2048;
+constexpr int kLLds = kLSlots * kLTile + kLProb + kLStats;
+static_assert(kLLds <= 160 * 1024, "gfx950 LDS per CU");
+constexpr int kLOwnPages = 512;                // block tables up to this wide are checked in place
+
+// Costs of a tile with more than 64 rows, of one with fewer, of entering a unit.
+constexpr int kLCost4 = 4, kLCost2 = 2, kLEnter = 6;
+constexpr int kLMinCost = 16;                  // of a range
+
+typedef float floatx16 __attribute__((ext_vector_type(16)));
+typedef uint32_t uint4v __attribute__((ext_vector_type(4)));
+typedef uint32_t uint2v __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) uint4v lds_uint4_t;
+typedef __attribute__((address_space(3))) uint2v lds_uint2_t;
+typedef __attribute__((address_space(3))) float lds_float_t;
+typedef __attribute__((address_space(3))) int lds_int_t;
+typedef __attribute__((address_space(3))) char lds_char_t;
+__device__ __forceinline__ lds_char_t* lds_at(uint32_t x) { return (lds_char_t*)(uintptr_t(x)); }
+
+__host__ __device__ __forceinline__ int l_swz(int row) {
+  return (((row >> 1) & 1) << 2) | ((row >> 2) & 3);
+}
+
+struct LatArgs {
+  const uint16_t* q;
+  const uint16_t* latent_new;
+  const uint16_t* pages;
+  const int32_t* block_table;
+  const int32_t* prefix_len;
+  const int32_t* q_offsets;
+  const uint32_t* tree_mask;
+  long long num_pages;
+  int page_shift, max_pages, W, R, max_rows, hq;
+  int chunks;  // flags of latent_pages per request, 0: the workgroups check
+  float scale2;
+  uint16_t* out;
+  float* lse;
+  int32_t* status;
+};
+
+// A unit whose partial sums have to be merged: those of ranges g - 1, g, ... (parts of them),
+// in the record of range g.
+struct LatCut {
+  int32_t parts, rows;
+  int64_t row;  // the first, of all rows of q
+};
+
+struct LatWs {
+  LatCut* cuts;    // [G]
+  int32_t* bad;    // [R][chunks] flags of latent_pages
+  float* part_ml;  // [G][2][128][4]: max, sum, sum of the weights used
+  float* part_o;   // [G][2][4][128][32][4]: 4 dims of each of 32 rows, 128 times, for four row tiles
+};
+
+__host__ inline int l_page_chunks(int max_pages) {
+  return max_pages <= kLOwnPages ? 0 : (max_pages + kPageChunk - 1) / kPageChunk;
+}
+
+__host__ inline LatWs l_layout(void* base, int R, int max_pages, int G, size_t* bytes) {
+  char* p = static_cast<char*>(base);
+  LatWs w;
+  w.cuts = reinterpret_cast<LatCut*>(p);
+  p += al(size_t(G) * sizeof(LatCut));
+  w.bad = reinterpret_cast<int32_t*>(p);
+  p += al(size_t(R) * size_t(l_page_chunks(max_pages)) * 4);
+  w.part_ml = reinterpret_cast<float*>(p);
+  p += al(size_t(G) * 2 * kLRows * 4 * sizeof(float));
+  w.part_o = reinterpret_cast<float*>(p);
+  p += al(size_t(G) * 2 * kLRows * kLC * sizeof(float));
+  if (bytes != nullptr) *bytes = size_t(p - static_cast<char*>(base));
+  return w;
+}
+
+// Pages of a request's prefix, or -1 if its length does not fit its table row.
+__device__ __forceinline__ int l_prefix_pages(long long P, const LatArgs& a) {
+  if (P < 0 || P > ((long long)a.max_pages << a.page_shift)) return -1;
+  return int((P + (1 << a.page_shift) - 1) >> a.page_shift);
+}
+
+__global__ __launch_bounds__(kPageChunk) void latent_pages_kernel(LatArgs a, int32_t* bad_flags) {
+  const int c = blockIdx.x, r = blockIdx.y;
+  const int np = l_prefix_pages(a.prefix_len[r], a);
+  const int e = c * kPageChunk + int(threadIdx.x);
+  int bad = 0;
+  if (e < np) {
+    const int pg = a.block_table[size_t(r) * size_t(a.max_pages) + size_t(e)];
+    bad = pg < 0 || pg >= a.num_pages;
+  }
+  bad = __syncthreads_or(bad);
+  if (threadIdx.x == 0) bad_flags[size_t(r) * gridDim.x + c] = bad;
+}
+
+// ---------------------------------------------------------------- plan ----
+// A request: its units are `full` of 128 rows and, if there are rows left, one more.
+struct LatLook {
+  int q0, n, P;
+  bool ok;
+  __device__ __forceinline__ int rows(const LatArgs& a) const { return n * a.hq; }
+  __device__ __forceinline__ int tree_tiles() const { return (n + kTileKeys - 1) / kTileKeys; }
+  __device__ __forceinline__ int tiles() const {
+    return tree_tiles() + int((unsigned(P) + kTileKeys - 1) / kTileKeys);
+  }
+};
+__device__ __forceinline__ LatLook l_look(const LatArgs& a, int r) {
+  LatLook x;
+  const int q0 = a.q_offsets[r], q1 = a.q_offsets[r + 1], P = a.prefix_len[r];
+  x.ok = q0 >= 0 && q1 >= q0 && q1 <= a.max_rows && l_prefix_pages(P, a) >= 0;
+  x.q0 = q0;
+  x.n = x.ok ? q1 - q0 : 0;
+  x.P = x.ok ? P : 0;
+  return x;
+}
+__device__ __forceinline__ int l_tile_cost(int rows) { return rows > kLRows / 2 ? kLCost4 : kLCost2; }
+__device__ __forceinline__ long long l_unit_cost(int tiles, int rows) {
+  return kLEnter + (long long)tiles * l_tile_cost(rows);
+}
+__device__ __forceinline__ long long l_cost(const LatArgs& a, const LatLook& x) {
+  if (x.n == 0) return 0;
+  const int rows = x.rows(a), rest = rows % kLRows;
+  return (rows / kLRows) * l_unit_cost(x.tiles(), kLRows) + (rest > 0 ? l_unit_cost(x.tiles(), rest) : 0);
+}
+
+__device__ __forceinline__ long long wave_scan64(long long v) {
+  const int lane = threadIdx.x & (kWave - 1);
+#pragma unroll
+  for (int d = 1; d < kWave; d *= 2) {
+    const long long o = __shfl_up(v, d);
+    if (lane >= d) v += o;
+  }
+  return v;
+}
+__device__ __forceinline__ long long uniform_ll(long long x) { return (long long)uniform64(uint64_t(x)); }
+
+struct LatRanges {
+  long long total;
+  int G;  // ranges
+  __device__ __forceinline__ long long first(int g) const { return total * g / G; }
+  // The range that holds cost x.
+  __device__ __forceinline__ int range_of(long long x) const {
+    int g = int(double(x) * G / double(total));
+    while (g > 0 && first(g) > x) --g;
+    while (g + 1 < G && first(g + 1) <= x) ++g;
+    return g;
+  }
+};
+
+// Where a workgroup is: request r (whose units start at cost at), unit j of it.
+struct LatWalk {
+  LatLook x;
+  int r, j;
+  long long at;
+};
+
+// Whether a request's pages are all in the pool (all threads; one barrier).
+__device__ __forceinline__ bool l_pages_ok(const LatArgs& a, const LatWs& ws, int r, int P) {
+  const int np = l_prefix_pages(P, a);
+  const bool own = a.chunks == 0;
+  const int n = own ? np : (np + kPageChunk - 1) / kPageChunk;
+  const int32_t* e = own ? a.block_table + size_t(r) * size_t(a.max_pages) : ws.bad + size_t(r) * size_t(a.chunks);
+  int bad = 0;
+  for (int i = threadIdx.x; i < n; i += kLThreads) {
+    const int v = e[i];
+    bad |= own ? v < 0 || v >= a.num_pages : v != 0;
+  }
+  return __syncthreads_or(bad) == 0;
+}
+
+// ---------------------------------------------------------------- main ----
+// Copies a wave's eight rows of a tile: 9 x 1 KB, to LDS address lds and every 4 KB on.  The
+// instructions' offset moves both addresses.  In inline assembly because the compiler would
+// wait for every copy in flight before each LDS read; M0 (the LDS address) is the
+// compiler's and is restored, and needs a wait state before a load reads it.
+__device__ __forceinline__ void l_copy(uint32_t lds, uint64_t base, uint32_t off) {
+  uint32_t saved;
+#define ECHO_L_NEXT(OFF)                                                                \
+  "s_add_u32 m0, m0, 0xf80\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3 offset:" OFF "\n\t"
+  asm volatile(
+      "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3\n\t"
+      ECHO_L_NEXT("0x80") ECHO_L_NEXT("0x100") ECHO_L_NEXT("0x180") ECHO_L_NEXT("0x200")
+      ECHO_L_NEXT("0x280") ECHO_L_NEXT("0x300") ECHO_L_NEXT("0x380") ECHO_L_NEXT("0x400")
+      "s_mov_b32 m0, %0"
+      : "=&s"(saved)
+      : "s"(lds), "v"(off), "s"(base)
+      : "memory", "scc");
+#undef ECHO_L_NEXT
+}
+constexpr int kLCopies = 9;  // loads of a wave per tile
+
+struct LatUnit {
+  int q0, n, P, r, row0, rows, tree_tiles;
+};
+
+// Sends for tile t of a unit.
+__device__ __forceinline__ void l_send(const LatArgs& a, const LatUnit& u, int t, uint32_t slot_lds) {
+  const int lane = threadIdx.x & (kWave - 1), w = wave_id();
+  uint64_t base;
+  int tn;
+  if (t < u.tree_tiles) {
+    base = reinterpret_cast<uint64_t>(a.latent_new) + uint64_t(u.q0 + t * kTileKeys) * kLRowBytes;
+    tn = u.n - t * kTileKeys;
+  } else {
+    const int key = (t - u.tree_tiles) * kTileKeys;
+    const_i32_t* bt = (const_i32_t*)(a.block_table + size_t(u.r) * size_t(a.max_pages));
+    const uint64_t row = (uint64_t(uint32_t(bt[key >> a.page_shift])) << a.page_shift) +
+                         uint32_t(key & ((1 << a.page_shift) - 1));
+    base = reinterpret_cast<uint64_t>(a.pages) + row * kLRowBytes;
+    tn = u.P - key;
+  }
+  const int key = 8 * w + (lane >> 3);
+  // (rows past the tile's keys: the last one again, so that nothing unwritten is multiplied)
+  const uint32_t off = uint32_t(min(key, tn - 1) * kLRowBytes + (((lane & 7) ^ l_swz(key)) << 4));
+  l_copy(__builtin_amdgcn_readfirstlane(slot_lds + uint32_t(w * 1024)), uniform64(base), off);
+}
+
+__device__ __forceinline__ float quad_max(float v) {  // over the four lanes of a row
+  v = fmaxf(v, __shfl_xor(v, 16));
+  return fmaxf(v, __shfl_xor(v, 32));
+}
+__device__ __forceinline__ float quad_sum(float v) {
+  v += __shfl_xor(v, 16);
+  return v + __shfl_xor(v, 32);
+}
+
+__device__ __forceinline__ void l_barrier() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// acc += A B with acc in accumulation registers.  In inline assembly because 128 rows x 128 dims
+// are all 256 of them, and the compiler holds other products' results there too, or
+// copies.  The compiler does not know the wait states around it: one after a vector
+// instruction that writes an operand, before; those before acc is read, l_settle.
+__device__ __forceinline__ void l_mfma(floatx16& acc, bf16x8 x, bf16x8 y) {
+  asm("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(acc) : "v"(x), "v"(y));
+}
+__device__ __forceinline__ void l_settle(floatx16& acc) { asm volatile("s_nop 15\n\ts_nop 15" : "+a"(acc)); }
+
+// Tiles [t0, t1) of a unit, then its output (whole) or partial sums (part).  QR: 16-row tiles of
+// a wave's part of Q; the unit has up to 64 QR rows.
+template <int QR>
+__device__ __forceinline__ void l_segment(const LatArgs& a, const LatWs& ws, const LatUnit& u, int t0,
+                                          int t1, bool whole, size_t part, uint32_t smem) {
+  constexpr int RT = 2 * QR;  // 32-row tiles of the unit
+  const int lane = threadIdx.x & (kWave - 1), w = wave_id();
+  const int l16 = lane & 15, quad = lane >> 4, h = lane >> 5;
+  const uint32_t prob = smem + kLSlots * kLTile, stats = prob + kLProb;
+  const size_t first = size_t(u.q0) * a.hq + size_t(u.row0);  // the unit's first row of q
+
+  for (int t = t0; t < min(t0 + kLSlots - 1, t1); ++t)
+    l_send(a, u, t, smem + uint32_t((t - t0) & (kLSlots - 1)) * kLTile);
+  // Q: row l16 of each 16-row tile, dims 32 ks + 8 quad .. (rows past the last: the last again)
+  bf16x8 q[QR][kLSteps];
+  int slot[QR];
+#pragma unroll
+  for (int i = 0; i < QR; ++i) {
+    const int row = min(16 * (QR * w + i) + l16, u.rows - 1);
+    const uint16_t* p = a.q + (first + row) * kLRow + 8 * quad;
+#pragma unroll
+    for (int ks = 0; ks < kLSteps; ++ks) q[i][ks] = as_bf16x8(*reinterpret_cast<const uint4*>(p + 32 * ks));
+    slot[i] = u.q0 + (u.row0 + row) / a.hq;
+  }
+  floatx16 o[RT][4];
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+    for (int ct = 0; ct < 4; ++ct) o[rt][ct] = floatx16{};
+  float m[QR], grow_at[QR], l[QR], lq[QR];
+#pragma unroll
+  for (int i = 0; i < QR; ++i) {
+    m[i] = grow_at[i] = -__builtin_inff();
+    l[i] = lq[i] = 0.0f;
+  }
+  // LDS offsets in a tile (the header of this file has the products' shapes)
+  const uint32_t ka = uint32_t(l16 * 128 + ((quad ^ l_swz(l16)) << 4));
+  const int vkey = 4 * h + (l16 >> 2);
+  const uint32_t vchunk = uint32_t((2 * (quad & 1) + ((l16 & 3) >> 1)) ^ l_swz(vkey));
+  const uint32_t va = uint32_t(2 * w * kLBlock + vkey * 128 + ((l16 & 1) << 3)) + (vchunk << 4);
+  const uint32_t pw = prob + uint32_t((QR == 2 ? w : w >> 1) * 2048 + ((QR == 2 ? 0 : 16 * (w & 1)) + l16) * 16 +
+                                      (quad & 1) * 512 + (quad >> 1) * 8);
+
+  for (int t = t0; t < t1; ++t) {
+    const int behind = min(t1 - 1 - t, kLSlots - 2);  // tiles sent after this one
+    if (behind >= 2) wait_vm<2 * kLCopies>();
+    else if (behind == 1) wait_vm<kLCopies>();
+    else wait_vm<0>();
+    l_barrier();  // every wave's part of the tile has landed; the last tile's slot is free
+    if (t + kLSlots - 1 < t1)
+      l_send(a, u, t + kLSlots - 1, smem + uint32_t((t + kLSlots - 1 - t0) & (kLSlots - 1)) * kLTile);
+    const uint32_t tile = smem + uint32_t((t - t0) & (kLSlots - 1)) * kLTile;
+    // S^T: keys 16 kt + 4 quad + r of row l16
+    floatx4 s[QR][2];
+#pragma unroll
+    for (int i = 0; i < QR; ++i) s[i][0] = s[i][1] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int ks = 0; ks < kLSteps; ++ks)
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt) {
+        const bf16x8 k = __builtin_bit_cast(
+            bf16x8, *(lds_uint4_t*)(lds_at((tile + ka) ^ uint32_t((ks & 1) << 6)) + (ks >> 1) * kLBlock + kt * 2048));
+#pragma unroll
+        for (int i = 0; i < QR; ++i) s[i][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[i][ks], s[i][kt], 0, 0, 0);
+      }
+    // masks: the tree's words, the prefix's last tile
+    const bool tree = t < u.tree_tiles;
+    const int tn = tree ? u.n - t * kTileKeys : u.P - (t - u.tree_tiles) * kTileKeys;
+    if (tree || tn < kTileKeys) {
+#pragma unroll
+      for (int i = 0; i < QR; ++i) {
+        uint32_t word = 0xFFFFFFFFu;
+        if (tree) word = t < a.W ? a.tree_mask[size_t(slot[i]) * a.W + t] : 0u;
+        if (tn < kTileKeys) word &= (1u << tn) - 1u;
+        word >>= 4 * quad;
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            s[i][kt][r] = ((word >> (16 * kt + r)) & 1u) ? s[i][kt][r] : -__builtin_inff();
+      }
+    }
+    // The reference is raised only when a logit exceeds it by more than 2^8, so that weights stay <= 256.
+    float top[QR];
+    bool up = false;
+#pragma unroll
+    for (int i = 0; i < QR; ++i) {
+      top[i] = fmaxf(fmaxf(fmaxf(s[i][0][0], s[i][0][1]), fmaxf(s[i][0][2], s[i][0][3])),
+                     fmaxf(fmaxf(s[i][1][0], s[i][1][1]), fmaxf(s[i][1][2], s[i][1][3]))) * a.scale2;
+      up |= top[i] > grow_at[i];
+    }
+    const bool raised = __ballot(up) != 0ull;
+    if (raised) {
+#pragma unroll
+      for (int i = 0; i < QR; ++i) {
+        const float mt = quad_max(top[i]);
+        const bool grow = mt > grow_at[i];
+        const float alpha = grow ? __builtin_amdgcn_exp2f(m[i] - mt) : 1.0f;  // 0 from -inf
+        l[i] *= alpha;
+        lq[i] *= alpha;
+        m[i] = grow ? mt : m[i];
+        grow_at[i] = m[i] + kRescaleSlack;
+        if (quad == 0) *(lds_float_t*)lds_at(stats + uint32_t((16 * (QR * w + i) + l16) * 4)) = alpha;
+      }
+    }
+    if (lane == 0) *(lds_int_t*)lds_at(stats + 512 + uint32_t(4 * w)) = raised ? 1 : 0;
+#pragma unroll
+    for (int i = 0; i < QR; ++i) {
+      const float neg_m = m[i] == -__builtin_inff() ? 0.0f : -m[i];
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt) {
+        float p[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i][kt][r], a.scale2, neg_m));
+        l[i] += (p[0] + p[1]) + (p[2] + p[3]);
+        const uint32_t x = pack_bf16x2(p[0], p[1]), y = pack_bf16x2(p[2], p[3]);
+        lq[i] = add_bf16x2(y, add_bf16x2(x, lq[i]));
+        *(lds_uint2_t*)(lds_at(pw) + kt * 1024 + i * 256) = uint2v{x, y};
+      }
+    }
+    wait_lds();
+    l_barrier();  // the weights are there
+    // O is scaled where a reference was raised
+    const uint4v flags = *(lds_uint4_t*)lds_at(stats + 512);
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      const uint32_t f0 = QR == 2 ? flags[rt & 3] : flags[(2 * rt) & 3], f1 = QR == 2 ? f0 : flags[(2 * rt + 1) & 3];
+      if (__builtin_amdgcn_readfirstlane(int(f0 | f1)) != 0) {
+        float alpha = *(lds_float_t*)lds_at(stats + uint32_t((32 * rt + (lane & 31)) * 4));
+        alpha = (quad & 1 ? f1 : f0) != 0 ? alpha : 1.0f;
+#pragma unroll
+        for (int ct = 0; ct < 4; ++ct) {
+          l_settle(o[rt][ct]);
+          o[rt][ct] *= alpha;
+        }
+      }
+    }
+#pragma unroll
+    for (int kg = 0; kg < 2; ++kg) {
+      bf16x8 pf[RT];
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt)
+        pf[rt] = __builtin_bit_cast(bf16x8, *(lds_uint4_t*)(lds_at(prob + uint32_t(lane * 16)) + rt * 2048 + kg * 1024));
+#pragma unroll
+      for (int ct = 0; ct < 4; ++ct) {
+        shortx4 v[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+          v[k] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+              (lds_shortx4_t*)(lds_at((tile + va) ^ uint32_t(((ct & 1) << 6) | (k << 5))) + (ct >> 1) * kLBlock +
+                               kg * 2048 + k * 1024));
+        const bf16x8 vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt)
+          l_mfma(o[rt][ct], vf, pf[rt]);
+      }
+    }
+  }
+
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+    for (int ct = 0; ct < 4; ++ct) l_settle(o[rt][ct]);
+  // the sums of a row are its wave's; every wave needs their inverses
+  float L[QR], Lq[QR];
+#pragma unroll
+  for (int i = 0; i < QR; ++i) {
+    L[i] = quad_sum(l[i]);
+    Lq[i] = quad_sum(lq[i]);
+    const int row = 16 * (QR * w + i) + l16;
+    if (quad == 0) {
+      *(lds_float_t*)lds_at(stats + 1024 + uint32_t(row * 4)) = Lq[i] > 0.0f ? 1.0f / Lq[i] : 0.0f;
+      if (row < u.rows) {
+        if (!whole)
+          *reinterpret_cast<floatx4*>(ws.part_ml + (part * kLRows + row) * 4) = floatx4{m[i], L[i], Lq[i], 0.0f};
+        else if (a.lse != nullptr)
+          a.lse[first + row] = L[i] > 0.0f ? (m[i] + log2f(L[i])) * kLn2 : -__builtin_inff();
+      }
+    }
+  }
+  wait_lds();
+  l_barrier();  // (the slots are free too)
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    const int row = 32 * rt + (lane & 31);
+    if (row < u.rows) {
+      if (whole) {
+        const float inv = *(lds_float_t*)lds_at(stats + 1024 + uint32_t(row * 4));
+        uint16_t* po = a.out + (first + row) * kLC + 128 * w + 4 * h;
+#pragma unroll
+        for (int ct = 0; ct < 4; ++ct)
+#pragma unroll
+          for (int r = 0; r < 16; r += 4)
+            *reinterpret_cast<uint2*>(po + 32 * ct + 2 * r) =
+                make_uint2(pack_bf16x2(o[rt][ct][r] * inv, o[rt][ct][r + 1] * inv),
+                           pack_bf16x2(o[rt][ct][r + 2] * inv, o[rt][ct][r + 3] * inv));
+      } else {
+        float* po = ws.part_o + ((part * 4 + rt) * 128 + 32 * w + h) * 128 + (lane & 31) * 4;
+#pragma unroll
+        for (int ct = 0; ct < 4; ++ct)
+#pragma unroll
+          for (int r = 0; r < 16; r += 4)
+            *reinterpret_cast<floatx4*>(po + (8 * ct + (r >> 1)) * 128) =
+                floatx4{o[rt][ct][r], o[rt][ct][r + 1], o[rt][ct][r + 2], o[rt][ct][r + 3]};
+      }
+    }
+  }
+}
+
+__global__ __launch_bounds__(kLThreads) __attribute__((amdgpu_waves_per_eu(1, 1))) void latent_main_kernel(
+    LatArgs a, LatWs ws) {
+  __shared__ __attribute__((aligned(1024))) char smem[kLLds];
+  const int tid = threadIdx.x, lane = tid & (kWave - 1), wid = wave_id();
+  const int nwg = int(gridDim.x);
+  // every thread counts the costs of K requests
+  long long* s_start = reinterpret_cast<long long*>(smem);  // [threads + 1]
+  long long* s_wave = s_start + kLThreads + 1;
+  const int K = (a.R + kLThreads - 1) / kLThreads;
+  long long mine = 0;
+  int bits = 0;
+  for (int i = 0; i < K; ++i) {
+    const int r = tid * K + i;
+    if (r >= a.R) break;
+    const LatLook x = l_look(a, r);
+    if (!x.ok) bits = ECHO_DATA_BAD_OFFSETS;
+    mine += l_cost(a, x);
+  }
+  if (blockIdx.x == 0) wave_status_or(a.status, bits);
+  const long long upto = wave_scan64(mine);
+  if (lane == kWave - 1) s_wave[wid] = upto;
+  __syncthreads();
+  long long before = 0, total = 0;
+#pragma unroll
+  for (int v = 0; v < kLWaves; ++v) {
+    if (v < wid) before += s_wave[v];
+    total += s_wave[v];
+  }
+  s_start[tid] = before + upto - mine;
+  __syncthreads();
+  LatRanges ranges;
+  ranges.total = uniform_ll(total);
+  ranges.G = int(min((long long)nwg, max(ranges.total / kLMinCost, 1ll)));
+  // neighbouring ranges, which share requests, run on one XCD (workgroup b is on XCD b % 8)
+  int g = blockIdx.x;
+  if (ranges.G == nwg && nwg % 8 == 0) g = (g & 7) * (nwg / 8) + (g >> 3);
+  if (g >= ranges.G || ranges.total == 0) {
+    if (tid == 0) ws.cuts[blockIdx.x].parts = 0;
+    return;
+  }
+  const long long lo = ranges.first(g), hi = ranges.first(g + 1);
+  // the last thread whose requests start at lo or before, and which of its requests it is
+  int th = 0;
+#pragma unroll
+  for (int v = 0; v < kLWaves; ++v) th += __popcll(__ballot(s_start[v * kWave + lane] <= lo));
+  th = __builtin_amdgcn_readfirstlane(th) - 1;
+  LatWalk w;
+  {
+    LatLook x = {};
+    const int r = th * K + lane;
+    if (lane < K && r < a.R) x = l_look(a, r);
+    const long long c = l_cost(a, x);
+    const long long end = s_start[th] + wave_scan64(c);
+    const int i = __ffsll((unsigned long long)__ballot(end > lo)) - 1;
+    w.r = th * K + i;
+    w.at = uniform_ll(__shfl(end - c, i));
+  }
+  __syncthreads();  // (the tiles take this memory)
+  const uint32_t base = __builtin_amdgcn_readfirstlane(uint32_t(reinterpret_cast<uintptr_t>((lds_void_t*)smem)));
+  w.j = -1;
+  bool cut_done = false;
+  while (true) {
+    // a request: its units from w.at on
+    w.r = __builtin_amdgcn_readfirstlane(w.r);
+    {
+      const LatLook x = l_look(a, w.r);
+      w.x.q0 = __builtin_amdgcn_readfirstlane(x.q0);
+      w.x.n = __builtin_amdgcn_readfirstlane(x.n);
+      w.x.P = __builtin_amdgcn_readfirstlane(x.P);
+    }
+    const bool ok = l_pages_ok(a, ws, w.r, w.x.P);
+    if (!ok && tid == 0) status_or(a.status, ECHO_DATA_BAD_OFFSETS);
+    const int rows = w.x.rows(a), T = w.x.tiles(), full = rows / kLRows;
+    const long long whole_unit = l_unit_cost(T, kLRows);
+    int j = 0;
+    if (lo > w.at && full > 0) j = int(min((lo - w.at) / whole_unit, (long long)full));
+    long long at = w.at + j * whole_unit;
+    for (; j * kLRows < rows && at < hi; ++j) {
+      LatUnit u;
+      u.q0 = w.x.q0;
+      u.n = w.x.n;
+      u.P = w.x.P;
+      u.r = w.r;
+      u.row0 = j * kLRows;
+      u.rows = min(kLRows, rows - u.row0);
+      u.tree_tiles = w.x.tree_tiles();
+      const int c = l_tile_cost(u.rows);
+      const long long t_at = at + kLEnter;  // where its tiles start
+      const int t0 = lo <= t_at ? 0 : int(min((lo - t_at + c - 1) / c, (long long)T));
+      const int t1 = hi <= t_at ? 0 : int(min((hi - t_at + c - 1) / c, (long long)T));
+      if (ok && t0 < t1) {
+        if (t0 > 0 && !cut_done) {
+          // (only a range's first unit can have started before it)
+          LatCut cut = {};
+          if (ranges.range_of(t_at) == g - 1) {
+            cut.parts = ranges.range_of(t_at + (long long)(T - 1) * c) - g + 2;
+            cut.rows = u.rows;
+            cut.row = (long long)u.q0 * a.hq + u.row0;
+          }
+          if (tid == 0) ws.cuts[g] = cut;
+          cut_done = true;
+        }
+        const bool whole = t0 == 0 && t1 == T;
+        const size_t part = size_t(g) * 2 + (t0 == 0 ? 1 : 0);
+        if (c == kLCost4)
+          l_segment<2>(a, ws, u, t0, t1, whole, part, base);
+        else
+          l_segment<1>(a, ws, u, t0, t1, whole, part, base);
+      }
+      at += l_unit_cost(T, u.rows);
+    }
+    if (at >= hi) break;
+    // the next request with rows
+    w.at = at;
+    int next = w.r + 1;
+    for (; next < a.R; next += kWave) {
+      LatLook x = {};
+      if (next + lane < a.R) x = l_look(a, next + lane);
+      const uint64_t in = __ballot(x.n > 0);
+      if (in != 0ull) {
+        next += __ffsll((unsigned long long)in) - 1;
+        break;
+      }
+    }
+    if (next >= a.R) break;
+    w.r = next;
+  }
+  if (!cut_done && tid == 0) ws.cuts[g].parts = 0;
+}
+
+// ------------------------------------------------------------- combine ----
+// Workgroup (g, y): rows 16 y .. 16 y + 15 of the unit in record g; a thread has 32 dims of a row.
+__global__ __launch_bounds__(256) void latent_combine_kernel(LatArgs a, LatWs ws) {
+  const int g = blockIdx.x;
+  const LatCut cut = ws.cuts[g];
+  if (cut.parts == 0) return;
+  const int row = blockIdx.y * 16 + (threadIdx.x & 15);
+  if (row >= cut.rows) return;
+  const int piece = threadIdx.x / 16;
+  float M = -__builtin_inff(), L = 0.0f, Lq = 0.0f;
+  floatx4 acc[8];
+#pragma unroll
+  for (int k = 0; k < 8; ++k) acc[k] = floatx4{0.f, 0.f, 0.f, 0.f};
+  for (int i = 0; i < cut.parts; ++i) {
+    const size_t part = size_t(g - 1 + i) * 2 + (i == 0 ? 1 : 0);
+    const floatx4 ml = *reinterpret_cast<const floatx4*>(ws.part_ml + (part * kLRows + row) * 4);
+    const float* po = ws.part_o + ((part * 4 + (row >> 5)) * 128 + 8 * piece) * 128 + (row & 31) * 4;
+    floatx4 v[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = *reinterpret_cast<const floatx4*>(po + k * 128);
+    const float m = fmaxf(M, ml[0]);
+    if (m == -__builtin_inff()) continue;
+    const float was = __builtin_amdgcn_exp2f(M - m), now = __builtin_amdgcn_exp2f(ml[0] - m);  // 0 from -inf
+    M = m;
+    L = __builtin_fmaf(now, ml[1], L * was);
+    Lq = __builtin_fmaf(now, ml[2], Lq * was);
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[k][e] = __builtin_fmaf(now, v[k][e], acc[k][e] * was);
+  }
+  const float inv = Lq > 0.0f ? 1.0f / Lq : 0.0f;
+  uint16_t* out = a.out + (cut.row + row) * kLC + 32 * piece;
+#pragma unroll
+  for (int k = 0; k < 8; k += 2)
+    *reinterpret_cast<uint4*>(out + 4 * k) =
+        make_uint4(pack_bf16x2(acc[k][0] * inv, acc[k][1] * inv), pack_bf16x2(acc[k][2] * inv, acc[k][3] * inv),
+                   pack_bf16x2(acc[k + 1][0] * inv, acc[k + 1][1] * inv),
+                   pack_bf16x2(acc[k + 1][2] * inv, acc[k + 1][3] * inv));
+  if (a.lse != nullptr && piece == 0)
+    a.lse[cut.row + row] = L > 0.0f ? (M + log2f(L)) * kLn2 : -__builtin_inff();
+}
+
+}  // namespace
+
+size_t attn_latent_workspace_bytes(int32_t R, int32_t max_pages) {
+  size_t n = 0;
+  l_layout(nullptr, R, max_pages, device_cu_count(), &n);
+  return n;
+}
+
+int32_t launch_tree_verify_attn_latent(const AttnLatentArgs& x, hipStream_t stream) {
+  (void)hipGetLastError();
+  const int G = device_cu_count();
+  const LatWs ws = l_layout(x.workspace, x.R, x.max_pages, G, nullptr);
+  LatArgs a;
+  a.q = x.q;
+  a.latent_new = x.latent_new;
+  a.pages = x.cache.pages;
+  a.block_table = x.block_table;
+  a.prefix_len = x.prefix_len;
+  a.q_offsets = x.q_offsets;
+  a.tree_mask = x.tree_mask;
+  a.num_pages = static_cast<long long>(x.cache.num_pages);
+  a.page_shift = 0;
+  while ((1 << a.page_shift) < x.cache.page_size) ++a.page_shift;
+  a.max_pages = x.max_pages;
+  a.W = x.mask_words;
+  a.R = x.R;
+  a.max_rows = x.max_rows;
+  a.hq = x.hq;
+  a.scale2 = x.sm_scale * kLog2e;
+  a.out = x.out;
+  a.lse = x.lse;
+  a.status = x.status;
+  a.chunks = l_page_chunks(a.max_pages);
+  if (a.chunks > 0)
+    hipLaunchKernelGGL(latent_pages_kernel, dim3(unsigned(a.chunks), unsigned(a.R)), dim3(kPageChunk), 0, stream, a,
+                       ws.bad);
+  hipLaunchKernelGGL(latent_main_kernel, dim3(unsigned(G)), dim3(kLThreads), 0, stream, a, ws);
+  const long long rows = (long long)a.max_rows * a.hq;
+  hipLaunchKernelGGL(latent_combine_kernel, dim3(unsigned(G), unsigned((rows < kLRows ? rows : kLRows) + 15) / 16),
+                     dim3(256), 0, stream, a, ws);
+  return hipGetLastError() == hipSuccess ? ECHO_OK : ECHO_ERR_HIP;
+}
+
+}  // namespace echo

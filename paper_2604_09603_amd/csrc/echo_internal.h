@@ -225,6 +225,26 @@ int32_t launch_commit_latent(const int32_t* q_offsets, const int32_t* accept_len
                              int32_t max_pages, const int32_t* prefix_len, int32_t* new_len,
                              int32_t* status, hipStream_t stream);
 
+struct AttnLatentArgs {
+  const uint16_t* q;
+  const uint16_t* latent_new;
+  LatentCacheArgs cache;
+  const int32_t* block_table;
+  int32_t max_pages;
+  const int32_t* prefix_len;
+  const int32_t* q_offsets;
+  const uint32_t* tree_mask;
+  int32_t mask_words;
+  int32_t R, max_rows, hq;
+  float sm_scale;
+  uint16_t* out;
+  float* lse;
+  void* workspace;
+  int32_t* status;
+};
+int32_t launch_tree_verify_attn_latent(const AttnLatentArgs& a, hipStream_t stream);
+size_t attn_latent_workspace_bytes(int32_t R, int32_t max_pages);
+
 // Fused step (front.hip): the end of the gate, flatten & pack and the attention plan
 // (contiguous cache) in one launch, after launch_gate_select_only (unless
 // front_gate_list is negative) and before launch_tree_verify_attn_main.

@@ -1,0 +1,306 @@
+"""GPU parity of the tree attention over the latent paged cache against the oracle, within the
+roundings that the call documents."""
+import numpy as np
+import pytest
+
+from oracle import latent, status as st
+from tests import gpu_common as gc
+from tests.test_gpu_latent import _bf, _bits, _dev, _log, _zeros
+
+pytestmark = pytest.mark.gpu
+NAN = 0x7FC0
+
+
+@pytest.fixture(autouse=True)
+def _need_gpu():
+    gc.require_gpu()
+
+
+def _tree(rng, n, W):
+    """Random ancestor masks of n slots."""
+    m = np.zeros((n, W), np.uint32)
+    for j in range(n):
+        if j:
+            m[j] = m[rng.integers(max(0, j - 5), j)]
+        m[j, j >> 5] |= np.uint32(1 << (j & 31))
+    return m
+
+
+def _case(rng, hq, slots, plens, ps, q_scale=1.0, spare=3, extra_pages=2, grow=None):
+    """NaN wherever no request has a row.  grow: keys whose scores rise along the prefix."""
+    R, cap = len(plens), sum(slots) + spare
+    W = (max(slots) + 31) // 32 if max(slots) else 1
+    qo = np.concatenate([[0], np.cumsum(slots)]).astype(np.int32)
+    mask = np.zeros((cap, W), np.uint32)
+    for r in range(R):
+        mask[qo[r]:qo[r + 1]] = _tree(rng, slots[r], W)
+    npg = [-(-p // ps) for p in plens]
+    perm = rng.permutation(sum(npg) + extra_pages)
+    bt = np.full((R, max(max(npg), 1)), -1, np.int32)
+    pages = np.full((len(perm), ps, 576), NAN, np.uint16)
+    at = 0
+    q = rng.standard_normal((cap, hq, 576)) * q_scale
+    for r in range(R):
+        bt[r, :npg[r]] = perm[at:at + npg[r]]
+        at += npg[r]
+        x = rng.standard_normal((npg[r] * ps, 576))
+        if grow is not None and plens[r] and slots[r]:
+            x = x * 0.2 + np.linspace(0, grow, len(x))[:, None] * q[qo[r], 0] / 576
+        x = _bf(x)
+        x[plens[r]:] = NAN
+        pages[bt[r, :npg[r]]] = x.reshape(npg[r], ps, 576)
+    new = _bf(rng.standard_normal((cap, 576)))
+    new[qo[-1]:] = NAN
+    return dict(R=R, hq=hq, cap=cap, W=W, ps=ps, q=_bf(q), new=new, pages=pages, bt=bt, plen=np.array(plens, np.int32),
+                qo=qo, mask=mask, scale=576 ** -0.5)
+
+
+def _buffers(c):
+    import torch
+    import paper_2604_09603_amd as pkg
+    from paper_2604_09603_amd.step import _aligned_workspace
+    out = torch.full((c["cap"], c["hq"], 512), float("nan"), dtype=torch.bfloat16, device="cuda:0")
+    lse = torch.full((c["cap"], c["hq"]), float("nan"), dtype=torch.float32, device="cuda:0")
+    ws = _aligned_workspace(pkg.tree_verify_attn_latent_workspace_size(c["R"], c["cap"], c["hq"], c["bt"].shape[1]),
+                            "cuda:0")
+    ws.fill_(0xFF)  # NaN everywhere
+    return out, lse, ws, _zeros(1)
+
+
+def _args(c, out, lse, ws, status):
+    return (_dev(c["q"]), _dev(c["new"]), _dev(c["pages"]), c["ps"], _dev(c["bt"]), _dev(c["plen"]), _dev(c["qo"]),
+            _dev(c["mask"]), c["W"], c["R"], c["cap"], c["hq"], 512, 64, c["scale"], out, lse, ws, status)
+
+
+def _run(c):
+    import torch
+    import paper_2604_09603_amd as pkg
+    out, lse, ws, status = _buffers(c)
+    pkg.echo_tree_verify_attn_latent(*_args(c, out, lse, ws, status))
+    torch.cuda.synchronize()
+    return out.float().cpu().numpy(), lse.cpu().numpy(), int(status.item())
+
+
+def _check(c, out, lse, status, want_status=0):
+    """Error bounds, per element.  With w a row's weights, v its values, o its output:
+    * the rounding of each w to bf16 (at most 2^-8 of it), sums of the rounded ones: the output
+      moves by at most 2^-8 / (1 - 2^-8) of the mean |v - o|;
+    * a score's fp32 error: 577 additions and products of 2^-24 each on sum |q k|, twice that for the
+      exponent's products; an exponential's 2^-22: a relative error of w, on the same mean;
+    * fp32 sums over n keys and up to 256 parts: a chain of n / 16 + 256 + 16 steps of 2^-24 of vmax;
+    * the output's own rounding, 2^-8 of it."""
+    ref = latent.tree_verify_attn_latent(c["q"], c["new"], c["pages"], c["bt"], c["plen"], c["qo"], c["mask"], c["hq"],
+                                         c["scale"])
+    assert status == ref["status"] == want_status
+    nq = max(int(c["qo"][-1]), 0)
+    live = ~np.isnan(ref["lse"])
+    assert np.all(np.isnan(out[:nq]) == ~live[..., None]), "rows written or not"
+    assert np.all(np.isnan(out[nq:])) and np.all(np.isnan(lse[nq:]))
+    if not live.any():
+        return
+    o, l = out[:nq][live].astype(np.float64), lse[:nq][live].astype(np.float64)
+    ro, rl = ref["out"][live], ref["lse"][live]
+    dz = ref["zabs"][live][:, None] * (2 * 577 * 2.0 ** -24)
+    keys = int(c["plen"].max()) + c["cap"]
+    tol = (ref["dev"][live] * (2.0 ** -8 / (1 - 2.0 ** -8) + dz + 2.0 ** -22)
+           + ref["vmax"][live][:, None] * (keys / 16 + 272) * 2.0 ** -24)
+    tol = tol * (1 + 2.0 ** -7) + np.abs(ro) * 2.0 ** -8
+    err = np.abs(o - ro)
+    assert np.all(err <= tol), f"off by {np.nanmax(err / np.maximum(tol, 1e-300)):.3f} of the bound"
+    empty = np.isneginf(rl)
+    assert np.array_equal(np.isneginf(l), empty) and np.all(o[empty] == 0)
+    f = ~empty
+    assert np.all(np.abs(l[f] - rl[f]) <= dz[f, 0] + 2.0 ** -18 + np.abs(rl[f]) * 2.0 ** -22)
+
+
+CASES = [
+    # hq, slots, prefixes, page
+    (1, [1], [0], 32), (1, [1], [1], 32), (1, [1, 1, 1], [31, 32, 33], 32), (16, [1], [640], 64),
+    (16, [1, 1, 1], [31, 96, 200], 64), (16, [3, 1], [64, 65], 64), (128, [1], [300], 128), (128, [1, 3], [129, 40], 32),
+    (64, [2, 1, 3], [96, 257, 0], 256), (20, [7, 0, 9], [130, 50, 1], 32), (5, [13, 26, 1], [33, 0, 777], 64),
+    (32, [5, 4, 2, 1], [500, 33, 64, 1000], 32), (16, [33, 64, 65], [10, 0, 70], 32), (3, [100, 17], [31, 100], 64),
+    (12, [6] * 9, [37 * i for i in range(9)], 32), (16, [8, 4], [1500, 900], 64), (127, [1, 2], [63, 31], 32),
+    (129, [1, 1], [95, 1], 32), (300, [1], [70], 64)]
+
+
+@pytest.mark.parametrize("case", range(len(CASES)))
+def test_attention_matches_oracle(case):
+    hq, slots, plens, ps = CASES[case]
+    rng = np.random.default_rng(100 + case)
+    _log(f"[latent attn] hq={hq} slots={slots} P={plens} page={ps}")
+    c = _case(rng, hq, slots, plens, ps, q_scale=[1.0, 3.0][case % 2])
+    _check(c, *_run(c))
+
+
+@pytest.mark.parametrize("grow", [50.0, 3000.0, -3000.0, 40000.0])
+@pytest.mark.parametrize("hq,slots,plens", [(16, [2, 1], [700, 900]), (64, [3, 1], [400, 65])])
+def test_attention_rising_and_falling_scores(hq, slots, plens, grow):
+    """References that are raised in many tiles, and parts whose weights vanish beside others."""
+    rng = np.random.default_rng(int(abs(grow)) + hq)
+    _log(f"[latent attn] grow={grow} hq={hq}")
+    c = _case(rng, hq, slots, plens, 32, grow=grow)
+    _check(c, *_run(c))
+
+
+def test_attention_long_prefixes_are_cut():
+    """Few requests over many workgroups: units of one range to many, equal and unequal."""
+    for k, (hq, slots, plens) in enumerate([(2, [1], [20000]), (2, [1, 2], [5000, 9001]), (70, [1], [4000]),
+                                            (1, [1] * 5, [3000, 0, 31, 8000, 1])]):
+        _log(f"[latent attn] cut hq={hq} P={plens}")
+        c = _case(np.random.default_rng(k), hq, slots, plens, 64)
+        _check(c, *_run(c))
+
+
+def test_attention_masks():
+    """Rows that see nothing, one key, or another row's node; mask words that stop short."""
+    rng = np.random.default_rng(8)
+    c = _case(rng, 24, [5, 40, 3], [0, 0, 64], 32)
+    c["mask"][0] = 0                      # sees nothing
+    c["mask"][1] = [0b10000, 0]           # a later node only
+    c["mask"][2] = 0xFFFFFFFF             # bits past the last slot
+    c["mask"][5:45, 1] = 0                # nodes 32 .. see nothing of their own tile
+    c["mask"][45] = 0                     # the prefix alone
+    _check(c, *_run(c))
+    c = _case(rng, 8, [40], [3], 32)      # one word for 40 slots: nodes past 31 are not seen
+    c["mask"], c["W"] = np.ascontiguousarray(c["mask"][:, :1]), 1
+    _check(c, *_run(c))
+
+
+def test_attention_skips_bad_requests():
+    rng = np.random.default_rng(9)
+    hq, ps = 16, 32
+    plens = [100, 200, 64, 130, 40, 90]
+    for bad in ("low", "high", "late", "length", "negative", "none"):
+        c = _case(rng, hq, [3, 9, 0, 2, 1, 4], plens, ps)
+        if bad == "low":
+            c["bt"][1, 0] = -1
+        elif bad == "high":
+            c["bt"][1, 1] = c["pages"].shape[0]
+        elif bad == "late":
+            c["bt"][1, 6] = 1 << 30
+        elif bad == "length":
+            c["plen"][1] = c["bt"].shape[1] * ps + 1
+        elif bad == "negative":
+            c["plen"][1] = -5
+        else:
+            c["bt"][2, :] = -7            # a request without slots: not looked at
+        _log(f"[latent attn] bad request: {bad}")
+        _check(c, *_run(c), 0 if bad == "none" else st.BAD_OFFSETS)
+
+
+def test_attention_bad_offsets():
+    rng = np.random.default_rng(10)
+    c = _case(rng, 16, [3, 2, 4], [40, 50, 60], 32)
+    c["qo"] = np.array([0, 3, 2, 9], np.int32)      # decreasing for request 1
+    ref_qo = c["qo"].copy()
+    out, lse, status = _run(c)
+    assert status == st.BAD_OFFSETS and np.all(np.isfinite(lse[:3]))
+    c["qo"] = np.array([0, 3, 5, c["cap"] + 1], np.int32)
+    out, lse, status = _run(c)
+    assert status == st.BAD_OFFSETS and np.all(np.isfinite(lse[:5])) and np.all(np.isnan(lse[5:]))
+    c["qo"] = np.array([-1, 3, 5, 9], np.int32)
+    out, lse, status = _run(c)
+    assert status == st.BAD_OFFSETS and np.all(np.isnan(lse[:3])) and np.all(np.isfinite(lse[3:9]))
+    assert ref_qo[1] == 3
+
+
+def test_attention_many_requests():
+    """More requests than workgroups, and than a workgroup has threads; most without slots."""
+    rng = np.random.default_rng(11)
+    for R, some in ((300, 1.0), (2000, 0.1)):
+        slots = (rng.random(R) < some).astype(int) * rng.integers(1, 3, R)
+        slots[0] = 0
+        plens = rng.integers(0, 70, R)
+        _log(f"[latent attn] R={R}")
+        c = _case(rng, 2, slots.tolist(), plens.tolist(), 32)
+        _check(c, *_run(c))
+
+
+def test_attention_wide_block_tables():
+    """Tables past the width that the main kernel checks by itself."""
+    rng = np.random.default_rng(12)
+    for bad in (False, True):
+        c = _case(rng, 4, [2, 1, 1], [90, 32 * 700, 64], 32)
+        assert c["bt"].shape[1] == 700
+        wide = np.full((3, 1200), -1, np.int32)
+        wide[:, :700] = c["bt"]
+        c["bt"] = wide
+        if bad:
+            c["bt"][1, 650] = -1
+        _check(c, *_run(c), st.BAD_OFFSETS if bad else 0)
+
+
+def test_attention_cache_beyond_four_gigabytes():
+    """Pages whose byte offsets pass 32 bits."""
+    import torch
+    import paper_2604_09603_amd as pkg
+    rng = np.random.default_rng(13)
+    c = _case(rng, 16, [2, 1], [100, 60], 64, extra_pages=0)
+    small = _run(c)
+    shift = 70000                                   # 70000 pages of 73728 bytes: 5.2 GB
+    pages = torch.empty((shift + c["pages"].shape[0], 64, 576), dtype=torch.bfloat16, device="cuda:0")
+    pages[shift:] = _dev(c["pages"])
+    out, lse, ws, status = _buffers(c)
+    a = list(_args(c, out, lse, ws, status))
+    a[2], a[4] = pages, _dev(np.where(c["bt"] >= 0, c["bt"] + shift, -1).astype(np.int32))
+    pkg.echo_tree_verify_attn_latent(*a)
+    assert np.array_equal(out.float().cpu().numpy(), small[0], equal_nan=True)
+    assert np.array_equal(lse.cpu().numpy(), small[1], equal_nan=True)
+
+
+def test_attention_captured_and_on_other_streams():
+    """Replays of a captured call over changed lengths, with eager work between them; two streams
+    with workspaces of their own."""
+    import torch
+    import paper_2604_09603_amd as pkg
+    rng = np.random.default_rng(14)
+    c = _case(rng, 16, [4, 1, 7], [300, 900, 64], 64)
+    out, lse, ws, status = _buffers(c)
+    a = _args(c, out, lse, ws, status)
+    pkg.echo_tree_verify_attn_latent(*a)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        pkg.echo_tree_verify_attn_latent(*a)
+    lens = [c["plen"].copy(), np.array([1, 0, 33], np.int32), np.array([290, 512, 0], np.int32), c["plen"].copy()]
+    for plen in lens:
+        a[5].copy_(torch.from_numpy(plen))
+        out.fill_(float("nan"))
+        lse.fill_(float("nan"))
+        x = torch.randn(256, 256, device="cuda:0")
+        (x @ x).sum().item()
+        graph.replay()
+        torch.cuda.synchronize()
+        _check(dict(c, plen=plen), out.float().cpu().numpy(), lse.cpu().numpy(), int(status.item()))
+    two = [_case(rng, 16, [2, 3], [2000, 100], 64), _case(rng, 64, [1, 1], [700, 1200], 64)]
+    bufs = [_buffers(c) for c in two]
+    args = [_args(c, *b) for c, b in zip(two, bufs)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(5):
+        for s, x in zip(streams, args):
+            pkg.echo_tree_verify_attn_latent(*x, stream=s)
+    torch.cuda.synchronize()
+    for c, b in zip(two, bufs):
+        _check(c, b[0].float().cpu().numpy(), b[1].cpu().numpy(), int(b[3].item()))
+
+
+def test_attention_is_deterministic_and_takes_no_lse():
+    import torch
+    import paper_2604_09603_amd as pkg
+    rng = np.random.default_rng(15)
+    c = _case(rng, 48, [3, 5, 1], [1500, 40, 3000], 128)
+    out, lse, ws, status = _buffers(c)
+    a = list(_args(c, out, lse, ws, status))
+    pkg.echo_tree_verify_attn_latent(*a)
+    first = _bits(out)
+    for _ in range(3):
+        out.fill_(float("nan"))
+        ws.fill_(0xFF)
+        pkg.echo_tree_verify_attn_latent(*a)
+        assert np.array_equal(_bits(out), first)
+    a[16] = None
+    out.fill_(float("nan"))
+    pkg.echo_tree_verify_attn_latent(*a)
+    assert np.array_equal(_bits(out), first)
+    torch.cuda.synchronize()

@@ -110,6 +110,41 @@ def test_store_without_rows_is_nothing():
     assert _store(rows=0, kv=None, slot_map=None) == pkg.OK
 
 
+def _attn(**kw):
+    a = dict(q=P(256), latent_new=P(256), **CACHE, block_table=P(256), max_pages=4, prefix_len=P(256), q_offsets=P(256),
+             tree_mask=P(256), mask_words=1, R=2, max_rows=4, hq=16, latent_dim=512, rope_dim=64, scale=0.1, out=P(256),
+             lse=None, ws=P(256), ws_bytes=None, status=None, stream=None)
+    a.update(kw)
+    if a["ws_bytes"] is None:
+        a["ws_bytes"] = pkg.tree_verify_attn_latent_workspace_size(2, 4, 16, 4)
+    return pkg.load().echo_tree_verify_attn_latent(*a.values())
+
+
+@pytest.mark.parametrize("bad,code", BAD_CACHE + [
+    (dict(R=0), INVALID), (dict(R=4096), UNSUPPORTED), (dict(max_rows=-1), INVALID), (dict(hq=0), INVALID),
+    (dict(mask_words=0), INVALID), (dict(max_pages=0), INVALID), (dict(max_pages=1 << 25), UNSUPPORTED),
+    (dict(max_rows=1 << 22), UNSUPPORTED), (dict(hq=1 << 24), UNSUPPORTED), (dict(scale=0.0), INVALID),
+    (dict(scale=NAN), INVALID), (dict(scale=INF), INVALID), (dict(scale=-0.1), INVALID), (dict(q=None), INVALID),
+    (dict(latent_new=None), INVALID), (dict(latent_new=P(8)), INVALID), (dict(q=P(8)), INVALID),
+    (dict(out=P(264)), INVALID), (dict(out=None), INVALID), (dict(block_table=None), INVALID),
+    (dict(prefix_len=None), INVALID), (dict(q_offsets=None), INVALID), (dict(tree_mask=None), INVALID),
+    (dict(ws=None), INVALID), (dict(ws=P(128)), WORKSPACE), (dict(ws_bytes=1024), WORKSPACE)])
+def test_attention_refuses(bad, code):
+    assert _attn(**bad) == code
+
+
+def test_attention_without_rows_is_nothing():
+    assert _attn(max_rows=0) == pkg.OK
+
+
+def test_workspace_sizes():
+    size = pkg.tree_verify_attn_latent_workspace_size
+    assert size(2, 4, 16, 4) > 0
+    assert size(4095, 4, 16, 1000) > size(4095, 4, 16, 1)
+    assert size(0, 4, 16, 4) == 0 and size(2, 4, 16, 0) == 0 and size(2, 4, 0, 4) == 0
+    assert size(2, 4, 16, 4, latent_dim=256) == 0 and size(2, 4, 16, 4, rope_dim=32) == 0
+
+
 def _commit(**kw):
     a = dict(q_offsets=P(256), accept_len=P(256), accept_slots=P(256), max_depth=4, latent_new=P(256), R=2, max_rows=4,
              latent_dim=512, rope_dim=64, **CACHE, block_table=P(256), max_pages=4, prefix_len=P(256), new_len=P(256),
