@@ -35,11 +35,16 @@ constexpr int kLSteps = kLRow / 32;            // products along a row of K
 // wave's transposed V read takes four chunks each, fall into 16 different sixteenths
 // of the banks.
 constexpr int kLBlock = kTileKeys * 128;       // 4 KB
-constexpr int kLTile = kLRowBytes * kTileKeys; // 36 KB
-constexpr int kLSlots = 4;
+// Four slots for the blocks that hold values (a tile is scored a step before its values are
+// taken, and two more are on their way), three for the block that only the scores see.
+constexpr int kLSlots = 4, kLRopeSlots = 3;
+constexpr int kLSlot = 8 * kLBlock;
 constexpr int kLProb = kLRows * kTileKeys * 2; // the weights of a tile
-constexpr int kLStats = 2048;
-constexpr int kLLds = kLSlots * kLTile + kLProb + kLStats;
+constexpr int kLRopeAt = kLSlots * kLSlot, kLProbAt = kLRopeAt + kLRopeSlots * kLBlock;
+constexpr int kLStatsAt = kLProbAt + 2 * kLProb;
+// (factors [2][128], flags [2][4], inverse sums [128])
+constexpr int kLFlagsAt = kLStatsAt + 2 * kLRows * 4, kLInvAt = kLFlagsAt + 32;
+constexpr int kLLds = kLInvAt + kLRows * 4;
 static_assert(kLLds <= 160 * 1024, "gfx950 LDS per CU");
 constexpr int kLOwnPages = 512;                // block tables up to this wide are checked in place
 
@@ -206,21 +211,23 @@ __device__ __forceinline__ bool l_pages_ok(const LatArgs& a, const LatWs& ws, in
 }
 
 // ---------------------------------------------------------------- main ----
-// Copies a wave's eight rows of a tile: 9 x 1 KB, to LDS address lds and every 4 KB on.  The
-// instructions' offset moves both addresses.  In inline assembly because the compiler would
-// wait for every copy in flight before each LDS read; M0 (the LDS address) is the
-// compiler's and is restored, and needs a wait state before a load reads it.
-__device__ __forceinline__ void l_copy(uint32_t lds, uint64_t base, uint32_t off) {
+// Copies a wave's eight rows of a tile: eight times 1 KB to LDS address lds and every 4 KB on, the
+// ninth to rope.  The instructions' offset moves both addresses.  In inline assembly
+// because the compiler would wait for every copy in flight before each LDS read; M0 (the
+// LDS address) is the compiler's and is restored, and needs a wait state before a load
+// reads it.
+__device__ __forceinline__ void l_copy(uint32_t lds, uint32_t rope, uint64_t base, uint32_t off) {
   uint32_t saved;
 #define ECHO_L_NEXT(OFF)                                                                \
   "s_add_u32 m0, m0, 0xf80\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3 offset:" OFF "\n\t"
   asm volatile(
       "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3\n\t"
       ECHO_L_NEXT("0x80") ECHO_L_NEXT("0x100") ECHO_L_NEXT("0x180") ECHO_L_NEXT("0x200")
-      ECHO_L_NEXT("0x280") ECHO_L_NEXT("0x300") ECHO_L_NEXT("0x380") ECHO_L_NEXT("0x400")
+      ECHO_L_NEXT("0x280") ECHO_L_NEXT("0x300") ECHO_L_NEXT("0x380")
+      "s_mov_b32 m0, %4\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3 offset:0x400\n\t"
       "s_mov_b32 m0, %0"
       : "=&s"(saved)
-      : "s"(lds), "v"(off), "s"(base)
+      : "s"(lds), "v"(off), "s"(base), "s"(rope - 0x400u)
       : "memory", "scc");
 #undef ECHO_L_NEXT
 }
@@ -230,8 +237,23 @@ struct LatUnit {
   int q0, n, P, r, row0, rows, tree_tiles;
 };
 
-// Sends for tile t of a unit.
-__device__ __forceinline__ void l_send(const LatArgs& a, const LatUnit& u, int t, uint32_t slot_lds) {
+// The pages of 64 tiles of a unit's prefix, tile at + i in lane i: one vector of loads, where
+// scalar ones would be waited for with every LDS read.
+struct LatTable {
+  int page, at;
+};
+__device__ __forceinline__ void l_fill(LatTable& tb, const LatArgs& a, const LatUnit& u, int t) {
+  const int lane = threadIdx.x & (kWave - 1);
+  tb.at = t;
+  const long long key = (long long)(t + lane - u.tree_tiles) * kTileKeys;
+  tb.page = 0;
+  if (key >= 0 && key < u.P)
+    tb.page = a.block_table[size_t(u.r) * size_t(a.max_pages) + size_t(key >> a.page_shift)];
+}
+
+// Sends for tile t of a unit, the n-th that its workgroup sends for.
+__device__ __forceinline__ void l_send(LatTable& tb, const LatArgs& a, const LatUnit& u, int t, int n,
+                                       uint32_t smem) {
   const int lane = threadIdx.x & (kWave - 1), w = wave_id();
   uint64_t base;
   int tn;
@@ -240,16 +262,19 @@ __device__ __forceinline__ void l_send(const LatArgs& a, const LatUnit& u, int t
     tn = u.n - t * kTileKeys;
   } else {
     const int key = (t - u.tree_tiles) * kTileKeys;
-    const_i32_t* bt = (const_i32_t*)(a.block_table + size_t(u.r) * size_t(a.max_pages));
-    const uint64_t row = (uint64_t(uint32_t(bt[key >> a.page_shift])) << a.page_shift) +
-                         uint32_t(key & ((1 << a.page_shift) - 1));
+    if (t >= tb.at + kWave) l_fill(tb, a, u, t);
+    const uint32_t page = uint32_t(__builtin_amdgcn_readlane(tb.page, t - tb.at));
+    const uint64_t row = (uint64_t(page) << a.page_shift) + uint32_t(key & ((1 << a.page_shift) - 1));
     base = reinterpret_cast<uint64_t>(a.pages) + row * kLRowBytes;
     tn = u.P - key;
   }
   const int key = 8 * w + (lane >> 3);
   // (rows past the tile's keys: the last one again, so that nothing unwritten is multiplied)
   const uint32_t off = uint32_t(min(key, tn - 1) * kLRowBytes + (((lane & 7) ^ l_swz(key)) << 4));
-  l_copy(__builtin_amdgcn_readfirstlane(slot_lds + uint32_t(w * 1024)), uniform64(base), off);
+  const uint32_t at = smem + uint32_t(w * 1024);
+  l_copy(__builtin_amdgcn_readfirstlane(at + uint32_t(n & (kLSlots - 1)) * kLSlot),
+         __builtin_amdgcn_readfirstlane(at + kLRopeAt + (unsigned(n) % kLRopeSlots) * kLBlock),
+         uniform64(base), off);
 }
 
 __device__ __forceinline__ float quad_max(float v) {  // over the four lanes of a row
@@ -276,79 +301,134 @@ __device__ __forceinline__ void l_mfma(floatx16& acc, bf16x8 x, bf16x8 y) {
 }
 __device__ __forceinline__ void l_settle(floatx16& acc) { asm volatile("s_nop 15\n\ts_nop 15" : "+a"(acc)); }
 
-// Tiles [t0, t1) of a unit, then its output (whole) or partial sums (part).  QR: 16-row tiles of
-// a wave's part of Q; the unit has up to 64 QR rows.
+#define ECHO_FENCE() __builtin_amdgcn_sched_barrier(0)
+
+// A wave's state over a unit.
 template <int QR>
-__device__ __forceinline__ void l_segment(const LatArgs& a, const LatWs& ws, const LatUnit& u, int t0,
-                                          int t1, bool whole, size_t part, uint32_t smem) {
-  constexpr int RT = 2 * QR;  // 32-row tiles of the unit
-  const int lane = threadIdx.x & (kWave - 1), w = wave_id();
-  const int l16 = lane & 15, quad = lane >> 4, h = lane >> 5;
-  const uint32_t prob = smem + kLSlots * kLTile, stats = prob + kLProb;
-  const size_t first = size_t(u.q0) * a.hq + size_t(u.row0);  // the unit's first row of q
-
-  for (int t = t0; t < min(t0 + kLSlots - 1, t1); ++t)
-    l_send(a, u, t, smem + uint32_t((t - t0) & (kLSlots - 1)) * kLTile);
-  // Q: row l16 of each 16-row tile, dims 32 ks + 8 quad .. (rows past the last: the last again)
-  bf16x8 q[QR][kLSteps];
-  int slot[QR];
-#pragma unroll
-  for (int i = 0; i < QR; ++i) {
-    const int row = min(16 * (QR * w + i) + l16, u.rows - 1);
-    const uint16_t* p = a.q + (first + row) * kLRow + 8 * quad;
-#pragma unroll
-    for (int ks = 0; ks < kLSteps; ++ks) q[i][ks] = as_bf16x8(*reinterpret_cast<const uint4*>(p + 32 * ks));
-    slot[i] = u.q0 + (u.row0 + row) / a.hq;
-  }
-  floatx16 o[RT][4];
-#pragma unroll
-  for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-    for (int ct = 0; ct < 4; ++ct) o[rt][ct] = floatx16{};
+struct LatState {
+  bf16x8 q[QR][kLSteps];   // row l16 of each 16-row tile, dims 32 ks + 8 quad ..
+  floatx16 o[2 * QR][4];   // O^T: row tile, dims 128 w + 32 ct + 8 (r >> 2) + 4 h + (r & 3)
   float m[QR], grow_at[QR], l[QR], lq[QR];
-#pragma unroll
-  for (int i = 0; i < QR; ++i) {
-    m[i] = grow_at[i] = -__builtin_inff();
-    l[i] = lq[i] = 0.0f;
-  }
-  // LDS offsets in a tile (the header of this file has the products' shapes)
-  const uint32_t ka = uint32_t(l16 * 128 + ((quad ^ l_swz(l16)) << 4));
-  const int vkey = 4 * h + (l16 >> 2);
-  const uint32_t vchunk = uint32_t((2 * (quad & 1) + ((l16 & 3) >> 1)) ^ l_swz(vkey));
-  const uint32_t va = uint32_t(2 * w * kLBlock + vkey * 128 + ((l16 & 1) << 3)) + (vchunk << 4);
-  const uint32_t pw = prob + uint32_t((QR == 2 ? w : w >> 1) * 2048 + ((QR == 2 ? 0 : 16 * (w & 1)) + l16) * 16 +
-                                      (quad & 1) * 512 + (quad >> 1) * 8);
+  int slot[QR];
+};
 
-  for (int t = t0; t < t1; ++t) {
-    const int behind = min(t1 - 1 - t, kLSlots - 2);  // tiles sent after this one
-    if (behind >= 2) wait_vm<2 * kLCopies>();
-    else if (behind == 1) wait_vm<kLCopies>();
+// One step: the scores of tile t + 1 (kScores), which is the n + 1-th copied, and the values of
+// tile t (kValues), the n-th.  The softmax of t + 1 is computed between the products of t.
+template <int QR, bool kScores, bool kValues>
+__device__ __forceinline__ void l_step(LatState<QR>& st, LatTable& tb, const LatArgs& a, const LatUnit& u, int t,
+                                       int t1, int n, uint32_t smem, uint32_t ka, uint32_t va, uint32_t pw) {
+  constexpr int RT = 2 * QR;  // 32-row tiles of the unit
+  constexpr int kAhead = 2;   // steps of 32 dims that K's reads are ahead of its products
+  const int lane = threadIdx.x & (kWave - 1), w = wave_id();
+  const int l16 = lane & 15, quad = lane >> 4;
+  // tile t + 1 has landed (t + 2 may be behind it), the weights of t are written
+  if (kScores) {
+    if (t + 2 < t1) wait_vm<kLCopies>();
     else wait_vm<0>();
-    l_barrier();  // every wave's part of the tile has landed; the last tile's slot is free
-    if (t + kLSlots - 1 < t1)
-      l_send(a, u, t + kLSlots - 1, smem + uint32_t((t + kLSlots - 1 - t0) & (kLSlots - 1)) * kLTile);
-    const uint32_t tile = smem + uint32_t((t - t0) & (kLSlots - 1)) * kLTile;
-    // S^T: keys 16 kt + 4 quad + r of row l16
-    floatx4 s[QR][2];
+  }
+  wait_lds();
+  l_barrier();
+  if (kScores && t + 3 < t1) l_send(tb, a, u, t + 3, n + 3, smem);
+
+  const uint32_t now = smem + uint32_t(n & (kLSlots - 1)) * kLSlot;
+  const uint32_t next = smem + uint32_t((n + 1) & (kLSlots - 1)) * kLSlot;
+  const uint32_t rope = smem + kLRopeAt + (unsigned(n + 1) % kLRopeSlots) * kLBlock;
+  const uint32_t buf = uint32_t(n & 1), buf1 = buf ^ 1u;
+  if (kValues) {  // O is scaled where a reference was raised
+    const uint4v flags = *(lds_uint4_t*)lds_at(smem + kLFlagsAt + 16 * buf);
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      const uint32_t f0 = QR == 2 ? flags[rt & 3] : flags[(2 * rt) & 3], f1 = QR == 2 ? f0 : flags[(2 * rt + 1) & 3];
+      if (__builtin_amdgcn_readfirstlane(int(f0 | f1)) != 0) {
+        float alpha = *(lds_float_t*)lds_at(smem + kLStatsAt + buf * (kLRows * 4) + uint32_t((32 * rt + (lane & 31)) * 4));
+        alpha = (quad & 1 ? f1 : f0) != 0 ? alpha : 1.0f;
+#pragma unroll
+        for (int ct = 0; ct < 4; ++ct) {
+          l_settle(st.o[rt][ct]);
+          st.o[rt][ct] *= alpha;
+        }
+      }
+    }
+  }
+  const uint32_t kb = next + ka, rb = rope + ka, vb = now + va;
+  const uint32_t pb = smem + kLProbAt + buf * kLProb + uint32_t(lane * 16);
+  bf16x8 kf[kAhead + 1][2], vf[2], pf[RT];
+  floatx4 s[QR][2];
+  const auto read_k = [&](int ks) {
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt)
+      kf[ks % (kAhead + 1)][kt] = __builtin_bit_cast(
+          bf16x8, ks < 16 ? *(lds_uint4_t*)(lds_at(kb ^ uint32_t((ks & 1) << 6)) + (ks >> 1) * kLBlock + kt * 2048)
+                          : *(lds_uint4_t*)(lds_at(rb ^ uint32_t((ks & 1) << 6)) + kt * 2048));
+  };
+  const auto read_v = [&](int g) {  // keys 16 (g / 4) .., dims 32 (g % 4) .. of the wave's
+    const int kg = g >> 2, ct = g & 3;
+    shortx4 v[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+      v[k] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+          (lds_shortx4_t*)(lds_at(vb ^ uint32_t(((ct & 1) << 6) | (k << 5))) + (ct >> 1) * kLBlock + kg * 2048 + k * 1024));
+    vf[g & 1] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7));
+  };
+  const auto read_p = [&](int kg, int rt) {
+    pf[rt] = __builtin_bit_cast(bf16x8, *(lds_uint4_t*)(lds_at(pb) + rt * 2048 + kg * 1024));
+  };
+  if (kScores) {
 #pragma unroll
     for (int i = 0; i < QR; ++i) s[i][0] = s[i][1] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int ks = 0; ks < kLSteps; ++ks)
+    for (int ks = 0; ks < kAhead; ++ks) read_k(ks);
+  }
+  if (kValues) {
+    read_v(0);
 #pragma unroll
-      for (int kt = 0; kt < 2; ++kt) {
-        const bf16x8 k = __builtin_bit_cast(
-            bf16x8, *(lds_uint4_t*)(lds_at((tile + ka) ^ uint32_t((ks & 1) << 6)) + (ks >> 1) * kLBlock + kt * 2048));
+    for (int rt = 0; rt < RT; ++rt) read_p(0, rt);
+  }
+  // S^T: keys 16 kt + 4 quad + r of row l16; three of the eight groups of products with V among its own
+  if (kScores) {
 #pragma unroll
-        for (int i = 0; i < QR; ++i) s[i][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[i][ks], s[i][kt], 0, 0, 0);
+    for (int ks = 0; ks < kLSteps; ++ks) {
+      if (ks + kAhead < kLSteps) read_k(ks + kAhead);
+      if (kValues && ks % 6 == 3) {
+        const int g = ks / 6;
+        read_v(g + 1);
+        ECHO_FENCE();
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) l_mfma(st.o[rt][g], vf[g & 1], pf[rt]);
       }
+      ECHO_FENCE();
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+        for (int i = 0; i < QR; ++i)
+          s[i][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[ks % (kAhead + 1)][kt], st.q[i][ks], s[i][kt], 0, 0, 0);
+      ECHO_FENCE();
+    }
+  }
+  if (kValues) {
+#pragma unroll
+    for (int g = kScores ? 3 : 0; g < 4; ++g) {
+      read_v(g + 1);
+      ECHO_FENCE();
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        l_mfma(st.o[rt][g], vf[g & 1], pf[rt]);
+        if (g == 3) read_p(1, rt);
+        ECHO_FENCE();
+      }
+    }
+  }
+  float neg_m[QR];
+  if (kScores) {
     // masks: the tree's words, the prefix's last tile
-    const bool tree = t < u.tree_tiles;
-    const int tn = tree ? u.n - t * kTileKeys : u.P - (t - u.tree_tiles) * kTileKeys;
+    const int tt = t + 1;
+    const bool tree = tt < u.tree_tiles;
+    const int tn = tree ? u.n - tt * kTileKeys : u.P - (tt - u.tree_tiles) * kTileKeys;
     if (tree || tn < kTileKeys) {
 #pragma unroll
       for (int i = 0; i < QR; ++i) {
         uint32_t word = 0xFFFFFFFFu;
-        if (tree) word = t < a.W ? a.tree_mask[size_t(slot[i]) * a.W + t] : 0u;
+        if (tree) word = tt < a.W ? a.tree_mask[size_t(st.slot[i]) * a.W + tt] : 0u;
         if (tn < kTileKeys) word &= (1u << tn) - 1u;
         word >>= 4 * quad;
 #pragma unroll
@@ -365,94 +445,115 @@ __device__ __forceinline__ void l_segment(const LatArgs& a, const LatWs& ws, con
     for (int i = 0; i < QR; ++i) {
       top[i] = fmaxf(fmaxf(fmaxf(s[i][0][0], s[i][0][1]), fmaxf(s[i][0][2], s[i][0][3])),
                      fmaxf(fmaxf(s[i][1][0], s[i][1][1]), fmaxf(s[i][1][2], s[i][1][3]))) * a.scale2;
-      up |= top[i] > grow_at[i];
+      up |= top[i] > st.grow_at[i];
     }
     const bool raised = __ballot(up) != 0ull;
     if (raised) {
 #pragma unroll
       for (int i = 0; i < QR; ++i) {
         const float mt = quad_max(top[i]);
-        const bool grow = mt > grow_at[i];
-        const float alpha = grow ? __builtin_amdgcn_exp2f(m[i] - mt) : 1.0f;  // 0 from -inf
-        l[i] *= alpha;
-        lq[i] *= alpha;
-        m[i] = grow ? mt : m[i];
-        grow_at[i] = m[i] + kRescaleSlack;
-        if (quad == 0) *(lds_float_t*)lds_at(stats + uint32_t((16 * (QR * w + i) + l16) * 4)) = alpha;
+        const bool grow = mt > st.grow_at[i];
+        const float alpha = grow ? __builtin_amdgcn_exp2f(st.m[i] - mt) : 1.0f;  // 0 from -inf
+        st.l[i] *= alpha;
+        st.lq[i] *= alpha;
+        st.m[i] = grow ? mt : st.m[i];
+        st.grow_at[i] = st.m[i] + kRescaleSlack;
+        if (quad == 0)
+          *(lds_float_t*)lds_at(smem + kLStatsAt + buf1 * (kLRows * 4) + uint32_t((16 * (QR * w + i) + l16) * 4)) = alpha;
       }
     }
-    if (lane == 0) *(lds_int_t*)lds_at(stats + 512 + uint32_t(4 * w)) = raised ? 1 : 0;
+    if (lane == 0) *(lds_int_t*)lds_at(smem + kLFlagsAt + 16 * buf1 + uint32_t(4 * w)) = raised ? 1 : 0;
 #pragma unroll
-    for (int i = 0; i < QR; ++i) {
-      const float neg_m = m[i] == -__builtin_inff() ? 0.0f : -m[i];
-#pragma unroll
-      for (int kt = 0; kt < 2; ++kt) {
-        float p[4];
-#pragma unroll
-        for (int r = 0; r < 4; ++r) p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i][kt][r], a.scale2, neg_m));
-        l[i] += (p[0] + p[1]) + (p[2] + p[3]);
-        const uint32_t x = pack_bf16x2(p[0], p[1]), y = pack_bf16x2(p[2], p[3]);
-        lq[i] = add_bf16x2(y, add_bf16x2(x, lq[i]));
-        *(lds_uint2_t*)(lds_at(pw) + kt * 1024 + i * 256) = uint2v{x, y};
-      }
-    }
-    wait_lds();
-    l_barrier();  // the weights are there
-    // O is scaled where a reference was raised
-    const uint4v flags = *(lds_uint4_t*)lds_at(stats + 512);
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-      const uint32_t f0 = QR == 2 ? flags[rt & 3] : flags[(2 * rt) & 3], f1 = QR == 2 ? f0 : flags[(2 * rt + 1) & 3];
-      if (__builtin_amdgcn_readfirstlane(int(f0 | f1)) != 0) {
-        float alpha = *(lds_float_t*)lds_at(stats + uint32_t((32 * rt + (lane & 31)) * 4));
-        alpha = (quad & 1 ? f1 : f0) != 0 ? alpha : 1.0f;
-#pragma unroll
-        for (int ct = 0; ct < 4; ++ct) {
-          l_settle(o[rt][ct]);
-          o[rt][ct] *= alpha;
-        }
-      }
-    }
-#pragma unroll
-    for (int kg = 0; kg < 2; ++kg) {
-      bf16x8 pf[RT];
-#pragma unroll
-      for (int rt = 0; rt < RT; ++rt)
-        pf[rt] = __builtin_bit_cast(bf16x8, *(lds_uint4_t*)(lds_at(prob + uint32_t(lane * 16)) + rt * 2048 + kg * 1024));
-#pragma unroll
-      for (int ct = 0; ct < 4; ++ct) {
-        shortx4 v[2];
-#pragma unroll
-        for (int k = 0; k < 2; ++k)
-          v[k] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-              (lds_shortx4_t*)(lds_at((tile + va) ^ uint32_t(((ct & 1) << 6) | (k << 5))) + (ct >> 1) * kLBlock +
-                               kg * 2048 + k * 1024));
-        const bf16x8 vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7));
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt)
-          l_mfma(o[rt][ct], vf, pf[rt]);
-      }
-    }
+    for (int i = 0; i < QR; ++i) neg_m[i] = st.m[i] == -__builtin_inff() ? 0.0f : -st.m[i];
   }
+  uint32_t half = 0;
+  const auto two = [&](int p) {  // weights 2 (p % 2) and the next of tile p / 2 % 2 of row tile p / 4
+    const int i = p >> 2, kt = (p >> 1) & 1, r = 2 * (p & 1);
+    const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i][kt][r], a.scale2, neg_m[i]));
+    const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i][kt][r + 1], a.scale2, neg_m[i]));
+    st.l[i] += x + y;
+    const uint32_t xy = pack_bf16x2(x, y);
+    st.lq[i] = add_bf16x2(xy, st.lq[i]);
+    if (r == 0) half = xy;
+    else *(lds_uint2_t*)(lds_at(pw + buf1 * kLProb) + kt * 1024 + i * 256) = uint2v{half, xy};
+  };
+  if (kValues) {
+#pragma unroll
+    for (int g = 4; g < 8; ++g) {
+      if (g < 7) read_v(g + 1);
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        ECHO_FENCE();
+        l_mfma(st.o[rt][g & 3], vf[g & 1], pf[rt]);
+        ECHO_FENCE();
+        if (kScores && (rt & 1) == 0) two(((g - 4) * RT + rt) >> 1);
+      }
+    }
+    ECHO_FENCE();
+  } else {
+#pragma unroll
+    for (int p = 0; p < 4 * QR; ++p) two(p);
+  }
+}
 
+// Tiles [t0, t1) of a unit, then its output (whole) or partial sums (part).  QR: 16-row tiles of
+// a wave's part of Q; the unit has up to 64 QR rows.
+template <int QR>
+__device__ __forceinline__ void l_segment(const LatArgs& a, const LatWs& ws, const LatUnit& u, int t0,
+                                          int t1, bool whole, size_t part, uint32_t smem) {
+  constexpr int RT = 2 * QR;
+  const int lane = threadIdx.x & (kWave - 1), w = wave_id();
+  const int l16 = lane & 15, quad = lane >> 4, h = lane >> 5;
+  const size_t first = size_t(u.q0) * a.hq + size_t(u.row0);  // the unit's first row of q
+
+  LatTable tb;
+  l_fill(tb, a, u, t0);
+  l_send(tb, a, u, t0, 0, smem);
+  if (t0 + 1 < t1) l_send(tb, a, u, t0 + 1, 1, smem);
+  LatState<QR> st;
+#pragma unroll
+  for (int i = 0; i < QR; ++i) {  // (rows past the last: the last again)
+    const int row = min(16 * (QR * w + i) + l16, u.rows - 1);
+    const uint16_t* p = a.q + (first + row) * kLRow + 8 * quad;
+#pragma unroll
+    for (int ks = 0; ks < kLSteps; ++ks) st.q[i][ks] = as_bf16x8(*reinterpret_cast<const uint4*>(p + 32 * ks));
+    st.slot[i] = u.q0 + (u.row0 + row) / a.hq;
+    st.m[i] = st.grow_at[i] = -__builtin_inff();
+    st.l[i] = st.lq[i] = 0.0f;
+  }
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-    for (int ct = 0; ct < 4; ++ct) l_settle(o[rt][ct]);
+    for (int ct = 0; ct < 4; ++ct) st.o[rt][ct] = floatx16{};
+  // LDS offsets in a tile
+  const uint32_t ka = uint32_t(l16 * 128 + ((quad ^ l_swz(l16)) << 4));
+  const int vkey = 4 * h + (l16 >> 2);
+  const uint32_t vchunk = uint32_t((2 * (quad & 1) + ((l16 & 3) >> 1)) ^ l_swz(vkey));
+  const uint32_t va = uint32_t(2 * w * kLBlock + vkey * 128 + ((l16 & 1) << 3)) + (vchunk << 4);
+  const uint32_t pw = smem + kLProbAt + uint32_t((QR == 2 ? w : w >> 1) * 2048 +
+                                                 ((QR == 2 ? 0 : 16 * (w & 1)) + l16) * 16 + (quad & 1) * 512 +
+                                                 (quad >> 1) * 8);
+  l_step<QR, true, false>(st, tb, a, u, t0 - 1, t1, -1, smem, ka, va, pw);
+#pragma unroll 1
+  for (int t = t0; t + 1 < t1; ++t) l_step<QR, true, true>(st, tb, a, u, t, t1, t - t0, smem, ka, va, pw);
+  l_step<QR, false, true>(st, tb, a, u, t1 - 1, t1, t1 - 1 - t0, smem, ka, va, pw);
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+    for (int ct = 0; ct < 4; ++ct) l_settle(st.o[rt][ct]);
+
   // the sums of a row are its wave's; every wave needs their inverses
-  float L[QR], Lq[QR];
 #pragma unroll
   for (int i = 0; i < QR; ++i) {
-    L[i] = quad_sum(l[i]);
-    Lq[i] = quad_sum(lq[i]);
+    const float L = quad_sum(st.l[i]), Lq = quad_sum(st.lq[i]);
     const int row = 16 * (QR * w + i) + l16;
     if (quad == 0) {
-      *(lds_float_t*)lds_at(stats + 1024 + uint32_t(row * 4)) = Lq[i] > 0.0f ? 1.0f / Lq[i] : 0.0f;
+      *(lds_float_t*)lds_at(smem + kLInvAt + uint32_t(row * 4)) = Lq > 0.0f ? 1.0f / Lq : 0.0f;
       if (row < u.rows) {
         if (!whole)
-          *reinterpret_cast<floatx4*>(ws.part_ml + (part * kLRows + row) * 4) = floatx4{m[i], L[i], Lq[i], 0.0f};
+          *reinterpret_cast<floatx4*>(ws.part_ml + (part * kLRows + row) * 4) = floatx4{st.m[i], L, Lq, 0.0f};
         else if (a.lse != nullptr)
-          a.lse[first + row] = L[i] > 0.0f ? (m[i] + log2f(L[i])) * kLn2 : -__builtin_inff();
+          a.lse[first + row] = L > 0.0f ? (st.m[i] + log2f(L)) * kLn2 : -__builtin_inff();
       }
     }
   }
@@ -463,15 +564,15 @@ __device__ __forceinline__ void l_segment(const LatArgs& a, const LatWs& ws, con
     const int row = 32 * rt + (lane & 31);
     if (row < u.rows) {
       if (whole) {
-        const float inv = *(lds_float_t*)lds_at(stats + 1024 + uint32_t(row * 4));
+        const float inv = *(lds_float_t*)lds_at(smem + kLInvAt + uint32_t(row * 4));
         uint16_t* po = a.out + (first + row) * kLC + 128 * w + 4 * h;
 #pragma unroll
         for (int ct = 0; ct < 4; ++ct)
 #pragma unroll
           for (int r = 0; r < 16; r += 4)
             *reinterpret_cast<uint2*>(po + 32 * ct + 2 * r) =
-                make_uint2(pack_bf16x2(o[rt][ct][r] * inv, o[rt][ct][r + 1] * inv),
-                           pack_bf16x2(o[rt][ct][r + 2] * inv, o[rt][ct][r + 3] * inv));
+                make_uint2(pack_bf16x2(st.o[rt][ct][r] * inv, st.o[rt][ct][r + 1] * inv),
+                           pack_bf16x2(st.o[rt][ct][r + 2] * inv, st.o[rt][ct][r + 3] * inv));
       } else {
         float* po = ws.part_o + ((part * 4 + rt) * 128 + 32 * w + h) * 128 + (lane & 31) * 4;
 #pragma unroll
@@ -479,7 +580,7 @@ __device__ __forceinline__ void l_segment(const LatArgs& a, const LatWs& ws, con
 #pragma unroll
           for (int r = 0; r < 16; r += 4)
             *reinterpret_cast<floatx4*>(po + (8 * ct + (r >> 1)) * 128) =
-                floatx4{o[rt][ct][r], o[rt][ct][r + 1], o[rt][ct][r + 2], o[rt][ct][r + 3]};
+                floatx4{st.o[rt][ct][r], st.o[rt][ct][r + 1], st.o[rt][ct][r + 2], st.o[rt][ct][r + 3]};
       }
     }
   }
