@@ -42,15 +42,18 @@ constexpr int kLSlot = 8 * kLBlock;
 constexpr int kLProb = kLRows * kTileKeys * 2; // the weights of a tile
 constexpr int kLRopeAt = kLSlots * kLSlot, kLProbAt = kLRopeAt + kLRopeSlots * kLBlock;
 constexpr int kLStatsAt = kLProbAt + 2 * kLProb;
-// (factors [2][128], flags [2][4], inverse sums [128])
-constexpr int kLFlagsAt = kLStatsAt + 2 * kLRows * 4, kLInvAt = kLFlagsAt + 32;
+// (factors [2][128], flags [2][4 waves], inverse sums [128])
+constexpr int kLFlagsAt = kLStatsAt + 2 * kLRows * 4, kLInvAt = kLFlagsAt + 16;
 constexpr int kLLds = kLInvAt + kLRows * 4;
 static_assert(kLLds <= 160 * 1024, "gfx950 LDS per CU");
 constexpr int kLOwnPages = 512;                // block tables up to this wide are checked in place
 
-// Costs of a tile with more than 64 rows, of one with fewer, of entering a unit.
-constexpr int kLCost4 = 4, kLCost2 = 2, kLEnter = 6;
-constexpr int kLMinCost = 16;                  // of a range
+// Costs of a tile of a unit with more than 64 rows, of one with fewer, of entering a unit (its rows
+// of Q, its first tile, its output); the smallest of a range, which is a power of two and
+// no smaller than a tile's, so that every range within a unit has a tile.
+constexpr int kLCost4 = 4, kLCost2 = 3, kLEnter = 16;
+constexpr int kLMinShift = 3;
+static_assert((1 << kLMinShift) >= kLCost4, "a tile in every range");
 
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 typedef uint32_t uint4v __attribute__((ext_vector_type(4)));
@@ -58,7 +61,8 @@ typedef uint32_t uint2v __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) uint4v lds_uint4_t;
 typedef __attribute__((address_space(3))) uint2v lds_uint2_t;
 typedef __attribute__((address_space(3))) float lds_float_t;
-typedef __attribute__((address_space(3))) int lds_int_t;
+typedef __attribute__((address_space(3))) uint32_t lds_uint_t;
+typedef __attribute__((address_space(3))) uint8_t lds_byte_t;
 typedef __attribute__((address_space(3))) char lds_char_t;
 __device__ __forceinline__ lds_char_t* lds_at(uint32_t x) { return (lds_char_t*)(uintptr_t(x)); }
 
@@ -176,27 +180,28 @@ __device__ __forceinline__ long long wave_scan64(long long v) {
 }
 __device__ __forceinline__ long long uniform_ll(long long x) { return (long long)uniform64(uint64_t(x)); }
 
+// Ranges 0 .. 2^shift - 1 of [0, total).
 struct LatRanges {
   long long total;
-  int G;  // ranges
-  __device__ __forceinline__ long long first(int g) const { return total * g / G; }
+  int shift;
+  __device__ __forceinline__ long long first(int g) const { return (total * g) >> shift; }
   // The range that holds cost x.
   __device__ __forceinline__ int range_of(long long x) const {
-    int g = int(double(x) * G / double(total));
+    const int n = 1 << shift;
+    int g = min(int(float(x) * float(n) * __builtin_amdgcn_rcpf(float(total))), n - 1);
     while (g > 0 && first(g) > x) --g;
-    while (g + 1 < G && first(g + 1) <= x) ++g;
+    while (g + 1 < n && first(g + 1) <= x) ++g;
     return g;
   }
 };
+// The first tile that starts at cost x or later, of T tiles of cost c from cost 0 on.
+__device__ __forceinline__ int l_tile_at(long long x, int c, int T) {
+  if (x <= 0) return 0;
+  if (x > (long long)(T - 1) * c) return T;
+  return int((unsigned(x) + unsigned(c - 1)) / unsigned(c));  // (T < 2^27)
+}
 
-// Where a workgroup is: request r (whose units start at cost at), unit j of it.
-struct LatWalk {
-  LatLook x;
-  int r, j;
-  long long at;
-};
-
-// Whether a request's pages are all in the pool (all threads; one barrier).
+// Whether a request's pages are all in the pool (all threads; waits for all loads, and a barrier).
 __device__ __forceinline__ bool l_pages_ok(const LatArgs& a, const LatWs& ws, int r, int P) {
   const int np = l_prefix_pages(P, a);
   const bool own = a.chunks == 0;
@@ -207,31 +212,22 @@ __device__ __forceinline__ bool l_pages_ok(const LatArgs& a, const LatWs& ws, in
     const int v = e[i];
     bad |= own ? v < 0 || v >= a.num_pages : v != 0;
   }
-  return __syncthreads_or(bad) == 0;
+  return __builtin_amdgcn_readfirstlane(__syncthreads_or(bad)) == 0;
 }
 
 // ---------------------------------------------------------------- main ----
-// Copies a wave's eight rows of a tile: eight times 1 KB to LDS address lds and every 4 KB on, the
-// ninth to rope.  The instructions' offset moves both addresses.  In inline assembly
-// because the compiler would wait for every copy in flight before each LDS read; M0 (the
-// LDS address) is the compiler's and is restored, and needs a wait state before a load
-// reads it.
-__device__ __forceinline__ void l_copy(uint32_t lds, uint32_t rope, uint64_t base, uint32_t off) {
-  uint32_t saved;
-#define ECHO_L_NEXT(OFF)                                                                \
-  "s_add_u32 m0, m0, 0xf80\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3 offset:" OFF "\n\t"
-  asm volatile(
-      "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3\n\t"
-      ECHO_L_NEXT("0x80") ECHO_L_NEXT("0x100") ECHO_L_NEXT("0x180") ECHO_L_NEXT("0x200")
-      ECHO_L_NEXT("0x280") ECHO_L_NEXT("0x300") ECHO_L_NEXT("0x380")
-      "s_mov_b32 m0, %4\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3 offset:0x400\n\t"
-      "s_mov_b32 m0, %0"
-      : "=&s"(saved)
-      : "s"(lds), "v"(off), "s"(base), "s"(rope - 0x400u)
-      : "memory", "scc");
-#undef ECHO_L_NEXT
-}
+// Piece B (of nine) of the copy of a wave's eight rows of a tile: 1 KB, from base + off + 128 B to
+// LDS address lds + 4096 B (B < 8) or rope.  The instruction's offset moves both addresses.
+// In inline assembly because the compiler would wait for every copy in flight before each
+// LDS read; M0, the LDS address, needs a wait state before a load reads it.
 constexpr int kLCopies = 9;  // loads of a wave per tile
+template <int B>
+__device__ __forceinline__ void l_copy(uint32_t lds, uint32_t rope, uint64_t base, uint32_t off) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 offset:%3"
+               :
+               : "s"(B < 8 ? lds + uint32_t(B * (kLBlock - 128)) : rope - 8 * 128u), "v"(off), "s"(base), "n"(B * 128)
+               : "memory", "m0");
+}
 
 struct LatUnit {
   int q0, n, P, r, row0, rows, tree_tiles;
@@ -249,32 +245,66 @@ __device__ __forceinline__ void l_fill(LatTable& tb, const LatArgs& a, const Lat
   tb.page = 0;
   if (key >= 0 && key < u.P)
     tb.page = a.block_table[size_t(u.r) * size_t(a.max_pages) + size_t(key >> a.page_shift)];
+  if (tb.page < 0 || tb.page >= a.num_pages) tb.page = 0;  // (read before the pages are checked)
+  asm volatile("" : "+v"(tb.page));  // (waited for here, not where every step would)
 }
 
-// Sends for tile t of a unit, the n-th that its workgroup sends for.
-__device__ __forceinline__ void l_send(LatTable& tb, const LatArgs& a, const LatUnit& u, int t, int n,
-                                       uint32_t smem) {
-  const int lane = threadIdx.x & (kWave - 1), w = wave_id();
+// The lane, formed where it is used: what would be kept from it over a step is reloaded from
+// memory, behind every copy in flight.
+__device__ __forceinline__ int l_lane() {
+  int x = int(__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u)));
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
+__device__ __forceinline__ int l_opaque(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
+// What the copies of a tile take: tile t of a unit, the n-th that its workgroup copies.
+struct LatCopy {
   uint64_t base;
+  uint32_t off, lds, rope;
+  template <int B>
+  __device__ __forceinline__ void piece() const { l_copy<B>(lds, rope, base, off); }
+};
+__device__ __forceinline__ LatCopy l_tile(LatTable& tb, const LatArgs& a, const LatUnit& u, int t, int n,
+                                          uint32_t smem) {
+  const int lane = l_lane(), w = wave_id();
+  LatCopy c;
   int tn;
   if (t < u.tree_tiles) {
-    base = reinterpret_cast<uint64_t>(a.latent_new) + uint64_t(u.q0 + t * kTileKeys) * kLRowBytes;
+    c.base = reinterpret_cast<uint64_t>(a.latent_new) + uint64_t(u.q0 + t * kTileKeys) * kLRowBytes;
     tn = u.n - t * kTileKeys;
   } else {
     const int key = (t - u.tree_tiles) * kTileKeys;
     if (t >= tb.at + kWave) l_fill(tb, a, u, t);
     const uint32_t page = uint32_t(__builtin_amdgcn_readlane(tb.page, t - tb.at));
     const uint64_t row = (uint64_t(page) << a.page_shift) + uint32_t(key & ((1 << a.page_shift) - 1));
-    base = reinterpret_cast<uint64_t>(a.pages) + row * kLRowBytes;
+    c.base = reinterpret_cast<uint64_t>(a.pages) + row * kLRowBytes;
     tn = u.P - key;
   }
+  c.base = uniform64(c.base);
   const int key = 8 * w + (lane >> 3);
   // (rows past the tile's keys: the last one again, so that nothing unwritten is multiplied)
-  const uint32_t off = uint32_t(min(key, tn - 1) * kLRowBytes + (((lane & 7) ^ l_swz(key)) << 4));
+  c.off = uint32_t(min(key, tn - 1) * kLRowBytes + (((lane & 7) ^ l_swz(key)) << 4));
   const uint32_t at = smem + uint32_t(w * 1024);
-  l_copy(__builtin_amdgcn_readfirstlane(at + uint32_t(n & (kLSlots - 1)) * kLSlot),
-         __builtin_amdgcn_readfirstlane(at + kLRopeAt + (unsigned(n) % kLRopeSlots) * kLBlock),
-         uniform64(base), off);
+  c.lds = __builtin_amdgcn_readfirstlane(at + uint32_t(n & (kLSlots - 1)) * kLSlot);
+  c.rope = __builtin_amdgcn_readfirstlane(at + kLRopeAt + (unsigned(n) % kLRopeSlots) * kLBlock);
+  return c;
+}
+__device__ __forceinline__ void l_send(LatTable& tb, const LatArgs& a, const LatUnit& u, int t, int n, uint32_t smem) {
+  const LatCopy c = l_tile(tb, a, u, t, n, smem);
+  c.piece<0>();
+  c.piece<1>();
+  c.piece<2>();
+  c.piece<3>();
+  c.piece<4>();
+  c.piece<5>();
+  c.piece<6>();
+  c.piece<7>();
+  c.piece<8>();
 }
 
 __device__ __forceinline__ float quad_max(float v) {  // over the four lanes of a row
@@ -308,19 +338,20 @@ template <int QR>
 struct LatState {
   bf16x8 q[QR][kLSteps];   // row l16 of each 16-row tile, dims 32 ks + 8 quad ..
   floatx16 o[2 * QR][4];   // O^T: row tile, dims 128 w + 32 ct + 8 (r >> 2) + 4 h + (r & 3)
-  float m[QR], grow_at[QR], l[QR], lq[QR];
+  float m[QR], l[QR], lq[QR];
   int slot[QR];
 };
 
 // One step: the scores of tile t + 1 (kScores), which is the n + 1-th copied, and the values of
-// tile t (kValues), the n-th.  The softmax of t + 1 is computed between the products of t.
+// tile t (kValues), the n-th; copies for tile t + 3.  A tile's 16-key groups x 32-dim
+// columns are eight groups of products with V: two are taken between the next tile's scores,
+// the others beside its softmax.
 template <int QR, bool kScores, bool kValues>
 __device__ __forceinline__ void l_step(LatState<QR>& st, LatTable& tb, const LatArgs& a, const LatUnit& u, int t,
                                        int t1, int n, uint32_t smem, uint32_t ka, uint32_t va, uint32_t pw) {
   constexpr int RT = 2 * QR;  // 32-row tiles of the unit
   constexpr int kAhead = 2;   // steps of 32 dims that K's reads are ahead of its products
-  const int lane = threadIdx.x & (kWave - 1), w = wave_id();
-  const int l16 = lane & 15, quad = lane >> 4;
+  const int w = wave_id();
   // tile t + 1 has landed (t + 2 may be behind it), the weights of t are written
   if (kScores) {
     if (t + 2 < t1) wait_vm<kLCopies>();
@@ -328,30 +359,13 @@ __device__ __forceinline__ void l_step(LatState<QR>& st, LatTable& tb, const Lat
   }
   wait_lds();
   l_barrier();
-  if (kScores && t + 3 < t1) l_send(tb, a, u, t + 3, n + 3, smem);
 
   const uint32_t now = smem + uint32_t(n & (kLSlots - 1)) * kLSlot;
   const uint32_t next = smem + uint32_t((n + 1) & (kLSlots - 1)) * kLSlot;
   const uint32_t rope = smem + kLRopeAt + (unsigned(n + 1) % kLRopeSlots) * kLBlock;
   const uint32_t buf = uint32_t(n & 1), buf1 = buf ^ 1u;
-  if (kValues) {  // O is scaled where a reference was raised
-    const uint4v flags = *(lds_uint4_t*)lds_at(smem + kLFlagsAt + 16 * buf);
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-      const uint32_t f0 = QR == 2 ? flags[rt & 3] : flags[(2 * rt) & 3], f1 = QR == 2 ? f0 : flags[(2 * rt + 1) & 3];
-      if (__builtin_amdgcn_readfirstlane(int(f0 | f1)) != 0) {
-        float alpha = *(lds_float_t*)lds_at(smem + kLStatsAt + buf * (kLRows * 4) + uint32_t((32 * rt + (lane & 31)) * 4));
-        alpha = (quad & 1 ? f1 : f0) != 0 ? alpha : 1.0f;
-#pragma unroll
-        for (int ct = 0; ct < 4; ++ct) {
-          l_settle(st.o[rt][ct]);
-          st.o[rt][ct] *= alpha;
-        }
-      }
-    }
-  }
   const uint32_t kb = next + ka, rb = rope + ka, vb = now + va;
-  const uint32_t pb = smem + kLProbAt + buf * kLProb + uint32_t(lane * 16);
+  const uint32_t pb = smem + kLProbAt + buf * kLProb + uint32_t(l_lane() * 16);
   bf16x8 kf[kAhead + 1][2], vf[2], pf[RT];
   floatx4 s[QR][2];
   const auto read_k = [&](int ks) {
@@ -367,34 +381,63 @@ __device__ __forceinline__ void l_step(LatState<QR>& st, LatTable& tb, const Lat
 #pragma unroll
     for (int k = 0; k < 2; ++k)
       v[k] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-          (lds_shortx4_t*)(lds_at(vb ^ uint32_t(((ct & 1) << 6) | (k << 5))) + (ct >> 1) * kLBlock + kg * 2048 + k * 1024));
+          (lds_shortx4_t*)(lds_at(uint32_t(l_opaque(int(vb))) ^ uint32_t(((ct & 1) << 6) | (k << 5))) + (ct >> 1) * kLBlock + kg * 2048 + k * 1024));
     vf[g & 1] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7));
   };
   const auto read_p = [&](int kg, int rt) {
     pf[rt] = __builtin_bit_cast(bf16x8, *(lds_uint4_t*)(lds_at(pb) + rt * 2048 + kg * 1024));
   };
+  const auto group = [&](int g) {
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) l_mfma(st.o[rt][g & 3], vf[g & 1], pf[rt]);
+  };
+
+  uint32_t flags = 0;  // (a byte for each wave)
+  if (kValues) flags = *(lds_uint_t*)lds_at(smem + kLFlagsAt + 4 * buf);
+  if (kScores) {
+#pragma unroll
+    for (int ks = 0; ks < kAhead; ++ks) read_k(ks);
+  }
+  LatCopy copy = {};
+  const bool send = kScores && kValues && t + 3 < t1;
+  if (send) copy = l_tile(tb, a, u, t + 3, n + 3, smem);
+  if (kValues) {
+    // O is scaled where a reference was raised
+    flags = uint32_t(__builtin_amdgcn_readfirstlane(int(flags)));
+    if (flags != 0) {
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        const uint32_t f = QR == 2 ? flags >> (8 * rt) : flags >> (16 * rt);
+        if ((f & (QR == 2 ? 0xFFu : 0xFFFFu)) != 0) {
+          const int lane = l_lane();
+          float alpha = *(lds_float_t*)lds_at(smem + kLStatsAt + buf * (kLRows * 4) + uint32_t((32 * rt + (lane & 31)) * 4));
+          if (QR == 1) alpha = ((f >> (8 * ((lane >> 4) & 1))) & 0xFFu) != 0 ? alpha : 1.0f;
+#pragma unroll
+          for (int ct = 0; ct < 4; ++ct) {
+            l_settle(st.o[rt][ct]);
+            st.o[rt][ct] *= alpha;
+          }
+        }
+      }
+    }
+  }
+  // S^T: keys 16 kt + 4 quad + r of row l16
   if (kScores) {
 #pragma unroll
     for (int i = 0; i < QR; ++i) s[i][0] = s[i][1] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int ks = 0; ks < kAhead; ++ks) read_k(ks);
-  }
-  if (kValues) {
-    read_v(0);
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) read_p(0, rt);
-  }
-  // S^T: keys 16 kt + 4 quad + r of row l16; three of the eight groups of products with V among its own
-  if (kScores) {
-#pragma unroll
     for (int ks = 0; ks < kLSteps; ++ks) {
       if (ks + kAhead < kLSteps) read_k(ks + kAhead);
-      if (kValues && ks % 6 == 3) {
-        const int g = ks / 6;
+      if (kValues && ks == 5) {
+        read_v(0);
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) read_p(0, rt);
+      }
+      if (kValues && (ks == 8 || ks == 13)) {
+        const int g = ks == 8 ? 0 : 1;
         read_v(g + 1);
         ECHO_FENCE();
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) l_mfma(st.o[rt][g], vf[g & 1], pf[rt]);
+        group(g);
       }
       ECHO_FENCE();
 #pragma unroll
@@ -403,66 +446,102 @@ __device__ __forceinline__ void l_step(LatState<QR>& st, LatTable& tb, const Lat
         for (int i = 0; i < QR; ++i)
           s[i][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[ks % (kAhead + 1)][kt], st.q[i][ks], s[i][kt], 0, 0, 0);
       ECHO_FENCE();
+      if (kValues && send) {
+        if (ks == 0) {
+          copy.piece<0>();
+          copy.piece<1>();
+        }
+        if (ks == 1) {
+          copy.piece<2>();
+          copy.piece<3>();
+        }
+        if (ks == 2) {
+          copy.piece<4>();
+          copy.piece<5>();
+        }
+        if (ks == 3) {
+          copy.piece<6>();
+          copy.piece<7>();
+        }
+        if (ks == 4) copy.piece<8>();
+      }
     }
-  }
-  if (kValues) {
+  } else if (kValues) {
+    read_v(0);
 #pragma unroll
-    for (int g = kScores ? 3 : 0; g < 4; ++g) {
+    for (int rt = 0; rt < RT; ++rt) read_p(0, rt);
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
       read_v(g + 1);
       ECHO_FENCE();
-#pragma unroll
-      for (int rt = 0; rt < RT; ++rt) {
-        l_mfma(st.o[rt][g], vf[g & 1], pf[rt]);
-        if (g == 3) read_p(1, rt);
-        ECHO_FENCE();
-      }
+      group(g);
+      ECHO_FENCE();
     }
   }
-  float neg_m[QR];
-  if (kScores) {
-    // masks: the tree's words, the prefix's last tile
-    const int tt = t + 1;
-    const bool tree = tt < u.tree_tiles;
-    const int tn = tree ? u.n - tt * kTileKeys : u.P - (tt - u.tree_tiles) * kTileKeys;
-    if (tree || tn < kTileKeys) {
-#pragma unroll
-      for (int i = 0; i < QR; ++i) {
-        uint32_t word = 0xFFFFFFFFu;
-        if (tree) word = tt < a.W ? a.tree_mask[size_t(st.slot[i]) * a.W + tt] : 0u;
-        if (tn < kTileKeys) word &= (1u << tn) - 1u;
-        word >>= 4 * quad;
-#pragma unroll
-        for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-          for (int r = 0; r < 4; ++r)
-            s[i][kt][r] = ((word >> (16 * kt + r)) & 1u) ? s[i][kt][r] : -__builtin_inff();
-      }
-    }
-    // The reference is raised only when a logit exceeds it by more than 2^8, so that weights stay <= 256.
-    float top[QR];
-    bool up = false;
+  const int tt = t + 1;
+  const bool tree = tt < u.tree_tiles;
+  const int tn = tree ? u.n - tt * kTileKeys : u.P - (tt - u.tree_tiles) * kTileKeys;
+  float top[QR], neg_m[QR];
+  if (kValues) {
+    read_v(3);
+    ECHO_FENCE();
+    l_mfma(st.o[0][2], vf[0], pf[0]);
+    ECHO_FENCE();
+  }
+  if (kScores && (tree || tn < kTileKeys)) {  // masks: the tree's words, the prefix's last tile
 #pragma unroll
     for (int i = 0; i < QR; ++i) {
-      top[i] = fmaxf(fmaxf(fmaxf(s[i][0][0], s[i][0][1]), fmaxf(s[i][0][2], s[i][0][3])),
-                     fmaxf(fmaxf(s[i][1][0], s[i][1][1]), fmaxf(s[i][1][2], s[i][1][3]))) * a.scale2;
-      up |= top[i] > st.grow_at[i];
+      const int quad = l_lane() >> 4;
+      uint32_t word = 0xFFFFFFFFu;
+      if (tree) word = tt < a.W ? a.tree_mask[size_t(l_opaque(st.slot[i])) * a.W + tt] : 0u;
+      if (tn < kTileKeys) word &= (1u << tn) - 1u;
+      word >>= 4 * quad;
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          s[i][kt][r] = ((word >> (16 * kt + r)) & 1u) ? s[i][kt][r] : -__builtin_inff();
     }
+  }
+  const auto max_of = [&](int i) {
+    top[i] = fmaxf(fmaxf(fmaxf(s[i][0][0], s[i][0][1]), fmaxf(s[i][0][2], s[i][0][3])),
+                   fmaxf(fmaxf(s[i][1][0], s[i][1][1]), fmaxf(s[i][1][2], s[i][1][3]))) * a.scale2;
+  };
+  if (kValues) {
+#pragma unroll
+    for (int rt = 1; rt < RT; ++rt) {
+      ECHO_FENCE();
+      l_mfma(st.o[rt][2], vf[0], pf[rt]);
+      ECHO_FENCE();
+      if (kScores && rt <= QR) max_of(rt - 1);
+    }
+    if (kScores && QR == RT) max_of(QR - 1);
+  } else if (kScores) {
+#pragma unroll
+    for (int i = 0; i < QR; ++i) max_of(i);
+  }
+  if (kScores) {
+    // The reference is raised only when a logit exceeds it by more than 2^8, so that weights stay <= 256.
+    bool up = false;
+#pragma unroll
+    for (int i = 0; i < QR; ++i) up |= top[i] > st.m[i] + kRescaleSlack;
     const bool raised = __ballot(up) != 0ull;
     if (raised) {
 #pragma unroll
       for (int i = 0; i < QR; ++i) {
         const float mt = quad_max(top[i]);
-        const bool grow = mt > st.grow_at[i];
+        const bool grow = mt > st.m[i] + kRescaleSlack;
         const float alpha = grow ? __builtin_amdgcn_exp2f(st.m[i] - mt) : 1.0f;  // 0 from -inf
         st.l[i] *= alpha;
         st.lq[i] *= alpha;
         st.m[i] = grow ? mt : st.m[i];
-        st.grow_at[i] = st.m[i] + kRescaleSlack;
-        if (quad == 0)
-          *(lds_float_t*)lds_at(smem + kLStatsAt + buf1 * (kLRows * 4) + uint32_t((16 * (QR * w + i) + l16) * 4)) = alpha;
+        const int lane = l_lane();
+        if (lane < 16)
+          *(lds_float_t*)lds_at(smem + kLStatsAt + buf1 * (kLRows * 4) + uint32_t((16 * (QR * w + i) + lane) * 4)) = alpha;
       }
     }
-    if (lane == 0) *(lds_int_t*)lds_at(smem + kLFlagsAt + 16 * buf1 + uint32_t(4 * w)) = raised ? 1 : 0;
+    if (l_lane() == 0) *(lds_byte_t*)lds_at(smem + kLFlagsAt + 4 * buf1 + uint32_t(w)) =
+        kValues && raised ? 1 : 0;  // (before the first values O is 0)
 #pragma unroll
     for (int i = 0; i < QR; ++i) neg_m[i] = st.m[i] == -__builtin_inff() ? 0.0f : -st.m[i];
   }
@@ -479,14 +558,16 @@ __device__ __forceinline__ void l_step(LatState<QR>& st, LatTable& tb, const Lat
   };
   if (kValues) {
 #pragma unroll
-    for (int g = 4; g < 8; ++g) {
+    for (int g = 3; g < 8; ++g) {
       if (g < 7) read_v(g + 1);
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) {
         ECHO_FENCE();
         l_mfma(st.o[rt][g & 3], vf[g & 1], pf[rt]);
         ECHO_FENCE();
-        if (kScores && (rt & 1) == 0) two(((g - 4) * RT + rt) >> 1);
+        if (g == 3) read_p(1, rt);
+        const int p = (g - 3) * RT + rt;
+        if (kScores && p < 4 * QR) two(p);
       }
     }
     ECHO_FENCE();
@@ -497,35 +578,42 @@ __device__ __forceinline__ void l_step(LatState<QR>& st, LatTable& tb, const Lat
 }
 
 // Tiles [t0, t1) of a unit, then its output (whole) or partial sums (part).  QR: 16-row tiles of
-// a wave's part of Q; the unit has up to 64 QR rows.
+// a wave's part of Q; the unit has up to 64 QR rows.  check: the request's pages have not
+// been looked at yet; false if they are not all in the pool, and nothing is written.
 template <int QR>
-__device__ __forceinline__ void l_segment(const LatArgs& a, const LatWs& ws, const LatUnit& u, int t0,
-                                          int t1, bool whole, size_t part, uint32_t smem) {
+__device__ __forceinline__ bool l_segment(const LatArgs& a, const LatWs& ws, const LatUnit& u, int t0,
+                                          int t1, bool whole, size_t part, bool check, uint32_t smem) {
   constexpr int RT = 2 * QR;
-  const int lane = threadIdx.x & (kWave - 1), w = wave_id();
-  const int l16 = lane & 15, quad = lane >> 4, h = lane >> 5;
+  const int w = wave_id();
   const size_t first = size_t(u.q0) * a.hq + size_t(u.row0);  // the unit's first row of q
 
+  LatState<QR> st;
+#pragma unroll
+  for (int i = 0; i < QR; ++i) {  // (rows past the last: the last again)
+    const int lane = l_lane();
+    const int row = min(16 * (QR * w + i) + (lane & 15), u.rows - 1);
+    const uint16_t* p = a.q + (first + row) * kLRow + 8 * (lane >> 4);
+#pragma unroll
+    for (int ks = 0; ks < kLSteps; ++ks) st.q[i][ks] = as_bf16x8(*reinterpret_cast<const uint4*>(p + 32 * ks));
+    st.slot[i] = u.q0 + (u.row0 + row) / a.hq;
+    st.m[i] = -__builtin_inff();
+    st.l[i] = st.lq[i] = 0.0f;
+  }
   LatTable tb;
   l_fill(tb, a, u, t0);
   l_send(tb, a, u, t0, 0, smem);
   if (t0 + 1 < t1) l_send(tb, a, u, t0 + 1, 1, smem);
-  LatState<QR> st;
-#pragma unroll
-  for (int i = 0; i < QR; ++i) {  // (rows past the last: the last again)
-    const int row = min(16 * (QR * w + i) + l16, u.rows - 1);
-    const uint16_t* p = a.q + (first + row) * kLRow + 8 * quad;
-#pragma unroll
-    for (int ks = 0; ks < kLSteps; ++ks) st.q[i][ks] = as_bf16x8(*reinterpret_cast<const uint4*>(p + 32 * ks));
-    st.slot[i] = u.q0 + (u.row0 + row) / a.hq;
-    st.m[i] = st.grow_at[i] = -__builtin_inff();
-    st.l[i] = st.lq[i] = 0.0f;
+  if (check && !l_pages_ok(a, ws, u.r, u.P)) {
+    wait_vm<0>();  // (nothing is on its way to LDS)
+    l_barrier();
+    return false;
   }
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
     for (int ct = 0; ct < 4; ++ct) st.o[rt][ct] = floatx16{};
   // LDS offsets in a tile
+  const int lane = l_lane(), l16 = lane & 15, quad = lane >> 4, h = lane >> 5;
   const uint32_t ka = uint32_t(l16 * 128 + ((quad ^ l_swz(l16)) << 4));
   const int vkey = 4 * h + (l16 >> 2);
   const uint32_t vchunk = uint32_t((2 * (quad & 1) + ((l16 & 3) >> 1)) ^ l_swz(vkey));
@@ -534,9 +622,11 @@ __device__ __forceinline__ void l_segment(const LatArgs& a, const LatWs& ws, con
                                                  ((QR == 2 ? 0 : 16 * (w & 1)) + l16) * 16 + (quad & 1) * 512 +
                                                  (quad >> 1) * 8);
   l_step<QR, true, false>(st, tb, a, u, t0 - 1, t1, -1, smem, ka, va, pw);
+  if (t0 + 2 < t1) l_send(tb, a, u, t0 + 2, 2, smem);
+  int t = t0;
 #pragma unroll 1
-  for (int t = t0; t + 1 < t1; ++t) l_step<QR, true, true>(st, tb, a, u, t, t1, t - t0, smem, ka, va, pw);
-  l_step<QR, false, true>(st, tb, a, u, t1 - 1, t1, t1 - 1 - t0, smem, ka, va, pw);
+  for (; t + 1 < t1; ++t) l_step<QR, true, true>(st, tb, a, u, t, t1, t - t0, smem, ka, va, pw);
+  l_step<QR, false, true>(st, tb, a, u, t, t1, t - t0, smem, ka, va, pw);
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
@@ -546,8 +636,9 @@ __device__ __forceinline__ void l_segment(const LatArgs& a, const LatWs& ws, con
 #pragma unroll
   for (int i = 0; i < QR; ++i) {
     const float L = quad_sum(st.l[i]), Lq = quad_sum(st.lq[i]);
-    const int row = 16 * (QR * w + i) + l16;
-    if (quad == 0) {
+    const int lane = l_lane();
+    const int row = 16 * (QR * w + i) + (lane & 15);
+    if (lane < 16) {
       *(lds_float_t*)lds_at(smem + kLInvAt + uint32_t(row * 4)) = Lq > 0.0f ? 1.0f / Lq : 0.0f;
       if (row < u.rows) {
         if (!whole)
@@ -559,31 +650,47 @@ __device__ __forceinline__ void l_segment(const LatArgs& a, const LatWs& ws, con
   }
   wait_lds();
   l_barrier();  // (the slots are free too)
+  if (whole) {
+    // O^T through the wave's own slot: 32 rows x 256 bytes, 16-byte chunk c of row r at c ^ (r & 15), so
+    // that a row's 256 bytes go out in one piece
+    const uint32_t own = smem + uint32_t(w) * kLSlot;
 #pragma unroll
-  for (int rt = 0; rt < RT; ++rt) {
-    const int row = 32 * rt + (lane & 31);
-    if (row < u.rows) {
-      if (whole) {
-        const float inv = *(lds_float_t*)lds_at(smem + kLInvAt + uint32_t(row * 4));
-        uint16_t* po = a.out + (first + row) * kLC + 128 * w + 4 * h;
+    for (int rt = 0; rt < RT; ++rt) {
+      const int lane = l_lane(), rl = lane & 31, h = lane >> 5;
+      const float inv = *(lds_float_t*)lds_at(smem + kLInvAt + uint32_t((32 * rt + rl) * 4));
 #pragma unroll
-        for (int ct = 0; ct < 4; ++ct)
+      for (int ct = 0; ct < 4; ++ct)
 #pragma unroll
-          for (int r = 0; r < 16; r += 4)
-            *reinterpret_cast<uint2*>(po + 32 * ct + 2 * r) =
-                make_uint2(pack_bf16x2(st.o[rt][ct][r] * inv, st.o[rt][ct][r + 1] * inv),
-                           pack_bf16x2(st.o[rt][ct][r + 2] * inv, st.o[rt][ct][r + 3] * inv));
-      } else {
-        float* po = ws.part_o + ((part * 4 + rt) * 128 + 32 * w + h) * 128 + (lane & 31) * 4;
+        for (int r = 0; r < 16; r += 4)
+          *(lds_uint2_t*)lds_at(own + uint32_t(rt * 8192 + rl * 256 + (((4 * ct + (r >> 2)) ^ (rl & 15)) << 4) + 8 * h)) =
+              uint2v{pack_bf16x2(st.o[rt][ct][r] * inv, st.o[rt][ct][r + 1] * inv),
+                     pack_bf16x2(st.o[rt][ct][r + 2] * inv, st.o[rt][ct][r + 3] * inv)};
+    }
+    const int lane = l_lane(), l16 = lane & 15, quad = lane >> 4;
+    uint16_t* po = a.out + first * kLC + 128 * w + 8 * l16;
 #pragma unroll
-        for (int ct = 0; ct < 4; ++ct)
+    for (int k = 0; k < 8 * RT; ++k) {
+      const int row = 4 * k + quad;
+      const uint4v x = *(lds_uint4_t*)lds_at(own + uint32_t(row * 256 + ((l16 ^ (row & 15)) << 4)));
+      if (row < u.rows) *reinterpret_cast<uint4v*>(po + size_t(row) * kLC) = x;
+    }
+    wait_lds();
+    l_barrier();  // (the next unit's tiles take the slots)
+  } else {
 #pragma unroll
-          for (int r = 0; r < 16; r += 4)
-            *reinterpret_cast<floatx4*>(po + (8 * ct + (r >> 1)) * 128) =
-                floatx4{st.o[rt][ct][r], st.o[rt][ct][r + 1], st.o[rt][ct][r + 2], st.o[rt][ct][r + 3]};
-      }
+    for (int rt = 0; rt < RT; ++rt) {
+      const int lane = l_lane(), h = lane >> 5;
+      if (32 * rt + (lane & 31) >= u.rows) continue;
+      float* po = ws.part_o + ((part * 4 + rt) * 128 + 32 * w + h) * 128 + (lane & 31) * 4;
+#pragma unroll
+      for (int ct = 0; ct < 4; ++ct)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4)
+          *reinterpret_cast<floatx4*>(po + (8 * ct + (r >> 1)) * 128) =
+              floatx4{st.o[rt][ct][r], st.o[rt][ct][r + 1], st.o[rt][ct][r + 2], st.o[rt][ct][r + 3]};
     }
   }
+  return true;
 }
 
 __global__ __launch_bounds__(kLThreads) __attribute__((amdgpu_waves_per_eu(1, 1))) void latent_main_kernel(
@@ -618,145 +725,144 @@ __global__ __launch_bounds__(kLThreads) __attribute__((amdgpu_waves_per_eu(1, 1)
   __syncthreads();
   LatRanges ranges;
   ranges.total = uniform_ll(total);
-  ranges.G = int(min((long long)nwg, max(ranges.total / kLMinCost, 1ll)));
+  // as many as there are workgroups, or fewer (powers of two)
+  ranges.shift = 31 - __builtin_clz(nwg);
+  while (ranges.shift > 0 && (ranges.total >> (ranges.shift + kLMinShift)) == 0) --ranges.shift;
   // neighbouring ranges, which share requests, run on one XCD (workgroup b is on XCD b % 8)
   int g = blockIdx.x;
-  if (ranges.G == nwg && nwg % 8 == 0) g = (g & 7) * (nwg / 8) + (g >> 3);
-  if (g >= ranges.G || ranges.total == 0) {
-    if (tid == 0) ws.cuts[blockIdx.x].parts = 0;
-    return;
-  }
+  if ((1 << ranges.shift) == nwg && nwg % 8 == 0) g = (g & 7) * (nwg / 8) + (g >> 3);
+  if (tid == 0) ws.cuts[g].parts = 0;  // (unless there is one: below, by the same thread)
+  if (g >= (1 << ranges.shift) || ranges.total == 0) return;
   const long long lo = ranges.first(g), hi = ranges.first(g + 1);
   // the last thread whose requests start at lo or before, and which of its requests it is
   int th = 0;
 #pragma unroll
   for (int v = 0; v < kLWaves; ++v) th += __popcll(__ballot(s_start[v * kWave + lane] <= lo));
   th = __builtin_amdgcn_readfirstlane(th) - 1;
-  LatWalk w;
+  LatLook x = {};
+  int r = th * K + lane;
+  if (lane < K && r < a.R) x = l_look(a, r);
+  long long at;  // where the request's units start
   {
-    LatLook x = {};
-    const int r = th * K + lane;
-    if (lane < K && r < a.R) x = l_look(a, r);
     const long long c = l_cost(a, x);
     const long long end = s_start[th] + wave_scan64(c);
     const int i = __ffsll((unsigned long long)__ballot(end > lo)) - 1;
-    w.r = th * K + i;
-    w.at = uniform_ll(__shfl(end - c, i));
+    r = th * K + i;
+    at = __shfl(end - c, i);
+    x.q0 = __shfl(x.q0, i);
+    x.n = __shfl(x.n, i);
+    x.P = __shfl(x.P, i);
   }
   __syncthreads();  // (the tiles take this memory)
   const uint32_t base = __builtin_amdgcn_readfirstlane(uint32_t(reinterpret_cast<uintptr_t>((lds_void_t*)smem)));
-  w.j = -1;
-  bool cut_done = false;
+  bool first_unit = true;
   while (true) {
-    // a request: its units from w.at on
-    w.r = __builtin_amdgcn_readfirstlane(w.r);
-    {
-      const LatLook x = l_look(a, w.r);
-      w.x.q0 = __builtin_amdgcn_readfirstlane(x.q0);
-      w.x.n = __builtin_amdgcn_readfirstlane(x.n);
-      w.x.P = __builtin_amdgcn_readfirstlane(x.P);
-    }
-    const bool ok = l_pages_ok(a, ws, w.r, w.x.P);
-    if (!ok && tid == 0) status_or(a.status, ECHO_DATA_BAD_OFFSETS);
-    const int rows = w.x.rows(a), T = w.x.tiles(), full = rows / kLRows;
+    // a request: its units from cost `at` on
+    r = __builtin_amdgcn_readfirstlane(r);
+    x.q0 = __builtin_amdgcn_readfirstlane(x.q0);
+    x.n = __builtin_amdgcn_readfirstlane(x.n);
+    x.P = __builtin_amdgcn_readfirstlane(x.P);
+    at = uniform_ll(at);
+    const int rows = x.rows(a), T = x.tiles(), full = rows / kLRows;
     const long long whole_unit = l_unit_cost(T, kLRows);
     int j = 0;
-    if (lo > w.at && full > 0) j = int(min((lo - w.at) / whole_unit, (long long)full));
-    long long at = w.at + j * whole_unit;
+    if (lo > at && full > 0) {
+      j = min(int(float(lo - at) * __builtin_amdgcn_rcpf(float(whole_unit))), full);
+      while (j > 0 && at + j * whole_unit > lo) --j;
+      while (j < full && at + (j + 1) * whole_unit <= lo) ++j;
+    }
+    at += j * whole_unit;
+    bool check = true, ok = true;
     for (; j * kLRows < rows && at < hi; ++j) {
       LatUnit u;
-      u.q0 = w.x.q0;
-      u.n = w.x.n;
-      u.P = w.x.P;
-      u.r = w.r;
+      u.q0 = x.q0;
+      u.n = x.n;
+      u.P = x.P;
+      u.r = r;
       u.row0 = j * kLRows;
       u.rows = min(kLRows, rows - u.row0);
-      u.tree_tiles = w.x.tree_tiles();
+      u.tree_tiles = x.tree_tiles();
       const int c = l_tile_cost(u.rows);
       const long long t_at = at + kLEnter;  // where its tiles start
-      const int t0 = lo <= t_at ? 0 : int(min((lo - t_at + c - 1) / c, (long long)T));
-      const int t1 = hi <= t_at ? 0 : int(min((hi - t_at + c - 1) / c, (long long)T));
+      const int t0 = l_tile_at(lo - t_at, c, T), t1 = l_tile_at(hi - t_at, c, T);
       if (ok && t0 < t1) {
-        if (t0 > 0 && !cut_done) {
-          // (only a range's first unit can have started before it)
-          LatCut cut = {};
-          if (ranges.range_of(t_at) == g - 1) {
-            cut.parts = ranges.range_of(t_at + (long long)(T - 1) * c) - g + 2;
-            cut.rows = u.rows;
-            cut.row = (long long)u.q0 * a.hq + u.row0;
-          }
-          if (tid == 0) ws.cuts[g] = cut;
-          cut_done = true;
-        }
         const bool whole = t0 == 0 && t1 == T;
         const size_t part = size_t(g) * 2 + (t0 == 0 ? 1 : 0);
-        if (c == kLCost4)
-          l_segment<2>(a, ws, u, t0, t1, whole, part, base);
-        else
-          l_segment<1>(a, ws, u, t0, t1, whole, part, base);
+        ok = c == kLCost4 ? l_segment<2>(a, ws, u, t0, t1, whole, part, check, base)
+                          : l_segment<1>(a, ws, u, t0, t1, whole, part, check, base);
+        check = false;
+        if (!ok && tid == 0) status_or(a.status, ECHO_DATA_BAD_OFFSETS);
+        // (only a range's first unit can have started before it, and the second of its ranges has the record)
+        if (ok && t0 > 0 && first_unit && ranges.range_of(t_at) == g - 1 && tid == 0) {
+          LatCut cut;
+          cut.parts = ranges.range_of(t_at + (long long)(T - 1) * c) - g + 2;
+          cut.rows = u.rows;
+          cut.row = (long long)u.q0 * a.hq + u.row0;
+          ws.cuts[g] = cut;
+        }
+        first_unit = false;
       }
       at += l_unit_cost(T, u.rows);
     }
     if (at >= hi) break;
     // the next request with rows
-    w.at = at;
-    int next = w.r + 1;
+    int next = r + 1;
     for (; next < a.R; next += kWave) {
-      LatLook x = {};
+      x = LatLook{};
       if (next + lane < a.R) x = l_look(a, next + lane);
       const uint64_t in = __ballot(x.n > 0);
       if (in != 0ull) {
-        next += __ffsll((unsigned long long)in) - 1;
+        const int i = __ffsll((unsigned long long)in) - 1;
+        next += i;
+        x.q0 = __shfl(x.q0, i);
+        x.n = __shfl(x.n, i);
+        x.P = __shfl(x.P, i);
         break;
       }
     }
     if (next >= a.R) break;
-    w.r = next;
+    r = next;
   }
-  if (!cut_done && tid == 0) ws.cuts[g].parts = 0;
 }
 
 // ------------------------------------------------------------- combine ----
-// Workgroup (g, y): rows 16 y .. 16 y + 15 of the unit in record g; a thread has 32 dims of a row.
+// Workgroup (g, y): of the unit in record g, rows 32 (y / 4) .. and dims 128 (y % 4) ..; a thread has
+// 16 dims of a row, in four pieces.
 __global__ __launch_bounds__(256) void latent_combine_kernel(LatArgs a, LatWs ws) {
   const int g = blockIdx.x;
   const LatCut cut = ws.cuts[g];
-  if (cut.parts == 0) return;
-  const int row = blockIdx.y * 16 + (threadIdx.x & 15);
-  if (row >= cut.rows) return;
-  const int piece = threadIdx.x / 16;
-  float M = -__builtin_inff(), L = 0.0f, Lq = 0.0f;
-  floatx4 acc[8];
-#pragma unroll
-  for (int k = 0; k < 8; ++k) acc[k] = floatx4{0.f, 0.f, 0.f, 0.f};
+  const int rt = blockIdx.y >> 2, rl = threadIdx.x & 31, row = 32 * rt + rl;
+  if (cut.parts == 0 || row >= cut.rows) return;
+  const int d4 = 32 * (blockIdx.y & 3) + (threadIdx.x >> 5);
+  const auto part = [&](int i) { return size_t(g - 1 + i) * 2 + (i == 0 ? 1 : 0); };
+  float M = -__builtin_inff();
+#pragma unroll 4
+  for (int i = 0; i < cut.parts; ++i) M = fmaxf(M, ws.part_ml[(part(i) * kLRows + row) * 4]);
+  const float ref = M == -__builtin_inff() ? 0.0f : M;  // (all weights 0)
+  float L = 0.0f, Lq = 0.0f;
+  floatx4 acc[4] = {};
+#pragma unroll 2
   for (int i = 0; i < cut.parts; ++i) {
-    const size_t part = size_t(g - 1 + i) * 2 + (i == 0 ? 1 : 0);
-    const floatx4 ml = *reinterpret_cast<const floatx4*>(ws.part_ml + (part * kLRows + row) * 4);
-    const float* po = ws.part_o + ((part * 4 + (row >> 5)) * 128 + 8 * piece) * 128 + (row & 31) * 4;
-    floatx4 v[8];
+    const floatx4 ml = *reinterpret_cast<const floatx4*>(ws.part_ml + (part(i) * kLRows + row) * 4);
+    const float* po = ws.part_o + ((part(i) * 4 + rt) * 128 + d4) * 128 + rl * 4;
+    floatx4 v[4];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = *reinterpret_cast<const floatx4*>(po + k * 128);
-    const float m = fmaxf(M, ml[0]);
-    if (m == -__builtin_inff()) continue;
-    const float was = __builtin_amdgcn_exp2f(M - m), now = __builtin_amdgcn_exp2f(ml[0] - m);  // 0 from -inf
-    M = m;
-    L = __builtin_fmaf(now, ml[1], L * was);
-    Lq = __builtin_fmaf(now, ml[2], Lq * was);
+    for (int k = 0; k < 4; ++k) v[k] = *reinterpret_cast<const floatx4*>(po + 8 * k * 128);
+    const float w = __builtin_amdgcn_exp2f(ml[0] - ref);
+    L = __builtin_fmaf(w, ml[1], L);
+    Lq = __builtin_fmaf(w, ml[2], Lq);
 #pragma unroll
-    for (int k = 0; k < 8; ++k)
+    for (int k = 0; k < 4; ++k)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) acc[k][e] = __builtin_fmaf(now, v[k][e], acc[k][e] * was);
+      for (int e = 0; e < 4; ++e) acc[k][e] = __builtin_fmaf(w, v[k][e], acc[k][e]);
   }
   const float inv = Lq > 0.0f ? 1.0f / Lq : 0.0f;
-  uint16_t* out = a.out + (cut.row + row) * kLC + 32 * piece;
+  uint16_t* out = a.out + (cut.row + row) * kLC + 4 * d4;
 #pragma unroll
-  for (int k = 0; k < 8; k += 2)
-    *reinterpret_cast<uint4*>(out + 4 * k) =
-        make_uint4(pack_bf16x2(acc[k][0] * inv, acc[k][1] * inv), pack_bf16x2(acc[k][2] * inv, acc[k][3] * inv),
-                   pack_bf16x2(acc[k + 1][0] * inv, acc[k + 1][1] * inv),
-                   pack_bf16x2(acc[k + 1][2] * inv, acc[k + 1][3] * inv));
-  if (a.lse != nullptr && piece == 0)
-    a.lse[cut.row + row] = L > 0.0f ? (M + log2f(L)) * kLn2 : -__builtin_inff();
+  for (int k = 0; k < 4; ++k)
+    *reinterpret_cast<uint2*>(out + 32 * k) =
+        make_uint2(pack_bf16x2(acc[k][0] * inv, acc[k][1] * inv), pack_bf16x2(acc[k][2] * inv, acc[k][3] * inv));
+  if (a.lse != nullptr && d4 == 0) a.lse[cut.row + row] = L > 0.0f ? (M + log2f(L)) * kLn2 : -__builtin_inff();
 }
 
 }  // namespace
@@ -797,7 +903,7 @@ int32_t launch_tree_verify_attn_latent(const AttnLatentArgs& x, hipStream_t stre
                        ws.bad);
   hipLaunchKernelGGL(latent_main_kernel, dim3(unsigned(G)), dim3(kLThreads), 0, stream, a, ws);
   const long long rows = (long long)a.max_rows * a.hq;
-  hipLaunchKernelGGL(latent_combine_kernel, dim3(unsigned(G), unsigned((rows < kLRows ? rows : kLRows) + 15) / 16),
+  hipLaunchKernelGGL(latent_combine_kernel, dim3(unsigned(G), unsigned((rows < kLRows ? rows : kLRows) + 31) / 32 * 4),
                      dim3(256), 0, stream, a, ws);
   return hipGetLastError() == hipSuccess ? ECHO_OK : ECHO_ERR_HIP;
 }
