@@ -235,20 +235,29 @@ struct LatUnit {
   int q0, n, P, r, row0, rows, tree_tiles;
 };
 
-// The pages of 64 tiles of a unit's prefix, tile at + i in lane i: one vector of loads, where
-// scalar ones would be waited for with every LDS read.
+// The addresses of 64 tiles of a unit, tile at + i in lane i: one vector of loads, where scalar ones
+// would be waited for with every LDS read.
 struct LatTable {
-  int page, at;
+  uint32_t lo, hi;
+  int at;
 };
 __device__ __forceinline__ void l_fill(LatTable& tb, const LatArgs& a, const LatUnit& u, int t) {
   const int lane = threadIdx.x & (kWave - 1);
   tb.at = t;
-  const long long key = (long long)(t + lane - u.tree_tiles) * kTileKeys;
-  tb.page = 0;
-  if (key >= 0 && key < u.P)
-    tb.page = a.block_table[size_t(u.r) * size_t(a.max_pages) + size_t(key >> a.page_shift)];
-  if (tb.page < 0 || tb.page >= a.num_pages) tb.page = 0;  // (read before the pages are checked)
-  asm volatile("" : "+v"(tb.page));  // (waited for here, not where every step would)
+  uint64_t base;
+  if (t + lane < u.tree_tiles) {
+    base = reinterpret_cast<uint64_t>(a.latent_new) + uint64_t(u.q0 + (t + lane) * kTileKeys) * kLRowBytes;
+  } else {
+    const long long key = (long long)(t + lane - u.tree_tiles) * kTileKeys;
+    int page = 0;
+    if (key < u.P) page = a.block_table[size_t(u.r) * size_t(a.max_pages) + size_t(key >> a.page_shift)];
+    if (page < 0 || page >= a.num_pages) page = 0;  // (read before the pages are checked)
+    const uint64_t row = (uint64_t(uint32_t(page)) << a.page_shift) + uint32_t(key & ((1 << a.page_shift) - 1));
+    base = reinterpret_cast<uint64_t>(a.pages) + row * kLRowBytes;
+  }
+  tb.lo = uint32_t(base);
+  tb.hi = uint32_t(base >> 32);
+  asm volatile("" : "+v"(tb.lo), "+v"(tb.hi));  // (waited for here, not where every step would)
 }
 
 // The lane, formed where it is used: what would be kept from it over a step is reloaded from
@@ -273,21 +282,13 @@ struct LatCopy {
 };
 __device__ __forceinline__ LatCopy l_tile(LatTable& tb, const LatArgs& a, const LatUnit& u, int t, int n,
                                           uint32_t smem) {
-  const int lane = l_lane(), w = wave_id();
+  const int w = wave_id();
   LatCopy c;
-  int tn;
-  if (t < u.tree_tiles) {
-    c.base = reinterpret_cast<uint64_t>(a.latent_new) + uint64_t(u.q0 + t * kTileKeys) * kLRowBytes;
-    tn = u.n - t * kTileKeys;
-  } else {
-    const int key = (t - u.tree_tiles) * kTileKeys;
-    if (t >= tb.at + kWave) l_fill(tb, a, u, t);
-    const uint32_t page = uint32_t(__builtin_amdgcn_readlane(tb.page, t - tb.at));
-    const uint64_t row = (uint64_t(page) << a.page_shift) + uint32_t(key & ((1 << a.page_shift) - 1));
-    c.base = reinterpret_cast<uint64_t>(a.pages) + row * kLRowBytes;
-    tn = u.P - key;
-  }
-  c.base = uniform64(c.base);
+  if (t >= tb.at + kWave) l_fill(tb, a, u, t);
+  c.base = uint64_t(uint32_t(__builtin_amdgcn_readlane(int(tb.lo), t - tb.at))) |
+           (uint64_t(uint32_t(__builtin_amdgcn_readlane(int(tb.hi), t - tb.at))) << 32);
+  const int tn = t < u.tree_tiles ? u.n - t * kTileKeys : u.P - (t - u.tree_tiles) * kTileKeys;
+  const int lane = l_lane();
   const int key = 8 * w + (lane >> 3);
   // (rows past the tile's keys: the last one again, so that nothing unwritten is multiplied)
   c.off = uint32_t(min(key, tn - 1) * kLRowBytes + (((lane & 7) ^ l_swz(key)) << 4));
@@ -396,45 +397,41 @@ __device__ __forceinline__ void l_step(LatState<QR>& st, LatTable& tb, const Lat
 
   uint32_t flags = 0;  // (a byte for each wave)
   if (kValues) flags = *(lds_uint_t*)lds_at(smem + kLFlagsAt + 4 * buf);
-  if (kScores) {
-#pragma unroll
-    for (int ks = 0; ks < kAhead; ++ks) read_k(ks);
-  }
-  LatCopy copy = {};
-  const bool send = kScores && kValues && t + 3 < t1;
-  if (send) copy = l_tile(tb, a, u, t + 3, n + 3, smem);
-  if (kValues) {
-    // O is scaled where a reference was raised
+  const auto rescale = [&] {  // O is scaled where a reference was raised
     flags = uint32_t(__builtin_amdgcn_readfirstlane(int(flags)));
-    if (flags != 0) {
+    if (flags == 0) return;
 #pragma unroll
-      for (int rt = 0; rt < RT; ++rt) {
-        const uint32_t f = QR == 2 ? flags >> (8 * rt) : flags >> (16 * rt);
-        if ((f & (QR == 2 ? 0xFFu : 0xFFFFu)) != 0) {
-          const int lane = l_lane();
-          float alpha = *(lds_float_t*)lds_at(smem + kLStatsAt + buf * (kLRows * 4) + uint32_t((32 * rt + (lane & 31)) * 4));
-          if (QR == 1) alpha = ((f >> (8 * ((lane >> 4) & 1))) & 0xFFu) != 0 ? alpha : 1.0f;
+    for (int rt = 0; rt < RT; ++rt) {
+      const uint32_t f = QR == 2 ? flags >> (8 * rt) : flags >> (16 * rt);
+      if ((f & (QR == 2 ? 0xFFu : 0xFFFFu)) != 0) {
+        const int lane = l_lane();
+        float alpha = *(lds_float_t*)lds_at(smem + kLStatsAt + buf * (kLRows * 4) + uint32_t((32 * rt + (lane & 31)) * 4));
+        if (QR == 1) alpha = ((f >> (8 * ((lane >> 4) & 1))) & 0xFFu) != 0 ? alpha : 1.0f;
 #pragma unroll
-          for (int ct = 0; ct < 4; ++ct) {
-            l_settle(st.o[rt][ct]);
-            st.o[rt][ct] *= alpha;
-          }
+        for (int ct = 0; ct < 4; ++ct) {
+          l_settle(st.o[rt][ct]);
+          st.o[rt][ct] *= alpha;
         }
       }
     }
-  }
+  };
+  const auto read_first = [&] {
+    read_v(0);
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) read_p(0, rt);
+  };
+  const bool send = kScores && kValues && t + 3 < t1;
+  LatCopy copy = {};
   // S^T: keys 16 kt + 4 quad + r of row l16
   if (kScores) {
+#pragma unroll
+    for (int ks = 0; ks < kAhead; ++ks) read_k(ks);
+    if (kValues) rescale();
 #pragma unroll
     for (int i = 0; i < QR; ++i) s[i][0] = s[i][1] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int ks = 0; ks < kLSteps; ++ks) {
       if (ks + kAhead < kLSteps) read_k(ks + kAhead);
-      if (kValues && ks == 5) {
-        read_v(0);
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) read_p(0, rt);
-      }
       if (kValues && (ks == 8 || ks == 13)) {
         const int g = ks == 8 ? 0 : 1;
         read_v(g + 1);
@@ -448,30 +445,34 @@ __device__ __forceinline__ void l_step(LatState<QR>& st, LatTable& tb, const Lat
         for (int i = 0; i < QR; ++i)
           s[i][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[ks % (kAhead + 1)][kt], st.q[i][ks], s[i][kt], 0, 0, 0);
       ECHO_FENCE();
-      if (kValues && send) {
-        if (ks == 0) {
-          copy.piece<0>();
-          copy.piece<1>();
+      // in the products' shadow: the copies of tile t + 3, the first operands of the products with V
+      if (kValues) {
+        if (ks == 0 && send) copy = l_tile(tb, a, u, t + 3, n + 3, smem);
+        if (send) {
+          if (ks == 1) {
+            copy.piece<0>();
+            copy.piece<1>();
+          }
+          if (ks == 2) {
+            copy.piece<2>();
+            copy.piece<3>();
+          }
+          if (ks == 3) {
+            copy.piece<4>();
+            copy.piece<5>();
+          }
+          if (ks == 4) {
+            copy.piece<6>();
+            copy.piece<7>();
+          }
+          if (ks == 5) copy.piece<8>();
         }
-        if (ks == 1) {
-          copy.piece<2>();
-          copy.piece<3>();
-        }
-        if (ks == 2) {
-          copy.piece<4>();
-          copy.piece<5>();
-        }
-        if (ks == 3) {
-          copy.piece<6>();
-          copy.piece<7>();
-        }
-        if (ks == 4) copy.piece<8>();
+        if (ks == 5) read_first();
       }
     }
   } else if (kValues) {
-    read_v(0);
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) read_p(0, rt);
+    rescale();
+    read_first();
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
       read_v(g + 1);
@@ -493,11 +494,10 @@ __device__ __forceinline__ void l_step(LatState<QR>& st, LatTable& tb, const Lat
   if (kScores && (tree || tn < kTileKeys)) {  // masks: the tree's words, the prefix's last tile
 #pragma unroll
     for (int i = 0; i < QR; ++i) {
-      const int quad = l_lane() >> 4;
       uint32_t word = 0xFFFFFFFFu;
       if (tree) word = tt < a.W ? a.tree_mask[size_t(l_opaque(st.slot[i])) * a.W + tt] : 0u;
       if (tn < kTileKeys) word &= (1u << tn) - 1u;
-      word >>= 4 * quad;
+      word >>= 4 * (l_lane() >> 4);
 #pragma unroll
       for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
@@ -511,23 +511,26 @@ __device__ __forceinline__ void l_step(LatState<QR>& st, LatTable& tb, const Lat
   };
   if (kValues) {
 #pragma unroll
-    for (int rt = 1; rt < RT; ++rt) {
+    for (int x = 1; x < 2 * RT; ++x) {  // the rest of group 2, and group 3
+      const int g = 2 + x / RT, rt = x % RT;
+      if (x == RT) read_v(4);
       ECHO_FENCE();
-      l_mfma(st.o[rt][2], vf[0], pf[rt]);
+      l_mfma(st.o[rt][g], vf[g & 1], pf[rt]);
       ECHO_FENCE();
-      if (kScores && rt <= QR) max_of(rt - 1);
+      if (g == 3) read_p(1, rt);
+      if (kScores && x <= QR) max_of(x - 1);
     }
-    if (kScores && QR == RT) max_of(QR - 1);
   } else if (kScores) {
 #pragma unroll
     for (int i = 0; i < QR; ++i) max_of(i);
   }
+  bool raised = false;
   if (kScores) {
     // The reference is raised only when a logit exceeds it by more than 2^8, so that weights stay <= 256.
     bool up = false;
 #pragma unroll
     for (int i = 0; i < QR; ++i) up |= top[i] > st.m[i] + kRescaleSlack;
-    const bool raised = __ballot(up) != 0ull;
+    raised = __ballot(up) != 0ull;
     if (raised) {
 #pragma unroll
       for (int i = 0; i < QR; ++i) {
@@ -542,40 +545,51 @@ __device__ __forceinline__ void l_step(LatState<QR>& st, LatTable& tb, const Lat
           *(lds_float_t*)lds_at(smem + kLStatsAt + buf1 * (kLRows * 4) + uint32_t((16 * (QR * w + i) + lane) * 4)) = alpha;
       }
     }
-    if (l_lane() == 0) *(lds_byte_t*)lds_at(smem + kLFlagsAt + 4 * buf1 + uint32_t(w)) =
-        kValues && raised ? 1 : 0;  // (before the first values O is 0)
 #pragma unroll
     for (int i = 0; i < QR; ++i) neg_m[i] = st.m[i] == -__builtin_inff() ? 0.0f : -st.m[i];
   }
+  // Weights 2 (p % 2) and the next of tile p / 2 % 2 of row tile p / 4: the exponentials of a pair beside
+  // one product, its sums and roundings beside the next, so that neither waits for the other.
+  float x0 = 0.0f, x1 = 0.0f;
   uint32_t half = 0;
-  const auto two = [&](int p) {  // weights 2 (p % 2) and the next of tile p / 2 % 2 of row tile p / 4
+  const auto weigh = [&](int p) {
     const int i = p >> 2, kt = (p >> 1) & 1, r = 2 * (p & 1);
-    const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i][kt][r], a.scale2, neg_m[i]));
-    const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i][kt][r + 1], a.scale2, neg_m[i]));
-    st.l[i] += x + y;
-    const uint32_t xy = pack_bf16x2(x, y);
+    x0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i][kt][r], a.scale2, neg_m[i]));
+    x1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i][kt][r + 1], a.scale2, neg_m[i]));
+  };
+  const auto take = [&](int p) {
+    const int i = p >> 2, kt = (p >> 1) & 1;
+    st.l[i] += x0 + x1;
+    const uint32_t xy = pack_bf16x2(x0, x1);
     st.lq[i] = add_bf16x2(xy, st.lq[i]);
-    if (r == 0) half = xy;
+    if ((p & 1) == 0) half = xy;
     else *(lds_uint2_t*)(lds_at(pw + buf1 * kLProb) + kt * 1024 + i * 256) = uint2v{half, xy};
+  };
+  const auto tell = [&] {  // (before the first values O is 0)
+    if (l_lane() == 0) *(lds_byte_t*)lds_at(smem + kLFlagsAt + 4 * buf1 + uint32_t(w)) = kValues && raised ? 1 : 0;
   };
   if (kValues) {
 #pragma unroll
-    for (int g = 3; g < 8; ++g) {
-      if (g < 7) read_v(g + 1);
-#pragma unroll
-      for (int rt = 0; rt < RT; ++rt) {
-        ECHO_FENCE();
-        l_mfma(st.o[rt][g & 3], vf[g & 1], pf[rt]);
-        ECHO_FENCE();
-        if (g == 3) read_p(1, rt);
-        const int p = (g - 3) * RT + rt;
-        if (kScores && p < 4 * QR) two(p);
+    for (int x = 0; x < 4 * RT; ++x) {
+      const int g = 4 + x / RT, rt = x % RT;
+      if (rt == 0 && g < 7) read_v(g + 1);
+      ECHO_FENCE();
+      l_mfma(st.o[rt][g & 3], vf[g & 1], pf[rt]);
+      ECHO_FENCE();
+      if (kScores) {
+        if ((x & 1) == 0) weigh(x >> 1);
+        else take(x >> 1);
       }
     }
     ECHO_FENCE();
-  } else {
+    if (kScores) tell();
+  } else if (kScores) {
 #pragma unroll
-    for (int p = 0; p < 4 * QR; ++p) two(p);
+    for (int p = 0; p < 4 * QR; ++p) {
+      weigh(p);
+      take(p);
+    }
+    tell();
   }
 }
 
