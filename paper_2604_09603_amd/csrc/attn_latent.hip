@@ -842,43 +842,63 @@ __global__ __launch_bounds__(kLThreads) __attribute__((amdgpu_waves_per_eu(1, 1)
 }
 
 // ------------------------------------------------------------- combine ----
+constexpr int kLParts = 4;  // partial sums per round trip
+
 // Workgroup (g, y): of the unit in record g, rows 32 (y / 4) .. and dims 128 (y % 4) ..; a thread has
-// 16 dims of a row, in four pieces.
+// 16 dims of a row, in four pieces.  Parts in the order of the ranges.
 __global__ __launch_bounds__(256) void latent_combine_kernel(LatArgs a, LatWs ws) {
   const int g = blockIdx.x;
-  const LatCut cut = ws.cuts[g];
+  const const_i32_t* rec = (const const_i32_t*)(ws.cuts + g);  // (scalar loads)
+  const int parts = rec[0], rows = rec[1];
   const int rt = blockIdx.y >> 2, rl = threadIdx.x & 31, row = 32 * rt + rl;
-  if (cut.parts == 0 || row >= cut.rows) return;
+  if (parts == 0 || row >= rows) return;
+  const int64_t first = int64_t(uint64_t(uint32_t(rec[2])) | (uint64_t(uint32_t(rec[3])) << 32));
   const int d4 = 32 * (blockIdx.y & 3) + (threadIdx.x >> 5);
-  const auto part = [&](int i) { return size_t(g - 1 + i) * 2 + (i == 0 ? 1 : 0); };
-  float M = -__builtin_inff();
-#pragma unroll 4
-  for (int i = 0; i < cut.parts; ++i) M = fmaxf(M, ws.part_ml[(part(i) * kLRows + row) * 4]);
-  const float ref = M == -__builtin_inff() ? 0.0f : M;  // (all weights 0)
-  float L = 0.0f, Lq = 0.0f;
+  float M = -__builtin_inff(), L = 0.0f, Lq = 0.0f;
   floatx4 acc[4] = {};
-#pragma unroll 2
-  for (int i = 0; i < cut.parts; ++i) {
-    const floatx4 ml = *reinterpret_cast<const floatx4*>(ws.part_ml + (part(i) * kLRows + row) * 4);
-    const float* po = ws.part_o + ((part(i) * 4 + rt) * 128 + d4) * 128 + rl * 4;
-    floatx4 v[4];
+  for (int i0 = 0; i0 < parts; i0 += kLParts) {  // (a batch's loads in one round trip)
+    floatx4 ml[kLParts], v[kLParts][4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) v[k] = *reinterpret_cast<const floatx4*>(po + 8 * k * 128);
-    const float w = __builtin_amdgcn_exp2f(ml[0] - ref);
-    L = __builtin_fmaf(w, ml[1], L);
-    Lq = __builtin_fmaf(w, ml[2], Lq);
+    for (int j = 0; j < kLParts; ++j) {
+      ml[j] = floatx4{-__builtin_inff(), 0.0f, 0.0f, 0.0f};
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
+      for (int k = 0; k < 4; ++k) v[j][k] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+      if (i0 + j < parts) {  // uniform
+        const size_t part = size_t(g - 1 + i0 + j) * 2 + (i0 + j == 0 ? 1 : 0);
+        ml[j] = *reinterpret_cast<const floatx4*>(ws.part_ml + (part * kLRows + row) * 4);
+        const float* po = ws.part_o + ((part * 4 + rt) * 128 + d4) * 128 + rl * 4;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) acc[k][e] = __builtin_fmaf(w, v[k][e], acc[k][e]);
+        for (int k = 0; k < 4; ++k) v[j][k] = *reinterpret_cast<const floatx4*>(po + 8 * k * 128);
+      }
+    }
+    float m = M;
+#pragma unroll
+    for (int j = 0; j < kLParts; ++j) m = fmaxf(m, ml[j][0]);
+    if (m == -__builtin_inff()) continue;
+    const float was = __builtin_amdgcn_exp2f(M - m);  // 0 from -inf
+    M = m;
+    L *= was;
+    Lq *= was;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) acc[k] *= was;
+#pragma unroll
+    for (int j = 0; j < kLParts; ++j) {
+      const float w = __builtin_amdgcn_exp2f(ml[j][0] - m);  // 0 from -inf
+      L = __builtin_fmaf(w, ml[j][1], L);
+      Lq = __builtin_fmaf(w, ml[j][2], Lq);
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[k][e] = __builtin_fmaf(w, v[j][k][e], acc[k][e]);
+    }
   }
   const float inv = Lq > 0.0f ? 1.0f / Lq : 0.0f;
-  uint16_t* out = a.out + (cut.row + row) * kLC + 4 * d4;
+  uint16_t* out = a.out + (first + row) * kLC + 4 * d4;
 #pragma unroll
   for (int k = 0; k < 4; ++k)
     *reinterpret_cast<uint2*>(out + 32 * k) =
         make_uint2(pack_bf16x2(acc[k][0] * inv, acc[k][1] * inv), pack_bf16x2(acc[k][2] * inv, acc[k][3] * inv));
-  if (a.lse != nullptr && d4 == 0) a.lse[cut.row + row] = L > 0.0f ? (M + log2f(L)) * kLn2 : -__builtin_inff();
+  if (a.lse != nullptr && d4 == 0) a.lse[first + row] = L > 0.0f ? (M + log2f(L)) * kLn2 : -__builtin_inff();
 }
 
 }  // namespace
