@@ -50,10 +50,11 @@ constexpr int kLLds = kLInvAt + kLRows * 4;
 static_assert(kLLds <= 160 * 1024, "gfx950 LDS per CU");
 constexpr int kLOwnPages = 512;                // block tables up to this wide are checked in place
 
-// Costs of a tile of a unit with more than 64 rows, of one with fewer, of entering a unit (its rows
-// of Q, its first tile, its output); the smallest of a range, which is a power of two and
-// no smaller than a tile's, so that every range within a unit has a tile.
-constexpr int kLCost4 = 4, kLCost2 = 3, kLEnter = 16;
+// Costs, in halves of a microsecond: of a tile of a unit with more than 64 rows, of one with fewer; of
+// entering such a unit (its rows of Q, its first tiles, its output); the smallest of a
+// range, which is a power of two and no smaller than a tile's, so that every range within
+// a unit has a tile.
+constexpr int kLCost4 = 4, kLCost2 = 3, kLEnter4 = 40, kLEnter2 = 16;
 constexpr int kLMinShift = 3;
 static_assert((1 << kLMinShift) >= kLCost4, "a tile in every range");
 
@@ -162,8 +163,9 @@ __device__ __forceinline__ LatLook l_look(const LatArgs& a, int r) {
   return x;
 }
 __device__ __forceinline__ int l_tile_cost(int rows) { return rows > kLRows / 2 ? kLCost4 : kLCost2; }
+__device__ __forceinline__ int l_enter_cost(int rows) { return rows > kLRows / 2 ? kLEnter4 : kLEnter2; }
 __device__ __forceinline__ long long l_unit_cost(int tiles, int rows) {
-  return kLEnter + (long long)tiles * l_tile_cost(rows);
+  return l_enter_cost(rows) + (long long)tiles * l_tile_cost(rows);
 }
 __device__ __forceinline__ long long l_cost(const LatArgs& a, const LatLook& x) {
   if (x.n == 0) return 0;
@@ -799,7 +801,7 @@ __global__ __launch_bounds__(kLThreads) __attribute__((amdgpu_waves_per_eu(1, 1)
       u.rows = min(kLRows, rows - u.row0);
       u.tree_tiles = x.tree_tiles();
       const int c = l_tile_cost(u.rows);
-      const long long t_at = at + kLEnter;  // where its tiles start
+      const long long t_at = at + l_enter_cost(u.rows);  // where its tiles start
       const int t0 = l_tile_at(lo - t_at, c, T), t1 = l_tile_at(hi - t_at, c, T);
       if (ok && t0 < t1) {
         const bool whole = t0 == 0 && t1 == T;
