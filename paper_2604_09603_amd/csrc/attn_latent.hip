@@ -223,11 +223,12 @@ __device__ __forceinline__ bool l_pages_ok(const LatArgs& a, const LatWs& ws, in
 // Piece B (of nine) of the copy of a wave's eight rows of a tile: 1 KB, from base + off + 128 B to
 // LDS address lds + 4096 B (B < 8) or rope.  The instruction's offset moves both addresses.
 // In inline assembly because the compiler would wait for every copy in flight before each
-// LDS read; M0, the LDS address, needs a wait state before a load reads it.
+// LDS read.  The compiler does not see a load here: M0, the LDS address, needs a wait state before
+// it, and scalars that a vector instruction wrote (base, by a lane's read) five.
 constexpr int kLCopies = 9;  // loads of a wave per tile
 template <int B>
 __device__ __forceinline__ void l_copy(uint32_t lds, uint32_t rope, uint64_t base, uint32_t off) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 offset:%3"
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %1, %2 offset:%3"
                :
                : "s"(B < 8 ? lds + uint32_t(B * (kLBlock - 128)) : rope - 8 * 128u), "v"(off), "s"(base), "n"(B * 128)
                : "memory", "m0");

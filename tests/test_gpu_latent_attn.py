@@ -304,3 +304,22 @@ def test_attention_is_deterministic_and_takes_no_lse():
     pkg.echo_tree_verify_attn_latent(*a)
     assert np.array_equal(_bits(out), first)
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("hq,slots", [(1, 1), (40, 2)])
+def test_attention_ranges_of_many_tiles(hq, slots):
+    """More tiles to a workgroup than it keeps addresses of; requests that share pages."""
+    rng = np.random.default_rng(16 + hq)
+    R, ps = 64, 64
+    c = _case(rng, hq, [slots] * R, [ps] * R, ps)
+    c["plen"] = rng.integers(8900, 9500, R).astype(np.int32)
+    full = np.flatnonzero(~np.any(c["pages"].reshape(len(c["pages"]), -1) == NAN, 1))
+    c["bt"] = full[rng.integers(0, len(full), (R, 149))].astype(np.int32)
+    _log(f"[latent attn] many tiles hq={hq}")
+    out, lse, status = _run(c)
+    assert status == 0 and np.all(np.isfinite(lse[:R * slots]))
+    for r in (0, 1, 20, 41, 63):  # (each alone in the oracle)
+        mine = slice(r * slots, (r + 1) * slots)
+        one = dict(c, R=1, cap=slots, qo=np.array([0, slots], np.int32), **{k: c[k][mine] for k in ("q", "new", "mask")},
+                   **{k: c[k][r:r + 1] for k in ("bt", "plen")})
+        _check(one, out[mine], lse[mine], status)
