@@ -506,10 +506,11 @@ def _head_strides(t, rows, heads, rot_dim):
     nothing)."""
     if t is None:
         return 0, 0
-    s = t.stride()
-    if len(s) != 3 or s[-1] != 1 or t.shape[1] != heads or t.shape[2] != rot_dim or t.shape[0] < rows:
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 3 or stride[2] != 1 or shape[1] != heads or shape[2] != rot_dim or shape[0] < rows:
         raise ValueError("q and k are [rows, heads, rot_dim] with contiguous dims")
-    return s[0] if t.shape[0] > 1 else heads * max(s[1], rot_dim), s[1] if heads > 1 else rot_dim
+    return (stride[0] if shape[0] > 1 else heads * max(stride[1], rot_dim),
+            stride[1] if heads > 1 else rot_dim)
 
 
 def echo_rope(q, q_out, k, k_out, positions, num_rows, hq, hk, rot_dim, layout, inv_freq, scale,
