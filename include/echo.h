@@ -78,6 +78,7 @@ typedef void* echo_stream_t; /* hipStream_t */
 #define ECHO_ROPE_HALF 0        /* pair i: dims i and i + rot_dim / 2               */
 #define ECHO_ROPE_INTERLEAVED 1 /* pair i: dims 2 i and 2 i + 1                     */
 #define ECHO_ROPE_MAX_DIM 1024  /* largest rotated part of a head                   */
+#define ECHO_ROPE_MAX_ROWS 16777215 /* most rows of an echo_rope or echo_store_latent */
 #define ECHO_ROPE_PLAIN 0       /* scalings of the frequencies:                     */
 #define ECHO_ROPE_LINEAR 1      /*   echo_rope_frequencies                          */
 #define ECHO_ROPE_BASE 2
@@ -539,7 +540,8 @@ int32_t echo_commit_kv_q8(const int32_t* q_offsets, const int32_t* accept_len,
  *   inv_freq     [rot_dim / 2] double, finite: a table of echo_rope_frequencies
  *   scale        finite (ECHO_ERR_INVALID_ARG)
  * Rows whose pointers are 16-byte aligned, strides multiples of 8 and rot_dim one of 16
- * go 16 bytes at a time.
+ * go 16 bytes at a time.  Limits: num_rows <= ECHO_ROPE_MAX_ROWS, 2^16 heads of q and k
+ * together, strides below 2^31.
  */
 int32_t echo_rope(const uint16_t* q, int64_t q_row_stride, int64_t q_head_stride, uint16_t* q_out,
                   int64_t q_out_row_stride, int64_t q_out_head_stride, int32_t num_q_heads,
@@ -599,7 +601,8 @@ int32_t echo_rope_frequencies(int32_t rot_dim, double base, int32_t scaling, dou
  *                leaves its row out of the cache; one of num_pages * page_size or more
  *                does too, with ECHO_DATA_BAD_OFFSETS.  The same slot twice: unspecified
  *                contents of that slot
- * One of latent_new and slot_map has to be given.
+ * One of latent_new and slot_map has to be given.  Limits: num_rows <= ECHO_ROPE_MAX_ROWS,
+ * kv_stride < 2^31.
  */
 int32_t echo_store_latent(const uint16_t* kv, int64_t kv_stride, const uint16_t* norm_weight,
                           float eps, const int32_t* positions, const double* inv_freq,

@@ -39,6 +39,7 @@ KV_BLOCK = 32
 ROPE_HALF = 0
 ROPE_INTERLEAVED = 1
 ROPE_MAX_DIM = 1024
+ROPE_MAX_ROWS = 16777215
 ROPE_SCALINGS = {"plain": 0, "linear": 1, "base": 2, "bands": 3, "smooth": 4}
 
 LATENT_DIM = 512

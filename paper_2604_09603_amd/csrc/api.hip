@@ -677,7 +677,8 @@ int32_t echo_rope(const uint16_t* q, int64_t q_row_stride, int64_t q_head_stride
   if (!isfinite(scale)) return ECHO_ERR_INVALID_ARG;
   // (a workgroup numbers a row's pairs of all heads in 32 bits)
   const int64_t heads = int64_t(num_q_heads) + num_k_heads;
-  if (rot_dim > ECHO_ROPE_MAX_DIM || heads > (1 << 16)) return ECHO_ERR_UNSUPPORTED;
+  if (rot_dim > ECHO_ROPE_MAX_DIM || heads > (1 << 16) || num_rows > ECHO_ROPE_MAX_ROWS)
+    return ECHO_ERR_UNSUPPORTED;
   if (num_rows == 0 || heads == 0) return ECHO_OK;
   if (!positions || !inv_freq) return ECHO_ERR_INVALID_ARG;
   if ((num_q_heads > 0 && (!q || !q_out)) || (num_k_heads > 0 && (!k || !k_out)))
@@ -784,7 +785,8 @@ int32_t echo_store_latent(const uint16_t* kv, int64_t kv_stride, const uint16_t*
                           int64_t num_pages, int32_t page_size, int32_t* status,
                           echo_stream_t stream) {
   if (num_rows < 0) return ECHO_ERR_INVALID_ARG;
-  if (!latent_dims_ok(latent_dim, rope_dim)) return ECHO_ERR_UNSUPPORTED;
+  if (!latent_dims_ok(latent_dim, rope_dim) || num_rows > ECHO_ROPE_MAX_ROWS)
+    return ECHO_ERR_UNSUPPORTED;
   if (layout != ECHO_ROPE_HALF && layout != ECHO_ROPE_INTERLEAVED) return ECHO_ERR_INVALID_ARG;
   if (norm_weight != nullptr && !(eps >= 0.0f && isfinite(eps))) return ECHO_ERR_INVALID_ARG;
   if (inv_freq != nullptr && !isfinite(rope_scale)) return ECHO_ERR_INVALID_ARG;

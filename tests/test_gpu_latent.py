@@ -323,3 +323,67 @@ def test_commit_matches_oracle(ps, in_place):
                            out, status=status)
     assert np.array_equal(_bits(pd), want) and np.array_equal(out.cpu().numpy(), wl)
     assert int(status.item()) == ws == st.BAD_OFFSETS
+
+
+def test_writers_on_other_streams_and_in_graphs():
+    """Two streams at once over buffers of their own; captured calls replayed with changed inputs."""
+    import torch
+    import paper_2604_09603_amd as pkg
+    rng = np.random.default_rng(31)
+    T, ps, f = 90, 32, latent.frequencies(64, 1e4)[0]
+    slots, npages = _slots_of([T], [7], ps, rng)
+    weight, df, ds = _dev(_bf(rng.standard_normal(512))), _dev(f), _dev(slots)
+    bt, qo = _dev(rng.permutation(npages).reshape(1, -1).astype(np.int32)), _dev([0, 5], np.int32)
+    path = np.full((1, 4), -1, np.int32)
+    path[0, :2] = 2, 4
+    alen, path = _dev([2], np.int32), _dev(path)
+
+    class Side:
+        def __init__(self):
+            self.kv, self.pos = torch.zeros((T, 576), dtype=torch.bfloat16, device="cuda:0"), _zeros(T)
+            self.new, self.q = torch.zeros_like(self.kv), torch.zeros((T, 9, 64), dtype=torch.bfloat16, device="cuda:0")
+            self.pages = torch.zeros((npages, ps, 576), dtype=torch.bfloat16, device="cuda:0")
+            self.plen, self.len = _zeros(1) + 30, _zeros(1)
+
+        def fill(self, seed):
+            r = np.random.default_rng(seed)
+            self.x, self.at = _bf(r.standard_normal((T, 576))), r.integers(0, 4000, T).astype(np.int32)
+            self.heads = _bf(r.standard_normal((T, 9, 64)))
+            for a, b in ((self.kv, self.x), (self.pos, self.at), (self.q, self.heads)):
+                a.copy_(_dev(b))
+
+        def calls(self, **kw):
+            _rope(self.q, self.q, None, None, self.pos, df, 1.0, 0, **kw)
+            _store(self.kv, weight, self.pos, df, 1.0, 0, new=self.new, slots=ds, pages=self.pages, ps=ps, **kw)
+            pkg.echo_commit_latent(qo, alen, path, 4, self.new, 1, T, 512, 64, self.pages, ps, bt, self.plen, self.len, **kw)
+
+        def check(self):
+            _rotated_ok(_bits(self.q), f64(self.heads), self.at, f, 1.0, 0)
+            new = _bits(self.new)
+            _rows_ok(new, self.x, _bits(weight), 1e-6, self.at, f, 1.0, 0)
+            want = np.zeros((npages * ps, 576), np.uint16)
+            want[slots] = new
+            want, wl, _ = latent.commit_latent([0, 5], [2], path.cpu().numpy(), new, want.reshape(npages, ps, 576),
+                                               bt.cpu().numpy(), [30])
+            assert np.array_equal(_bits(self.pages), want) and self.len.item() == wl[0] == 33
+
+    sides, streams = [Side(), Side()], [torch.cuda.Stream(), torch.cuda.Stream()]
+    for k, s in enumerate(sides):
+        s.fill(k)
+    torch.cuda.synchronize()
+    for s, stream in zip(sides, streams):
+        s.calls(stream=stream)
+    torch.cuda.synchronize()
+    for s in sides:
+        s.check()
+    s = sides[0]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        s.calls()
+    for k in range(3):
+        s.fill(10 + k)
+        x = torch.randn(256, 256, device="cuda:0")
+        (x @ x).sum().item()
+        graph.replay()
+        torch.cuda.synchronize()
+        s.check()

@@ -168,7 +168,8 @@ def test_constants_match_the_header():
                            "echo.h")) as f:
         text = f.read()
     for name, v in [("ROPE_HALF", pkg.ROPE_HALF), ("ROPE_INTERLEAVED", pkg.ROPE_INTERLEAVED),
-                    ("ROPE_MAX_DIM", pkg.ROPE_MAX_DIM), ("LATENT_DIM", pkg.LATENT_DIM),
+                    ("ROPE_MAX_DIM", pkg.ROPE_MAX_DIM), ("ROPE_MAX_ROWS", pkg.ROPE_MAX_ROWS),
+                    ("LATENT_DIM", pkg.LATENT_DIM),
                     ("LATENT_ROPE_DIM", pkg.LATENT_ROPE_DIM)]:
         assert f"#define ECHO_{name} {v} " in text, name
     for name, v in pkg.ROPE_SCALINGS.items():
@@ -183,3 +184,8 @@ def test_binding_refuses_views_it_cannot_describe():
     for bad in (x, x[..., ::2], x[:2, :, :32], x[:, :4, :32], x[..., 0]):
         with pytest.raises(ValueError):
             call(bad)
+
+
+def test_rows_past_the_largest_launch_are_refused():
+    assert _rope(rows=pkg.ROPE_MAX_ROWS + 1) == _rope(rows=2 ** 31 - 1) == UNSUPPORTED
+    assert _store(rows=pkg.ROPE_MAX_ROWS + 1) == UNSUPPORTED
