@@ -205,18 +205,37 @@ __device__ __forceinline__ int l_tile_at(long long x, int c, int T) {
   return int((unsigned(x) + unsigned(c - 1)) / unsigned(c));  // (T < 2^27)
 }
 
-// Whether a request's pages are all in the pool (all threads; waits for all loads, and a barrier).
-__device__ __forceinline__ bool l_pages_ok(const LatArgs& a, const LatWs& ws, int r, int P) {
-  const int np = l_prefix_pages(P, a);
-  const bool own = a.chunks == 0;
-  const int n = own ? np : (np + kPageChunk - 1) / kPageChunk;
-  const int32_t* e = own ? a.block_table + size_t(r) * size_t(a.max_pages) : ws.bad + size_t(r) * size_t(a.chunks);
+// The lane, formed where it is used: what would be kept from it over a step is reloaded from
+// memory, behind every copy in flight.
+__device__ __forceinline__ int l_lane() {
+  int x = int(__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u)));
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
+__device__ __forceinline__ int l_opaque(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
+// Whether a thread sees a page of a request that is not in the pool (for an or over all threads).
+__device__ __forceinline__ int l_pages_bad(const LatArgs& a, const LatWs& ws, int r, int P) {
+  const int np = l_prefix_pages(P, a), tid = wave_id() * kWave + l_lane();
   int bad = 0;
-  for (int i = threadIdx.x; i < n; i += kLThreads) {
-    const int v = e[i];
-    bad |= own ? v < 0 || v >= a.num_pages : v != 0;
+  if (a.chunks == 0) {
+    static_assert(kLOwnPages <= 2 * kLThreads, "two entries a thread, in one round trip");
+    const int32_t* e = a.block_table + size_t(r) * size_t(a.max_pages);
+    int v[2] = {0, 0};
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+      if (tid + k * kLThreads < np) v[k] = e[tid + k * kLThreads];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) bad |= v[k] < 0 || (v[k] > 0 && v[k] >= a.num_pages);
+  } else {
+    const int32_t* e = ws.bad + size_t(r) * size_t(a.chunks);
+    for (int i = tid; i < (np + kPageChunk - 1) / kPageChunk; i += kLThreads) bad |= e[i] != 0;
   }
-  return __builtin_amdgcn_readfirstlane(__syncthreads_or(bad)) == 0;
+  return bad;
 }
 
 // ---------------------------------------------------------------- main ----
@@ -245,7 +264,7 @@ struct LatTable {
   int at;
 };
 __device__ __forceinline__ void l_fill(LatTable& tb, const LatArgs& a, const LatUnit& u, int t) {
-  const int lane = threadIdx.x & (kWave - 1);
+  const int lane = l_lane();
   tb.at = t;
   uint64_t base;
   if (t + lane < u.tree_tiles) {
@@ -261,19 +280,6 @@ __device__ __forceinline__ void l_fill(LatTable& tb, const LatArgs& a, const Lat
   tb.lo = uint32_t(base);
   tb.hi = uint32_t(base >> 32);
   asm volatile("" : "+v"(tb.lo), "+v"(tb.hi));  // (waited for here, not where every step would)
-}
-
-// The lane, formed where it is used: what would be kept from it over a step is reloaded from
-// memory, behind every copy in flight.
-__device__ __forceinline__ int l_lane() {
-  int x = int(__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u)));
-  asm volatile("" : "+v"(x));
-  return x;
-}
-
-__device__ __forceinline__ int l_opaque(int x) {
-  asm volatile("" : "+v"(x));
-  return x;
 }
 
 // What the copies of a tile take: tile t of a unit, the n-th that its workgroup copies.
@@ -606,6 +612,13 @@ __device__ __forceinline__ bool l_segment(const LatArgs& a, const LatWs& ws, con
   const int w = wave_id();
   const size_t first = size_t(u.q0) * a.hq + size_t(u.row0);  // the unit's first row of q
 
+  // Page ids first, then the first tiles' copies, then Q, of which there is most: loads return in
+  // order.
+  const int bad = check ? l_pages_bad(a, ws, u.r, u.P) : 0;
+  LatTable tb;
+  l_fill(tb, a, u, t0);
+  l_send(tb, a, u, t0, 0, smem);
+  if (t0 + 1 < t1) l_send(tb, a, u, t0 + 1, 1, smem);
   LatState<QR> st;
 #pragma unroll
   for (int i = 0; i < QR; ++i) {  // (rows past the last: the last again)
@@ -618,11 +631,7 @@ __device__ __forceinline__ bool l_segment(const LatArgs& a, const LatWs& ws, con
     st.m[i] = -__builtin_inff();
     st.l[i] = st.lq[i] = 0.0f;
   }
-  LatTable tb;
-  l_fill(tb, a, u, t0);
-  l_send(tb, a, u, t0, 0, smem);
-  if (t0 + 1 < t1) l_send(tb, a, u, t0 + 1, 1, smem);
-  if (check && !l_pages_ok(a, ws, u.r, u.P)) {
+  if (check && __builtin_amdgcn_readfirstlane(__syncthreads_or(bad)) != 0) {
     wait_vm<0>();  // (nothing is on its way to LDS)
     l_barrier();
     return false;
