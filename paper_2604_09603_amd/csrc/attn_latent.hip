@@ -854,33 +854,33 @@ __global__ __launch_bounds__(kLThreads) __attribute__((amdgpu_waves_per_eu(1, 1)
 }
 
 // ------------------------------------------------------------- combine ----
-constexpr int kLParts = 4;  // partial sums per round trip
+constexpr int kLParts = 8;  // partial sums per round trip
 
-// Workgroup (g, y): of the unit in record g, rows 32 (y / 4) .. and dims 128 (y % 4) ..; a thread has
-// 16 dims of a row, in four pieces.  Parts in the order of the ranges.
+// Workgroup (g, y): of the unit in record g, rows 32 (y / 8) .. and dims 64 (y % 8) ..; a thread has
+// eight dims of a row, in two pieces.  Parts in the order of the ranges.
 __global__ __launch_bounds__(256) void latent_combine_kernel(LatArgs a, LatWs ws) {
   const int g = blockIdx.x;
   const const_i32_t* rec = (const const_i32_t*)(ws.cuts + g);  // (scalar loads)
   const int parts = rec[0], rows = rec[1];
-  const int rt = blockIdx.y >> 2, rl = threadIdx.x & 31, row = 32 * rt + rl;
+  const int rt = int(blockIdx.y) / 8, rl = threadIdx.x & 31, row = 32 * rt + rl;
   if (parts == 0 || row >= rows) return;
   const int64_t first = int64_t(uint64_t(uint32_t(rec[2])) | (uint64_t(uint32_t(rec[3])) << 32));
-  const int d4 = 32 * (blockIdx.y & 3) + (threadIdx.x >> 5);
+  const int d4 = 16 * int(blockIdx.y & 7) + (threadIdx.x >> 5);
   float M = -__builtin_inff(), L = 0.0f, Lq = 0.0f;
-  floatx4 acc[4] = {};
+  floatx4 acc[2] = {};
   for (int i0 = 0; i0 < parts; i0 += kLParts) {  // (a batch's loads in one round trip)
-    floatx4 ml[kLParts], v[kLParts][4];
+    floatx4 ml[kLParts], v[kLParts][2];
 #pragma unroll
     for (int j = 0; j < kLParts; ++j) {
       ml[j] = floatx4{-__builtin_inff(), 0.0f, 0.0f, 0.0f};
 #pragma unroll
-      for (int k = 0; k < 4; ++k) v[j][k] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+      for (int k = 0; k < 2; ++k) v[j][k] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
       if (i0 + j < parts) {  // uniform
         const size_t part = size_t(g - 1 + i0 + j) * 2 + (i0 + j == 0 ? 1 : 0);
         ml[j] = *reinterpret_cast<const floatx4*>(ws.part_ml + (part * kLRows + row) * 4);
         const float* po = ws.part_o + ((part * 4 + rt) * 128 + d4) * 128 + rl * 4;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) v[j][k] = *reinterpret_cast<const floatx4*>(po + 8 * k * 128);
+        for (int k = 0; k < 2; ++k) v[j][k] = *reinterpret_cast<const floatx4*>(po + 8 * k * 128);
       }
     }
     float m = M;
@@ -892,14 +892,14 @@ __global__ __launch_bounds__(256) void latent_combine_kernel(LatArgs a, LatWs ws
     L *= was;
     Lq *= was;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) acc[k] *= was;
+    for (int k = 0; k < 2; ++k) acc[k] *= was;
 #pragma unroll
     for (int j = 0; j < kLParts; ++j) {
       const float w = __builtin_amdgcn_exp2f(ml[j][0] - m);  // 0 from -inf
       L = __builtin_fmaf(w, ml[j][1], L);
       Lq = __builtin_fmaf(w, ml[j][2], Lq);
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
+      for (int k = 0; k < 2; ++k)
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[k][e] = __builtin_fmaf(w, v[j][k][e], acc[k][e]);
     }
@@ -907,7 +907,7 @@ __global__ __launch_bounds__(256) void latent_combine_kernel(LatArgs a, LatWs ws
   const float inv = Lq > 0.0f ? 1.0f / Lq : 0.0f;
   uint16_t* out = a.out + (first + row) * kLC + 4 * d4;
 #pragma unroll
-  for (int k = 0; k < 4; ++k)
+  for (int k = 0; k < 2; ++k)
     *reinterpret_cast<uint2*>(out + 32 * k) =
         make_uint2(pack_bf16x2(acc[k][0] * inv, acc[k][1] * inv), pack_bf16x2(acc[k][2] * inv, acc[k][3] * inv));
   if (a.lse != nullptr && d4 == 0) a.lse[first + row] = L > 0.0f ? (M + log2f(L)) * kLn2 : -__builtin_inff();
@@ -951,7 +951,7 @@ int32_t launch_tree_verify_attn_latent(const AttnLatentArgs& x, hipStream_t stre
                        ws.bad);
   hipLaunchKernelGGL(latent_main_kernel, dim3(unsigned(G)), dim3(kLThreads), 0, stream, a, ws);
   const long long rows = (long long)a.max_rows * a.hq;
-  hipLaunchKernelGGL(latent_combine_kernel, dim3(unsigned(G), unsigned((rows < kLRows ? rows : kLRows) + 31) / 32 * 4),
+  hipLaunchKernelGGL(latent_combine_kernel, dim3(unsigned(G), unsigned((rows < kLRows ? rows : kLRows) + 31) / 32 * 8),
                      dim3(256), 0, stream, a, ws);
   return hipGetLastError() == hipSuccess ? ECHO_OK : ECHO_ERR_HIP;
 }
