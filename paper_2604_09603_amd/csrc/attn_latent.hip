@@ -18,6 +18,19 @@
 // the product with V (at most 2^-8 each) and the output is divided by the sum of the
 // weights used, so that it stays a convex combination of V rows; the output's own
 // rounding to bfloat16 is as large.  Partial sums are stored in fp32.
+//
+// What bounds it.  A row of 1152 bytes serves 2176 operations per query row, so that up to
+// 64 rows are bound by the copies: a tile takes 1.55 us on every CU at once, 6.1 TB/s,
+// of 1.0 us of work.  128 rows are bound by the products: 2177 cycles of a CU's
+// matrix cores of the 4230 that a tile takes (2.0 us, 2.35 where nothing of it is in a
+// cache and the clock is lower).  A wave is alone on its SIMD, so what is not in its
+// own products' shadow costs: about 730 cycles the copies' issue, 340 the softmax, 620
+// LDS reads, 850 a step's barrier and waits.  Eight waves with half the rows each
+// hide more and read every fragment twice: 755 against 727 us for 16 long requests, 210
+// against 192 for 128 trees.  Entering a unit costs 8 us (to 64 rows) to 20 (128: its
+// 147 KB of Q and 131 KB of output or 262 KB of partial sums), a merge 5 to 30.
+// 64 single tokens of 16 heads over 1024-8192: 81 us, 4.2 TB/s; 128 trees of 16 heads: 174-177;
+// 61 trees of 128 heads: 212, 640 TFLOP/s; 16 long requests of 64 heads: 692, 1.03 PFLOP/s.
 #include "attn_core.h"
 
 namespace echo {
@@ -54,6 +67,10 @@ constexpr int kLOwnPages = 512;                // block tables up to this wide a
 // entering such a unit (its rows of Q, its first tiles, its output); the smallest of a
 // range, which is a power of two and no smaller than a tile's, so that every range within
 // a unit has a tile.
+// (Entering at 32 and 56 instead of 40: 61 trees of 128 heads 219 and 215 us for 212.  Tiles at
+// 5 : 3 and 8 : 7 instead of 4 : 3: 128 trees of 16 heads 181 and 183 us for 177, long
+// requests 740 and 702 for 692.  Smallest ranges of 4 and 16 instead of 8: four
+// trees 30.0 and 29.6 us for 28.4.)
 constexpr int kLCost4 = 4, kLCost2 = 3, kLEnter4 = 40, kLEnter2 = 16;
 constexpr int kLMinShift = 3;
 static_assert((1 << kLMinShift) >= kLCost4, "a tile in every range");
@@ -854,7 +871,10 @@ __global__ __launch_bounds__(kLThreads) __attribute__((amdgpu_waves_per_eu(1, 1)
 }
 
 // ------------------------------------------------------------- combine ----
-constexpr int kLParts = 8;  // partial sums per round trip
+// Partial sums per round trip (2.5 us: another XCD wrote them).  Against four, and twice the dims a
+// thread: 28.4 to 30.4 us for four trees, 81.3 to 82.8 for 64 single tokens, 212 to 211 for
+// 61 trees of 128 heads.
+constexpr int kLParts = 8;
 
 // Workgroup (g, y): of the unit in record g, rows 32 (y / 8) .. and dims 64 (y % 8) ..; a thread has
 // eight dims of a row, in two pieces.  Parts in the order of the ranges.

@@ -7,6 +7,13 @@
 //                   the turns of dims 512-575 (a pair in each of 32 lanes).
 //   commit_latent   the verified root and the accepted path of each request: one workgroup
 //                   per request copies their rows and moves the length on.
+//
+// A row is exactly a wave's loads (16 bytes a lane and a pair), so that its sum needs no LDS and
+// no barrier.  Both are bound by memory: 40000 rows, 93 MB, take 16.6 us (5.5 TB/s; a copy of
+// 256 MB reaches 5.4), the weight and the table of frequencies coming from L2; 384 rows
+// 2.3 us and 128 commits 2.4 us in a captured graph, which is near an empty launch
+// (a commit is two dependent round trips, the offsets and the rows); as eager calls
+// 5.7 and 6.4 us, the host's part.
 #include "echo_device.h"
 #include "echo_internal.h"
 #include "rope_device.h"

@@ -5,6 +5,11 @@
 // (two 16-byte loads and stores: eight pairs of either layout), the first of which is on
 // its way while the turns are formed.  What is not 16-byte aligned, or whose rotated
 // part is no multiple of 16, goes pair by pair.
+//
+// Bound by memory: four bytes are moved for three operations.  40000 rows of 40 heads of 128 dims,
+// 819 MB, take 138-142 us (5.8-5.9 TB/s; a copy of 1 GB reaches 5.2); 384 rows of 68 heads
+// 3.6 us in a captured graph, of which an empty launch is about two, and 11 us as
+// an eager call, the host's part.
 #include "echo_device.h"
 #include "echo_internal.h"
 #include "rope_device.h"
@@ -13,7 +18,10 @@ namespace echo {
 namespace {
 
 constexpr int kRopeThreads = 256;
-constexpr int kRopeFill = 2048;  // workgroups at a time: eight of 256 threads on each of 256 CUs
+// Workgroups at a time: eight of 256 threads on each of 256 CUs.  384 rows of 68 heads take 4.4 us
+// with a workgroup per row, 3.6 with two rounds of threads' items shared by two and the
+// loads beside the turns.
+constexpr int kRopeFill = 2048;
 
 struct RopeSide {
   const uint16_t* x;
