@@ -4,7 +4,8 @@
 //
 //   latent_pages    checks the page ids (small tables: the main kernel's workgroups do).
 //   latent_main     persistent, one workgroup of four waves per CU.  A unit is up to 128 of a
-//                   request's rows (verify slots x heads, which lie one after another); its
+//                   request's rows (verify slots x heads, which lie one after another), 64
+//                   where there is little work; its
 //                   tiles are 32 keys each, first the tree's, then the prefix's.  The tiles
 //                   of all units are cut into ranges of equal cost, one per workgroup, which
 //                   every workgroup finds by itself from the requests' lengths.
@@ -160,7 +161,7 @@ __global__ __launch_bounds__(kPageChunk) void latent_pages_kernel(LatArgs a, int
 }
 
 // ---------------------------------------------------------------- plan ----
-// A request: its units are `full` of 128 rows and, if there are rows left, one more.
+// A request: its units are `full` of 2^us rows (128 or 64) and, if there are rows left, one more.
 struct LatLook {
   int q0, n, P;
   bool ok;
@@ -184,10 +185,10 @@ __device__ __forceinline__ int l_enter_cost(int rows) { return rows > kLRows / 2
 __device__ __forceinline__ long long l_unit_cost(int tiles, int rows) {
   return l_enter_cost(rows) + (long long)tiles * l_tile_cost(rows);
 }
-__device__ __forceinline__ long long l_cost(const LatArgs& a, const LatLook& x) {
+__device__ __forceinline__ long long l_cost(const LatArgs& a, const LatLook& x, int us) {
   if (x.n == 0) return 0;
-  const int rows = x.rows(a), rest = rows % kLRows;
-  return (rows / kLRows) * l_unit_cost(x.tiles(), kLRows) + (rest > 0 ? l_unit_cost(x.tiles(), rest) : 0);
+  const int rows = x.rows(a), rest = rows & ((1 << us) - 1);
+  return (rows >> us) * l_unit_cost(x.tiles(), 1 << us) + (rest > 0 ? l_unit_cost(x.tiles(), rest) : 0);
 }
 
 __device__ __forceinline__ long long wave_scan64(long long v) {
@@ -234,6 +235,9 @@ __device__ __forceinline__ int l_opaque(int x) {
   asm volatile("" : "+v"(x));
   return x;
 }
+// A value that all lanes have, in a scalar register (the compiler, which knows that it is uniform, would
+// leave what vector instructions computed in vector ones, and all that follows from it).
+__device__ __forceinline__ int l_scalar(int x) { return __builtin_amdgcn_readfirstlane(l_opaque(x)); }
 
 // Whether a thread sees a page of a request that is not in the pool (for an or over all threads).
 __device__ __forceinline__ int l_pages_bad(const LatArgs& a, const LatWs& ws, int r, int P) {
@@ -272,6 +276,7 @@ __device__ __forceinline__ void l_copy(uint32_t lds, uint32_t rope, uint64_t bas
 
 struct LatUnit {
   int q0, n, P, r, row0, rows, tree_tiles;
+  int w;  // the wave, in a scalar register (formed in a step, the thread's number is reloaded from memory)
 };
 
 // The addresses of 64 tiles of a unit, tile at + i in lane i: one vector of loads, where scalar ones
@@ -308,7 +313,7 @@ struct LatCopy {
 };
 __device__ __forceinline__ LatCopy l_tile(LatTable& tb, const LatArgs& a, const LatUnit& u, int t, int n,
                                           uint32_t smem) {
-  const int w = wave_id();
+  const int w = u.w;
   LatCopy c;
   if (t >= tb.at + kWave) l_fill(tb, a, u, t);
   c.base = uint64_t(uint32_t(__builtin_amdgcn_readlane(int(tb.lo), t - tb.at))) |
@@ -380,7 +385,7 @@ __device__ __forceinline__ void l_step(LatState<QR>& st, LatTable& tb, const Lat
                                        int t1, int n, uint32_t smem, uint32_t ka, uint32_t va, uint32_t pw) {
   constexpr int RT = 2 * QR;  // 32-row tiles of the unit
   constexpr int kAhead = 2;   // steps of 32 dims that K's reads are ahead of its products
-  const int w = wave_id();
+  const int w = u.w;
   // tile t + 1 has landed (t + 2 may be behind it), the weights of t are written
   if (kScores) {
     if (t + 2 < t1) wait_vm<kLCopies>();
@@ -626,7 +631,7 @@ template <int QR>
 __device__ __forceinline__ bool l_segment(const LatArgs& a, const LatWs& ws, const LatUnit& u, int t0,
                                           int t1, bool whole, size_t part, bool check, uint32_t smem) {
   constexpr int RT = 2 * QR;
-  const int w = wave_id();
+  const int w = u.w;
   const size_t first = size_t(u.q0) * a.hq + size_t(u.row0);  // the unit's first row of q
 
   // Page ids first, then the first tiles' copies, then Q, of which there is most: loads return in
@@ -741,30 +746,53 @@ __device__ __forceinline__ bool l_segment(const LatArgs& a, const LatWs& ws, con
 __global__ __launch_bounds__(kLThreads) __attribute__((amdgpu_waves_per_eu(1, 1))) void latent_main_kernel(
     LatArgs a, LatWs ws) {
   __shared__ __attribute__((aligned(1024))) char smem[kLLds];
-  const int tid = threadIdx.x, lane = tid & (kWave - 1), wid = wave_id();
+  const int tid = threadIdx.x, lane = tid & (kWave - 1);
+  int wid = wave_id();
+  asm volatile("" : "+s"(wid));
   const int nwg = int(gridDim.x);
   // every thread counts the costs of K requests
   long long* s_start = reinterpret_cast<long long*>(smem);  // [threads + 1]
-  long long* s_wave = s_start + kLThreads + 1;
+  long long* s_wave = s_start + kLThreads + 1;  // [2][waves]
   const int K = (a.R + kLThreads - 1) / kLThreads;
-  long long mine = 0;
+  long long mine = 0, mine64 = 0;  // with units of 128 rows, and of 64
   int bits = 0;
   for (int i = 0; i < K; ++i) {
     const int r = tid * K + i;
     if (r >= a.R) break;
     const LatLook x = l_look(a, r);
     if (!x.ok) bits = ECHO_DATA_BAD_OFFSETS;
-    mine += l_cost(a, x);
+    mine += l_cost(a, x, 7);
+    mine64 += l_cost(a, x, 6);
   }
   if (blockIdx.x == 0) wave_status_or(a.status, bits);
-  const long long upto = wave_scan64(mine);
-  if (lane == kWave - 1) s_wave[wid] = upto;
+  long long upto = wave_scan64(mine);
+  const long long upto64 = wave_scan64(mine64);
+  if (lane == kWave - 1) {
+    s_wave[wid] = upto;
+    s_wave[kLWaves + wid] = upto64;
+  }
   __syncthreads();
-  long long before = 0, total = 0;
+  long long before = 0, total = 0, before64 = 0, total64 = 0;
 #pragma unroll
   for (int v = 0; v < kLWaves; ++v) {
-    if (v < wid) before += s_wave[v];
+    if (v < wid) {
+      before += s_wave[v];
+      before64 += s_wave[kLWaves + v];
+    }
     total += s_wave[v];
+    total64 += s_wave[kLWaves + v];
+  }
+  // Units of 64 rows where entering one of 128 takes longer than its tiles, of which it has two thirds of the
+  // other's per row: 4 trees of 16 heads 22.6 us for 27.9, one token of 128 heads 17.9 for 24.7, 40
+  // of them over 2000-3000 tokens 65.5 for 69.9; units of 64 rows throughout: 61 trees of
+  // 128 heads would have 1.4 times the work.
+  const bool small = uniform_ll(total64 - total) < (long long)(kLEnter4 - kLEnter2) * nwg;
+  const int us = l_scalar(small ? 6 : 7);
+  if (small) {
+    upto = upto64;
+    mine = mine64;
+    before = before64;
+    total = total64;
   }
   s_start[tid] = before + upto - mine;
   __syncthreads();
@@ -789,7 +817,7 @@ __global__ __launch_bounds__(kLThreads) __attribute__((amdgpu_waves_per_eu(1, 1)
   if (lane < K && r < a.R) x = l_look(a, r);
   long long at;  // where the request's units start
   {
-    const long long c = l_cost(a, x);
+    const long long c = l_cost(a, x, us);
     const long long end = s_start[th] + wave_scan64(c);
     const int i = __ffsll((unsigned long long)__ballot(end > lo)) - 1;
     r = th * K + i;
@@ -803,33 +831,35 @@ __global__ __launch_bounds__(kLThreads) __attribute__((amdgpu_waves_per_eu(1, 1)
   bool first_unit = true;
   while (true) {
     // a request: its units from cost `at` on
-    r = __builtin_amdgcn_readfirstlane(r);
-    x.q0 = __builtin_amdgcn_readfirstlane(x.q0);
-    x.n = __builtin_amdgcn_readfirstlane(x.n);
-    x.P = __builtin_amdgcn_readfirstlane(x.P);
+    r = l_scalar(r);
+    x.q0 = l_scalar(x.q0);
+    x.n = l_scalar(x.n);
+    x.P = l_scalar(x.P);
     at = uniform_ll(at);
-    const int rows = x.rows(a), T = x.tiles(), full = rows / kLRows;
-    const long long whole_unit = l_unit_cost(T, kLRows);
+    const int rows = x.rows(a), T = x.tiles(), full = rows >> us;
+    const long long whole_unit = l_unit_cost(T, 1 << us);
     int j = 0;
     if (lo > at && full > 0) {
       j = min(int(float(lo - at) * __builtin_amdgcn_rcpf(float(whole_unit))), full);
       while (j > 0 && at + j * whole_unit > lo) --j;
       while (j < full && at + (j + 1) * whole_unit <= lo) ++j;
+      j = l_scalar(j);
     }
     at += j * whole_unit;
     bool check = true, ok = true;
-    for (; j * kLRows < rows && at < hi; ++j) {
+    for (; j << us < rows && at < hi; ++j) {
       LatUnit u;
+      u.w = wid;
       u.q0 = x.q0;
       u.n = x.n;
       u.P = x.P;
       u.r = r;
-      u.row0 = j * kLRows;
-      u.rows = min(kLRows, rows - u.row0);
+      u.row0 = l_scalar(j << us);
+      u.rows = l_scalar(min(1 << us, rows - u.row0));
       u.tree_tiles = x.tree_tiles();
       const int c = l_tile_cost(u.rows);
       const long long t_at = at + l_enter_cost(u.rows);  // where its tiles start
-      const int t0 = l_tile_at(lo - t_at, c, T), t1 = l_tile_at(hi - t_at, c, T);
+      const int t0 = l_scalar(l_tile_at(lo - t_at, c, T)), t1 = l_scalar(l_tile_at(hi - t_at, c, T));
       if (ok && t0 < t1) {
         const bool whole = t0 == 0 && t1 == T;
         const size_t part = size_t(g) * 2 + (t0 == 0 ? 1 : 0);

@@ -323,3 +323,70 @@ def test_attention_ranges_of_many_tiles(hq, slots):
         one = dict(c, R=1, cap=slots, qo=np.array([0, slots], np.int32), **{k: c[k][mine] for k in ("q", "new", "mask")},
                    **{k: c[k][r:r + 1] for k in ("bt", "plen")})
         _check(one, out[mine], lse[mine], status)
+
+
+def _among(c, rng, fillers=40, tokens=6000):
+    """The requests of c with others behind them whose work makes the units as large as they get: the
+    outputs and the status of c's own."""
+    hq, ps, nq, W = c["hq"], c["ps"], max(int(c["qo"][-1]), 0), c["W"]
+    n = -(-128 // hq)
+    assert n <= 32 * W and int(c["qo"][-1]) <= c["cap"] and 2 * tokens // 32 * fillers > 2 * 6144
+    cap = nq + n * fillers + 2
+    fill = dict(q=_bf(rng.standard_normal((cap - nq, hq, 576))), new=_bf(rng.standard_normal((cap - nq, 576))),
+                mask=np.zeros((cap - nq, W), np.uint32))
+    fill["mask"][:, 0] = 1
+    own = len(c["pages"])
+    pages = np.concatenate([c["pages"], _bf(rng.standard_normal((64, ps, 576)))])
+    bt = np.full((c["R"] + fillers, max(c["bt"].shape[1], -(-tokens // ps))), -1, np.int32)
+    bt[:c["R"], :c["bt"].shape[1]] = c["bt"]
+    bt[c["R"]:] = own + rng.integers(0, 64, (fillers, bt.shape[1]))
+    big = dict(c, R=c["R"] + fillers, cap=cap, pages=pages, bt=bt, plen=np.concatenate([c["plen"], np.full(fillers, tokens, np.int32)]),
+               qo=np.concatenate([c["qo"], nq + n * np.arange(1, fillers + 1)]).astype(np.int32),
+               **{k: np.concatenate([c[k][:nq], v]) for k, v in fill.items()})
+    big["bt"][:c["R"]] = np.where(big["bt"][:c["R"]] == own, len(pages), big["bt"][:c["R"]])  # (past the pool as before)
+    out, lse, status = _run(big)
+    assert np.all(np.isfinite(lse[nq:nq + n * fillers]))
+    mine = [np.full((c["cap"],) + x.shape[1:], np.nan, np.float32) for x in (out, lse)]
+    for a, b in zip(mine, (out, lse)):
+        a[:nq] = b[:nq]
+    return mine[0], mine[1], status
+
+
+@pytest.mark.parametrize("case", [k for k, (hq, slots, _, _) in enumerate(CASES) if hq * max(slots) > 64])
+def test_attention_large_units_match_oracle(case):
+    hq, slots, plens, ps = CASES[case]
+    rng = np.random.default_rng(200 + case)
+    _log(f"[latent attn] large units hq={hq} slots={slots} P={plens} page={ps}")
+    c = _case(rng, hq, slots, plens, ps, q_scale=[1.0, 3.0][case % 2])
+    if hq * 32 * c["W"] < 128:  # (mask words for the others' slots)
+        c["mask"], c["W"] = np.pad(c["mask"], ((0, 0), (0, -(-128 // hq // 32)))), c["W"] + -(-128 // hq // 32)
+    _check(c, *_among(c, rng))
+
+
+@pytest.mark.parametrize("grow", [50.0, 3000.0, -3000.0, 40000.0])
+def test_attention_large_units_rising_and_falling_scores(grow):
+    rng = np.random.default_rng(int(abs(grow)))
+    c = _case(rng, 64, [3, 2], [700, 65], 32, grow=grow)
+    _log(f"[latent attn] large units grow={grow}")
+    _check(c, *_among(c, rng))
+
+
+def test_attention_large_units_masks_and_bad_requests():
+    rng = np.random.default_rng(17)
+    c = _case(rng, 24, [5, 40, 4], [0, 0, 64], 32)
+    c["mask"][0] = 0
+    c["mask"][1] = [0b10000, 0]
+    c["mask"][2] = 0xFFFFFFFF
+    c["mask"][5:45, 1] = 0
+    c["mask"][45] = 0
+    _check(c, *_among(c, rng))
+    for bad in ("low", "high", "length"):
+        c = _case(rng, 16, [5, 9, 0, 7], [100, 200, 64, 130], 32)
+        if bad == "low":
+            c["bt"][1, 0] = -1
+        elif bad == "high":
+            c["bt"][1, 6] = c["pages"].shape[0]
+        else:
+            c["plen"][1] = -5
+        _log(f"[latent attn] large units, bad request: {bad}")
+        _check(c, *_among(c, rng), st.BAD_OFFSETS)
