@@ -387,3 +387,40 @@ def test_writers_on_other_streams_and_in_graphs():
         graph.replay()
         torch.cuda.synchronize()
         s.check()
+
+
+@pytest.mark.parametrize("layout", LAYOUTS)
+@pytest.mark.parametrize("rows,hq,hk,rot,at,wide", [
+    (5000, 3, 1, 16, 0, 16), (2100, 1, 0, 8, 8, 24), (4099, 2, 1, 24, 72, 96), (6001, 1, 1, 6, 0, 6), (2048, 1, 0, 2, 0, 2),
+    (3000, 5, 3, 48, 4, 56), (2500, 1, 1, 40, 2, 42), (300, 20, 1, 24, 0, 24), (7, 64, 4, 120, 8, 128)])
+def test_rope_many_short_rows_and_narrow_vectors(rows, hq, hk, rot, at, wide, layout):
+    """Workgroups of several rows, the last of them partly past the rows that exist; parts that start or
+    end 16, 8 or 4 bytes into a head."""
+    import torch
+    rng = np.random.default_rng(rows + rot)
+    f, scale = latent.frequencies(rot, 1e4) if rot > 2 else (np.ones(1), 1.0)
+    pos, n = rng.integers(0, 5000, rows), rows - 3
+    x = [_bf(rng.standard_normal((rows, h, wide))) for h in (hq, hk)]
+    _log(f"[rope] rows={rows} heads={hq}+{hk} rot={rot} at={at} of {wide} layout={layout}")
+    d = [_dev(v) if v.size else None for v in x]
+    y = [torch.full((rows, v.shape[1], rot), 7.0, dtype=torch.bfloat16, device="cuda:0") for v in d if v is not None]
+    y += [None] * (2 - len(y))
+    status = _zeros(1)
+    views = [v if v is None else v[..., at:at + rot] for v in d]
+    _rope(views[0], y[0], views[1], y[1], _dev(pos, np.int32), _dev(np.array(f)), scale, layout,
+          row_count=_dev([n], np.int32), status=status)
+    for v, out in zip(x, y):
+        if out is None:
+            continue
+        got = _bits(out)
+        _rotated_ok(got[:n], f64(v[:n, :, at:at + rot]), pos[:n], np.array(f), scale, layout)
+        assert np.all(f64(got[n:]) == 7.0)
+    assert int(status.item()) == 0
+    for v, t in zip(x, views):  # in place
+        if t is not None:
+            _rope(t, t, None, None, _dev(pos, np.int32), _dev(np.array(f)), scale, layout)
+    for v, t, out in zip(x, d, y):
+        if t is not None:
+            got = _bits(t)
+            assert np.array_equal(got[:n, :, at:at + rot], _bits(out)[:n])
+            assert np.array_equal(got[..., :at], v[..., :at]) and np.array_equal(got[..., at + rot:], v[..., at + rot:])
