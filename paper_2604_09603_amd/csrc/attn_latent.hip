@@ -76,6 +76,14 @@ constexpr int kLCost4 = 4, kLCost2 = 3, kLEnter4 = 40, kLEnter2 = 16;
 constexpr int kLMinShift = 3;
 static_assert((1 << kLMinShift) >= kLCost4, "a tile in every range");
 
+// Partial sums per round trip (2.5 us: another XCD wrote them).  Against four, and twice the dims a
+// thread: 28.4 to 30.4 us for four trees, 81.3 to 82.8 for 64 single tokens, 212 to 211 for
+// 61 trees of 128 heads.
+constexpr int kLParts = 8;
+// What a round trip costs.  With fewer and larger ranges where that saves more of them: one token of 20 heads over
+// 8000 keys 33.6 us for 41.5, two of 128 heads over 6000 41.2 for 49.8, six of 16 over 5000 33.6 for 38.8.
+constexpr int kLTrip = 5;
+
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 typedef uint32_t uint4v __attribute__((ext_vector_type(4)));
 typedef uint32_t uint2v __attribute__((ext_vector_type(2)));
@@ -191,13 +199,19 @@ __device__ __forceinline__ long long l_cost(const LatArgs& a, const LatLook& x, 
   return (rows >> us) * l_unit_cost(x.tiles(), 1 << us) + (rest > 0 ? l_unit_cost(x.tiles(), rest) : 0);
 }
 
+template <int kCtrl, int kRowMask>
+__device__ __forceinline__ long long dpp_move64(long long x) {
+  return (long long)(uint64_t(dpp_move<kCtrl, kRowMask>(0u, uint32_t(x))) |
+                     (uint64_t(dpp_move<kCtrl, kRowMask>(0u, uint32_t(uint64_t(x) >> 32))) << 32));
+}
+// Inclusive prefix sum across a wave (all lanes active).
 __device__ __forceinline__ long long wave_scan64(long long v) {
-  const int lane = threadIdx.x & (kWave - 1);
-#pragma unroll
-  for (int d = 1; d < kWave; d *= 2) {
-    const long long o = __shfl_up(v, d);
-    if (lane >= d) v += o;
-  }
+  v += dpp_move64<kDppRowShr + 1, 0xf>(v);
+  v += dpp_move64<kDppRowShr + 2, 0xf>(v);
+  v += dpp_move64<kDppRowShr + 4, 0xf>(v);
+  v += dpp_move64<kDppRowShr + 8, 0xf>(v);
+  v += dpp_move64<kDppRowBcast15, 0xa>(v);
+  v += dpp_move64<kDppRowBcast31, 0xc>(v);
   return v;
 }
 __device__ __forceinline__ long long uniform_ll(long long x) { return (long long)uniform64(uint64_t(x)); }
@@ -752,10 +766,10 @@ __global__ __launch_bounds__(kLThreads) __attribute__((amdgpu_waves_per_eu(1, 1)
   const int nwg = int(gridDim.x);
   // every thread counts the costs of K requests
   long long* s_start = reinterpret_cast<long long*>(smem);  // [threads + 1]
-  long long* s_wave = s_start + kLThreads + 1;  // [2][waves]
+  long long* s_wave = s_start + kLThreads + 1;  // [3][waves]
   const int K = (a.R + kLThreads - 1) / kLThreads;
   long long mine = 0, mine64 = 0;  // with units of 128 rows, and of 64
-  int bits = 0;
+  int bits = 0, longest = 0;
   for (int i = 0; i < K; ++i) {
     const int r = tid * K + i;
     if (r >= a.R) break;
@@ -763,13 +777,16 @@ __global__ __launch_bounds__(kLThreads) __attribute__((amdgpu_waves_per_eu(1, 1)
     if (!x.ok) bits = ECHO_DATA_BAD_OFFSETS;
     mine += l_cost(a, x, 7);
     mine64 += l_cost(a, x, 6);
+    if (x.n > 0) longest = max(longest, x.tiles());
   }
   if (blockIdx.x == 0) wave_status_or(a.status, bits);
   long long upto = wave_scan64(mine);
   const long long upto64 = wave_scan64(mine64);
+  longest = int(wave_max(uint32_t(longest)));
   if (lane == kWave - 1) {
     s_wave[wid] = upto;
     s_wave[kLWaves + wid] = upto64;
+    s_wave[2 * kLWaves + wid] = longest;
   }
   __syncthreads();
   long long before = 0, total = 0, before64 = 0, total64 = 0;
@@ -781,6 +798,7 @@ __global__ __launch_bounds__(kLThreads) __attribute__((amdgpu_waves_per_eu(1, 1)
     }
     total += s_wave[v];
     total64 += s_wave[kLWaves + v];
+    longest = max(longest, int(s_wave[2 * kLWaves + v]));
   }
   // Units of 64 rows where entering one of 128 takes longer than its tiles, of which it has two thirds of the
   // other's per row: 4 trees of 16 heads 22.6 us for 27.9, one token of 128 heads 17.9 for 24.7, 40
@@ -801,6 +819,14 @@ __global__ __launch_bounds__(kLThreads) __attribute__((amdgpu_waves_per_eu(1, 1)
   // as many as there are workgroups, or fewer (powers of two)
   ranges.shift = 31 - __builtin_clz(nwg);
   while (ranges.shift > 0 && (ranges.total >> (ranges.shift + kLMinShift)) == 0) --ranges.shift;
+  // Fewer where that saves more round trips of the merge than it costs: ranges of twice the size, half the parts.
+  const float unit = float(l_unit_cost(longest, 1 << us)) * __builtin_amdgcn_rcpf(float(ranges.total));
+  while (ranges.shift > 0) {
+    const float range = float(ranges.total >> ranges.shift), parts = unit * float(1 << ranges.shift);
+    if (range >= kLTrip * (__builtin_ceilf(parts / kLParts) - __builtin_ceilf(parts / (2 * kLParts)))) break;
+    --ranges.shift;
+  }
+  ranges.shift = l_scalar(ranges.shift);
   // neighbouring ranges, which share requests, run on one XCD (workgroup b is on XCD b % 8)
   int g = blockIdx.x;
   if ((1 << ranges.shift) == nwg && nwg % 8 == 0) g = (g & 7) * (nwg / 8) + (g >> 3);
@@ -901,10 +927,6 @@ __global__ __launch_bounds__(kLThreads) __attribute__((amdgpu_waves_per_eu(1, 1)
 }
 
 // ------------------------------------------------------------- combine ----
-// Partial sums per round trip (2.5 us: another XCD wrote them).  Against four, and twice the dims a
-// thread: 28.4 to 30.4 us for four trees, 81.3 to 82.8 for 64 single tokens, 212 to 211 for
-// 61 trees of 128 heads.
-constexpr int kLParts = 8;
 
 // Workgroup (g, y): of the unit in record g, rows 32 (y / 8) .. and dims 64 (y % 8) ..; a thread has
 // eight dims of a row, in two pieces.  Parts in the order of the ranges.
