@@ -633,7 +633,10 @@ int32_t echo_store_latent(const uint16_t* kv, int64_t kv_stride, const uint16_t*
  *              that sees no key
  * q, latent_new and out 16-byte aligned.  A request whose offsets, length or pages cannot
  * be is skipped (ECHO_DATA_BAD_OFFSETS; the pages of requests without slots are not
- * looked at).  Limits: max_rows * Hq < 2^26, max_pages_per_request * page_size < 2^31.
+ * looked at).  Limits: max_rows * Hq < 2^26, max_pages_per_request * page_size < 2^31, and the
+ * sum over all requests of ceil(slots * Hq / 128) * (keys / 32 + 12), keys being those of the
+ * prefix and the slots, < 2^29 (offsets and lengths that ask for more, seconds of
+ * work: nothing is computed, ECHO_DATA_BAD_OFFSETS).
  * Deterministic.  The workspace: echo_tree_verify_attn_latent_workspace_size; its bulk,
  * 135 MB on 256 CUs, is the same for every batch.
  */

@@ -8,7 +8,8 @@
 //                   where there is little work; its
 //                   tiles are 32 keys each, first the tree's, then the prefix's.  The tiles
 //                   of all units are cut into ranges of equal cost, one per workgroup, which
-//                   every workgroup finds by itself from the requests' lengths.
+//                   every workgroup finds by itself from the requests' lengths; where that
+//                   is faster, a range is a whole unit.
 //                   A tile is copied HBM -> LDS once and used twice.  S^T = K Q^T: each wave
 //                   has 32 (or 16) rows, its part of Q stays in registers.  The weights go
 //                   through LDS.  O^T += V^T P^T: each wave has 128 of the 512 dims for all
@@ -83,6 +84,8 @@ constexpr int kLParts = 8;
 // What a round trip costs.  With fewer and larger ranges where that saves more of them: one token of 20 heads over
 // 8000 keys 33.6 us for 41.5, two of 128 heads over 6000 41.2 for 49.8, six of 16 over 5000 33.6 for 38.8.
 constexpr int kLTrip = 5;
+constexpr int kLMerge = 4, kLMergeRows = 5;  // of a merge, and of 5 x 128 rows of parts, 2.6 MB written and read
+
 
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 typedef uint32_t uint4v __attribute__((ext_vector_type(4)));
@@ -190,39 +193,30 @@ __device__ __forceinline__ LatLook l_look(const LatArgs& a, int r) {
 }
 __device__ __forceinline__ int l_tile_cost(int rows) { return rows > kLRows / 2 ? kLCost4 : kLCost2; }
 __device__ __forceinline__ int l_enter_cost(int rows) { return rows > kLRows / 2 ? kLEnter4 : kLEnter2; }
-__device__ __forceinline__ long long l_unit_cost(int tiles, int rows) {
-  return l_enter_cost(rows) + (long long)tiles * l_tile_cost(rows);
+__device__ __forceinline__ int l_unit_cost(int tiles, int rows) {
+  return l_enter_cost(rows) + tiles * l_tile_cost(rows);  // (tiles < 2^27)
 }
-__device__ __forceinline__ long long l_cost(const LatArgs& a, const LatLook& x, int us) {
+// Costs are summed in 32 bits and saturate; a batch of 2^31 or more (four seconds) is refused.
+__device__ __forceinline__ uint32_t l_cost(const LatArgs& a, const LatLook& x, int us) {
   if (x.n == 0) return 0;
   const int rows = x.rows(a), rest = rows & ((1 << us) - 1);
-  return (rows >> us) * l_unit_cost(x.tiles(), 1 << us) + (rest > 0 ? l_unit_cost(x.tiles(), rest) : 0);
+  const uint64_t c = uint64_t(uint32_t(rows >> us)) * uint32_t(l_unit_cost(x.tiles(), 1 << us)) +
+                     uint32_t(rest > 0 ? l_unit_cost(x.tiles(), rest) : 0);
+  return (c >> 32) != 0 ? 0xFFFFFFFFu : uint32_t(c);
 }
-
-template <int kCtrl, int kRowMask>
-__device__ __forceinline__ long long dpp_move64(long long x) {
-  return (long long)(uint64_t(dpp_move<kCtrl, kRowMask>(0u, uint32_t(x))) |
-                     (uint64_t(dpp_move<kCtrl, kRowMask>(0u, uint32_t(uint64_t(x) >> 32))) << 32));
+__device__ __forceinline__ int l_units(const LatArgs& a, const LatLook& x, int us) {
+  return (x.rows(a) + (1 << us) - 1) >> us;
 }
-// Inclusive prefix sum across a wave (all lanes active).
-__device__ __forceinline__ long long wave_scan64(long long v) {
-  v += dpp_move64<kDppRowShr + 1, 0xf>(v);
-  v += dpp_move64<kDppRowShr + 2, 0xf>(v);
-  v += dpp_move64<kDppRowShr + 4, 0xf>(v);
-  v += dpp_move64<kDppRowShr + 8, 0xf>(v);
-  v += dpp_move64<kDppRowBcast15, 0xa>(v);
-  v += dpp_move64<kDppRowBcast31, 0xc>(v);
-  return v;
-}
-__device__ __forceinline__ long long uniform_ll(long long x) { return (long long)uniform64(uint64_t(x)); }
+struct AddSatOp {
+  __device__ uint32_t operator()(uint32_t a, uint32_t b) const { return __builtin_elementwise_add_sat(a, b); }
+};
 
 // Ranges 0 .. 2^shift - 1 of [0, total).
 struct LatRanges {
-  long long total;
-  int shift;
-  __device__ __forceinline__ long long first(int g) const { return (total * g) >> shift; }
+  int total, shift;
+  __device__ __forceinline__ int first(int g) const { return int((uint64_t(uint32_t(total)) * uint32_t(g)) >> shift); }
   // The range that holds cost x.
-  __device__ __forceinline__ int range_of(long long x) const {
+  __device__ __forceinline__ int range_of(int x) const {
     const int n = 1 << shift;
     int g = min(int(float(x) * float(n) * __builtin_amdgcn_rcpf(float(total))), n - 1);
     while (g > 0 && first(g) > x) --g;
@@ -230,11 +224,11 @@ struct LatRanges {
     return g;
   }
 };
-// The first tile that starts at cost x or later, of T tiles of cost c from cost 0 on.
-__device__ __forceinline__ int l_tile_at(long long x, int c, int T) {
+// The first tile that starts at cost x or later, of T tiles of cost c (kLCost4 or kLCost2) from cost 0 on.
+__device__ __forceinline__ int l_tile_at(int x, int c, int T) {
   if (x <= 0) return 0;
-  if (x > (long long)(T - 1) * c) return T;
-  return int((unsigned(x) + unsigned(c - 1)) / unsigned(c));  // (T < 2^27)
+  if (x > (T - 1) * c) return T;
+  return c == kLCost4 ? (x + kLCost4 - 1) / kLCost4 : (x + kLCost2 - 1) / kLCost2;
 }
 
 // The lane, formed where it is used: what would be kept from it over a step is reloaded from
@@ -764,87 +758,104 @@ __global__ __launch_bounds__(kLThreads) __attribute__((amdgpu_waves_per_eu(1, 1)
   int wid = wave_id();
   asm volatile("" : "+s"(wid));
   const int nwg = int(gridDim.x);
-  // every thread counts the costs of K requests
-  long long* s_start = reinterpret_cast<long long*>(smem);  // [threads + 1]
-  long long* s_wave = s_start + kLThreads + 1;  // [3][waves]
+  // every thread counts the costs and units of K requests, with units of 128 rows and of 64
+  uint32_t* s_start = reinterpret_cast<uint32_t*>(smem);  // [threads]
+  uint4* s_sums = reinterpret_cast<uint4*>(smem) + kLThreads / 4;  // [waves]: costs, units
+  uint32_t* s_longest = reinterpret_cast<uint32_t*>(s_sums + kLWaves);  // [waves]
   const int K = (a.R + kLThreads - 1) / kLThreads;
-  long long mine = 0, mine64 = 0;  // with units of 128 rows, and of 64
-  int bits = 0, longest = 0;
+  uint32_t mine = 0, mine64 = 0;
+  int bits = 0, longest = 0, units = 0, units64 = 0;
   for (int i = 0; i < K; ++i) {
     const int r = tid * K + i;
     if (r >= a.R) break;
     const LatLook x = l_look(a, r);
     if (!x.ok) bits = ECHO_DATA_BAD_OFFSETS;
-    mine += l_cost(a, x, 7);
-    mine64 += l_cost(a, x, 6);
+    mine = AddSatOp{}(mine, l_cost(a, x, 7));
+    mine64 = AddSatOp{}(mine64, l_cost(a, x, 6));
+    units += l_units(a, x, 7);
+    units64 += l_units(a, x, 6);
     if (x.n > 0) longest = max(longest, x.tiles());
   }
-  if (blockIdx.x == 0) wave_status_or(a.status, bits);
-  long long upto = wave_scan64(mine);
-  const long long upto64 = wave_scan64(mine64);
+  const uint32_t upto = wave_scan(mine, 0u, AddSatOp{}), upto64 = wave_scan(mine64, 0u, AddSatOp{});
+  const int upto_n = wave_inclusive_sum(units), upto_n64 = wave_inclusive_sum(units64);
   longest = int(wave_max(uint32_t(longest)));
   if (lane == kWave - 1) {
-    s_wave[wid] = upto;
-    s_wave[kLWaves + wid] = upto64;
-    s_wave[2 * kLWaves + wid] = longest;
+    s_sums[wid] = make_uint4(upto, upto64, uint32_t(upto_n), uint32_t(upto_n64));
+    s_longest[wid] = uint32_t(longest);
   }
   __syncthreads();
-  long long before = 0, total = 0, before64 = 0, total64 = 0;
+  uint32_t before[4] = {}, all[4] = {};
+  longest = 0;
 #pragma unroll
   for (int v = 0; v < kLWaves; ++v) {
-    if (v < wid) {
-      before += s_wave[v];
-      before64 += s_wave[kLWaves + v];
+    const uint4 x4 = s_sums[v];
+    const uint32_t x[4] = {x4.x, x4.y, x4.z, x4.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if (v < wid) before[k] = AddSatOp{}(before[k], x[k]);
+      all[k] = AddSatOp{}(all[k], x[k]);
     }
-    total += s_wave[v];
-    total64 += s_wave[kLWaves + v];
-    longest = max(longest, int(s_wave[2 * kLWaves + v]));
+    longest = max(longest, int(s_longest[v]));
   }
+  longest = l_scalar(longest);
+  const uint32_t total128 = uint32_t(l_scalar(int(all[0]))), total64 = uint32_t(l_scalar(int(all[1])));
   // Units of 64 rows where entering one of 128 takes longer than its tiles, of which it has two thirds of the
   // other's per row: 4 trees of 16 heads 22.6 us for 27.9, one token of 128 heads 17.9 for 24.7, 40
   // of them over 2000-3000 tokens 65.5 for 69.9; units of 64 rows throughout: 61 trees of
   // 128 heads would have 1.4 times the work.
-  const bool small = uniform_ll(total64 - total) < (long long)(kLEnter4 - kLEnter2) * nwg;
-  const int us = l_scalar(small ? 6 : 7);
-  if (small) {
-    upto = upto64;
-    mine = mine64;
-    before = before64;
-    total = total64;
-  }
-  s_start[tid] = before + upto - mine;
-  __syncthreads();
+  const bool small = int(total64 - total128) < (kLEnter4 - kLEnter2) * nwg && int(total64) >= 0;
+  const int us = small ? 6 : 7;
+  const uint32_t total = small ? total64 : total128;
+  if (int(total) < 0) bits = ECHO_DATA_BAD_OFFSETS;  // 2^31 or more
+  if (blockIdx.x == 0) wave_status_or(a.status, bits);
   LatRanges ranges;
-  ranges.total = uniform_ll(total);
+  ranges.total = max(int(total), 0);
   // as many as there are workgroups, or fewer (powers of two)
-  ranges.shift = 31 - __builtin_clz(nwg);
+  const int most = 31 - __builtin_clz(nwg);
+  ranges.shift = most;
   while (ranges.shift > 0 && (ranges.total >> (ranges.shift + kLMinShift)) == 0) --ranges.shift;
   // Fewer where that saves more round trips of the merge than it costs: ranges of twice the size, half the parts.
-  const float unit = float(l_unit_cost(longest, 1 << us)) * __builtin_amdgcn_rcpf(float(ranges.total));
+  const int unit = l_unit_cost(longest, 1 << us);
   while (ranges.shift > 0) {
-    const float range = float(ranges.total >> ranges.shift), parts = unit * float(1 << ranges.shift);
-    if (range >= kLTrip * (__builtin_ceilf(parts / kLParts) - __builtin_ceilf(parts / (2 * kLParts)))) break;
+    const int range = ranges.total >> ranges.shift;
+    if (unit <= kLParts * range) break;  // (one round trip)
+    const int trips = l_scalar((unit / range + kLParts - 1) / kLParts);
+    if (range >= kLTrip * (trips / 2)) break;
     --ranges.shift;
   }
-  ranges.shift = l_scalar(ranges.shift);
+  // Or none is cut, if the longest unit takes no longer than a range with a unit entered in its middle and the
+  // merge of what was cut (its start, and the parts' bytes): 116 single tokens over 50-83 keys 18.9 us
+  // for 21.5, 16 trees of 11 slots over 65-83 20.1 for 23.7, 30 trees of 32 heads over 26-54 20.1 for 29.1.
+  const int n = l_scalar(int(small ? all[3] : all[2])), range = ranges.total >> ranges.shift;
+  const int rows_most = int(min((long long)a.max_rows * a.hq, (long long)n << us) >> 7);
+  const int merge = l_scalar(kLMerge + (rows_most << ranges.shift) / max(min(n, 1 << 20) * kLMergeRows, 1));
+  const bool whole = n > 0 && n <= (1 << most) && unit > range && unit <= range + (small ? kLEnter2 : kLEnter4) + merge;
+  if (whole) {
+    ranges.total = n;
+    ranges.shift = min(32 - __builtin_clz(n), most);
+  }
+  s_start[tid] = whole ? uint32_t(small ? int(before[3]) + upto_n64 - units64 : int(before[2]) + upto_n - units)
+                       : (small ? before[1] + upto64 - mine64 : before[0] + upto - mine);
+  __syncthreads();
   // neighbouring ranges, which share requests, run on one XCD (workgroup b is on XCD b % 8)
   int g = blockIdx.x;
   if ((1 << ranges.shift) == nwg && nwg % 8 == 0) g = (g & 7) * (nwg / 8) + (g >> 3);
   if (tid == 0) ws.cuts[g].parts = 0;  // (unless there is one: below, by the same thread)
   if (g >= (1 << ranges.shift) || ranges.total == 0) return;
-  const long long lo = ranges.first(g), hi = ranges.first(g + 1);
+  const int lo = ranges.first(g), hi = ranges.first(g + 1);
+  if (lo >= hi) return;
   // the last thread whose requests start at lo or before, and which of its requests it is
   int th = 0;
 #pragma unroll
-  for (int v = 0; v < kLWaves; ++v) th += __popcll(__ballot(s_start[v * kWave + lane] <= lo));
+  for (int v = 0; v < kLWaves; ++v) th += __popcll(__ballot(int(s_start[v * kWave + lane]) <= lo));
   th = __builtin_amdgcn_readfirstlane(th) - 1;
   LatLook x = {};
   int r = th * K + lane;
   if (lane < K && r < a.R) x = l_look(a, r);
-  long long at;  // where the request's units start
+  int at;  // where the request's units start
   {
-    const long long c = l_cost(a, x, us);
-    const long long end = s_start[th] + wave_scan64(c);
+    const int c = whole ? l_units(a, x, us) : int(l_cost(a, x, us));
+    const int end = int(s_start[th]) + wave_inclusive_sum(c);
     const int i = __ffsll((unsigned long long)__ballot(end > lo)) - 1;
     r = th * K + i;
     at = __shfl(end - c, i);
@@ -861,17 +872,17 @@ __global__ __launch_bounds__(kLThreads) __attribute__((amdgpu_waves_per_eu(1, 1)
     x.q0 = l_scalar(x.q0);
     x.n = l_scalar(x.n);
     x.P = l_scalar(x.P);
-    at = uniform_ll(at);
+    at = l_scalar(at);
     const int rows = x.rows(a), T = x.tiles(), full = rows >> us;
-    const long long whole_unit = l_unit_cost(T, 1 << us);
+    const int full_unit = whole ? 1 : l_unit_cost(T, 1 << us);
     int j = 0;
     if (lo > at && full > 0) {
-      j = min(int(float(lo - at) * __builtin_amdgcn_rcpf(float(whole_unit))), full);
-      while (j > 0 && at + j * whole_unit > lo) --j;
-      while (j < full && at + (j + 1) * whole_unit <= lo) ++j;
+      j = min(int(float(lo - at) * __builtin_amdgcn_rcpf(float(full_unit))), full);
+      while (j > 0 && at + j * full_unit > lo) --j;
+      while (j < full && at + (j + 1) * full_unit <= lo) ++j;
       j = l_scalar(j);
     }
-    at += j * whole_unit;
+    at += j * full_unit;
     bool check = true, ok = true;
     for (; j << us < rows && at < hi; ++j) {
       LatUnit u;
@@ -884,26 +895,26 @@ __global__ __launch_bounds__(kLThreads) __attribute__((amdgpu_waves_per_eu(1, 1)
       u.rows = l_scalar(min(1 << us, rows - u.row0));
       u.tree_tiles = x.tree_tiles();
       const int c = l_tile_cost(u.rows);
-      const long long t_at = at + l_enter_cost(u.rows);  // where its tiles start
-      const int t0 = l_scalar(l_tile_at(lo - t_at, c, T)), t1 = l_scalar(l_tile_at(hi - t_at, c, T));
+      const int t_at = at + l_enter_cost(u.rows);  // where its tiles start
+      const int t0 = l_scalar(whole ? 0 : l_tile_at(lo - t_at, c, T));
+      const int t1 = l_scalar(whole ? T : l_tile_at(hi - t_at, c, T));
       if (ok && t0 < t1) {
-        const bool whole = t0 == 0 && t1 == T;
         const size_t part = size_t(g) * 2 + (t0 == 0 ? 1 : 0);
-        ok = c == kLCost4 ? l_segment<2>(a, ws, u, t0, t1, whole, part, check, base)
-                          : l_segment<1>(a, ws, u, t0, t1, whole, part, check, base);
+        ok = c == kLCost4 ? l_segment<2>(a, ws, u, t0, t1, t0 == 0 && t1 == T, part, check, base)
+                          : l_segment<1>(a, ws, u, t0, t1, t0 == 0 && t1 == T, part, check, base);
         check = false;
         if (!ok && tid == 0) status_or(a.status, ECHO_DATA_BAD_OFFSETS);
         // (only a range's first unit can have started before it, and the second of its ranges has the record)
         if (ok && t0 > 0 && first_unit && ranges.range_of(t_at) == g - 1 && tid == 0) {
           LatCut cut;
-          cut.parts = ranges.range_of(t_at + (long long)(T - 1) * c) - g + 2;
+          cut.parts = ranges.range_of(t_at + (T - 1) * c) - g + 2;
           cut.rows = u.rows;
           cut.row = (long long)u.q0 * a.hq + u.row0;
           ws.cuts[g] = cut;
         }
         first_unit = false;
       }
-      at += l_unit_cost(T, u.rows);
+      at += whole ? 1 : l_unit_cost(T, u.rows);
     }
     if (at >= hi) break;
     // the next request with rows

@@ -390,3 +390,44 @@ def test_attention_large_units_masks_and_bad_requests():
             c["plen"][1] = -5
         _log(f"[latent attn] large units, bad request: {bad}")
         _check(c, *_among(c, rng), st.BAD_OFFSETS)
+
+
+def _same_page(plens, max_pages, ps=1 << 20):
+    """Requests whose block tables name one page of equal rows over and over."""
+    import torch
+    rng = np.random.default_rng(18)
+    R, row = len(plens), _bf(rng.standard_normal(576))
+    c = dict(R=R, hq=1, cap=R, W=1, ps=ps, q=np.zeros((R, 1, 576), np.uint16), new=np.tile(row, (R, 1)),
+             bt=np.zeros((R, max_pages), np.int32), plen=np.array(plens, np.int32), qo=np.arange(R + 1, dtype=np.int32),
+             mask=np.ones((R, 1), np.uint32), scale=0.05, pages=np.zeros((1, 1, 576), np.uint16))
+    out, lse, ws, status = _buffers(c)
+    a = list(_args(c, out, lse, ws, status))
+    a[2] = torch.empty((1, ps, 576), dtype=torch.bfloat16, device="cuda:0")
+    a[2][:] = _dev(row)
+    return row, a, out, lse, status
+
+
+def test_attention_very_long_prefix():
+    """2^28 keys of equal rows and scores.  A workgroup's chain of sums is 2^16 steps of 16 keys, of O and of the
+    weights' sum: 2^-24 each, and the output's rounding; the sums of whole numbers below 2^24 are
+    exact, a part's, and a merge of 256 of them is off by 2^-24 each."""
+    import paper_2604_09603_amd as pkg
+    row, a, out, lse, status = _same_page([1 << 28], 257)
+    _log("[latent attn] 2^28 keys")
+    pkg.echo_tree_verify_attn_latent(*a)
+    v, o = latent.bf16_to_f64(row[:512]), out.float().cpu().numpy()[0, 0].astype(np.float64)
+    assert int(status.item()) == 0
+    assert np.all(np.abs(o - v) <= np.abs(v) * (2 * 2.0 ** 16 * 2.0 ** -24 + 2.0 ** -8) * (1 + 2.0 ** -7))
+    assert abs(float(lse.item()) - np.log(2.0 ** 28 + 1)) <= 256 * 2.0 ** -24 + 2.0 ** -18
+
+
+def test_attention_refuses_more_work_than_it_counts():
+    """16 requests of 2^31 keys: nothing is computed."""
+    import torch
+    import paper_2604_09603_amd as pkg
+    n = 2047 << 20
+    _, a, out, lse, status = _same_page([n] * 16, 2047)
+    _log("[latent attn] too much work")
+    pkg.echo_tree_verify_attn_latent(*a)
+    assert int(status.item()) == st.BAD_OFFSETS
+    assert torch.all(torch.isnan(out)) and torch.all(torch.isnan(lse))
