@@ -31,8 +31,9 @@
 // hide more and read every fragment twice: 755 against 727 us for 16 long requests, 210
 // against 192 for 128 trees.  Entering a unit costs 8 us (to 64 rows) to 20 (128: its
 // 147 KB of Q and 131 KB of output or 262 KB of partial sums), a merge 5 to 30.
-// 64 single tokens of 16 heads over 1024-8192: 81 us, 4.2 TB/s; 128 trees of 16 heads: 174-177;
-// 61 trees of 128 heads: 212, 640 TFLOP/s; 16 long requests of 64 heads: 692, 1.03 PFLOP/s.
+// 4 trees of 16 heads over 256 keys: 20 us; 64 single tokens over 1024-8192: 79, 4.3 TB/s; 128 trees:
+// 172-175; 61 trees of 128 heads: 212-216, 640 TFLOP/s; 16 long requests of 64 heads: 681-692,
+// 1.03 PFLOP/s.
 #include "attn_core.h"
 
 namespace echo {
