@@ -96,6 +96,7 @@ typedef __attribute__((address_space(3))) uint2v lds_uint2_t;
 typedef __attribute__((address_space(3))) float lds_float_t;
 typedef __attribute__((address_space(3))) uint32_t lds_uint_t;
 typedef __attribute__((address_space(3))) uint8_t lds_byte_t;
+typedef __attribute__((address_space(3))) int32_t lds_int_t;
 typedef __attribute__((address_space(3))) char lds_char_t;
 __device__ __forceinline__ lds_char_t* lds_at(uint32_t x) { return (lds_char_t*)(uintptr_t(x)); }
 
@@ -382,7 +383,6 @@ struct LatState {
   bf16x8 q[QR][kLSteps];   // row l16 of each 16-row tile, dims 32 ks + 8 quad ..
   floatx16 o[2 * QR][4];   // O^T: row tile, dims 128 w + 32 ct + 8 (r >> 2) + 4 h + (r & 3)
   float m[QR], l[QR], lq[QR];
-  int slot[QR];
 };
 
 // One step: the scores of tile t + 1 (kScores), which is the n + 1-th copied, and the values of
@@ -407,7 +407,11 @@ __device__ __forceinline__ void l_step(LatState<QR>& st, LatTable& tb, const Lat
   const uint32_t next = smem + uint32_t((n + 1) & (kLSlots - 1)) * kLSlot;
   const uint32_t rope = smem + kLRopeAt + (unsigned(n + 1) % kLRopeSlots) * kLBlock;
   const uint32_t buf = uint32_t(n & 1), buf1 = buf ^ 1u;
-  const uint32_t kb = next + ka, rb = rope + ka, vb = now + va;
+  const uint32_t kb = next + ka, rb = rope + ka;
+  // V's addresses, kept: formed at each read they were 40 instructions a step, 2.5% of 61 trees of 128 heads.
+  uint32_t vat[2][2];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) vat[k >> 1][k & 1] = uint32_t(l_opaque(int((now + va) ^ uint32_t(((k >> 1) << 6) | ((k & 1) * 48)))));
   const uint32_t pb = smem + kLProbAt + buf * kLProb + uint32_t(l_lane() * 16);
   bf16x8 kf[kAhead + 1][2], vf[2], pf[RT];
   floatx4 s[QR][2];
@@ -424,7 +428,7 @@ __device__ __forceinline__ void l_step(LatState<QR>& st, LatTable& tb, const Lat
 #pragma unroll
     for (int k = 0; k < 2; ++k)
       v[k] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-          (lds_shortx4_t*)(lds_at(uint32_t(l_opaque(int(vb))) ^ uint32_t(((ct & 1) << 6) | (k * 48))) + (ct >> 1) * kLBlock + kg * 2048 + k * 1024));
+          (lds_shortx4_t*)(lds_at(vat[ct & 1][k]) + (ct >> 1) * kLBlock + kg * 2048 + k * 1024));
     vf[g & 1] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7));
   };
   const auto read_p = [&](int kg, int rt) {
@@ -535,7 +539,10 @@ __device__ __forceinline__ void l_step(LatState<QR>& st, LatTable& tb, const Lat
 #pragma unroll
     for (int i = 0; i < QR; ++i) {
       uint32_t word = 0xFFFFFFFFu;
-      if (tree) word = tt < a.W ? a.tree_mask[size_t(l_opaque(st.slot[i])) * a.W + tt] : 0u;
+      if (tree) {
+        const int slot = *(lds_int_t*)lds_at(smem + kLInvAt + uint32_t((16 * (QR * w + i) + (l_lane() & 15)) * 4));
+        word = tt < a.W ? a.tree_mask[size_t(slot) * a.W + tt] : 0u;
+      }
       if (tn < kTileKeys) word &= (1u << tn) - 1u;
       word >>= 4 * (l_lane() >> 4);
 #pragma unroll
@@ -658,7 +665,8 @@ __device__ __forceinline__ bool l_segment(const LatArgs& a, const LatWs& ws, con
     const uint16_t* p = a.q + (first + row) * kLRow + 8 * (lane >> 4);
 #pragma unroll
     for (int ks = 0; ks < kLSteps; ++ks) st.q[i][ks] = as_bf16x8(*reinterpret_cast<const uint4*>(p + 32 * ks));
-    st.slot[i] = u.q0 + (u.row0 + row) / a.hq;
+    // (for the tree's masks; the sums take the place)
+    if (lane < 16) *(lds_int_t*)lds_at(smem + kLInvAt + uint32_t((16 * (QR * w + i) + lane) * 4)) = u.q0 + (u.row0 + row) / a.hq;
     st.m[i] = -__builtin_inff();
     st.l[i] = st.lq[i] = 0.0f;
   }
