@@ -24,16 +24,16 @@
 // What bounds it.  A row of 1152 bytes serves 2176 operations per query row, so that up to
 // 64 rows are bound by the copies: a tile takes 1.55 us on every CU at once, 6.1 TB/s,
 // of 1.0 us of work.  128 rows are bound by the products: 2177 cycles of a CU's
-// matrix cores of the 4230 that a tile takes (2.0 us, 2.35 where nothing of it is in a
-// cache and the clock is lower).  A wave is alone on its SIMD, so what is not in its
-// own products' shadow costs: about 730 cycles the copies' issue, 340 the softmax, 620
-// LDS reads, 850 a step's barrier and waits.  Eight waves with half the rows each
+// matrix cores of the 4050 that a tile takes (1.9 us, 2.3 where nothing of it is in a
+// cache and the clock is lower).  A wave is alone on its SIMD and issues an instruction in
+// four cycles at best: of the 600 of a step those between products run in their shadow,
+// the others, its start and its end, cost their own time.  Eight waves with half the rows each
 // hide more and read every fragment twice: 755 against 727 us for 16 long requests, 210
 // against 192 for 128 trees.  Entering a unit costs 8 us (to 64 rows) to 20 (128: its
 // 147 KB of Q and 131 KB of output or 262 KB of partial sums), a merge 5 to 30.
 // 4 trees of 16 heads over 256 keys: 20 us; 64 single tokens over 1024-8192: 79, 4.3 TB/s; 128 trees:
-// 172-175; 61 trees of 128 heads: 212-216, 640 TFLOP/s; 16 long requests of 64 heads: 681-692,
-// 1.03 PFLOP/s.
+// 172-175; 61 trees of 128 heads: 206-213, 650 TFLOP/s; 16 long requests of 64 heads: 670-705,
+// 1.01-1.06 PFLOP/s (ranges over several cards, whose clocks differ).
 #include "attn_core.h"
 
 namespace echo {
@@ -489,27 +489,24 @@ __device__ __forceinline__ void l_step(LatState<QR>& st, LatTable& tb, const Lat
         for (int i = 0; i < QR; ++i)
           s[i][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[ks % (kAhead + 1)][kt], st.q[i][ks], s[i][kt], 0, 0, 0);
       ECHO_FENCE();
-      // in the products' shadow: the copies of tile t + 3, the first operands of the products with V
+      // In the products' shadow: the copies of tile t + 3 (in two lots; one to a step of 32 dims, nine of them, or
+      // all in one cost 1-2% of the cycles more), the first operands of the products with V.
       if (kValues) {
         if (ks == 0 && send) copy = l_tile(tb, a, u, t + 3, n + 3, smem);
         if (send) {
-          if (ks == 1) {
+          if (ks == 2) {
             copy.piece<0>();
             copy.piece<1>();
-          }
-          if (ks == 2) {
             copy.piece<2>();
             copy.piece<3>();
-          }
-          if (ks == 3) {
             copy.piece<4>();
-            copy.piece<5>();
           }
           if (ks == 4) {
+            copy.piece<5>();
             copy.piece<6>();
             copy.piece<7>();
+            copy.piece<8>();
           }
-          if (ks == 5) copy.piece<8>();
         }
         if (ks == 5) read_first();
       }
