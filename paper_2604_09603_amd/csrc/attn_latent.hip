@@ -32,8 +32,8 @@
 // against 192 for 128 trees.  Entering a unit costs 8 us (to 64 rows) to 20 (128: its
 // 147 KB of Q and 131 KB of output or 262 KB of partial sums), a merge 5 to 30.
 // 4 trees of 16 heads over 256 keys: 20 us; 64 single tokens over 1024-8192: 79, 4.3 TB/s; 128 trees:
-// 172-175; 61 trees of 128 heads: 206-213, 650 TFLOP/s; 16 long requests of 64 heads: 670-705,
-// 1.01-1.06 PFLOP/s (ranges over several cards, whose clocks differ).
+// 172-176; 61 trees of 128 heads: 203-211, 650 TFLOP/s; 16 long requests of 64 heads: 650-680,
+// 1.05-1.09 PFLOP/s (over several cards, whose clocks differ).
 #include "attn_core.h"
 
 namespace echo {
@@ -85,6 +85,7 @@ constexpr int kLParts = 8;
 // What a round trip costs.  With fewer and larger ranges where that saves more of them: one token of 20 heads over
 // 8000 keys 33.6 us for 41.5, two of 128 heads over 6000 41.2 for 49.8, six of 16 over 5000 33.6 for 38.8.
 constexpr int kLTrip = 5;
+constexpr int kLTwo = 64;  // the smallest range whose units are taken out of order
 constexpr int kLMerge = 4, kLMergeRows = 5;  // of a merge, and of 5 x 128 rows of parts, 2.6 MB written and read
 
 
@@ -871,75 +872,103 @@ __global__ __launch_bounds__(kLThreads) __attribute__((amdgpu_waves_per_eu(1, 1)
   }
   __syncthreads();  // (the tiles take this memory)
   const uint32_t base = __builtin_amdgcn_readfirstlane(uint32_t(reinterpret_cast<uintptr_t>((lds_void_t*)smem)));
-  bool first_unit = true;
-  while (true) {
-    // a request: its units from cost `at` on
-    r = l_scalar(r);
-    x.q0 = l_scalar(x.q0);
-    x.n = l_scalar(x.n);
-    x.P = l_scalar(x.P);
-    at = l_scalar(at);
-    const int rows = x.rows(a), T = x.tiles(), full = rows >> us;
-    const int full_unit = whole ? 1 : l_unit_cost(T, 1 << us);
+  // The unit that the range starts in, if it did before it: last, so that units that start in it, of which a
+  // request often has one in each of its ranges, go over the same keys at once (16 long requests read
+  // 2.2 GB instead of 3.0, and the clock is higher for it: 666 us for 691; 61 trees of 128 heads
+  // 203 for 206).  Only where a request has several units and ranges are long, as it takes time to find out.
+  r = l_scalar(r);
+  x.q0 = l_scalar(x.q0);
+  x.n = l_scalar(x.n);
+  x.P = l_scalar(x.P);
+  at = l_scalar(at);
+  const auto unit_of = [&](const LatLook& y, int y_at, int from) {  // the one that starts at cost `from` or before it
+    const int full = y.rows(a) >> us, full_unit = whole ? 1 : l_unit_cost(y.tiles(), 1 << us);
     int j = 0;
-    if (lo > at && full > 0) {
-      j = min(int(float(lo - at) * __builtin_amdgcn_rcpf(float(full_unit))), full);
-      while (j > 0 && at + j * full_unit > lo) --j;
-      while (j < full && at + (j + 1) * full_unit <= lo) ++j;
+    if (from > y_at && full > 0) {
+      j = min(int(float(from - y_at) * __builtin_amdgcn_rcpf(float(full_unit))), full);
+      while (j > 0 && y_at + j * full_unit > from) --j;
+      while (j < full && y_at + (j + 1) * full_unit <= from) ++j;
       j = l_scalar(j);
     }
-    at += j * full_unit;
-    bool check = true, ok = true;
-    for (; j << us < rows && at < hi; ++j) {
-      LatUnit u;
-      u.w = wid;
-      u.q0 = x.q0;
-      u.n = x.n;
-      u.P = x.P;
-      u.r = r;
-      u.row0 = l_scalar(j << us);
-      u.rows = l_scalar(min(1 << us, rows - u.row0));
-      u.tree_tiles = x.tree_tiles();
-      const int c = l_tile_cost(u.rows);
-      const int t_at = at + l_enter_cost(u.rows);  // where its tiles start
-      const int t0 = l_scalar(whole ? 0 : l_tile_at(lo - t_at, c, T));
-      const int t1 = l_scalar(whole ? T : l_tile_at(hi - t_at, c, T));
-      if (ok && t0 < t1) {
-        const size_t part = size_t(g) * 2 + (t0 == 0 ? 1 : 0);
-        ok = c == kLCost4 ? l_segment<2>(a, ws, u, t0, t1, t0 == 0 && t1 == T, part, check, base)
-                          : l_segment<1>(a, ws, u, t0, t1, t0 == 0 && t1 == T, part, check, base);
-        check = false;
-        if (!ok && tid == 0) status_or(a.status, ECHO_DATA_BAD_OFFSETS);
-        // (only a range's first unit can have started before it, and the second of its ranges has the record)
-        if (ok && t0 > 0 && first_unit && ranges.range_of(t_at) == g - 1 && tid == 0) {
-          LatCut cut;
-          cut.parts = ranges.range_of(t_at + (T - 1) * c) - g + 2;
-          cut.rows = u.rows;
-          cut.row = (long long)u.q0 * a.hq + u.row0;
-          ws.cuts[g] = cut;
+    return j;
+  };
+  const LatLook x0 = x;
+  const int r0 = r, at0 = at;
+  int split = hi;  // where that unit ends
+  if (!whole && range >= kLTwo && x0.rows(a) > 1 << us) {
+    const int T = x0.tiles(), j = unit_of(x0, at0, lo), rows = min(1 << us, x0.rows(a) - (j << us));
+    const int start = at0 + j * l_unit_cost(T, 1 << us);
+    if (lo > start + l_enter_cost(rows)) split = l_scalar(min(start + l_unit_cost(T, rows), hi));
+  }
+  const bool two = split < hi;
+#pragma unroll 1
+  for (int pass = two ? 0 : 1; pass < 2; ++pass) {
+    const int from = pass == 0 ? split : lo, to = pass == 1 && two ? split : hi;
+    r = r0;
+    x = x0;
+    at = at0;
+    while (true) {
+      // a request: its units from cost `at` on
+      r = l_scalar(r);
+      x.q0 = l_scalar(x.q0);
+      x.n = l_scalar(x.n);
+      x.P = l_scalar(x.P);
+      at = l_scalar(at);
+      const int rows = x.rows(a), T = x.tiles(), full = rows >> us;
+      const int full_unit = whole ? 1 : l_unit_cost(T, 1 << us);
+      int j = unit_of(x, at, from);
+      at += j * full_unit;
+      bool check = true, ok = true;
+      for (; j << us < rows && at < to; ++j) {
+        LatUnit u;
+        u.w = wid;
+        u.q0 = x.q0;
+        u.n = x.n;
+        u.P = x.P;
+        u.r = r;
+        u.row0 = l_scalar(j << us);
+        u.rows = l_scalar(min(1 << us, rows - u.row0));
+        u.tree_tiles = x.tree_tiles();
+        const int c = l_tile_cost(u.rows);
+        const int t_at = at + l_enter_cost(u.rows);  // where its tiles start
+        const int t0 = l_scalar(whole ? 0 : l_tile_at(from - t_at, c, T));
+        const int t1 = l_scalar(whole ? T : l_tile_at(to - t_at, c, T));
+        if (ok && t0 < t1) {
+          const size_t part = size_t(g) * 2 + (t0 == 0 ? 1 : 0);
+          ok = c == kLCost4 ? l_segment<2>(a, ws, u, t0, t1, t0 == 0 && t1 == T, part, check, base)
+                            : l_segment<1>(a, ws, u, t0, t1, t0 == 0 && t1 == T, part, check, base);
+          check = false;
+          if (!ok && tid == 0) status_or(a.status, ECHO_DATA_BAD_OFFSETS);
+          // (the second of a unit's ranges has the record)
+          if (ok && t0 > 0 && ranges.range_of(t_at) == g - 1 && tid == 0) {
+            LatCut cut;
+            cut.parts = ranges.range_of(t_at + (T - 1) * c) - g + 2;
+            cut.rows = u.rows;
+            cut.row = (long long)u.q0 * a.hq + u.row0;
+            ws.cuts[g] = cut;
+          }
         }
-        first_unit = false;
+        at += whole ? 1 : l_unit_cost(T, u.rows);
       }
-      at += whole ? 1 : l_unit_cost(T, u.rows);
-    }
-    if (at >= hi) break;
-    // the next request with rows
-    int next = r + 1;
-    for (; next < a.R; next += kWave) {
-      x = LatLook{};
-      if (next + lane < a.R) x = l_look(a, next + lane);
-      const uint64_t in = __ballot(x.n > 0);
-      if (in != 0ull) {
-        const int i = __ffsll((unsigned long long)in) - 1;
-        next += i;
-        x.q0 = __shfl(x.q0, i);
-        x.n = __shfl(x.n, i);
-        x.P = __shfl(x.P, i);
-        break;
+      if (at >= to) break;
+      // the next request with rows
+      int next = r + 1;
+      for (; next < a.R; next += kWave) {
+        x = LatLook{};
+        if (next + lane < a.R) x = l_look(a, next + lane);
+        const uint64_t in = __ballot(x.n > 0);
+        if (in != 0ull) {
+          const int i = __ffsll((unsigned long long)in) - 1;
+          next += i;
+          x.q0 = __shfl(x.q0, i);
+          x.n = __shfl(x.n, i);
+          x.P = __shfl(x.P, i);
+          break;
+        }
       }
+      if (next >= a.R) break;
+      r = next;
     }
-    if (next >= a.R) break;
-    r = next;
   }
 }
 

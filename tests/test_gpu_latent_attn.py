@@ -431,3 +431,27 @@ def test_attention_refuses_more_work_than_it_counts():
     pkg.echo_tree_verify_attn_latent(*a)
     assert int(status.item()) == st.BAD_OFFSETS
     assert torch.all(torch.isnan(out)) and torch.all(torch.isnan(lse))
+
+
+@pytest.mark.parametrize("hq,slots", [(100, 3), (128, 2)])
+def test_attention_units_of_a_request_side_by_side(hq, slots):
+    """Long ranges that start in one unit of a request and hold the start of its next: taken out of order."""
+    rng = np.random.default_rng(19 + hq)
+    R, ps = 30, 64
+    c = _case(rng, hq, [slots] * R, [ps] * R, ps)
+    c["plen"] = rng.integers(2900, 3900, R).astype(np.int32)
+    full = np.flatnonzero(~np.any(c["pages"].reshape(len(c["pages"]), -1) == NAN, 1))
+    c["bt"] = full[rng.integers(0, len(full), (R, 61))].astype(np.int32)
+    bad = 11                                            # found bad again when its first unit's end is done last
+    c["bt"][bad, 30] = -1
+    _log(f"[latent attn] side by side hq={hq}")
+    out, lse, status = _run(c)
+    assert status == st.BAD_OFFSETS
+    live = np.ones(R * slots, bool)
+    live[bad * slots:(bad + 1) * slots] = False
+    assert np.all(np.isfinite(lse[:R * slots]) == live[:, None]) and np.all(np.isnan(out[:R * slots][~live]))
+    for r in (0, 10, 12, 29):  # (each alone in the oracle)
+        mine = slice(r * slots, (r + 1) * slots)
+        one = dict(c, R=1, cap=slots, qo=np.array([0, slots], np.int32), **{k: c[k][mine] for k in ("q", "new", "mask")},
+                   **{k: c[k][r:r + 1] for k in ("bt", "plen")})
+        _check(one, out[mine], lse[mine], 0)
