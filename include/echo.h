@@ -618,9 +618,11 @@ int32_t echo_store_latent(const uint16_t* kv, int64_t kv_stride, const uint16_t*
  * the tree's slots,
  *   z_j = sm_scale * <q, row_j> over 576 dims,  out = softmax(z) row[0 .. 511]
  * With one slot per request it is plain decoding.  Scores, softmax and sums are fp32;
- * each probability is rounded to bf16 for the product with the rows (2^-8) and the
- * output divided by the sum of the weights used; rows that are split between workgroups
- * are merged from fp32 sums.
+ * rows that are split between workgroups are merged from fp32 sums.  For the product
+ * with the rows each probability is rounded to bf16.  In requests of up to 32 rows
+ * (slots * Hq) the residual enters the product too, so that 2^-16 of it is left; in
+ * larger ones 2^-8 is (but for up to 32 rows past the last 64 or 128), and the output
+ * is divided by the sum of the weights used.
  * Cached values that are NaN or infinite, and such inputs, give unspecified outputs for
  * the rows of their request; rows past a request's prefix are not used, whatever they
  * hold.

@@ -16,10 +16,16 @@
 //                   rows, so that a fragment of V serves all of them.
 //   latent_combine  merges the partial sums of units that several workgroups share.
 //
-// Softmax statistics and sums are fp32.  The weights p are rounded to bfloat16 for
-// the product with V (at most 2^-8 each) and the output is divided by the sum of the
-// weights used, so that it stays a convex combination of V rows; the output's own
-// rounding to bfloat16 is as large.  Partial sums are stored in fp32.
+// Softmax statistics and sums are fp32, and so are stored partial sums.  For the product with V
+// the weights p are rounded to bfloat16.  A unit of up to 32 rows fills one of the two row tiles that
+// its products have anyway: the other takes the same rows' p - bf16(p), summed into the same O, so that
+// 2^-16 of p is left, in no more time (a tile 1.02 us for 1.02 with 16 rows, 1.17 for 1.17 with 32,
+// nothing of it from HBM; 100 single tokens of 32 heads 42.7 us for 42.1).  Larger units leave
+// 2^-8 and divide by the sum of the weights used, so that the output stays a convex
+// combination of V rows; the output's own rounding to bfloat16 is as large.  There the rests would be
+// products of their own: in units of 64 rows a tile takes 1.45 us instead of 1.17 (64 single tokens of
+// 16 heads 92 us for 81, 4 trees 20.6 for 20.0), in units of 128 half as many products again and 16 KB of
+// LDS, of which 2 are left.
 //
 // What bounds it.  A row of 1152 bytes serves 2176 operations per query row, so that up to
 // 64 rows are bound by the copies: a tile takes 1.55 us on every CU at once, 6.1 TB/s,
@@ -45,6 +51,7 @@ constexpr int kLWaves = 4;
 constexpr int kLThreads = kLWaves * kWave;
 constexpr int kLRows = 128;                    // rows of a unit
 constexpr int kLSteps = kLRow / 32;            // products along a row of K
+constexpr int kLRestRows = 32;                 // up to here a unit's weights are kept in two numbers
 // A tile in LDS: nine blocks (64 dims) of 32 rows x 128 bytes.  The 16-byte chunk c of row r
 // is at chunk position c ^ f(r), with bits 3, (2 xor 3), 1 of r as bits 0, 1, 2 of f.  A 16-byte
 // read goes in phases of 16 lanes, which are not neighbours (of the first 32: 0-3, 12-15,
@@ -389,13 +396,15 @@ struct LatState {
 // One step: the scores of tile t + 1 (kScores), which is the n + 1-th copied, and the values of
 // tile t (kValues), the n-th; copies for tile t + 3.  A tile's 16-key groups x 32-dim
 // columns are eight groups of products with V: two are taken between the next tile's scores,
-// the others beside its softmax.
-template <int QR, bool kScores, bool kValues>
+// the others beside its softmax.  kRest: rows 32 .. 63 are rows 0 .. 31 once more, of whose
+// weights waves 2 and 3 take p - bf16(p).
+template <int QR, bool kRest, bool kScores, bool kValues>
 __device__ __forceinline__ void l_step(LatState<QR>& st, LatTable& tb, const LatArgs& a, const LatUnit& u, int t,
                                        int t1, int n, uint32_t smem, uint32_t ka, uint32_t va, uint32_t pw) {
   constexpr int RT = 2 * QR;  // 32-row tiles of the unit
   constexpr int kAhead = 2;   // steps of 32 dims that K's reads are ahead of its products
   const int w = u.w;
+  const uint32_t rest = 0u - uint32_t(w >> 1);  // all bits in waves 2 and 3
   // tile t + 1 has landed (t + 2 may be behind it), the weights of t are written
   if (kScores) {
     if (t + 2 < t1) wait_vm<kLCopies>();
@@ -437,7 +446,7 @@ __device__ __forceinline__ void l_step(LatState<QR>& st, LatTable& tb, const Lat
   };
   const auto group = [&](int g) {
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) l_mfma(st.o[rt][g & 3], vf[g & 1], pf[rt]);
+    for (int rt = 0; rt < RT; ++rt) l_mfma(st.o[kRest ? 0 : rt][g & 3], vf[g & 1], pf[rt]);
   };
 
   uint32_t flags = 0;  // (a byte for each wave)
@@ -446,7 +455,7 @@ __device__ __forceinline__ void l_step(LatState<QR>& st, LatTable& tb, const Lat
     flags = uint32_t(__builtin_amdgcn_readfirstlane(int(flags)));
     if (flags == 0) return;
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
+    for (int rt = 0; rt < (kRest ? 1 : RT); ++rt) {
       const uint32_t f = QR == 2 ? flags >> (8 * rt) : flags >> (16 * rt);
       if ((f & (QR == 2 ? 0xFFu : 0xFFFFu)) != 0) {
         const int lane = l_lane();
@@ -560,7 +569,7 @@ __device__ __forceinline__ void l_step(LatState<QR>& st, LatTable& tb, const Lat
       const int g = 2 + x / RT, rt = x % RT;
       if (x == RT) read_v(4);
       ECHO_FENCE();
-      l_mfma(st.o[rt][g], vf[g & 1], pf[rt]);
+      l_mfma(st.o[kRest ? 0 : rt][g], vf[g & 1], pf[rt]);
       ECHO_FENCE();
       if (g == 3) read_p(1, rt);
       if (kScores && x <= QR) max_of(x - 1);
@@ -605,8 +614,13 @@ __device__ __forceinline__ void l_step(LatState<QR>& st, LatTable& tb, const Lat
   const auto take = [&](int p) {
     const int i = p >> 2, kt = (p >> 1) & 1;
     st.l[i] += x0 + x1;
-    const uint32_t xy = pack_bf16x2(x0, x1);
-    st.lq[i] = add_bf16x2(xy, st.lq[i]);
+    uint32_t xy = pack_bf16x2(x0, x1);
+    if (kRest) {  // (the differences are exact; the sum is st.l)
+      const uint32_t sub = xy & rest;
+      xy = pack_bf16x2(x0 - __uint_as_float(sub << 16), x1 - __uint_as_float(sub & 0xFFFF0000u));
+    } else {
+      st.lq[i] = add_bf16x2(xy, st.lq[i]);
+    }
     if ((p & 1) == 0) half = xy;
     else *(lds_uint2_t*)(lds_at(pw + buf1 * kLProb) + kt * 1024 + i * 256) = uint2v{half, xy};
   };
@@ -619,7 +633,7 @@ __device__ __forceinline__ void l_step(LatState<QR>& st, LatTable& tb, const Lat
       const int g = 4 + x / RT, rt = x % RT;
       if (rt == 0 && g < 7) read_v(g + 1);
       ECHO_FENCE();
-      l_mfma(st.o[rt][g & 3], vf[g & 1], pf[rt]);
+      l_mfma(st.o[kRest ? 0 : rt][g & 3], vf[g & 1], pf[rt]);
       ECHO_FENCE();
       if (kScores) {
         if ((x & 1) == 0) weigh(x >> 1);
@@ -641,10 +655,10 @@ __device__ __forceinline__ void l_step(LatState<QR>& st, LatTable& tb, const Lat
 // Tiles [t0, t1) of a unit, then its output (whole) or partial sums (part).  QR: 16-row tiles of
 // a wave's part of Q; the unit has up to 64 QR rows.  check: the request's pages have not
 // been looked at yet; false if they are not all in the pool, and nothing is written.
-template <int QR>
+template <int QR, bool kRest>
 __device__ __forceinline__ bool l_segment(const LatArgs& a, const LatWs& ws, const LatUnit& u, int t0,
                                           int t1, bool whole, size_t part, bool check, uint32_t smem) {
-  constexpr int RT = 2 * QR;
+  constexpr int OT = kRest ? 1 : 2 * QR;  // 32-row tiles of O
   const int w = u.w;
   const size_t first = size_t(u.q0) * a.hq + size_t(u.row0);  // the unit's first row of q
 
@@ -659,7 +673,7 @@ __device__ __forceinline__ bool l_segment(const LatArgs& a, const LatWs& ws, con
 #pragma unroll
   for (int i = 0; i < QR; ++i) {  // (rows past the last: the last again)
     const int lane = l_lane();
-    const int row = min(16 * (QR * w + i) + (lane & 15), u.rows - 1);
+    const int row = min((16 * (QR * w + i) + (lane & 15)) & (kRest ? 31 : 127), u.rows - 1);
     const uint16_t* p = a.q + (first + row) * kLRow + 8 * (lane >> 4);
 #pragma unroll
     for (int ks = 0; ks < kLSteps; ++ks) st.q[i][ks] = as_bf16x8(*reinterpret_cast<const uint4*>(p + 32 * ks));
@@ -674,7 +688,7 @@ __device__ __forceinline__ bool l_segment(const LatArgs& a, const LatWs& ws, con
     return false;
   }
 #pragma unroll
-  for (int rt = 0; rt < RT; ++rt)
+  for (int rt = 0; rt < OT; ++rt)
 #pragma unroll
     for (int ct = 0; ct < 4; ++ct) st.o[rt][ct] = floatx16{};
   // LDS offsets in a tile
@@ -686,21 +700,21 @@ __device__ __forceinline__ bool l_segment(const LatArgs& a, const LatWs& ws, con
   const uint32_t pw = smem + kLProbAt + uint32_t((QR == 2 ? w : w >> 1) * 2048 +
                                                  ((QR == 2 ? 0 : 16 * (w & 1)) + l16) * 16 + (quad & 1) * 512 +
                                                  (quad >> 1) * 8);
-  l_step<QR, true, false>(st, tb, a, u, t0 - 1, t1, -1, smem, ka, va, pw);
+  l_step<QR, kRest, true, false>(st, tb, a, u, t0 - 1, t1, -1, smem, ka, va, pw);
   if (t0 + 2 < t1) l_send(tb, a, u, t0 + 2, 2, smem);
   int t = t0;
 #pragma unroll 1
-  for (; t + 1 < t1; ++t) l_step<QR, true, true>(st, tb, a, u, t, t1, t - t0, smem, ka, va, pw);
-  l_step<QR, false, true>(st, tb, a, u, t, t1, t - t0, smem, ka, va, pw);
+  for (; t + 1 < t1; ++t) l_step<QR, kRest, true, true>(st, tb, a, u, t, t1, t - t0, smem, ka, va, pw);
+  l_step<QR, kRest, false, true>(st, tb, a, u, t, t1, t - t0, smem, ka, va, pw);
 #pragma unroll
-  for (int rt = 0; rt < RT; ++rt)
+  for (int rt = 0; rt < OT; ++rt)
 #pragma unroll
     for (int ct = 0; ct < 4; ++ct) l_settle(st.o[rt][ct]);
 
   // the sums of a row are its wave's; every wave needs their inverses
 #pragma unroll
   for (int i = 0; i < QR; ++i) {
-    const float L = quad_sum(st.l[i]), Lq = quad_sum(st.lq[i]);
+    const float L = quad_sum(st.l[i]), Lq = kRest ? L : quad_sum(st.lq[i]);
     const int lane = l_lane();
     const int row = 16 * (QR * w + i) + (lane & 15);
     if (lane < 16) {
@@ -720,7 +734,7 @@ __device__ __forceinline__ bool l_segment(const LatArgs& a, const LatWs& ws, con
     // that a row's 256 bytes go out in one piece
     const uint32_t own = smem + uint32_t(w) * kLSlot;
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
+    for (int rt = 0; rt < OT; ++rt) {
       const int lane = l_lane(), rl = lane & 31, h = lane >> 5;
       const float inv = *(lds_float_t*)lds_at(smem + kLInvAt + uint32_t((32 * rt + rl) * 4));
 #pragma unroll
@@ -734,7 +748,7 @@ __device__ __forceinline__ bool l_segment(const LatArgs& a, const LatWs& ws, con
     const int lane = l_lane(), l16 = lane & 15, quad = lane >> 4;
     uint16_t* po = a.out + first * kLC + 128 * w + 8 * l16;
 #pragma unroll
-    for (int k = 0; k < 8 * RT; ++k) {
+    for (int k = 0; k < 8 * OT; ++k) {
       const int row = 4 * k + quad;
       const uint4v x = *(lds_uint4_t*)lds_at(own + uint32_t(row * 256 + ((l16 ^ (row & 15)) << 4)));
       if (row < u.rows) *reinterpret_cast<uint4v*>(po + size_t(row) * kLC) = x;
@@ -743,7 +757,7 @@ __device__ __forceinline__ bool l_segment(const LatArgs& a, const LatWs& ws, con
     l_barrier();  // (the next unit's tiles take the slots)
   } else {
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
+    for (int rt = 0; rt < OT; ++rt) {
       const int lane = l_lane(), h = lane >> 5;
       if (32 * rt + (lane & 31) >= u.rows) continue;
       float* po = ws.part_o + ((part * 4 + rt) * 128 + 32 * w + h) * 128 + (lane & 31) * 4;
@@ -935,8 +949,10 @@ __global__ __launch_bounds__(kLThreads) __attribute__((amdgpu_waves_per_eu(1, 1)
         const int t1 = l_scalar(whole ? T : l_tile_at(to - t_at, c, T));
         if (ok && t0 < t1) {
           const size_t part = size_t(g) * 2 + (t0 == 0 ? 1 : 0);
-          ok = c == kLCost4 ? l_segment<2>(a, ws, u, t0, t1, t0 == 0 && t1 == T, part, check, base)
-                            : l_segment<1>(a, ws, u, t0, t1, t0 == 0 && t1 == T, part, check, base);
+          const bool all = t0 == 0 && t1 == T;
+          ok = c == kLCost4           ? l_segment<2, false>(a, ws, u, t0, t1, all, part, check, base)
+               : u.rows <= kLRestRows ? l_segment<1, true>(a, ws, u, t0, t1, all, part, check, base)
+                                      : l_segment<1, false>(a, ws, u, t0, t1, all, part, check, base);
           check = false;
           if (!ok && tid == 0) status_or(a.status, ECHO_DATA_BAD_OFFSETS);
           // (the second of a unit's ranges has the record)

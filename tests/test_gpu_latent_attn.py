@@ -455,3 +455,58 @@ def test_attention_units_of_a_request_side_by_side(hq, slots):
         one = dict(c, R=1, cap=slots, qo=np.array([0, slots], np.int32), **{k: c[k][mine] for k in ("q", "new", "mask")},
                    **{k: c[k][r:r + 1] for k in ("bt", "plen")})
         _check(one, out[mine], lse[mine], 0)
+
+
+def _check_units_of_32(c, unit, out, lse, status):
+    """Bounds of the last rows of each request, past whole units of `unit`: 32 at most, whose weights are taken in
+    two bfloat16 numbers.  With w a row's weights, v its values, o its output:
+    * w less its rounding to bf16 (2^-8 of it) is rounded to bf16 again, 2^-16 of w is left: 2^-16 of the mean
+      |v|, which is at most the mean |v - o| and |o|;
+    * a score's and an exponential's error and the output's own rounding as in _check;
+    * fp32 sums: O's chain of two steps per 16 keys, the weights' of four per 32, each and a merge's 272 off by
+      2^-24 a step."""
+    ref = latent.tree_verify_attn_latent(c["q"], c["new"], c["pages"], c["bt"], c["plen"], c["qo"], c["mask"], c["hq"],
+                                         c["scale"])
+    assert status == ref["status"] == 0
+    rows = np.concatenate([np.arange(a * c["hq"] + (b - a) * c["hq"] // unit * unit, b * c["hq"])
+                           for a, b in zip(c["qo"], c["qo"][1:])])
+    assert max((b - a) * c["hq"] % unit for a, b in zip(c["qo"], c["qo"][1:])) <= 32 and len(rows)
+    o, ro, dev = (x.reshape(-1, 512)[rows].astype(np.float64) for x in (out, ref["out"], ref["dev"]))
+    zabs, vmax, l, rl = (x.reshape(-1, 1)[rows] for x in (ref["zabs"], ref["vmax"], lse, ref["lse"]))
+    keys = int(c["plen"].max()) + c["cap"]
+    tol = ((dev + np.abs(ro)) * 2.0 ** -16 + dev * (zabs * (2 * 577 * 2.0 ** -24) + 2.0 ** -22)
+           + vmax * 2 * (keys / 8 + 272) * 2.0 ** -24)
+    tol = tol * (1 + 2.0 ** -7) + np.abs(ro) * 2.0 ** -8
+    err = np.abs(o - ro)
+    assert np.all(err <= tol), f"off by {(err / np.maximum(tol, 1e-300)).max():.3f} of the bound"
+    assert np.array_equal(np.isneginf(l), np.isneginf(rl)) and np.all(o[np.isneginf(rl[:, 0])] == 0)
+
+
+@pytest.mark.parametrize("hq,slots,plens", [
+    (16, [1, 2, 1, 2], [1, 0, 5, 40]), (1, [1, 30, 3], [2, 0, 33]), (32, [1, 1], [3, 129]), (5, [6, 1], [31, 700]),
+    (80, [1, 2], [4, 100]), (20, [1], [5000])])
+def test_attention_units_of_32_rows_keep_their_weights(hq, slots, plens):
+    """Cut and whole.  Small scores, whose fp32 error would hide a weight's rounding; rows of few keys, in whose
+    outputs each would show."""
+    rng = np.random.default_rng(21 + hq)
+    _log(f"[latent attn] units of 32 hq={hq} P={plens}")
+    c = _case(rng, hq, slots, plens, 32, q_scale=0.2)
+    _check_units_of_32(c, 64, *_run(c))
+
+
+@pytest.mark.parametrize("hq,slots,plens", [(16, [1, 2, 9], [3, 40, 700]), (32, [1, 5], [9, 300])])
+def test_attention_units_of_32_rows_among_large_ones(hq, slots, plens):
+    """Behind or beside units of 128 rows."""
+    rng = np.random.default_rng(23 + hq)
+    _log(f"[latent attn] units of 32 among large ones hq={hq} P={plens}")
+    c = _case(rng, hq, slots, plens, 32, q_scale=0.2)
+    _check_units_of_32(c, 128, *_among(c, rng))
+
+
+@pytest.mark.parametrize("grow", [50.0, 3000.0, -3000.0, 40000.0])
+def test_attention_units_of_32_rows_rising_and_falling_scores(grow):
+    """References that are raised in many tiles, of the rows and of their second tile alike."""
+    rng = np.random.default_rng(int(abs(grow)))
+    _log(f"[latent attn] units of 32 grow={grow}")
+    c = _case(rng, 16, [2, 1, 1], [700, 900, 33], 32, grow=grow)
+    _check_units_of_32(c, 64, *_run(c))
