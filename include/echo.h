@@ -595,7 +595,8 @@ int32_t echo_rope_frequencies(int32_t rot_dim, double base, int32_t scaling, dou
  *   norm_weight  [512] bf16, 16-byte aligned; null: dims 0-511 are copied
  *   inv_freq     [32] double; null: dims 512-575 are copied (positions are not read)
  *   row_count    as for echo_rope
- *   latent_new   [num_rows][576] bf16 (nullable), 16-byte aligned; not kv itself
+ *   latent_new   [num_rows][576] bf16 (nullable), 16-byte aligned; apart from kv's rows
+ *                (first to last), or kv itself with kv_stride 576
  *   slot_map     [num_rows] int64 (nullable; then pages, num_pages and page_size are not
  *                looked at): as echo_build_block_tables writes them.  A negative slot
  *                leaves its row out of the cache; one of num_pages * page_size or more

@@ -799,6 +799,15 @@ int32_t echo_store_latent(const uint16_t* kv, int64_t kv_stride, const uint16_t*
   if ((reinterpret_cast<uintptr_t>(kv) | reinterpret_cast<uintptr_t>(norm_weight) |
        reinterpret_cast<uintptr_t>(latent_new)) & 15u)
     return ECHO_ERR_INVALID_ARG;
+  // A row is read before it is written, but in no order with other rows: in place only where none moves.
+  const bool in_place = latent_new == kv && (kv_stride == ECHO_LATENT_DIM + ECHO_LATENT_ROPE_DIM || num_rows == 1);
+  if (latent_new != nullptr && !in_place) {
+    const uintptr_t row = (ECHO_LATENT_DIM + ECHO_LATENT_ROPE_DIM) * sizeof(uint16_t);
+    const uintptr_t x = reinterpret_cast<uintptr_t>(kv), y = reinterpret_cast<uintptr_t>(latent_new);
+    const uintptr_t before = uintptr_t(num_rows - 1);
+    if (x < y + before * row + row && y < x + before * uintptr_t(kv_stride) * sizeof(uint16_t) + row)
+      return ECHO_ERR_INVALID_ARG;
+  }
   echo::LatentCacheArgs c{nullptr, 0, 0};
   if (slot_map != nullptr) {
     const int32_t rc = cache_latent_args(pages, num_pages, page_size, &c);

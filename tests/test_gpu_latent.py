@@ -248,6 +248,24 @@ def test_store_matches_oracle(lens, starts, ps, stride, layout):
     assert torch.equal(pd2.view(torch.int16), pd.view(torch.int16))
 
 
+def test_store_in_place():
+    """Rows of kv themselves, where none moves; one row of a wider matrix."""
+    import torch
+    rng = np.random.default_rng(4)
+    kv, weight = _bf(rng.standard_normal((3001, 640))), _bf(rng.standard_normal(512))
+    pos, (f, s) = rng.integers(0, 5000, 3001), latent.frequencies(64, 1e4)
+    args = (_dev(weight), _dev(pos, np.int32), _dev(f), s, 1)
+    x = _dev(kv)[:, :576].contiguous()
+    want = torch.zeros_like(x)
+    _store(x, *args, new=want)
+    _store(x, *args, new=x)
+    assert torch.equal(x.view(torch.int16), want.view(torch.int16))
+    one = _dev(kv)[:1]
+    _store(one[:, :576], *args, new=one)
+    assert torch.equal(one[0, :576].view(torch.int16), want[0].view(torch.int16))
+    assert np.array_equal(_bits(one)[0, 576:], kv[0, 576:])
+
+
 def test_store_without_norm_or_rotation():
     import torch
     rng = np.random.default_rng(1)

@@ -189,3 +189,11 @@ def test_binding_refuses_views_it_cannot_describe():
 def test_rows_past_the_largest_launch_are_refused():
     assert _rope(rows=pkg.ROPE_MAX_ROWS + 1) == _rope(rows=2 ** 31 - 1) == UNSUPPORTED
     assert _store(rows=pkg.ROPE_MAX_ROWS + 1) == UNSUPPORTED
+
+
+@pytest.mark.parametrize("kv,new,stride,rows", [
+    (4096, 4096, 640, 3),                     # in place, but rows move: one would go over another's input
+    (4096, 4096 + 1152, 576, 3), (4096 + 1152, 4096, 576, 3), (4096, 4096 + 2 * 1280 + 1136, 640, 3),
+    (4096 + 3 * 1152 - 16, 4096, 640, 3), (4096, 4096 + 16, 576, 1)])
+def test_store_refuses_rows_that_overlap(kv, new, stride, rows):
+    assert _store(kv=P(kv), latent_new=P(new), stride=stride, rows=rows, slot_map=None) == INVALID
