@@ -63,6 +63,8 @@ GATE_SCRATCH_BYTES = 8 << 20
 
 _lib = None
 _raw_stream = _device = None  # the current stream's handle, and the current device: set by load()
+_int32 = _int64 = _float32 = _float64 = None  # torch's types, and those of 16 bits that hold bf16: too
+_bits16 = ()
 
 _P = ctypes.c_void_p
 _I32 = ctypes.c_int32
@@ -139,7 +141,7 @@ class EchoError(RuntimeError):
 
 def load(path: str = LIB_PATH) -> ctypes.CDLL:
     """Load libecho (once).  Raises if it has not been built."""
-    global _lib, _raw_stream, _device
+    global _lib, _raw_stream, _device, _int32, _int64, _float32, _float64, _bits16
     if _lib is not None:
         return _lib
     if not os.path.exists(path):
@@ -151,6 +153,8 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     # (a torch without GPU support has no streams, but the calls' refusals work there too)
     _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
     _device = torch.cuda.current_device
+    _int32, _int64, _float32, _float64 = torch.int32, torch.int64, torch.float32, torch.float64
+    _bits16 = (torch.bfloat16, torch.int16, torch.uint16)
     lib = ctypes.CDLL(path)
     for name, (res, args) in _SIGS.items():
         fn = getattr(lib, name)
@@ -502,6 +506,17 @@ def echo_build_block_tables(want_len, R, page_size, block_table, num_held, num_h
     return code
 
 
+def _dense(name, t, dtype, n):
+    """Refuse a tensor whose elements are not n or more of dtype, one after another."""
+    if t is not None and (t.dtype is not dtype or t.numel() < n or not t.is_contiguous()):
+        raise ValueError(f"{name}: {n} contiguous elements of {dtype}, not {tuple(t.shape)} of {t.dtype}")
+
+
+def _dense_bits16(name, t, n):
+    if t is not None and (t.dtype not in _bits16 or t.numel() < n or not t.is_contiguous()):
+        raise ValueError(f"{name}: {n} contiguous bf16, not {tuple(t.shape)} of {t.dtype}")
+
+
 def _head_strides(t, rows, heads, rot_dim):
     """Row and head strides of [rows, heads, rot_dim] (the stride of a dimension of size 1 says
     nothing)."""
@@ -523,9 +538,12 @@ def echo_rope(q, q_out, k, k_out, positions, num_rows, hq, hk, rot_dim, layout, 
     qor, qoh = _head_strides(q_out, num_rows, hq, rot_dim)
     kr, kh = _head_strides(k, num_rows, hk, rot_dim)
     kor, koh = _head_strides(k_out, num_rows, hk, rot_dim)
-    code = load().echo_rope(_ptr(q), qr, qh, _ptr(q_out), qor, qoh, hq, _ptr(k), kr, kh, _ptr(k_out),
-                            kor, koh, hk, _ptr(positions), num_rows, _ptr(row_count), rot_dim, layout,
-                            _ptr(inv_freq), scale, _ptr(status), _stream(stream))
+    lib = load()
+    _dense("positions", positions, _int32, num_rows)
+    _dense("inv_freq", inv_freq, _float64, rot_dim // 2)
+    code = lib.echo_rope(_ptr(q), qr, qh, _ptr(q_out), qor, qoh, hq, _ptr(k), kr, kh, _ptr(k_out),
+                         kor, koh, hk, _ptr(positions), num_rows, _ptr(row_count), rot_dim, layout,
+                         _ptr(inv_freq), scale, _ptr(status), _stream(stream))
     if check:
         _check(code, "echo_rope")
     return code
@@ -550,14 +568,25 @@ def echo_store_latent(kv, norm_weight, eps, positions, inv_freq, rope_scale, lay
     tree (latent_new), or both.  Device tensors; kv is [num_rows, 576] bf16 bits whose rows may
     be strided, norm_weight [512] bf16 bits or None, inv_freq float64 [32] or None, slot_map
     int64."""
-    s = kv.stride()
-    if s[-1] != 1:
-        raise ValueError("the dims of a row of kv must be contiguous")
-    code = load().echo_store_latent(
-        _ptr(kv), s[0] if kv.shape[0] > 1 else latent_dim + rope_dim, _ptr(norm_weight), eps,
-        _ptr(positions), _ptr(inv_freq), rope_scale, layout, num_rows, _ptr(row_count), latent_dim,
-        rope_dim, _ptr(latent_new), _ptr(slot_map), _ptr(pages),
-        0 if pages is None else pages.shape[0], page_size, _ptr(status), _stream(stream))
+    lib = load()
+    s, shape, row = kv.stride(), kv.shape, latent_dim + rope_dim
+    if len(s) != 2 or s[1] != 1 or shape[0] < num_rows or shape[1] < row or kv.dtype not in _bits16:
+        raise ValueError("kv is [num_rows, latent_dim + rope_dim] bf16 with contiguous dims")
+    _dense_bits16("norm_weight", norm_weight, latent_dim)
+    if inv_freq is not None:
+        _dense("positions", positions, _int32, num_rows)
+        _dense("inv_freq", inv_freq, _float64, rope_dim // 2)
+    _dense_bits16("latent_new", latent_new, num_rows * row)
+    num_pages = 0
+    if slot_map is not None:
+        _dense("slot_map", slot_map, _int64, num_rows)
+        num_pages = 0 if pages is None else pages.shape[0]
+        _dense_bits16("pages", pages, num_pages * page_size * row)
+    code = lib.echo_store_latent(
+        _ptr(kv), s[0] if shape[0] > 1 else row, _ptr(norm_weight), eps, _ptr(positions),
+        _ptr(inv_freq), rope_scale, layout, num_rows, _ptr(row_count), latent_dim, rope_dim,
+        _ptr(latent_new), _ptr(slot_map), _ptr(pages), num_pages, page_size, _ptr(status),
+        _stream(stream))
     if check:
         _check(code, "echo_store_latent")
     return code
@@ -576,12 +605,23 @@ def echo_tree_verify_attn_latent(q, latent_new, pages, page_size, block_table, p
     """Verification attention over a latent paged cache (absorbed form).  Device tensors; q is
     [max_rows, Hq, 576] bf16 bits, latent_new [max_rows, 576], pages [num_pages, page_size, 576],
     out [max_rows, Hq, 512]."""
-    code = load().echo_tree_verify_attn_latent(
-        _ptr(q), _ptr(latent_new), _ptr(pages), pages.shape[0], page_size, _ptr(block_table),
-        block_table.shape[1], _ptr(prefix_len), _ptr(q_offsets), _ptr(tree_mask), mask_words, R,
-        max_rows, hq, latent_dim, rope_dim, float(sm_scale), _ptr(out), _ptr(lse),
-        _ptr(workspace), workspace.numel() * workspace.element_size(), _ptr(status),
-        _stream(stream))
+    lib = load()
+    row, rows = latent_dim + rope_dim, max_rows * hq
+    num_pages, max_pages = pages.shape[0], block_table.shape[1]
+    for name, t, n in (("q", q, rows * row), ("latent_new", latent_new, max_rows * row),
+                       ("pages", pages, num_pages * page_size * row), ("out", out, rows * latent_dim)):
+        _dense_bits16(name, t, n)
+    for name, t, n in (("block_table", block_table, R * max_pages), ("prefix_len", prefix_len, R),
+                       ("q_offsets", q_offsets, R + 1)):
+        _dense(name, t, _int32, n)
+    if tree_mask.element_size() != 4 or tree_mask.numel() < max_rows * mask_words or not tree_mask.is_contiguous():
+        raise ValueError("tree_mask is [max_rows, mask_words] words of 32 bits")
+    _dense("lse", lse, _float32, rows)
+    code = lib.echo_tree_verify_attn_latent(
+        _ptr(q), _ptr(latent_new), _ptr(pages), num_pages, page_size, _ptr(block_table), max_pages,
+        _ptr(prefix_len), _ptr(q_offsets), _ptr(tree_mask), mask_words, R, max_rows, hq, latent_dim,
+        rope_dim, float(sm_scale), _ptr(out), _ptr(lse), _ptr(workspace),
+        workspace.numel() * workspace.element_size(), _ptr(status), _stream(stream))
     if check:
         _check(code, "echo_tree_verify_attn_latent")
     return code

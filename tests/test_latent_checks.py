@@ -197,3 +197,58 @@ def test_rows_past_the_largest_launch_are_refused():
     (4096 + 3 * 1152 - 16, 4096, 640, 3), (4096, 4096 + 16, 576, 1)])
 def test_store_refuses_rows_that_overlap(kv, new, stride, rows):
     assert _store(kv=P(kv), latent_new=P(new), stride=stride, rows=rows, slot_map=None) == INVALID
+
+
+def _bad_views(good, other):
+    """Of a tensor that a call reads in one piece: another type, fewer elements, one that is strided."""
+    import torch
+    wide = torch.zeros(good.shape[:-1] + (2 * good.shape[-1],), dtype=good.dtype)
+    return [good.to(other), good.reshape(-1)[:-1], wide[..., ::2]]
+
+
+def _refused(call, args, checks):
+    import torch
+    for name, other in checks:
+        for bad in _bad_views(args[name], other):
+            with pytest.raises(ValueError, match=name):
+                call(**dict(args, **{name: bad}))
+    assert all(isinstance(v, (int, float, torch.Tensor)) or v is None for v in args.values())
+
+
+def test_binding_refuses_rope_tables_of_other_types():
+    import torch
+    q = torch.zeros((4, 8, 64), dtype=torch.bfloat16)
+    args = dict(q=q, q_out=q, k=None, k_out=None, positions=torch.zeros(4, dtype=torch.int32), num_rows=4, hq=8, hk=0,
+                rot_dim=64, layout=0, inv_freq=torch.zeros(32, dtype=torch.float64), scale=1.0)
+    _refused(pkg.echo_rope, args, [("positions", torch.int64), ("inv_freq", torch.float32)])
+
+
+def test_binding_refuses_rows_it_would_misread_storing():
+    import torch
+    bf = lambda *s: torch.zeros(s, dtype=torch.bfloat16)  # noqa: E731
+    args = dict(kv=bf(3, 576), norm_weight=bf(512), eps=1e-6, positions=torch.zeros(3, dtype=torch.int32),
+                inv_freq=torch.zeros(32, dtype=torch.float64), rope_scale=1.0, layout=0, num_rows=3, latent_dim=512,
+                rope_dim=64, latent_new=bf(3, 576), slot_map=torch.zeros(3, dtype=torch.int64), pages=bf(2, 32, 576),
+                page_size=32)
+    _refused(pkg.echo_store_latent, args, [
+        ("norm_weight", torch.float32), ("positions", torch.int64), ("inv_freq", torch.float32),
+        ("latent_new", torch.float16), ("slot_map", torch.int32), ("pages", torch.float32)])
+    for kv in (bf(2, 576), bf(3, 575), bf(1, 3, 576), bf(3, 1152)[:, ::2], bf(3, 576).float(), bf(576, 3).t()):
+        with pytest.raises(ValueError, match="kv"):
+            pkg.echo_store_latent(**dict(args, kv=kv))
+
+
+def test_binding_refuses_tensors_it_would_misread_attending():
+    import torch
+    bf = lambda *s: torch.zeros(s, dtype=torch.bfloat16)  # noqa: E731
+    ints = lambda *s: torch.zeros(s, dtype=torch.int32)  # noqa: E731
+    args = dict(q=bf(4, 16, 576), latent_new=bf(4, 576), pages=bf(2, 32, 576), page_size=32, block_table=ints(2, 3),
+                prefix_len=ints(2), q_offsets=ints(3), tree_mask=ints(4, 2), mask_words=2, R=2, max_rows=4, hq=16,
+                latent_dim=512, rope_dim=64, sm_scale=0.1, out=bf(4, 16, 512),
+                lse=torch.zeros((4, 16), dtype=torch.float32), workspace=bf(64))
+    _refused(pkg.echo_tree_verify_attn_latent, args, [
+        ("q", torch.float32), ("latent_new", torch.float16), ("pages", torch.float32), ("prefix_len", torch.int64),
+        ("q_offsets", torch.int64), ("tree_mask", torch.int64), ("out", torch.float32), ("lse", torch.float64)])
+    for bt in (ints(1, 3), ints(2, 6)[:, ::2], ints(2, 3).long()):
+        with pytest.raises(ValueError, match="block_table"):
+            pkg.echo_tree_verify_attn_latent(**dict(args, block_table=bt))
