@@ -525,8 +525,7 @@ def _head_strides(t, rows, heads, rot_dim):
     shape, stride = t.shape, t.stride()
     if len(shape) != 3 or stride[2] != 1 or shape[1] != heads or shape[2] != rot_dim or shape[0] < rows:
         raise ValueError("q and k are [rows, heads, rot_dim] with contiguous dims")
-    return (stride[0] if shape[0] > 1 else heads * max(stride[1], rot_dim),
-            stride[1] if heads > 1 else rot_dim)
+    return stride[0] if shape[0] > 1 else 0, stride[1] if heads > 1 else rot_dim
 
 
 def echo_rope(q, q_out, k, k_out, positions, num_rows, hq, hk, rot_dim, layout, inv_freq, scale,

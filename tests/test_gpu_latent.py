@@ -248,6 +248,22 @@ def test_store_matches_oracle(lens, starts, ps, stride, layout):
     assert torch.equal(pd2.view(torch.int16), pd.view(torch.int16))
 
 
+def test_rope_one_row_of_heads_far_apart():
+    """The row stride of a tensor of one row says nothing, whatever its head stride."""
+    import torch
+    import paper_2604_09603_amd as pkg
+    rng = np.random.default_rng(5)
+    far = 1 << 28                                   # (times 8 heads: 2^31)
+    x = torch.empty(7 * far + 64, dtype=torch.bfloat16, device="cuda:0").as_strided((1, 8, 64), (1, far, 1))
+    x.copy_(_dev(_bf(rng.standard_normal((1, 8, 64)))))
+    near, want = x.contiguous(), torch.zeros((1, 8, 64), dtype=torch.bfloat16, device="cuda:0")
+    f, s = latent.frequencies(64, 1e4)
+    pos, f = _dev([4097], np.int32), _dev(f)
+    pkg.echo_rope(near, want, None, None, pos, 1, 8, 0, 64, 0, f, s)
+    pkg.echo_rope(x, x, None, None, pos, 1, 8, 0, 64, 0, f, s)
+    assert torch.equal(x.contiguous().view(torch.int16), want.view(torch.int16))
+
+
 def test_store_in_place():
     """Rows of kv themselves, where none moves; one row of a wider matrix."""
     import torch
