@@ -557,7 +557,8 @@ int32_t echo_rope(const uint16_t* q, int64_t q_row_stride, int64_t q_head_stride
  *   ECHO_ROPE_PLAIN   as they are
  *   ECHO_ROPE_LINEAR  f_i / factor (positions pressed together)
  *   ECHO_ROPE_BASE    of the base base * factor^(rot_dim / (rot_dim - 2)): the longest
- *                     wave is stretched by factor, the shortest is kept (rot_dim > 2)
+ *                     wave is stretched by factor, the shortest is kept (rot_dim > 2;
+ *                     that base finite too)
  *   ECHO_ROPE_BANDS   f_i / factor above the dim whose wave turns low_turns times within
  *                     original_len positions, f_i below the one that turns high_turns
  *                     times, a linear ramp over the dims between (whole ones); *scale is

@@ -730,6 +730,7 @@ int32_t echo_rope_frequencies(int32_t rot_dim, double base, int32_t scaling, dou
   const double two_pi = 6.283185307179586;
   const double n = rot_dim;
   if (scaling == ECHO_ROPE_BASE) base *= pow(factor, n / (n - 2.0));
+  if (!isfinite(base)) return ECHO_ERR_INVALID_ARG;
   double lo = 0.0, hi = 0.0;  // ECHO_ROPE_BANDS: the ramp's first and last dims (of pairs)
   if (scaling == ECHO_ROPE_BANDS) {
     const auto dim_of = [&](double turns) {

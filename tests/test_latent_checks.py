@@ -252,3 +252,8 @@ def test_binding_refuses_tensors_it_would_misread_attending():
     for bt in (ints(1, 3), ints(2, 6)[:, ::2], ints(2, 3).long()):
         with pytest.raises(ValueError, match="block_table"):
             pkg.echo_tree_verify_attn_latent(**dict(args, block_table=bt))
+
+
+@pytest.mark.parametrize("rot,base,factor", [(4, 1e4, 1e160), (64, 1e300, 1e10), (128, 1.0e308, 2.0)])
+def test_frequencies_refuse_a_base_that_overflows(rot, base, factor):
+    assert _freq(rot=rot, base=base, factor=factor, scaling=2) == INVALID
