@@ -510,3 +510,30 @@ def test_attention_units_of_32_rows_rising_and_falling_scores(grow):
     _log(f"[latent attn] units of 32 grow={grow}")
     c = _case(rng, 16, [2, 1, 1], [700, 900, 33], 32, grow=grow)
     _check_units_of_32(c, 64, *_run(c))
+
+
+@pytest.mark.parametrize("qo", [[0, 3, 2, 9], [5, 2, 9, 9], [0, 5, 3, 3], [0, 3, 5, 13], [-1, 3, 5, 9], [0, 3, 1 << 30, 9]])
+def test_attention_values_beside_bad_offsets(qo):
+    """Each well-formed request against the oracle with it alone; slots of no such request are left as they were, a
+    slot of two holds either's output."""
+    rng = np.random.default_rng(25)
+    c = _case(rng, 16, [3, 2, 4], [40, 50, 60], 32)
+    assert c["cap"] == 12
+    c["qo"] = np.array(qo, np.int32)
+    _log(f"[latent attn] offsets {qo}")
+    out, lse, status = _run(c)
+    assert status == st.BAD_OFFSETS
+    own = [np.arange(a, b) if 0 <= a <= b <= 12 else np.arange(0) for a, b in zip(qo, qo[1:])]
+    owners = np.bincount(np.concatenate(own).astype(int), minlength=12)
+    assert np.all(np.isnan(out[owners == 0])) and np.all(np.isnan(lse[owners == 0]))
+    for r, mine in enumerate(own):
+        if len(mine) == 0:
+            continue
+        one = dict(c, R=1, cap=len(mine), qo=np.array([0, len(mine)], np.int32),
+                   **{k: c[k][mine] for k in ("q", "new", "mask")}, **{k: c[k][r:r + 1] for k in ("bt", "plen")})
+        o, l = out[mine], lse[mine]
+        if np.any(owners[mine] > 1):  # (of which the oracle says what it may be)
+            ref = latent.tree_verify_attn_latent(*(one[k] for k in ("q", "new", "pages", "bt", "plen", "qo", "mask",
+                                                                    "hq", "scale")))
+            o[owners[mine] > 1], l[owners[mine] > 1] = ref["out"][owners[mine] > 1], ref["lse"][owners[mine] > 1]
+        _check(one, o, l, 0)
