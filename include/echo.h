@@ -539,9 +539,9 @@ int32_t echo_commit_kv_q8(const int32_t* q_offsets, const int32_t* accept_len,
  *   rot_dim      even, 2 .. ECHO_ROPE_MAX_DIM
  *   inv_freq     [rot_dim / 2] double, finite: a table of echo_rope_frequencies
  *   scale        finite (ECHO_ERR_INVALID_ARG)
- * Where all pointers are 16-byte aligned, the strides multiples of 8 and rot_dim one of 16,
- * values go 16 bytes at a time; at half of that each, 8 bytes; else 2.  Limits: num_rows <= ECHO_ROPE_MAX_ROWS, 2^16 heads of q and k
- * together, strides below 2^31.
+ * Where all pointers are 16-byte aligned, the strides multiples of 8 and rot_dim one of
+ * 16, values go 16 bytes at a time; at half of that each, 8 bytes; else 2.  Limits:
+ * num_rows <= ECHO_ROPE_MAX_ROWS, 2^16 heads of q and k together, strides below 2^31.
  */
 int32_t echo_rope(const uint16_t* q, int64_t q_row_stride, int64_t q_head_stride, uint16_t* q_out,
                   int64_t q_out_row_stride, int64_t q_out_head_stride, int32_t num_q_heads,

@@ -284,6 +284,8 @@ __device__ __forceinline__ int l_pages_bad(const LatArgs& a, const LatWs& ws, in
 // LDS read.  The compiler does not see a load here: M0, the LDS address, needs a wait state before
 // it, and scalars that a vector instruction wrote (base, by a lane's read) five.
 constexpr int kLCopies = 9;  // loads of a wave per tile
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"  // (M0 is reserved: nothing of the compiler's is kept in it)
 template <int B>
 __device__ __forceinline__ void l_copy(uint32_t lds, uint32_t rope, uint64_t base, uint32_t off) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %1, %2 offset:%3"
@@ -291,6 +293,7 @@ __device__ __forceinline__ void l_copy(uint32_t lds, uint32_t rope, uint64_t bas
                : "s"(B < 8 ? lds + uint32_t(B * (kLBlock - 128)) : rope - 8 * 128u), "v"(off), "s"(base), "n"(B * 128)
                : "memory", "m0");
 }
+#pragma clang diagnostic pop
 
 struct LatUnit {
   int q0, n, P, r, row0, rows, tree_tiles;
@@ -580,7 +583,7 @@ __device__ __forceinline__ void l_step(LatState<QR>& st, LatTable& tb, const Lat
   }
   bool raised = false;
   if (kScores) {
-    // The reference is raised only when a logit exceeds it by more than 2^8, so that weights stay <= 256.
+    // The reference is raised only when a logit (in powers of two) exceeds it by more than 8: weights stay <= 2^8.
     bool up = false;
 #pragma unroll
     for (int i = 0; i < QR; ++i) up |= top[i] > st.m[i] + kRescaleSlack;
@@ -928,7 +931,7 @@ __global__ __launch_bounds__(kLThreads) __attribute__((amdgpu_waves_per_eu(1, 1)
       x.n = l_scalar(x.n);
       x.P = l_scalar(x.P);
       at = l_scalar(at);
-      const int rows = x.rows(a), T = x.tiles(), full = rows >> us;
+      const int rows = x.rows(a), T = x.tiles();
       const int full_unit = whole ? 1 : l_unit_cost(T, 1 << us);
       int j = unit_of(x, at, from);
       at += j * full_unit;

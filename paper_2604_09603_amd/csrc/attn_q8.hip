@@ -301,7 +301,7 @@ __device__ __forceinline__ void q8_check(Q8Walk& w, const Q8Args& a, const Q8Pag
                                          int j) {
   const int lane = threadIdx.x & (kWave - 1);
   for (; j < pages.n; j += 2 * kWave)  // (two loads at a time)
-    bad |= pages.bad(a, j + lane) | pages.bad(a, j + kWave + lane);
+    bad |= int(pages.bad(a, j + lane)) | int(pages.bad(a, j + kWave + lane));
   w.bad = __ballot(bad) != 0ull;
   w.met |= w.bad;
 }
