@@ -37,9 +37,11 @@
 // hide more and read every fragment twice: 755 against 727 us for 16 long requests, 210
 // against 192 for 128 trees.  Entering a unit costs 8 us (to 64 rows) to 20 (128: its
 // 147 KB of Q and 131 KB of output or 262 KB of partial sums), a merge 5 to 30.
-// 4 trees of 16 heads over 256 keys: 20 us; 64 single tokens over 1024-8192: 79, 4.3 TB/s; 128 trees:
-// 172-176; 61 trees of 128 heads: 203-211, 650 TFLOP/s; 16 long requests of 64 heads: 650-680,
-// 1.05-1.09 PFLOP/s (over several cards, whose clocks differ).
+// 4 trees of 16 heads over 256 keys: 20 us; 64 single tokens over 1024-8192: 79-83, 4.1-4.3 TB/s; 128
+// trees: 172-180; 61 trees of 128 heads: 203-213, 640-670 TFLOP/s; 16 long requests of 64 heads:
+// 645-720, 0.99-1.10 PFLOP/s (over several cards, whose clocks differ).  Of the 512 registers a lane, 56
+// values more are in scratch memory and 106 scalars in lanes: reloaded where a unit is entered and left, not
+// in the loops over its tiles.
 #include "attn_core.h"
 
 namespace echo {

@@ -13,7 +13,7 @@
 // 256 MB reaches 5.4), the weight and the table of frequencies coming from L2; 384 rows
 // 2.3 us and 128 commits 2.4 us in a captured graph, which is near an empty launch
 // (a commit is two dependent round trips, the offsets and the rows); as eager calls
-// 5.7 and 6.4 us, the host's part.
+// 6.9 and 6.4 us, the host's part.
 #include "echo_device.h"
 #include "echo_internal.h"
 #include "rope_device.h"

@@ -9,7 +9,7 @@
 //
 // Bound by memory: four bytes are moved for three operations.  40000 rows of 40 heads of 128 dims,
 // 819 MB, take 138-142 us (5.8-5.9 TB/s; a copy of 1 GB reaches 5.2); 384 rows of 68 heads
-// 3.7 us in a captured graph, of which an empty launch is about two, and 11 us as
+// 3.7 us in a captured graph, of which an empty launch is about two, and 11.5 us as
 // an eager call, the host's part.
 #include "echo_device.h"
 #include "echo_internal.h"
